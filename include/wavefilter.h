@@ -19,6 +19,10 @@
  *   6. wf_filter_attend  steps 1-5 fused; the sparse cache is never
  *                      materialised.
  *
+ * Beside that path: a prompt cache kept in 8 or 4 bits (wf_cache_store,
+ * wf_cache_load) and attention of a batch whose sequences share a prompt
+ * (wf_prefix_attn), over all of it or over its selected tokens.
+ *
  * Conventions shared by every entry point
  * ---------------------------------------
  *  - A "unit" is one (batch, head) pair; units are independent.  Tensors are
@@ -413,6 +417,128 @@ const char* wf_filter_attend_recursive_kernel_name(const wf_params* p,
  * is row-wise.  With the heads of a group adjacent, Q [batch][g * heads_kv]
  * [q_len][d] is already [batch][heads_kv][g * q_len][d]: pass heads =
  * heads_kv and q_len = g * q_len (at most WF_MAX_Q_LEN). */
+
+/* ---------------------------------------------------------------------
+ * A cache of K and V rows in 8 or 4 bits.  A block is 32 consecutive
+ * channels of one row.  It shares a power of two 2^(x - 127), x its exponent
+ * byte: the smallest one with x >= 1 for which the block's largest magnitude
+ * is at most the format's largest number (E4M3 448, E2M1 6).  The codes are
+ * the channels divided by it (exact) and rounded to the format, to nearest,
+ * ties to even, subnormals kept: the only rounding of a stored value.  A
+ * block that holds a NaN or an infinity has x = 255 and codes 0.
+ *   codes Kc, Vc  [batch][heads][capacity][d] bytes for E4M3 (bits: sign, 4
+ *                 exponent, 3 mantissa), [..][d / 2] for E2M1 (sign, 2
+ *                 exponent, 1 mantissa; channel 2 i in the low half of byte i)
+ *   exps  Kx, Vx  [batch][heads][capacity][d / 32] bytes
+ * A value reads back as its code times the float whose bits are x << 23: 0
+ * for x = 0 (rows of a cache cleared to zero bytes), NaN for x = 255.
+ * --------------------------------------------------------------------- */
+enum { WF_CACHE_PLAIN = 0, /* no quantisation: rows of the call's dtype
+                              (wf_prefix_attn only)                      */
+       WF_CACHE_E4M3 = 1, WF_CACHE_E2M1 = 2 };
+
+typedef struct wf_cache_params {
+    int32_t batch;    /* >= 1                                              */
+    int32_t heads;    /* >= 1, K/V heads                                   */
+    int32_t capacity; /* rows a unit's cache holds, >= 1                   */
+    int32_t head_dim; /* d: 64 or 128                                      */
+    int32_t rows;     /* rows per unit that this call moves, >= 0          */
+    int32_t first;    /* cache row of row 0 where row_idx is NULL          */
+    int32_t dtype;    /* WF_BF16 or WF_F32: K and V                        */
+    int32_t format;   /* WF_CACHE_E4M3 or WF_CACHE_E2M1                    */
+} wf_cache_params;
+
+/*
+ * Quantises rows as they are written: row r of a unit goes to its cache row
+ * row_idx[b][r], or first + r where row_idx is NULL (first + rows <=
+ * capacity).  All other cache rows keep their bytes.
+ *   K, V     [batch][heads][rows][d]   dtype
+ *   row_idx  nullable [batch][rows]    int32, shared by a sequence's heads;
+ *            a row with an index outside [0, capacity) (padding) is not
+ *            written.  The indices inside must differ within a sequence:
+ *            what a row named twice holds is undefined (the host cannot
+ *            read device memory).
+ *   Kc, Kx, Vc, Vx   the cache, in/out
+ * rows = 0 queues nothing (the pointers are not looked at).
+ */
+wf_status wf_cache_store(const wf_cache_params* p, const void* K, const void* V,
+                         const int32_t* row_idx, void* Kc, void* Kx, void* Vc,
+                         void* Vx, void* stream);
+
+/*
+ * Reads rows back: row r of a unit's output is its cache row
+ * row_idx[b][h][r], or first + r where row_idx is NULL.
+ *   row_idx  nullable [batch][heads][rows] int32, in any order and as often
+ *            as wanted (wf_scan_select's tok_idx, the tokens of regions);
+ *            an index outside [0, capacity) gives a row of zeros
+ *   K, V     [batch][heads][rows][d]   dtype out (rounded to nearest even;
+ *            exact where the value is no subnormal of bf16)
+ * rows = 0 queues nothing.
+ */
+wf_status wf_cache_load(const wf_cache_params* p, const void* Kc, const void* Kx,
+                        const void* Vc, const void* Vx, const int32_t* row_idx,
+                        void* K, void* V, void* stream);
+
+/* ---------------------------------------------------------------------
+ * Attention of a batch whose sequences share a prompt: sequence n of
+ * batch = prefixes * share has prefix n / share and rows of its own.  Query
+ * head a (of heads * group) reads K/V head a / group.  Every query row of a
+ * sequence sees the keys of its prefix and its own rows, no mask otherwise
+ * (the bidirectional form of eq. 3); the prefix is read once for all rows of
+ * the sequences that share it.
+ *   O   = sum_j w_j v_j, w = softmax(scale q k_j) over those keys
+ *   lse = log sum_j exp(scale q k_j)
+ * A row that sees no key has O = 0 and lse = -inf.
+ * --------------------------------------------------------------------- */
+typedef struct wf_prefix_params {
+    int32_t prefixes;    /* >= 1                                            */
+    int32_t share;       /* sequences per prefix, >= 1                      */
+    int32_t heads;       /* K/V heads, >= 1                                 */
+    int32_t group;       /* query heads per K/V head, >= 1                  */
+    int32_t q_len;       /* B: query rows of a sequence, >= 1               */
+    int32_t head_dim;    /* d: 64 or 128                                    */
+    int32_t prefix_cap;  /* rows of K and V per (prefix, head), >= 0        */
+    int32_t prefix_rows; /* rows attended, >= 0: the first ones, at most
+                            prefix_cap, or a list of this length            */
+    int32_t tail_cap;    /* T: rows of Kt and Vt per (sequence, head), >= 0 */
+    int32_t dtype;       /* WF_BF16 or WF_F32: Q, Kt, Vt, O                 */
+    int32_t format;      /* K, V: WF_CACHE_PLAIN (dtype) or as stored by
+                            wf_cache_store with batch = prefixes            */
+    float scale;         /* softmax scale; 0 selects 1/sqrt(d)              */
+} wf_prefix_params;
+
+/* Workspace bytes wf_prefix_attn needs (0 if it needs none or the parameters
+ * are invalid). */
+size_t wf_prefix_workspace_bytes(const wf_prefix_params* p);
+
+/*
+ *   Q           [prefixes share][heads group][B][d]       dtype
+ *   K, V        [prefixes][heads][prefix_cap][d]           dtype, or codes
+ *   Kx, Vx      exponent bytes of K, V; NULL for WF_CACHE_PLAIN
+ *   row_idx     nullable [prefixes][heads][prefix_rows]    int32 list of
+ *               prefix rows (wf_scan_select's tok_idx of the shared prompt),
+ *               each in [0, prefix_cap): ids outside are taken as the nearest
+ *               row inside
+ *   prefix_len  nullable [prefixes] int32: only the first prefix_len[i] rows
+ *               (or list entries) of prefix i are seen
+ *   Kt, Vt      [prefixes share][heads][T][d]              dtype; NULL iff T
+ *               == 0
+ *   tail_len    nullable [prefixes share] int32: only the first tail_len[n]
+ *               own rows of sequence n are seen
+ *               (lengths outside are taken as the nearest one inside; rows
+ *               past a length may hold anything)
+ *   O           [prefixes share][heads group][B][d]        dtype out
+ *   lse         nullable [prefixes share][heads group][B]  fp32 out
+ *   workspace   >= wf_prefix_workspace_bytes(p), 256-byte aligned
+ * K, V (and Kx, Vx) may be NULL where prefix_rows == 0; at least one of
+ * prefix_rows and tail_cap is above 0.
+ */
+wf_status wf_prefix_attn(const wf_prefix_params* p, const void* Q, const void* K,
+                         const void* Kx, const void* V, const void* Vx,
+                         const int32_t* row_idx, const int32_t* prefix_len,
+                         const void* Kt, const void* Vt, const int32_t* tail_len,
+                         void* O, float* lse, void* workspace,
+                         size_t workspace_bytes, void* stream);
 
 /* Loads the library's kernels onto the current device and sets up its
  * per-device state, so that no later call stalls for it (otherwise the

@@ -21,6 +21,7 @@ HAAR, DB2 = 0, 1
 EXT_SYMMETRIC, EXT_PERIODIC = 0, 1
 BF16, F32 = 0, 1
 OP_SKIM, OP_SCAN, OP_ATTN, OP_FUSED, OP_CACHED, OP_SHARED = 0, 1, 2, 3, 4, 5
+CACHE_PLAIN, CACHE_E4M3, CACHE_E2M1 = 0, 1, 2
 MAX_LEVELS, MAX_Q_LEN = 10, 256
 NOALLOC_SCRATCH_BYTES = 32 << 20
 
@@ -42,7 +43,8 @@ EXPORTED = ("wf_workspace_bytes", "wf_effective_budget", "wf_dwt_keys",
             "wf_filter_attend_recursive", "wf_filter_attend_recursive_timed",
             "wf_filter_attend_recursive_kernels",
             "wf_filter_attend_recursive_kernel_name",
-            "wf_init", "wf_status_str", "wf_last_error")
+            "wf_cache_store", "wf_cache_load", "wf_prefix_workspace_bytes",
+            "wf_prefix_attn", "wf_init", "wf_status_str", "wf_last_error")
 
 
 class WfParams(ctypes.Structure):
@@ -53,6 +55,19 @@ class WfParams(ctypes.Structure):
 
     def as_dict(self) -> dict:
         return {n: getattr(self, n) for n, _ in self._fields_}
+
+
+class WfCacheParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "batch", "heads", "capacity", "head_dim", "rows", "first", "dtype",
+        "format")]
+
+
+class WfPrefixParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "prefixes", "share", "heads", "group", "q_len", "head_dim",
+        "prefix_cap", "prefix_rows", "tail_cap", "dtype", "format")] + [
+        ("scale", ctypes.c_float)]
 
 
 class WfError(RuntimeError):
@@ -71,6 +86,7 @@ def _load() -> ctypes.CDLL:
     P = ctypes.POINTER(WfParams)
     vp, sz, i32 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int32
     fp, ip = ctypes.POINTER(ctypes.c_float), ctypes.POINTER(ctypes.c_int32)
+    CP, PP = ctypes.POINTER(WfCacheParams), ctypes.POINTER(WfPrefixParams)
     sig = {
         "wf_workspace_bytes": (sz, [P, i32]),
         "wf_effective_budget": (i32, [P]),
@@ -117,6 +133,12 @@ def _load() -> ctypes.CDLL:
                                               ctypes.POINTER(vp), i32]),
         "wf_filter_attend_recursive_kernels": (i32, [P]),
         "wf_filter_attend_recursive_kernel_name": (ctypes.c_char_p, [P, i32]),
+        "wf_cache_store": (ctypes.c_int, [CP, vp, vp, vp, vp, vp, vp, vp, vp]),
+        "wf_cache_load": (ctypes.c_int, [CP, vp, vp, vp, vp, vp, vp, vp, vp]),
+        "wf_prefix_workspace_bytes": (sz, [PP]),
+        "wf_prefix_attn": (ctypes.c_int,
+                           [PP, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp,
+                            vp, sz, vp]),
         "wf_init": (ctypes.c_int, []),
         "wf_status_str": (ctypes.c_char_p, [ctypes.c_int]),
         "wf_last_error": (ctypes.c_char_p, []),
@@ -137,6 +159,10 @@ def library() -> ctypes.CDLL:
 
 # ------------------------------------------------------------ parameters
 
+_DTYPES = {"bf16": BF16, "f32": F32, torch.bfloat16: BF16, torch.float32: F32}
+_FORMATS = {None: CACHE_PLAIN, "e4m3": CACHE_E4M3, "e2m1": CACHE_E2M1}
+
+
 def make_params(*, batch: int, heads: int, ctx_len: int, head_dim: int,
                 q_len: int, levels: int, segments: int, budget: int,
                 gen_len: int = 0, wavelet: str | int = "haar",
@@ -145,8 +171,7 @@ def make_params(*, batch: int, heads: int, ctx_len: int, head_dim: int,
     w = {"haar": HAAR, "db2": DB2}.get(wavelet, wavelet)
     b = {"symmetric": EXT_SYMMETRIC, "periodic": EXT_PERIODIC}.get(boundary,
                                                                    boundary)
-    dt = {"bf16": BF16, "f32": F32, torch.bfloat16: BF16,
-          torch.float32: F32}.get(dtype, dtype)
+    dt = _DTYPES.get(dtype, dtype)
     return WfParams(batch, heads, ctx_len, head_dim, q_len, gen_len, levels,
                     w, b, dt, segments, budget, scale)
 
@@ -619,6 +644,163 @@ def filter_attend_recursive(p: WfParams, proportions, Q, K, V, Kg=None,
     wf_filter_attend_recursive(p, proportions, Q, K, V, Kg, Vg, O, tok,
                                workspace, stream, kept_idx=kept)
     return (O, tok, kept) if want_kept else (O, tok)
+
+
+# ------------------------------------------------------------ quantised cache
+# K and V rows in 8 (e4m3) or 4 bits (e2m1), a power of two per 32 channels.
+
+def make_cache_params(*, batch: int, heads: int, capacity: int, head_dim: int,
+                      rows: int, first: int = 0, dtype: str | int = "bf16",
+                      format: str | int = "e4m3") -> WfCacheParams:
+    """rows: the rows per unit that a call moves (first: its first cache row
+    where no row list is given)."""
+    return WfCacheParams(batch, heads, capacity, head_dim, rows, first,
+                         _DTYPES.get(dtype, dtype),
+                         _FORMATS.get(format, format))
+
+
+def _code_bytes(head_dim: int, format: int) -> int:
+    """Bytes of one row's codes."""
+    return head_dim // 2 if format == CACHE_E2M1 else head_dim
+
+
+def alloc_cache(p: WfCacheParams, device) -> tuple[torch.Tensor, ...]:
+    """A cache (Kc, Kx, Vc, Vx) whose rows all read back as zeros."""
+    unit = (p.batch, p.heads, p.capacity)
+    shapes = [unit + (_code_bytes(p.head_dim, p.format),),
+              unit + (p.head_dim // 32,)] * 2
+    return tuple(torch.zeros(s, dtype=torch.uint8, device=device)
+                 for s in shapes)
+
+
+def _expect_device(*tensors) -> None:
+    """Every tensor on the current device, which the kernels run on."""
+    for t in tensors:
+        if t is not None and t.device.type == "cuda" \
+                and t.device.index != torch.cuda.current_device():
+            raise ValueError(f"a tensor on {t.device}, the current device is "
+                             f"cuda:{torch.cuda.current_device()}")
+
+
+def _expect_cache(p, K, V, row_idx, idx_rows, Kc, Kx, Vc, Vx) -> None:
+    U, d = _units(p), p.head_dim
+    for name, t in (("K", K), ("V", V)):
+        _expect(t, name, torch_dtype(p), U * p.rows * d)
+    _expect(row_idx, "row_idx", torch.int32, idx_rows * p.rows, nullable=True)
+    for name, t, n in (("Kc", Kc, _code_bytes(d, p.format)), ("Kx", Kx, d // 32),
+                       ("Vc", Vc, _code_bytes(d, p.format)), ("Vx", Vx, d // 32)):
+        _expect(t, name, torch.uint8, U * p.capacity * n)
+    _expect_device(K, V, row_idx, Kc, Kx, Vc, Vx)
+
+
+def wf_cache_store(p, K, V, row_idx, Kc, Kx, Vc, Vx, stream=None):
+    _expect_cache(p, K, V, row_idx, p.batch, Kc, Kx, Vc, Vx)
+    _check(_lib.wf_cache_store(ctypes.byref(p), _ptr(K), _ptr(V),
+                               _ptr(row_idx), _ptr(Kc), _ptr(Kx), _ptr(Vc),
+                               _ptr(Vx), _stream(stream)))
+
+
+def wf_cache_load(p, Kc, Kx, Vc, Vx, row_idx, K, V, stream=None):
+    _expect_cache(p, K, V, row_idx, _units(p), Kc, Kx, Vc, Vx)
+    _check(_lib.wf_cache_load(ctypes.byref(p), _ptr(Kc), _ptr(Kx), _ptr(Vc),
+                              _ptr(Vx), _ptr(row_idx), _ptr(K), _ptr(V),
+                              _stream(stream)))
+
+
+def cache_load(p: WfCacheParams, cache, row_idx=None, stream=None):
+    """Allocates K and V [batch, heads, rows, d] and runs wf_cache_load of a
+    cache (Kc, Kx, Vc, Vx).  Returns (K, V)."""
+    with torch.cuda.stream(_torch_stream(stream)):
+        K, V = (torch.empty((p.batch, p.heads, p.rows, p.head_dim),
+                            dtype=torch_dtype(p), device=cache[0].device)
+                for _ in range(2))
+    wf_cache_load(p, *cache, row_idx, K, V, stream)
+    return K, V
+
+
+# ------------------------------------------------------------ shared prefix
+# Sequences n share .. n share + share - 1 have the rows of prefix n, and each
+# has rows of its own.
+
+def make_prefix_params(*, prefixes: int = 1, share: int, heads: int,
+                       group: int = 1, q_len: int, head_dim: int,
+                       prefix_cap: int, prefix_rows: int | None = None,
+                       tail_cap: int = 0, dtype: str | int = "bf16",
+                       format: str | int | None = None,
+                       scale: float = 0.0) -> WfPrefixParams:
+    """prefix_rows: the rows attended (all prefix_cap by default), or the
+    length of a row list; format: None for K and V of dtype, else that of the
+    cache they are kept in."""
+    return WfPrefixParams(prefixes, share, heads, group, q_len, head_dim,
+                          prefix_cap,
+                          prefix_cap if prefix_rows is None else prefix_rows,
+                          tail_cap, _DTYPES.get(dtype, dtype),
+                          _FORMATS.get(format, format), scale)
+
+
+def prefix_workspace_bytes(p: WfPrefixParams) -> int:
+    return int(_lib.wf_prefix_workspace_bytes(ctypes.byref(p)))
+
+
+def alloc_prefix_workspace(p: WfPrefixParams, device) -> torch.Tensor | None:
+    nb = prefix_workspace_bytes(p)
+    return torch.empty(nb, dtype=torch.uint8, device=device) if nb else None
+
+
+def _expect_prefix(p, Q, K, Kx, V, Vx, row_idx, prefix_len, Kt, Vt, tail_len,
+                   O, lse) -> None:
+    dt, d = torch_dtype(p), p.head_dim
+    seqs, units = p.prefixes * p.share, p.prefixes * p.heads
+    rows = seqs * p.heads * p.group * p.q_len
+    plain = p.format == CACHE_PLAIN
+    for name, t in (("Q", Q), ("O", O)):
+        _expect(t, name, dt, rows * d)
+    _expect(lse, "lse", torch.float32, rows, nullable=True)
+    for name, t in (("K", K), ("V", V)):
+        _expect(t, name, dt if plain else torch.uint8, units * p.prefix_cap *
+                (d if plain else _code_bytes(d, p.format)),
+                nullable=p.prefix_rows == 0)
+    for name, t in (("Kx", Kx), ("Vx", Vx)):
+        _expect(t, name, torch.uint8, 0 if plain else
+                units * p.prefix_cap * (d // 32),
+                nullable=plain or p.prefix_rows == 0)
+    _expect(row_idx, "row_idx", torch.int32, units * p.prefix_rows,
+            nullable=True)
+    _expect(prefix_len, "prefix_len", torch.int32, p.prefixes, nullable=True)
+    for name, t in (("Kt", Kt), ("Vt", Vt)):
+        _expect(t, name, dt, seqs * p.heads * p.tail_cap * d,
+                nullable=p.tail_cap == 0)
+    _expect(tail_len, "tail_len", torch.int32, seqs, nullable=True)
+    _expect_device(Q, K, Kx, V, Vx, row_idx, prefix_len, Kt, Vt, tail_len, O,
+                   lse)
+
+
+def wf_prefix_attn(p, Q, K, Kx, V, Vx, row_idx, prefix_len, Kt, Vt, tail_len,
+                   O, lse, workspace, stream=None):
+    _expect_prefix(p, Q, K, Kx, V, Vx, row_idx, prefix_len, Kt, Vt, tail_len,
+                   O, lse)
+    ws, nb = _ws(workspace)
+    _check(_lib.wf_prefix_attn(
+        ctypes.byref(p), _ptr(Q), _ptr(K), _ptr(Kx), _ptr(V), _ptr(Vx),
+        _ptr(row_idx), _ptr(prefix_len), _ptr(Kt), _ptr(Vt), _ptr(tail_len),
+        _ptr(O), _ptr(lse), ws, nb, _stream(stream)))
+
+
+def prefix_attend(p: WfPrefixParams, Q, K, V, Kx=None, Vx=None, row_idx=None,
+                  prefix_len=None, Kt=None, Vt=None, tail_len=None,
+                  workspace=None, want_lse: bool = False, stream=None):
+    """Allocates O (and lse) and runs wf_prefix_attn.  Returns O, or (O, lse)
+    when want_lse.  What it allocates belongs to the stream the kernels run
+    on."""
+    with torch.cuda.stream(_torch_stream(stream)):
+        O = torch.empty_like(Q)
+        lse = (torch.empty(Q.shape[:-1], dtype=torch.float32, device=Q.device)
+               if want_lse else None)
+        if workspace is None:
+            workspace = alloc_prefix_workspace(p, Q.device)
+    wf_prefix_attn(p, Q, K, Kx, V, Vx, row_idx, prefix_len, Kt, Vt, tail_len,
+                   O, lse, workspace, stream)
+    return (O, lse) if want_lse else O
 
 
 # ------------------------------------------------------------ allocation

@@ -832,6 +832,135 @@ static wf_status recursive_impl(const wf_params* p, const float* prop, const voi
   return ok();
 }
 
+// ------------------------------------------------------------ quantised cache
+
+static wf_status check_cache(const wf_cache_params* p) {
+  if (!p) return fail(WF_ERR_INVALID_ARG, "params is NULL");
+  if (p->batch < 1 || p->heads < 1)
+    return fail(WF_ERR_INVALID_ARG, "batch (%d) and heads (%d) must be >= 1", p->batch, p->heads);
+  if (p->capacity < 1) return fail(WF_ERR_INVALID_ARG, "capacity %d < 1", p->capacity);
+  if (p->head_dim != 64 && p->head_dim != 128)
+    return fail(WF_ERR_UNSUPPORTED, "head_dim %d: only 64 and 128 are built", p->head_dim);
+  if (p->rows < 0) return fail(WF_ERR_INVALID_ARG, "rows %d < 0", p->rows);
+  if (p->dtype != WF_BF16 && p->dtype != WF_F32)
+    return fail(WF_ERR_INVALID_ARG, "unknown dtype %d", p->dtype);
+  if (p->format != WF_CACHE_E4M3 && p->format != WF_CACHE_E2M1)
+    return fail(WF_ERR_INVALID_ARG, "unknown cache format %d", p->format);
+  if ((long)p->batch * p->heads > (1L << 24))
+    return fail(WF_ERR_UNSUPPORTED, "batch*heads = %ld exceeds 2^24", (long)p->batch * p->heads);
+  if (cache_groups(*p) > INT32_MAX)
+    return fail(WF_ERR_UNSUPPORTED, "%ld rows in one call are too many",
+                (long)p->batch * p->heads * p->rows);
+  return WF_OK;
+}
+
+static wf_status cache_impl(const wf_cache_params* p, bool store, const void* K, const void* V,
+                            const int32_t* row_idx, const void* Kc, const void* Kx,
+                            const void* Vc, const void* Vx, void* stream) {
+  WF_TRY(check_cache(p));
+  if (p->rows == 0) return ok();
+  WF_TRY(check_ptr(K, "K", false));
+  WF_TRY(check_ptr(V, "V", false));
+  WF_TRY(check_ptr(row_idx, "row_idx", true));
+  WF_TRY(check_ptr(Kc, "Kc", false));
+  WF_TRY(check_ptr(Kx, "Kx", false));
+  WF_TRY(check_ptr(Vc, "Vc", false));
+  WF_TRY(check_ptr(Vx, "Vx", false));
+  if (!row_idx && (p->first < 0 || (long)p->first + p->rows > p->capacity))
+    return fail(WF_ERR_INVALID_ARG, "rows %d .. %ld are outside the capacity %d", p->first,
+                (long)p->first + p->rows, p->capacity);
+  (void)hipGetLastError();
+  WF_HIP(launch_cache(*p, store, K, V, row_idx, Kc, Kx, Vc, Vx, static_cast<hipStream_t>(stream)),
+         store ? "cache_store" : "cache_load");
+  return ok();
+}
+
+// ------------------------------------------------------------ shared prefix
+
+static wf_status check_prefix(const wf_prefix_params* p, PrefixPlan* plan) {
+  if (!p) return fail(WF_ERR_INVALID_ARG, "params is NULL");
+  if (p->prefixes < 1 || p->share < 1 || p->heads < 1 || p->group < 1 || p->q_len < 1)
+    return fail(WF_ERR_INVALID_ARG,
+                "prefixes (%d), share (%d), heads (%d), group (%d) and q_len (%d) must be >= 1",
+                p->prefixes, p->share, p->heads, p->group, p->q_len);
+  if (p->head_dim != 64 && p->head_dim != 128)
+    return fail(WF_ERR_UNSUPPORTED, "head_dim %d: only 64 and 128 are built", p->head_dim);
+  if (p->prefix_cap < 0 || p->prefix_rows < 0 || p->tail_cap < 0)
+    return fail(WF_ERR_INVALID_ARG, "prefix_cap (%d), prefix_rows (%d) and tail_cap (%d) must be >= 0",
+                p->prefix_cap, p->prefix_rows, p->tail_cap);
+  if (p->prefix_rows == 0 && p->tail_cap == 0)
+    return fail(WF_ERR_INVALID_ARG, "neither prefix rows nor own rows");
+  if (p->prefix_rows > 0 && p->prefix_cap == 0)
+    return fail(WF_ERR_INVALID_ARG, "prefix_rows %d of an empty prefix", p->prefix_rows);
+  if (p->prefix_cap > (1 << 30) || p->prefix_rows > (1 << 30) || p->tail_cap > (1 << 30))
+    return fail(WF_ERR_UNSUPPORTED, "more than 2^30 rows");
+  if (p->dtype != WF_BF16 && p->dtype != WF_F32)
+    return fail(WF_ERR_INVALID_ARG, "unknown dtype %d", p->dtype);
+  if (p->format != WF_CACHE_PLAIN && p->format != WF_CACHE_E4M3 && p->format != WF_CACHE_E2M1)
+    return fail(WF_ERR_INVALID_ARG, "unknown cache format %d", p->format);
+  if (!std::isfinite(p->scale)) return fail(WF_ERR_INVALID_ARG, "scale is not finite");
+  // every product below stays in 64 bits: each factor is held to 2^31 in turn
+  long rows = 1;
+  for (long f : {(long)p->prefixes, (long)p->share, (long)p->heads, (long)p->group, (long)p->q_len}) {
+    rows *= f;
+    if (rows > (1L << 30))
+      return fail(WF_ERR_UNSUPPORTED, "more than 2^30 query rows in one call");
+  }
+  *plan = plan_prefix(*p);
+  if (plan->items + 7 + plan->titems > INT32_MAX)
+    return fail(WF_ERR_UNSUPPORTED, "too many workgroups in one call");
+  return WF_OK;
+}
+
+static wf_status prefix_impl(const wf_prefix_params* p, const void* Q, const void* K,
+                             const void* Kx, const void* V, const void* Vx,
+                             const int32_t* row_idx, const int32_t* prefix_len, const void* Kt,
+                             const void* Vt, const int32_t* tail_len, void* O, float* lse,
+                             void* ws, size_t ws_bytes, void* stream) {
+  PrefixPlan plan;
+  WF_TRY(check_prefix(p, &plan));
+  WF_TRY(check_ptr(Q, "Q", false));
+  WF_TRY(check_ptr(O, "O", false));
+  WF_TRY(check_ptr(lse, "lse", true));
+  WF_TRY(check_ptr(row_idx, "row_idx", true));
+  WF_TRY(check_ptr(prefix_len, "prefix_len", true));
+  WF_TRY(check_ptr(tail_len, "tail_len", true));
+  if (p->prefix_rows > 0) {
+    WF_TRY(check_ptr(K, "K", false));
+    WF_TRY(check_ptr(V, "V", false));
+    if (p->format != WF_CACHE_PLAIN) {
+      WF_TRY(check_ptr(Kx, "Kx", false));
+      WF_TRY(check_ptr(Vx, "Vx", false));
+    }
+    if (!row_idx && p->prefix_rows > p->prefix_cap)
+      return fail(WF_ERR_INVALID_ARG, "prefix_rows %d exceeds prefix_cap %d", p->prefix_rows,
+                  p->prefix_cap);
+  }
+  if (p->tail_cap > 0) {
+    WF_TRY(check_ptr(Kt, "Kt", false));
+    WF_TRY(check_ptr(Vt, "Vt", false));
+  }
+  WF_TRY(check_workspace(ws, ws_bytes, plan.part_bytes + plan.pstat_bytes));
+  (void)hipGetLastError();
+  PrefixArgs a{};
+  a.Q = Q;
+  a.K = K;
+  a.V = V;
+  a.Kx = static_cast<const uint8_t*>(Kx);
+  a.Vx = static_cast<const uint8_t*>(Vx);
+  a.list = row_idx;
+  a.plen = prefix_len;
+  a.Kt = Kt;
+  a.Vt = Vt;
+  a.tlen = tail_len;
+  a.O = O;
+  a.lse = lse;
+  a.part = static_cast<float*>(ws);
+  a.pstat = ws ? reinterpret_cast<float*>(at(ws, plan.part_bytes)) : nullptr;
+  WF_HIP(launch_prefix(*p, a, static_cast<hipStream_t>(stream)), "prefix_attn");
+  return ok();
+}
+
 }  // namespace wf
 
 using namespace wf;
@@ -1107,12 +1236,40 @@ const char* wf_filter_attend_recursive_kernel_name(const wf_params* p, int32_t i
   return rec_kernel_name(*p, i);
 }
 
+wf_status wf_cache_store(const wf_cache_params* p, const void* K, const void* V,
+                         const int32_t* row_idx, void* Kc, void* Kx, void* Vc, void* Vx,
+                         void* stream) {
+  return cache_impl(p, true, K, V, row_idx, Kc, Kx, Vc, Vx, stream);
+}
+
+wf_status wf_cache_load(const wf_cache_params* p, const void* Kc, const void* Kx, const void* Vc,
+                        const void* Vx, const int32_t* row_idx, void* K, void* V, void* stream) {
+  return cache_impl(p, false, K, V, row_idx, Kc, Kx, Vc, Vx, stream);
+}
+
+size_t wf_prefix_workspace_bytes(const wf_prefix_params* p) {
+  PrefixPlan plan;
+  if (check_prefix(p, &plan) != WF_OK) return 0;
+  return plan.part_bytes + plan.pstat_bytes;
+}
+
+wf_status wf_prefix_attn(const wf_prefix_params* p, const void* Q, const void* K, const void* Kx,
+                         const void* V, const void* Vx, const int32_t* row_idx,
+                         const int32_t* prefix_len, const void* Kt, const void* Vt,
+                         const int32_t* tail_len, void* O, float* lse, void* workspace,
+                         size_t workspace_bytes, void* stream) {
+  return prefix_impl(p, Q, K, Kx, V, Vx, row_idx, prefix_len, Kt, Vt, tail_len, O, lse, workspace,
+                     workspace_bytes, stream);
+}
+
 wf_status wf_init(void) {
   WF_HIP(load_fast_kernels(), "loading the token-skim kernels");
   WF_HIP(load_scan_kernels(), "loading the scan kernels");
   WF_HIP(load_attn_kernels(), "loading the attention kernels");
   WF_HIP(load_skim_kernels(), "loading the skim kernels");
   WF_HIP(load_dwt_kernels(), "loading the DWT kernels");
+  WF_HIP(load_cache_kernels(), "loading the cache kernels");
+  WF_HIP(load_prefix_kernels(), "loading the prefix-attention kernels");
   void* scratch_ptr = nullptr;  // this file's code object and its scratch array
   WF_TRY(scratch_of_current_device(&scratch_ptr));
   return ok();

@@ -179,4 +179,50 @@ struct BlockWeightsArgs {
   int WPU;              // workgroups (block slices) per unit
 };
 
+struct CacheArgs {
+  void* K;              // [U][rows][D]
+  void* V;
+  const int32_t* idx;   // nullable: store [batch][rows], load [U][rows]
+  void* Kc;             // [U][cap][D] or [U][cap][D / 2] codes
+  void* Kx;             // [U][cap][D / 32] exponent bytes
+  void* Vc;
+  void* Vx;
+  int heads, rows, cap, first;
+  int blocks;           // workgroups per unit
+};
+
+// Work of one kind (the prefix, or the sequences' own rows) of a prefix
+// attention: units x splits of their keys x blocks of their query rows.
+struct PrefixPart {
+  int items;            // workgroups
+  int splits;           // key ranges per unit
+  int rps;              // keys per range (multiple of the tile)
+  int mblocks;          // blocks of query rows per unit
+  int M;                // query rows per unit
+  int kw;               // waves that take keys of a tile in turn (the others: query rows)
+};
+
+struct PrefixArgs {
+  const void* Q;        // [sequences][heads][R][D]
+  const void* K;        // [prefixes][heads][cap][D], or codes
+  const void* V;
+  const uint8_t* Kx;    // exponent bytes (quantised prefix)
+  const uint8_t* Vx;
+  const int32_t* list;  // nullable [prefixes][heads][rows]
+  const int32_t* plen;  // nullable [prefixes]
+  const void* Kt;       // [sequences][heads][T][D]
+  const void* Vt;
+  const int32_t* tlen;  // nullable [sequences]
+  void* O;              // [sequences][heads][R][D]
+  float* lse;           // nullable [sequences][heads][R]
+  float* part;          // [rows][slots][D] unnormalised partial outputs
+  float* pstat;         // [rows][slots][2] reference (log2 units), sum
+  PrefixPart p, t;      // the prefix; the sequences' own rows
+  int heads, share, R;  // R: group * q_len
+  int cap, rows, T;
+  int slots;            // p.splits + t.splits (1: no merge)
+  int ids;              // row ids in LDS (0: dense)
+  float scale;
+};
+
 }  // namespace wf

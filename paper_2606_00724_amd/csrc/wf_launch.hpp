@@ -299,4 +299,29 @@ hipError_t launch_attn_combine(const wf_params& p, long nrows,
                                const float* part, const float* pstat, void* O,
                                int fine, hipStream_t s);
 
+// The quantised cache: rows written (store) or read back.  cache_groups: the
+// workgroups of such a call.
+long cache_groups(const wf_cache_params& p);
+hipError_t launch_cache(const wf_cache_params& p, bool store, const void* K, const void* V,
+                        const int32_t* idx, const void* Kc, const void* Kx, const void* Vc,
+                        const void* Vx, hipStream_t s);
+hipError_t load_cache_kernels();
+
+// Attention over a shared prefix: its split into workgroups, and the two
+// launches (partials, merge).
+struct PrefixArgs;
+struct PrefixPlan {
+  int qw;            // 32-row query blocks per wave
+  int slots;         // partials per query row
+  int ids;           // row ids in LDS
+  long items, titems;  // workgroups for the prefix and for the sequences' own rows
+  int splits, rps, mblocks, kw;
+  int tsplits, trps, tmblocks, tkw;
+  size_t part_bytes, pstat_bytes;  // workspace (0 where a row has one partial)
+  size_t lds_bytes;
+};
+PrefixPlan plan_prefix(const wf_prefix_params& p);
+hipError_t launch_prefix(const wf_prefix_params& p, PrefixArgs& a, hipStream_t s);
+hipError_t load_prefix_kernels();
+
 }  // namespace wf
