@@ -30,6 +30,11 @@ HIPCC_FLAGS = [
     "-Wall", "-Wno-unused-function", "-Wno-unused-variable",
     f"-I{INCLUDE}",
 ]
+# The products of these files take their accumulators from either half of the
+# register file, whichever they are allocated to; by default they would all be
+# in the accumulation half, and the softmax between two products moves them
+# (prefix attention, 64 query rows a wave: 240 moves for 32 products).
+EXTRA_FLAGS = {"wf_prefix.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
 def hipcc() -> str:
@@ -46,7 +51,8 @@ def sources() -> list[str]:
 
 def _compile(src: str) -> str:
     obj = os.path.join(BUILD, os.path.basename(src)[:-4] + ".o")
-    cmd = [hipcc(), *HIPCC_FLAGS, "-c", src, "-o", obj]
+    cmd = [hipcc(), *HIPCC_FLAGS, *EXTRA_FLAGS.get(os.path.basename(src), []),
+           "-c", src, "-o", obj]
     res = subprocess.run(cmd, capture_output=True, text=True)
     # hipcc's host pass warns that it does not know the packed-fp32 feature
     noise = "packed-fp32-ops' is not a recognized feature"

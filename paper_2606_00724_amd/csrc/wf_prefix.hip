@@ -72,35 +72,161 @@ struct PrefixWave {
   u32x4 q[QW][QS];
   f32x16 O[QW][DT];
   float mref[QW], l[QW];
+  float nref[QW];  // -mref, 0 while that is -inf
+  bool neg;  // a negative scale: the scores change sign (and c2 is positive)
 
-  // 32 keys (rows sb .. sb + 31 of the tile, nr of the tile's rows valid)
-  __device__ __forceinline__ void step(const unsigned char* Kb, const unsigned char* Vb, int sb,
-                                       int nr, float c2) {
-    const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31;
-    f32x16 s[QW];
+  // LDS byte offsets of the lane's operands in a 32-row block (the swizzle goes
+  // by the row mod 16, so one offset serves all blocks).  The granules of a row
+  // differ in bits that the swizzle is XORed into, so that those of the other
+  // operands are this one's XOR a constant.
+  uint32_t ko, vo;
+  __device__ __forceinline__ void offsets() {
+    const int lane = threadIdx.x & 63, h = lane >> 5, i16 = lane & 15;
+    ko = tile_offset<T, G>(lane & 31, h);
+    // in each 16-lane group lane i points at row t0 + i / 4, channels c0 + 4 (i %
+    // 4) .. + 3, and receives rows t0 .. t0 + 3 of channel c0 + i
+    const int t0 = 4 * h + (i16 >> 2), c0 = (lane & 16) + 4 * (i16 & 3);
+    vo = tile_offset<T, G>(t0, c0 >> 3) + 2 * (c0 & 7);
+  }
+
+  // The lane's operand j of K in the block at LDS offset `at`: 16 bytes of its
+  // row, granule 2 j + h.
+  __device__ __forceinline__ u32x4 key(uint32_t at, int j) const {
+    return *(const __attribute__((address_space(3))) u32x4*)(size_t)((at + ko) ^ (32u * j));
+  }
+  __device__ __forceinline__ void keys(uint32_t at, u32x4 (&kf)[QS]) const {
+#pragma unroll
+    for (int j = 0; j < QS; ++j) kf[j] = key(at, j);
+  }
+  // Half of the lane's operand of V^T of 16 of the block's rows (bf16): rows 16
+  // kb + 8 k + 4 h .. + 3 of channel 32 d + l % 32.  (Eight rows on, the swizzle
+  // flips a granule's bit 1.)
+  __device__ __forceinline__ u32x2 val(uint32_t at, int kb, int d, int k) const {
+    return __builtin_bit_cast(
+        u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                   (__attribute__((address_space(3))) v4i16p*)(size_t)(
+                       ((at + vo) ^ (64u * d + 32u * k)) + (2 * kb + k) * 128 * G)));
+  }
+  // s = scores of 32 keys; lane: keys 8 (i / 4) + 4 h + i % 4 of query l % 32
+  __device__ __forceinline__ void scores(const u32x4 (&kf)[QS], f32x16 (&s)[QW]) const {
 #pragma unroll
     for (int b = 0; b < QW; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
 #pragma unroll
     for (int j = 0; j < QS; ++j) {
-      const u32x4 kf =
-          *reinterpret_cast<const u32x4*>(Kb + tile_offset<T, G>(sb + l32, 2 * j + h));
 #pragma unroll
       for (int b = 0; b < QW; ++b) {
         if constexpr (BF) {
-          s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf),
+          s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[j]),
                                                          __builtin_bit_cast(bf16x8, q[b][j]), s[b],
                                                          0, 0, 0);
         } else {
-          const f32x4 kv = __builtin_bit_cast(f32x4, kf), qv = __builtin_bit_cast(f32x4, q[b][j]);
+          const f32x4 kv = __builtin_bit_cast(f32x4, kf[j]), qv = __builtin_bit_cast(f32x4, q[b][j]);
 #pragma unroll
           for (int e = 0; e < 4; ++e)
             s[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(kv[e], qv[e], s[b], 0, 0, 0);
         }
       }
     }
-    // the lane holds keys sb + 8 (i / 4) + 4 h + i % 4 of query l % 32
+  }
+  __device__ __forceinline__ static void maxima(const f32x16 (&s)[QW], float (&mx)[QW]) {
+#pragma unroll
+    for (int b = 0; b < QW; ++b) {
+      float m = fmaxf(s[b][0], s[b][1]);
+#pragma unroll
+      for (int i = 2; i < 16; i += 2) m = fmaxf(m, fmaxf(s[b][i], s[b][i + 1]));
+      mx[b] = m;
+    }
+  }
+  // The reference moves only when a score passes it by 2^8: weights then stay
+  // below 2^8, their sums far from the fp32 range, and a rescale of the outputs
+  // is rare.
+  __device__ __forceinline__ void raise(const float (&mx)[QW], float c2) {
+    bool grow = false;
+#pragma unroll
+    for (int b = 0; b < QW; ++b) grow |= mx[b] * c2 > mref[b] + 8.f;
+    if (__builtin_amdgcn_ballot_w64(grow) != 0) {
+#pragma unroll
+      for (int b = 0; b < QW; ++b) {
+        const float mn = fmaxf(mref[b], fmaxf(mx[b], partner32(mx[b])) * c2);
+        const float al = mref[b] > -INFINITY ? __builtin_amdgcn_exp2f(mref[b] - mn) : 0.f;
+        mref[b] = mn;
+        nref[b] = mn > -INFINITY ? -mn : 0.f;
+        l[b] *= al;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) O[b][d][i] *= al;
+      }
+    }
+  }
+  // Weights of keys i0 .. i0 + 7 of the lane's, and their sum into l.  (The
+  // unrounded product less the reference: scores of thousands keep their
+  // differences.  While every score so far is -inf, their weights are 2^-inf =
+  // 0.)
+  __device__ __forceinline__ void weights(f32x16 (&s)[QW], int i0, float c2) {
+#pragma unroll
+    for (int b = 0; b < QW; ++b) {
+#pragma unroll
+      for (int i = i0; i < i0 + 8; ++i)
+        s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], c2, nref[b]));
+      l[b] += ((s[b][i0] + s[b][i0 + 1]) + (s[b][i0 + 2] + s[b][i0 + 3])) +
+              ((s[b][i0 + 4] + s[b][i0 + 5]) + (s[b][i0 + 6] + s[b][i0 + 7]));
+    }
+  }
+  // O^T += V^T P^T over 16 keys (bf16: the weights rounded to half a step of
+  // bf16, as the products' operands are)
+  __device__ __forceinline__ void add16(const f32x16 (&s)[QW], int kb, const u32x4 (&vf)[DT]) {
+    u32x4 pf[QW];
+#pragma unroll
+    for (int b = 0; b < QW; ++b)
+      pf[b] = u32x4{pack_bf16x2(s[b][8 * kb], s[b][8 * kb + 1]),
+                    pack_bf16x2(s[b][8 * kb + 2], s[b][8 * kb + 3]),
+                    pack_bf16x2(s[b][8 * kb + 4], s[b][8 * kb + 5]),
+                    pack_bf16x2(s[b][8 * kb + 6], s[b][8 * kb + 7])};
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int b = 0; b < QW; ++b)
+        O[b][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[d]),
+                                                          __builtin_bit_cast(bf16x8, pf[b]),
+                                                          O[b][d], 0, 0, 0);
+  }
+  // the same over the block's 32 keys in fp32
+  __device__ __forceinline__ void add32(const f32x16 (&s)[QW], const unsigned char* Vb, int sb) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int r = sb + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3);
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        const int c = 32 * d + (lane & 31);
+        const float vf =
+            *reinterpret_cast<const float*>(Vb + tile_offset<T, G>(r, c >> 2) + 4 * (c & 3));
+#pragma unroll
+        for (int b = 0; b < QW; ++b)
+          O[b][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, s[b][i], O[b][d], 0, 0, 0);
+      }
+    }
+  }
+
+  // 32 keys (rows sb .. sb + 31 of the tile, nr of the tile's rows valid)
+  __device__ __forceinline__ void step(const unsigned char* Kb, const unsigned char* Vb, int sb,
+                                       int nr, float c2) {
+    const uint32_t kat = lds_offset(Kb) + sb * 16 * G, vat = lds_offset(Vb) + sb * 16 * G;
+    const int h = (threadIdx.x & 63) >> 5;
+    u32x4 kf[QS];
+    f32x16 s[QW];
+    float mx[QW];
+    keys(kat, kf);
+    scores(kf, s);
+    if (neg) {
+#pragma unroll
+      for (int b = 0; b < QW; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[b][i] = -s[b][i];
+    }
     if (sb + 32 > nr) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
@@ -109,94 +235,103 @@ struct PrefixWave {
         for (int b = 0; b < QW; ++b) s[b][i] = off ? -INFINITY : s[b][i];
       }
     }
-    float mx[QW];
-    bool grow = false;
-#pragma unroll
-    for (int b = 0; b < QW; ++b) {
-      float m = s[b][0];
-#pragma unroll
-      for (int i = 1; i < 16; ++i) m = fmaxf(m, s[b][i]);
-      mx[b] = m * c2;
-      grow |= mx[b] > mref[b] + 8.f;
-    }
-    // The reference moves only when a score passes it by 2^8: weights then stay
-    // below 2^8, their sums far from the fp32 range, and a rescale of the
-    // outputs is rare.
-    if (__builtin_amdgcn_ballot_w64(grow) != 0) {
-#pragma unroll
-      for (int b = 0; b < QW; ++b) {
-        const float mn = fmaxf(mref[b], fmaxf(mx[b], partner32(mx[b])));
-        const float al = mref[b] > -INFINITY ? __builtin_amdgcn_exp2f(mref[b] - mn) : 0.f;
-        mref[b] = mn;
-        l[b] *= al;
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) O[b][d][i] *= al;
-      }
-    }
-#pragma unroll
-    for (int b = 0; b < QW; ++b) {
-      // (while every score so far is -inf, their weights are 2^-inf = 0)
-      const float ref = mref[b] > -INFINITY ? mref[b] : 0.f;
-      float z = 0.f;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        // (the unrounded product: scores of thousands keep their differences)
-        s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], c2, -ref));
-        z += s[b][i];
-      }
-      l[b] += z;
-    }
+    maxima(s, mx);
+    raise(mx, c2);
+    weights(s, 0, c2);
+    weights(s, 8, c2);
     if constexpr (BF) {
-      const uint32_t vb = lds_offset(Vb);
-      const int i16 = lane & 15;
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
-        u32x4 pf[QW];
-#pragma unroll
-        for (int b = 0; b < QW; ++b)
-          pf[b] = u32x4{pack_bf16x2(s[b][8 * kb], s[b][8 * kb + 1]),
-                        pack_bf16x2(s[b][8 * kb + 2], s[b][8 * kb + 3]),
-                        pack_bf16x2(s[b][8 * kb + 4], s[b][8 * kb + 5]),
-                        pack_bf16x2(s[b][8 * kb + 6], s[b][8 * kb + 7])};
-        const int t0 = sb + 16 * kb + 4 * h + (i16 >> 2);
+        u32x4 vf[DT];
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
-          // in each 16-lane group lane i points at row t0 + i / 4, channels c0 +
-          // 4 (i % 4) .. + 3, and receives rows t0 .. t0 + 3 of channel c0 + i
-          const int c0 = 32 * d + (lane & 16) + 4 * (i16 & 3);
-          const uint32_t o = 2 * (c0 & 7);
-          const v4i16p lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (__attribute__((address_space(3))) v4i16p*)(size_t)(
-                  vb + tile_offset<T, G>(t0, c0 >> 3) + o));
-          const v4i16p hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (__attribute__((address_space(3))) v4i16p*)(size_t)(
-                  vb + tile_offset<T, G>(t0 + 8, c0 >> 3) + o));
-          const u32x2 l2 = __builtin_bit_cast(u32x2, lo), h2 = __builtin_bit_cast(u32x2, hi);
-          const u32x4 vf = {l2[0], l2[1], h2[0], h2[1]};
-#pragma unroll
-          for (int b = 0; b < QW; ++b)
-            O[b][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                __builtin_bit_cast(bf16x8, vf), __builtin_bit_cast(bf16x8, pf[b]), O[b][d], 0, 0,
-                0);
+          const u32x2 lo = val(vat, kb, d, 0), hi = val(vat, kb, d, 1);
+          vf[d] = u32x4{lo[0], lo[1], hi[0], hi[1]};
         }
+        add16(s, kb, vf);
       }
     } else {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int r = sb + 8 * (i >> 2) + 4 * h + (i & 3);
-#pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          const int c = 32 * d + l32;
-          const float vf = *reinterpret_cast<const float*>(Vb + tile_offset<T, G>(r, c >> 2) +
-                                                           4 * (c & 3));
-#pragma unroll
-          for (int b = 0; b < QW; ++b)
-            O[b][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, s[b][i], O[b][d], 0, 0, 0);
-        }
-      }
+      add32(s, Vb, sb);
     }
+  }
+
+  // A block of the pipelined loop (bf16): the softmax and the product with V
+  // of one block (scores s, values at LDS offset vat) beside the scores sn of
+  // the next one (its keys kf in registers; refilled with those at knext).  A
+  // wave issues in order and waits for the matrix pipe at its next product, so
+  // only what stands between two products runs beside them: every product is
+  // followed by its share of the vector work, and the barriers hold that order.
+  __device__ __forceinline__ void block(uint32_t vat, uint32_t knext, u32x4 (&kf)[QS],
+                                        f32x16 (&s)[QW], f32x16 (&sn)[QW], float (&mx)[QW],
+                                        float c2) {
+    raise(mx, c2);
+    float z[QW];
+#pragma unroll
+    for (int b = 0; b < QW; ++b) z[b] = 0.f;
+    u32x4 p0[QW], p1[QW], v0[DT], v1[DT];
+    // weight e of 16 keys (of the block's first or second half)
+    auto weight = [&](int half, int e) __attribute__((always_inline)) {
+      const int b = e >> 3, i = 8 * half + (e & 7);
+      s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], c2, nref[b]));
+      z[b] += s[b][i];
+      if (e & 1) (half ? p1 : p0)[b][(e & 7) >> 1] = pack_bf16x2(s[b][i - 1], s[b][i]);
+    };
+    auto value = [&](int r) __attribute__((always_inline)) {
+      const int kb = r / (2 * DT), d = (r >> 1) % DT, k = r & 1;
+      const u32x2 y = val(vat, kb, d, k);
+      (kb ? v1 : v0)[d][2 * k] = y[0];
+      (kb ? v1 : v0)[d][2 * k + 1] = y[1];
+    };
+    constexpr int NQ = QS * QW, NV = DT * QW;  // products with K, with half of V
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+      const int j = n / QW, b = n % QW;
+      f32x16 c;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) c[i] = j ? sn[b][i] : 0.f;
+      sn[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[j]),
+                                                      __builtin_bit_cast(bf16x8, q[b][j]), c, 0, 0,
+                                                      0);
+#pragma unroll
+      for (int r = n * 4 * DT / NQ; r < (n + 1) * 4 * DT / NQ; ++r) value(r);
+#pragma unroll
+      for (int e = n * 8 * QW / NQ; e < (n + 1) * 8 * QW / NQ; ++e) weight(0, e);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int n = 0; n < NV; ++n) {
+      const int d = n / QW, b = n % QW;
+      O[b][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v0[d]),
+                                                        __builtin_bit_cast(bf16x8, p0[b]), O[b][d],
+                                                        0, 0, 0);
+#pragma unroll
+      for (int e = n * 8 * QW / NV; e < (n + 1) * 8 * QW / NV; ++e) weight(1, e);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int b = 0; b < QW; ++b) {
+      l[b] += z[b];
+      mx[b] = sn[b][0];
+    }
+#pragma unroll
+    for (int n = 0; n < NV; ++n) {
+      const int d = n / QW, b = n % QW;
+      O[b][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v1[d]),
+                                                        __builtin_bit_cast(bf16x8, p1[b]), O[b][d],
+                                                        0, 0, 0);
+#pragma unroll
+      for (int j = n * QS / NV; j < (n + 1) * QS / NV; ++j)
+        kf[j] = key(knext, j);
+#pragma unroll
+      for (int e = n * 8 * QW / NV; e < (n + 1) * 8 * QW / NV; ++e) {
+        const int i = 2 * (e & 7);
+        mx[e >> 3] = fmaxf(mx[e >> 3], fmaxf(sn[e >> 3][i], sn[e >> 3][i + 1]));
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    // (what is used after the block only would be moved there)
+#pragma unroll
+    for (int b = 0; b < QW; ++b) asm volatile("" : "+v"(l[b]), "+v"(mx[b]));
   }
 };
 
@@ -244,25 +379,45 @@ struct QuantStage {
         const int p = i * kPrefixBlock + threadIdx.x, r = p / PPR, pc = p % PPR;
         if (PT % kPrefixBlock != 0 && p >= PT) break;
         const float s = block_scale(x[m][i]);
+        unsigned char* dst = m ? Vb : Kb;
+        if constexpr (sizeof(T) == 2) {
+          // v_cvt_scalef32_pk_bf16: two codes times the power of two, rounded to
+          // nearest even (equal to decode8 and pack_bf16x2 for every code and
+          // exponent byte 1 .. 255; byte 0 means 0 and not 2^-127)
+          const u32x4 c = x[m][i] ? w[m][i] : u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
-        for (int k = 0; k < CPP / 8; ++k) {  // eight channels each
-          float v[8];
-          u32x2 c;
-          if constexpr (FMT == WF_CACHE_E4M3)
-            c = u32x2{w[m][i][2 * k], w[m][i][2 * k + 1]};
-          else
-            c = u32x2{w[m][i][k], 0u};
-          decode8<FMT>(c, s, v);
-          unsigned char* dst = m ? Vb : Kb;
-          const int g = pc * (CPP / 8) + k;  // eight channels: one granule of bf16, two of fp32
-          if constexpr (sizeof(T) == 2) {
-            *reinterpret_cast<u32x4*>(dst + tile_offset<T, G>(r, g)) =
-                u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
-                      pack_bf16x2(v[6], v[7])};
-          } else {
-            *reinterpret_cast<f32x4*>(dst + tile_offset<T, G>(r, 2 * g)) =
-                f32x4{v[0], v[1], v[2], v[3]};
-            *reinterpret_cast<f32x4*>(dst + tile_offset<T, G>(r, 2 * g + 1)) =
+          for (int k = 0; k < CPP / 8; ++k) {  // eight channels, one granule each
+            u32x4 g;
+            if constexpr (FMT == WF_CACHE_E4M3) {
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                g[2 * e] = __builtin_bit_cast(
+                    uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[2 * k + e], s, false));
+                g[2 * e + 1] = __builtin_bit_cast(
+                    uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[2 * k + e], s, true));
+              }
+            } else {
+              g[0] = __builtin_bit_cast(uint32_t,
+                                        __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[k], s, 0));
+              g[1] = __builtin_bit_cast(uint32_t,
+                                        __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[k], s, 1));
+              g[2] = __builtin_bit_cast(uint32_t,
+                                        __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[k], s, 2));
+              g[3] = __builtin_bit_cast(uint32_t,
+                                        __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[k], s, 3));
+            }
+            *reinterpret_cast<u32x4*>(dst + tile_offset<T, G>(r, pc * (CPP / 8) + k)) = g;
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < CPP / 8; ++k) {  // eight channels, two granules each
+            float v[8];
+            const u32x2 c = FMT == WF_CACHE_E4M3 ? u32x2{w[m][i][2 * k % 4], w[m][i][(2 * k + 1) % 4]}
+                                                 : u32x2{w[m][i][k], 0u};
+            decode8<FMT>(c, s, v);
+            const int g = 2 * (pc * (CPP / 8) + k);
+            *reinterpret_cast<f32x4*>(dst + tile_offset<T, G>(r, g)) = f32x4{v[0], v[1], v[2], v[3]};
+            *reinterpret_cast<f32x4*>(dst + tile_offset<T, G>(r, g + 1)) =
                 f32x4{v[4], v[5], v[6], v[7]};
           }
         }
@@ -276,7 +431,8 @@ __global__ __launch_bounds__(kPrefixBlock, 1) void prefix_attn_kernel(PrefixArgs
   constexpr int KT = W::KT, G = W::G, MB = W::MB, DT = W::DT, QS = W::QS;
   extern __shared__ __align__(16) unsigned char smem[];  // [2][K, V] tiles, then row ids
   int32_t* ids = reinterpret_cast<int32_t*>(smem + 4 * MB);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = lane >> 5, l32 = lane & 31;
 
   // The workgroup's item.  Prefix items first, their blocks of query rows
@@ -307,16 +463,17 @@ __global__ __launch_bounds__(kPrefixBlock, 1) void prefix_attn_kernel(PrefixArgs
     return ((long)n * a.heads + head) * a.R + (own ? m : m % a.R);
   };
   W w;
+  w.offsets();
   const float c2 = fabsf(a.scale) * kLog2e;
-  const uint32_t flip = a.scale < 0.f ? (W::BF ? 0x80008000u : 0x80000000u) : 0u;
+  w.neg = a.scale < 0.f;
 #pragma unroll
   for (int b = 0; b < QW; ++b) {
     const T* src = reinterpret_cast<const T*>(a.Q) + row_of(min(m0 + 32 * b + l32, M - 1)) * D;
 #pragma unroll
     for (int j = 0; j < QS; ++j)
-      w.q[b][j] = reinterpret_cast<const u32x4*>(src)[2 * j + h] ^ u32x4{flip, flip, flip, flip};
+      w.q[b][j] = reinterpret_cast<const u32x4*>(src)[2 * j + h];
     w.mref[b] = -INFINITY;
-    w.l[b] = 0.f;
+    w.nref[b] = w.l[b] = 0.f;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -334,7 +491,7 @@ __global__ __launch_bounds__(kPrefixBlock, 1) void prefix_attn_kernel(PrefixArgs
     rows.id0 = k0;
     // the next kPrefixIds ids of a list, from tile t on, when tile t starts them
     // (no wave reads older ones: tile t - 1 has been queued by all)
-    auto stage_ids = [&](int t) {
+    auto stage_ids = [&](int t) __attribute__((always_inline)) {
       if (!rows.ids || t * KT % kPrefixIds != 0) return;  // uniform
       rows.id0 = k0 + t * KT;
       lds_barrier();
@@ -342,30 +499,89 @@ __global__ __launch_bounds__(kPrefixBlock, 1) void prefix_attn_kernel(PrefixArgs
         ids[i] = a.list[(long)unit * a.rows + rows.id0 + i];
       __syncthreads();
     };
-    // the products of tile t, in `buf`
-    auto compute = [&](int t, int buf) {
-      unsigned char* Kb = smem + buf * 2 * MB;
-      unsigned char* Vb = Kb + MB;
-      const int nr = min(KT, nk - t * KT);
-      if (nr < KT) {
-        // rows past the range repeat its last one: 0 there, as 0 times an
-        // infinite value is NaN
-        for (int i = nr * G + threadIdx.x; i < KT * G; i += kPrefixBlock)
-          reinterpret_cast<u32x4*>(Vb)[i] = u32x4{0u, 0u, 0u, 0u};
-        lds_barrier();
+    // The query operands, loaded above: here, so that the compiler's wait for them
+    // is no wait for a tile later on.  Those of 64 rows of 128 channels are put
+    // into the accumulation half of the registers, from where the products take
+    // them: in the other half they were copied there and back in every block.
+    auto queries = [&]() __attribute__((always_inline)) {
+      __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+      if constexpr (W::BF && QW * QS >= 16) {
+#pragma unroll
+        for (int b = 0; b < QW; ++b)
+#pragma unroll
+          for (int j = 0; j < QS; ++j) asm volatile("" : "+a"(w.q[b][j]));
       }
-      if (active)
-        for (int sb = 32 * kw; sb < nr; sb += 32 * KW) w.step(Kb, Vb, sb, nr, c2);
+    };
+    // The tiles in turn, through two LDS slots.  arrive(t): tile t is in its slot
+    // for every wave; leave(t): no wave reads tile t any more.
+    auto run = [&](auto&& arrive, auto&& leave) __attribute__((always_inline)) {
+      // whole tiles in the pipelined loop (bf16)
+      const int nf = !W::BF || w.neg ? 0 : nk / KT;
+      auto slot_of = [&](int t) { return smem + (t & 1) * 2 * MB; };
+      arrive(0);
+      if constexpr (W::BF) {
+        if (nf > 0) {
+          const int nb = KT / 32 / KW;  // blocks of a tile that are the wave's
+          // LDS offset of the wave's i-th block in tile t
+          const uint32_t lds0 = lds_offset(smem) + kw * 512 * G;
+          const int stride = KW * 512 * G;
+          auto at = [&](int t, int i) { return lds0 + (t & 1) * 2 * MB + i * stride; };
+          u32x4 kf[QS];
+          f32x16 s0[QW], s1[QW];
+          float mx[QW];
+          w.keys(at(0, 0), kf);
+          w.scores(kf, s0);
+          W::maxima(s0, mx);
+          if (nb > 1) w.keys(at(0, 1), kf);
+          const int n = nf * nb;
+          int t = 0, i = 0;
+          auto one = [&](f32x16(&s)[QW], f32x16(&sn)[QW]) __attribute__((always_inline)) {
+            const bool last = i == nb - 1;
+            if (last && t + 1 < nt) {
+              arrive(t + 1);
+              w.keys(at(t + 1, 0), kf);  // (a partial tile's: not used)
+            }
+            // the keys after next, where they are in the next block's tile
+            const bool two = last ? nb > 1 && t + 1 < nt : i + 2 < nb;
+            const uint32_t next = last ? at(t + two, two) : at(t, two ? i + 2 : i);
+            // (also for query rows past the last: they repeat it)
+            w.block(at(t, i) + MB, next, kf, s, sn, mx, c2);
+            if (last) leave(t);
+            t += last ? 1 : 0;
+            i = last ? 0 : i + 1;
+          };
+          for (int j = 0; j < n; j += 2) {
+            one(s0, s1);
+            if (j + 1 < n) one(s1, s0);
+          }
+        }
+      }
+      for (int t = nf; t < nt; ++t) {
+        if (t > nf) arrive(t);
+        const int nr = min(KT, nk - t * KT);
+        unsigned char* Vb = slot_of(t) + MB;
+        if (nr < KT) {  // rows past the range repeat its last one: 0 there, as 0
+                        // times an infinite value is NaN
+          for (int i = nr * G + threadIdx.x; i < KT * G; i += kPrefixBlock)
+            reinterpret_cast<u32x4*>(Vb)[i] = u32x4{0u, 0u, 0u, 0u};
+          lds_barrier();
+        }
+        if (active)
+          for (int sb = 32 * kw; sb < nr; sb += 32 * KW) w.step(slot_of(t), Vb, sb, nr, c2);
+        leave(t);
+      }
     };
     if (FMT == WF_CACHE_PLAIN || own) {
-      // tiles stream through two LDS slots by direct loads
+      // direct loads to LDS, up to two tiles ahead
       const T* Kg = reinterpret_cast<const T*>(own ? a.Kt : a.K) + (long)unit * rows.cap * D;
       const T* Vg = reinterpret_cast<const T*>(own ? a.Vt : a.V) + (long)unit * rows.cap * D;
       constexpr int IPW = KT * G / (64 * kPrefixWaves);  // loads per wave and matrix
       constexpr int RPI = 64 / G;
       const uint32_t lds0 = lds_offset(smem);
-      auto issue = [&](int t) {
+      int issued = 0;  // tiles queued so far
+      auto issue = [&](int t) __attribute__((always_inline)) {
         stage_ids(t);
+        issued = t + 1;
         const uint32_t at = lds0 + (t & 1) * 2 * MB;
         long off[IPW];
 #pragma unroll
@@ -381,41 +597,38 @@ __global__ __launch_bounds__(kPrefixBlock, 1) void prefix_attn_kernel(PrefixArgs
           async_load16<false>(Vg + off[i], __builtin_amdgcn_readfirstlane(to + MB));
         }
       };
-      // consume the q operands before loads are queued: the compiler's own wait
-      // for them then sits here
-#pragma unroll
-      for (int b = 0; b < QW; ++b)
-#pragma unroll
-        for (int j = 0; j < QS; ++j) asm volatile("" ::"v"(w.q[b][j]));
       issue(0);
-      for (int t = 0; t < nt; ++t) {
-        if (t + 1 < nt) {
-          issue(t + 1);
-          wait_vmcnt_chunks<2 * IPW>(1);
-        } else {
-          wait_vmcnt_chunks<2 * IPW>(0);
-        }
-        lds_barrier();  // tile t visible
-        compute(t, t & 1);
-        lds_barrier();  // everyone is past tile t
-      }
+      queries();
+      if (nt > 1) issue(1);
+      run(
+          [&](int t) __attribute__((always_inline)) {
+            // tile t + 1 may be in flight: it is queued when tile t - 1 is left,
+            // after tile t arrives in the pipelined loop, before in the other
+            wait_vmcnt_chunks<2 * IPW>(issued > t + 1 ? 1 : 0);
+            lds_barrier();
+          },
+          [&](int t) __attribute__((always_inline)) {
+            lds_barrier();
+            if (t + 2 < nt) issue(t + 2);
+          });
     } else {
       // codes are loaded to registers a tile ahead, and decoded into LDS
       if constexpr (FMT != WF_CACHE_PLAIN) {
         QuantStage<T, D, FMT> st;
         stage_ids(0);
         st.load(a, rows, unit, 0);
-        for (int t = 0; t < nt; ++t) {
-          unsigned char* Kb = smem + (t & 1) * 2 * MB;
-          st.commit(Kb, Kb + MB);
-          if (t + 1 < nt) {
-            stage_ids(t + 1);
-            st.load(a, rows, unit, (t + 1) * KT);
-          }
-          lds_barrier();  // tile t visible, everyone is past tile t - 1
-          compute(t, t & 1);
-        }
-        lds_barrier();
+        queries();
+        run(
+            [&](int t) __attribute__((always_inline)) {
+              unsigned char* Kb = smem + (t & 1) * 2 * MB;
+              st.commit(Kb, Kb + MB);
+              if (t + 1 < nt) {
+                stage_ids(t + 1);
+                st.load(a, rows, unit, (t + 1) * KT);
+              }
+              lds_barrier();
+            },
+            [&](int) __attribute__((always_inline)) { lds_barrier(); });
       }
     }
   }
@@ -515,37 +728,73 @@ __global__ __launch_bounds__(kPrefixBlock, 1) void prefix_attn_kernel(PrefixArgs
   }
 }
 
-// Merges the partials of each query row: a thread takes eight channels.
-template <typename T>
+// Merges the partials of each query row.  A thread takes eight channels of every
+// SG-th partial of a row, four of them in flight; the SG threads of a row's
+// channels meet in LDS.  (33 partials of 256 rows: 24 us with SG = 1.)
+template <typename T, int SG>
 __global__ __launch_bounds__(kBlock) void prefix_merge_kernel(PrefixArgs a, long rows, int D) {
-  const int tpr = D / 8;
-  const long row = (long)blockIdx.x * (kBlock / tpr) + threadIdx.x / tpr;
-  if (row >= rows) return;
-  const int c0 = (threadIdx.x % tpr) * 8;
-  const float* st = a.pstat + row * a.slots * 2;
-  float M = -INFINITY;
-  for (int s = 0; s < a.slots; ++s) M = fmaxf(M, st[2 * s]);
-  float z = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < a.slots; ++s) {
-    const float m = st[2 * s], zs = st[2 * s + 1];
-    if (m == -INFINITY && zs == 0.f) continue;  // an empty range has no output
-    const float f = m > -INFINITY ? __builtin_amdgcn_exp2f(m - M) : 1.f;  // (zs NaN)
-    const f32x4* src = reinterpret_cast<const f32x4*>(a.part + (row * a.slots + s) * D + c0);
-    const f32x4 x = src[0], y = src[1];
-    z += f * zs;
+  const int tpr = D / 8, rpb = kBlock / (tpr * SG);
+  const int c = threadIdx.x % tpr, sg = threadIdx.x / tpr % SG, rl = threadIdx.x / (tpr * SG);
+  const long row = (long)blockIdx.x * rpb + rl;
+  float M = -INFINITY, z = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  // one partial into the running ones; an empty range (-inf, 0) has no output
+  auto add = [&](float m, float zs, const float* x) {
+    if (m == -INFINITY && zs == 0.f) return;
+    const float mn = fmaxf(M, m);
+    // (all scores -inf or NaN: zs says it)
+    const float f = m > -INFINITY ? __builtin_amdgcn_exp2f(m - mn) : 1.f;
+    const float g = M > -INFINITY ? __builtin_amdgcn_exp2f(M - mn) : 1.f;
+    M = mn;
+    z = z * g + f * zs;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      o[e] += f * x[e];
-      o[4 + e] += f * y[e];
+    for (int e = 0; e < 8; ++e) o[e] = o[e] * g + f * x[e];
+  };
+  if (row < rows) {
+    const float* st = a.pstat + row * a.slots * 2;
+    const float* src = a.part + row * a.slots * D + 8 * c;
+    constexpr int F = 4;
+    for (int s0 = sg; s0 < a.slots; s0 += F * SG) {
+      float m[F], zs[F];
+      f32x4 x[F][2];
+#pragma unroll
+      for (int k = 0; k < F; ++k) {
+        const int s = min(s0 + k * SG, a.slots - 1);
+        m[k] = s0 + k * SG < a.slots ? st[2 * s] : -INFINITY;
+        zs[k] = s0 + k * SG < a.slots ? st[2 * s + 1] : 0.f;
+        x[k][0] = reinterpret_cast<const f32x4*>(src + (long)s * D)[0];
+        x[k][1] = reinterpret_cast<const f32x4*>(src + (long)s * D)[1];
+      }
+#pragma unroll
+      for (int k = 0; k < F; ++k) {
+        const float v[8] = {x[k][0][0], x[k][0][1], x[k][0][2], x[k][0][3],
+                            x[k][1][0], x[k][1][1], x[k][1][2], x[k][1][3]};
+        add(m[k], zs[k], v);
+      }
     }
   }
+  if constexpr (SG > 1) {
+    __shared__ float sh[kBlock][11];  // (odd stride: no bank met twice)
+    float* mine = sh[threadIdx.x];
+    mine[0] = M;
+    mine[1] = z;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) mine[2 + e] = o[e];
+    __syncthreads();
+    if (sg != 0) return;  // no barrier follows
+#pragma unroll
+    for (int k = 1; k < SG; ++k) {
+      const float* other = sh[threadIdx.x + k * tpr];
+      add(other[0], other[1], other + 2);
+    }
+  }
+  if (row >= rows) return;
   const float inv = z == 0.f ? 0.f : 1.f / z;
 #pragma unroll
   for (int e = 0; e < 8; ++e) o[e] *= inv;
-  T* dst = reinterpret_cast<T*>(a.O) + row * D + c0;
+  T* dst = reinterpret_cast<T*>(a.O) + row * D + 8 * c;
   put4<T>(dst, o[0], o[1], o[2], o[3]);
   put4<T>(dst + 4, o[4], o[5], o[6], o[7]);
-  if (a.lse && c0 == 0) a.lse[row] = z == 0.f ? -INFINITY : (M + __log2f(z)) * kLn2;
+  if (a.lse && c == 0) a.lse[row] = z == 0.f ? -INFINITY : (M + __log2f(z)) * kLn2;
 }
 
 // ------------------------------------------------------------ host side
@@ -625,6 +874,26 @@ static hipError_t prefix_launch(const PrefixArgs& a, size_t lds, hipStream_t s) 
   return hipGetLastError();
 }
 
+// Threads per row and channels in the merge: enough for every partial of a row to
+// be in flight.
+template <typename T>
+static hipError_t merge_launch(const PrefixArgs& a, long rows, int D, hipStream_t s) {
+  const int sg = a.slots <= 4 ? 1 : a.slots <= 16 ? 4 : 16;
+  auto go = [&](auto n) {
+    constexpr int SG = decltype(n)::value;
+    const int rpb = kBlock / (D / 8 * SG);
+    hipLaunchKernelGGL((prefix_merge_kernel<T, SG>), dim3((unsigned)((rows + rpb - 1) / rpb)),
+                       dim3(kBlock), 0, s, a, rows, D);
+  };
+  if (sg == 1)
+    go(std::integral_constant<int, 1>{});
+  else if (sg == 4)
+    go(std::integral_constant<int, 4>{});
+  else
+    go(std::integral_constant<int, 16>{});
+  return hipGetLastError();
+}
+
 hipError_t launch_prefix(const wf_prefix_params& p, PrefixArgs& a, hipStream_t s) {
   const PrefixPlan l = plan_prefix(p);
   a.heads = p.heads;
@@ -659,13 +928,8 @@ hipError_t launch_prefix(const wf_prefix_params& p, PrefixArgs& a, hipStream_t s
   hipError_t e = p.dtype == WF_BF16 ? by_dim(bf16_t{}) : by_dim(float{});
   if (e != hipSuccess || l.slots == 1) return e;
   const long rows = (long)p.prefixes * p.share * p.heads * a.R;
-  const int rpb = kBlock / (p.head_dim / 8);
-  const dim3 grid((unsigned)((rows + rpb - 1) / rpb));
-  if (p.dtype == WF_BF16)
-    hipLaunchKernelGGL(prefix_merge_kernel<bf16_t>, grid, dim3(kBlock), 0, s, a, rows, p.head_dim);
-  else
-    hipLaunchKernelGGL(prefix_merge_kernel<float>, grid, dim3(kBlock), 0, s, a, rows, p.head_dim);
-  return hipGetLastError();
+  return p.dtype == WF_BF16 ? merge_launch<bf16_t>(a, rows, p.head_dim, s)
+                            : merge_launch<float>(a, rows, p.head_dim, s);
 }
 
 hipError_t load_prefix_kernels() {
