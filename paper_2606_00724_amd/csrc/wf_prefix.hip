@@ -255,16 +255,57 @@ struct PrefixWave {
     }
   }
 
-  // A block of the pipelined loop (bf16): the softmax and the product with V
-  // of one block (scores s, values at LDS offset vat) beside the scores sn of
-  // the next one (its keys kf in registers; refilled with those at knext).  A
-  // wave issues in order and waits for the matrix pipe at its next product, so
-  // only what stands between two products runs beside them: every product is
-  // followed by its share of the vector work, and the barriers hold that order.
+  // The pipelined loop (bf16) keeps the next block's scores in log2 units less
+  // the reference, t = s c2 - mref, and their maximum mx.  Before the block's
+  // weights are taken the reference is raised where t passes it (see raise).
+  float limit[QW];  // 8; -inf while the reference is -inf
+  __device__ __forceinline__ void raise_shifted(f32x16 (&t)[QW], const float (&mx)[QW]) {
+    bool grow = false;
+#pragma unroll
+    for (int b = 0; b < QW; ++b) grow |= mx[b] > limit[b];
+    if (__builtin_amdgcn_ballot_w64(grow) != 0) {
+#pragma unroll
+      for (int b = 0; b < QW; ++b) {
+        const float up = fmaxf(mx[b], partner32(mx[b]));
+        const bool first = mref[b] == -INFINITY;
+        const float mn = first ? up : fmaxf(mref[b], mref[b] + up);
+        const float by = mn > -INFINITY ? mn + nref[b] : 0.f;  // (nref: 0 or -mref)
+        const float al = first ? 0.f : __builtin_amdgcn_exp2f(-by);
+        mref[b] = mn;
+        nref[b] = mn > -INFINITY ? -mn : 0.f;
+        limit[b] = mn > -INFINITY ? 8.f : -INFINITY;
+        l[b] *= al;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) t[b][i] -= by;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) O[b][d][i] *= al;
+      }
+    }
+  }
+  __device__ __forceinline__ void shift(f32x16 (&t)[QW], float (&mx)[QW], float c2) const {
+#pragma unroll
+    for (int b = 0; b < QW; ++b) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) t[b][i] = fmaf(t[b][i], c2, nref[b]);
+      mx[b] = fmaxf(t[b][0], t[b][1]);
+#pragma unroll
+      for (int i = 2; i < 16; i += 2) mx[b] = fmaxf(mx[b], fmaxf(t[b][i], t[b][i + 1]));
+    }
+  }
+
+  // A block of that loop: weights of one block (shifted scores s) and their
+  // product with V (at LDS offset vat) beside the scores sn of the next block
+  // (its keys kf in registers; refilled with those at knext).  A wave issues in
+  // order and waits for the matrix pipe at its next product, so only what stands
+  // between two products runs beside them: every product (32 cycles) is followed
+  // by its share of the vector work, four to six instructions, and the barriers
+  // hold that order.
   __device__ __forceinline__ void block(uint32_t vat, uint32_t knext, u32x4 (&kf)[QS],
                                         f32x16 (&s)[QW], f32x16 (&sn)[QW], float (&mx)[QW],
                                         float c2) {
-    raise(mx, c2);
+    raise_shifted(s, mx);
     float z[QW];
 #pragma unroll
     for (int b = 0; b < QW; ++b) z[b] = 0.f;
@@ -272,9 +313,14 @@ struct PrefixWave {
     // weight e of 16 keys (of the block's first or second half)
     auto weight = [&](int half, int e) __attribute__((always_inline)) {
       const int b = e >> 3, i = 8 * half + (e & 7);
-      s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], c2, nref[b]));
+      s[b][i] = __builtin_amdgcn_exp2f(s[b][i]);
       z[b] += s[b][i];
-      if (e & 1) (half ? p1 : p0)[b][(e & 7) >> 1] = pack_bf16x2(s[b][i - 1], s[b][i]);
+      if (e & 1) {
+        // (each weight rounded to bf16, as the products' operands are)
+        uint32_t w = pack_bf16x2(s[b][i - 1], s[b][i]);
+        asm volatile("" : "+v"(w), "+v"(z[b]));  // here, and not where it is used
+        (half ? p1 : p0)[b][(e & 7) >> 1] = w;
+      }
     };
     auto value = [&](int r) __attribute__((always_inline)) {
       const int kb = r / (2 * DT), d = (r >> 1) % DT, k = r & 1;
@@ -309,31 +355,43 @@ struct PrefixWave {
       __builtin_amdgcn_sched_barrier(0);
     }
 #pragma unroll
-    for (int b = 0; b < QW; ++b) {
-      l[b] += z[b];
-      mx[b] = sn[b][0];
-    }
-#pragma unroll
     for (int n = 0; n < NV; ++n) {
       const int d = n / QW, b = n % QW;
       O[b][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v1[d]),
                                                         __builtin_bit_cast(bf16x8, p1[b]), O[b][d],
                                                         0, 0, 0);
 #pragma unroll
-      for (int j = n * QS / NV; j < (n + 1) * QS / NV; ++j)
-        kf[j] = key(knext, j);
+      for (int j = n * QS / NV; j < (n + 1) * QS / NV; ++j) kf[j] = key(knext, j);
 #pragma unroll
       for (int e = n * 8 * QW / NV; e < (n + 1) * 8 * QW / NV; ++e) {
-        const int i = 2 * (e & 7);
-        mx[e >> 3] = fmaxf(mx[e >> 3], fmaxf(sn[e >> 3][i], sn[e >> 3][i + 1]));
+        const int g = e >> 3, i = 2 * (e & 7);
+        sn[g][i] = fmaf(sn[g][i], c2, nref[g]);
+        sn[g][i + 1] = fmaf(sn[g][i + 1], c2, nref[g]);
+        const float two = fmaxf(sn[g][i], sn[g][i + 1]);
+        mx[g] = i ? fmaxf(mx[g], two) : two;
+        asm volatile("" : "+v"(mx[g]));
       }
       __builtin_amdgcn_sched_barrier(0);
     }
-    // (what is used after the block only would be moved there)
 #pragma unroll
-    for (int b = 0; b < QW; ++b) asm volatile("" : "+v"(l[b]), "+v"(mx[b]));
+    for (int b = 0; b < QW; ++b) {
+      l[b] += z[b];
+      asm volatile("" : "+v"(l[b]));
+    }
   }
 };
+
+// 16 bytes per lane from base + off straight to LDS (lane l's at `lds` + 16 l).
+// Waited for as async_load16's.
+__device__ __forceinline__ void tile_load(const void* base, uint32_t off, uint32_t lds) {
+  asm volatile(
+      "s_mov_b32 m0, %2\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %0, %1"
+      :
+      : "v"(off), "s"(base), "s"(lds)
+      : "memory", "m0");
+}
 
 template <typename T>
 __device__ __forceinline__ void put4(T* p, float a, float b, float c, float d);
@@ -473,6 +531,7 @@ __global__ __launch_bounds__(kPrefixBlock, 1) void prefix_attn_kernel(PrefixArgs
     for (int j = 0; j < QS; ++j)
       w.q[b][j] = reinterpret_cast<const u32x4*>(src)[2 * j + h];
     w.mref[b] = -INFINITY;
+    w.limit[b] = -INFINITY;
     w.nref[b] = w.l[b] = 0.f;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
@@ -531,7 +590,7 @@ __global__ __launch_bounds__(kPrefixBlock, 1) void prefix_attn_kernel(PrefixArgs
           float mx[QW];
           w.keys(at(0, 0), kf);
           w.scores(kf, s0);
-          W::maxima(s0, mx);
+          w.shift(s0, mx, c2);
           if (nb > 1) w.keys(at(0, 1), kf);
           const int n = nf * nb;
           int t = 0, i = 0;
@@ -577,24 +636,35 @@ __global__ __launch_bounds__(kPrefixBlock, 1) void prefix_attn_kernel(PrefixArgs
       const T* Vg = reinterpret_cast<const T*>(own ? a.Vt : a.V) + (long)unit * rows.cap * D;
       constexpr int IPW = KT * G / (64 * kPrefixWaves);  // loads per wave and matrix
       constexpr int RPI = 64 / G;
-      const uint32_t lds0 = lds_offset(smem);
+      constexpr int RB = D * W::ES;                      // bytes of a row
+      const uint32_t lds0 = lds_offset(smem) + 1024u * IPW * wave;
+      // byte offsets of the lane's loads in a tile of consecutive rows
+      uint32_t off[IPW];
+#pragma unroll
+      for (int i = 0; i < IPW; ++i) {
+        const int r = (wave * IPW + i) * RPI + lane / G;
+        off[i] = r * RB + 16 * ((lane % G) ^ tile_swz<T, G>(r));
+      }
       int issued = 0;  // tiles queued so far
       auto issue = [&](int t) __attribute__((always_inline)) {
         stage_ids(t);
         issued = t + 1;
         const uint32_t at = lds0 + (t & 1) * 2 * MB;
-        long off[IPW];
+        if (!rows.ids && nk - t * KT >= KT) {  // uniform
+          const T* kt = Kg + (long)(k0 + t * KT) * D;
+          const T* vt = Vg + (long)(k0 + t * KT) * D;
 #pragma unroll
-        for (int i = 0; i < IPW; ++i) {
-          const int r = (wave * IPW + i) * RPI + lane / G;
-          const int k = (lane % G) ^ tile_swz<T, G>(r);
-          off[i] = rows(t * KT + r) * D + W::EPV * k;
-        }
+          for (int i = 0; i < IPW; ++i) tile_load(kt, off[i], at + 1024u * i);
 #pragma unroll
-        for (int i = 0; i < IPW; ++i) {
-          const uint32_t to = at + 1024u * (wave * IPW + i);
-          async_load16<false>(Kg + off[i], __builtin_amdgcn_readfirstlane(to));
-          async_load16<false>(Vg + off[i], __builtin_amdgcn_readfirstlane(to + MB));
+          for (int i = 0; i < IPW; ++i) tile_load(vt, off[i], at + MB + 1024u * i);
+        } else {
+#pragma unroll 1
+          for (int i = 0; i < IPW; ++i) {
+            const int r = (wave * IPW + i) * RPI + lane / G;
+            const long o = rows(t * KT + r) * D + W::EPV * ((lane % G) ^ tile_swz<T, G>(r));
+            async_load16<false>(Kg + o, __builtin_amdgcn_readfirstlane(at + 1024u * i));
+            async_load16<false>(Vg + o, __builtin_amdgcn_readfirstlane(at + MB + 1024u * i));
+          }
         }
       };
       issue(0);
