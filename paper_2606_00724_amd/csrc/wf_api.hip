@@ -907,7 +907,7 @@ static wf_status check_prefix(const wf_prefix_params* p, PrefixPlan* plan) {
       return fail(WF_ERR_UNSUPPORTED, "more than 2^30 query rows in one call");
   }
   *plan = plan_prefix(*p);
-  if (plan->items + 7 + plan->titems > INT32_MAX)
+  if (plan->items + 7 > INT32_MAX || plan->titems > INT32_MAX)
     return fail(WF_ERR_UNSUPPORTED, "too many workgroups in one call");
   return WF_OK;
 }
@@ -957,7 +957,7 @@ static wf_status prefix_impl(const wf_prefix_params* p, const void* Q, const voi
   a.lse = lse;
   a.part = static_cast<float*>(ws);
   a.pstat = ws ? reinterpret_cast<float*>(at(ws, plan.part_bytes)) : nullptr;
-  WF_HIP(launch_prefix(*p, a, static_cast<hipStream_t>(stream)), "prefix_attn");
+  WF_HIP(launch_prefix(*p, plan, a, static_cast<hipStream_t>(stream)), "prefix_attn");
   return ok();
 }
 

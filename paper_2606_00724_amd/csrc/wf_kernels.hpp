@@ -191,15 +191,32 @@ struct CacheArgs {
   int blocks;           // workgroups per unit
 };
 
-// Work of one kind (the prefix, or the sequences' own rows) of a prefix
-// attention: units x splits of their keys x blocks of their query rows.
+// Work of one kernel of the prefix attention: units x ranges of their keys x
+// blocks of their query rows.
 struct PrefixPart {
   int items;            // workgroups
   int splits;           // key ranges per unit
   int rps;              // keys per range (multiple of the tile)
   int mblocks;          // blocks of query rows per unit
   int M;                // query rows per unit
-  int kw;               // waves that take keys of a tile in turn (the others: query rows)
+  int kw;               // waves that take the keys of a tile in turn
+  int qw;               // 32-row blocks per wave (prefix), waves over rows (own keys)
+};
+
+// Division of 0 <= n < 2^31 by a constant d >= 1: with 2^(l-1) < d <= 2^l, n times
+// ceil(2^(31 + l) / d), shifted right by 31 + l, is the quotient (Granlund and
+// Montgomery 1994).
+struct FastDiv {
+  uint32_t mul;
+  int shift;            // l - 1; -1 for d = 1
+  static FastDiv by(uint32_t d) {
+    int l = 0;
+    while ((1ull << l) < d) ++l;
+    return FastDiv{(uint32_t)(((1ull << (31 + l)) + d - 1) / d), l - 1};
+  }
+  __device__ __forceinline__ int operator()(int n) const {
+    return shift < 0 ? n : (int)(__umulhi((uint32_t)n, mul) >> shift);
+  }
 };
 
 struct PrefixArgs {
@@ -215,13 +232,14 @@ struct PrefixArgs {
   const int32_t* tlen;  // nullable [sequences]
   void* O;              // [sequences][heads][R][D]
   float* lse;           // nullable [sequences][heads][R]
-  float* part;          // [rows][slots][D] unnormalised partial outputs
-  float* pstat;         // [rows][slots][2] reference (log2 units), sum
+  float* part;          // [query rows][slots][D] unnormalised partial outputs
+  float* pstat;         // [query rows][slots][2] reference (log2 units), sum
   PrefixPart p, t;      // the prefix; the sequences' own rows
   int heads, share, R;  // R: group * q_len
+  FastDiv by_R;
   int cap, rows, T;
-  int slots;            // p.splits + t.splits (1: no merge)
-  int ids;              // row ids in LDS (0: dense)
+  int slots;            // partials per query row
+  int whole;            // the prefix kernel writes O itself
   float scale;
 };
 

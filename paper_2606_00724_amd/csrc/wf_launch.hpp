@@ -307,21 +307,25 @@ hipError_t launch_cache(const wf_cache_params& p, bool store, const void* K, con
                         const void* Vx, hipStream_t s);
 hipError_t load_cache_kernels();
 
-// Attention over a shared prefix: its split into workgroups, and the two
-// launches (partials, merge).
+// Attention over a shared prefix: its split into workgroups, and the launches.
 struct PrefixArgs;
 struct PrefixPlan {
-  int qw;            // 32-row query blocks per wave
-  int slots;         // partials per query row
-  int ids;           // row ids in LDS
-  long items, titems;  // workgroups for the prefix and for the sequences' own rows
-  int splits, rps, mblocks, kw;
-  int tsplits, trps, tmblocks, tkw;
-  size_t part_bytes, pstat_bytes;  // workspace (0 where a row has one partial)
-  size_t lds_bytes;
+  // the prefix: workgroups, ranges per unit, keys per range, blocks of query
+  // rows per unit, waves over the keys of a tile, 32-row blocks per wave
+  long items;
+  int splits, rps, mblocks, kw, qw;
+  size_t lds_bytes, ids_bytes;  // LDS, with a list of rows
+  // the sequences' own rows: workgroups, blocks of query rows, waves over the
+  // keys, waves over the query rows
+  long titems;
+  int tmblocks, tkw, tqw;
+  size_t tlds_bytes;
+  int slots;                       // partials per query row
+  size_t part_bytes, pstat_bytes;  // workspace (0: no partials)
 };
 PrefixPlan plan_prefix(const wf_prefix_params& p);
-hipError_t launch_prefix(const wf_prefix_params& p, PrefixArgs& a, hipStream_t s);
+hipError_t launch_prefix(const wf_prefix_params& p, const PrefixPlan& plan, PrefixArgs& a,
+                         hipStream_t s);
 hipError_t load_prefix_kernels();
 
 }  // namespace wf

@@ -2,12 +2,13 @@
 //
 // For a K/V head of a prefix, the query rows of all its sequences and of the
 // head's group are one block of M = share * group * q_len rows that sees the
-// same keys: the prefix is read once for all of them.  A sequence's own rows
-// are a second, shorter key range of its R = group * q_len rows.  A workgroup
-// takes a block of query rows and a range of keys of either kind and leaves an
-// unnormalised output with the rows' reference (log2 units) and sum of
-// weights; a second kernel merges a row's partials (none is needed where it
-// has one).
+// same keys: the prefix is read once for all of them.  A workgroup of the
+// first kernel takes a block of those rows and a range of the prefix's keys
+// and leaves an unnormalised output with the rows' reference (log2 units) and
+// sum of weights.  The second kernel takes a sequence's R = group * q_len rows
+// over its own keys and merges the partials of the prefix into them; where
+// there are no own keys it only merges, and where there is one range it is not
+// needed.
 //
 // S^T = K Q^T on 32 x 32 products: a lane then holds 16 scores of one query
 // row, so that the softmax needs no lane exchange except one of the maximum
@@ -23,30 +24,35 @@ namespace wf {
 constexpr int kPrefixBlock = 256;
 constexpr int kPrefixWaves = kPrefixBlock / kWave;
 constexpr int kPrefixIds = 4096;  // row ids in LDS at once (whole tiles)
+constexpr int kTileRows = 64;     // keys of an LDS tile
 
 typedef short v4i16p __attribute__((ext_vector_type(4)));
 
-// keys per LDS tile
-template <typename T>
-constexpr int kTile = sizeof(T) == 2 ? 128 : 64;
-
-// Granules (16 bytes) of a row are stored in slot k ^ tile_swz(r) so that no
-// LDS read below meets a bank twice: 16 rows at one granule (K), four rows of
-// 64 bytes (bf16 V, transposed reads), and rows r and r + 4 of 128 bytes (fp32
-// V) lie on different banks.
-template <typename T, int G>
-__device__ __forceinline__ int tile_swz(int r) {
-  if constexpr (sizeof(T) == 4) return ((r & 4) << 1) | ((r & 3) << 1) | ((r >> 3) & 1);
-  if constexpr (G == 16) return ((r & 3) << 2) | ((r >> 2) & 3);
-  return ((r & 2) << 1) | ((r >> 2) & 3);  // 128-byte rows
+// A tile of K or V in LDS: the 64-byte pieces of its rows, piece-major, so that
+// every operand of a lane is at a constant from its first one.  In a piece of K
+// the 16-byte granule k is in slot k ^ ((r >> 2) & 3): the 16 rows that are read
+// at one granule then meet all banks.  V, whose transposed reads take whole
+// pieces of four rows, stays in order.
+constexpr int kPiece = kTileRows * 64;  // bytes from piece to piece
+template <typename T, int D>
+struct TileGeom {
+  static constexpr int RB = D * (int)sizeof(T);  // bytes of a row
+  static constexpr int NP = RB / 64;             // pieces of a row
+  static constexpr int MB = kTileRows * RB;      // bytes of a K (or V) tile
+  // tiles in LDS: the pipelined loop has one in use, the next one visible, one
+  // in flight and one being queued; four do not fit with fp32 rows of 128
+  static constexpr int SLOTS = 8 * MB > 131072 ? 2 : 4;
+};
+// LDS offset of granule k of row r
+__device__ __forceinline__ int key_offset(int r, int k) {
+  return (k >> 2) * kPiece + r * 64 + 16 * ((k & 3) ^ ((r >> 2) & 3));
 }
-template <typename T, int G>
-__device__ __forceinline__ int tile_offset(int r, int k) {
-  return r * (16 * G) + 16 * (k ^ tile_swz<T, G>(r));
+__device__ __forceinline__ int val_offset(int r, int k) {
+  return (k >> 2) * kPiece + r * 64 + 16 * (k & 3);
 }
 
-// The rows of a workgroup's key range: row i of tile t is key k0 + t * tile +
-// i, at most its last one.
+// The rows of a workgroup's key range: row i of the range is key k0 + i, at
+// most its last one.
 struct KeyRows {
   const int32_t* ids;   // LDS: rows of keys id0, id0 + 1, ... (list), or null
   int cap;              // rows of the unit
@@ -59,53 +65,77 @@ struct KeyRows {
   }
 };
 
-template <typename T, int D, int FMT, int QW>
+// A wave's 32 QW query rows: operands, outputs and running softmax.
+template <typename T, int D, int QW>
 struct PrefixWave {
+  using Geom = TileGeom<T, D>;
   static constexpr bool BF = sizeof(T) == 2;
-  static constexpr int ES = sizeof(T), EPV = 16 / ES;
-  static constexpr int G = D / EPV;              // granules per row
-  static constexpr int KT = kTile<T>;
-  static constexpr int MB = KT * D * ES;         // bytes of a K (or V) tile
   static constexpr int QS = BF ? D / 16 : D / 8; // 16-byte query operands per lane
   static constexpr int DT = D / 32;              // 32-channel output tiles
 
   u32x4 q[QW][QS];
   f32x16 O[QW][DT];
   float mref[QW], l[QW];
-  float nref[QW];  // -mref, 0 while that is -inf
+  float nref[QW];   // -mref, 0 while that is -inf
+  float limit[QW];  // 8; -inf while the reference is -inf
   bool neg;  // a negative scale: the scores change sign (and c2 is positive)
+  // LDS byte offsets of the lane's first operands in a 32-row block of a tile
+  uint32_t ko[2], vo;
 
-  // LDS byte offsets of the lane's operands in a 32-row block (the swizzle goes
-  // by the row mod 16, so one offset serves all blocks).  The granules of a row
-  // differ in bits that the swizzle is XORed into, so that those of the other
-  // operands are this one's XOR a constant.
-  uint32_t ko, vo;
-  __device__ __forceinline__ void offsets() {
-    const int lane = threadIdx.x & 63, h = lane >> 5, i16 = lane & 15;
-    ko = tile_offset<T, G>(lane & 31, h);
-    // in each 16-lane group lane i points at row t0 + i / 4, channels c0 + 4 (i %
-    // 4) .. + 3, and receives rows t0 .. t0 + 3 of channel c0 + i
+  __device__ __forceinline__ void init(float scale) {
+    const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, i16 = lane & 15;
+    neg = scale < 0.f;
+    ko[0] = key_offset(l32, h);
+    ko[1] = key_offset(l32, 2 + h);
+    // bf16: in each 16-lane group lane i points at row t0 + i / 4, channels c0 +
+    // 4 (i % 4) .. + 3, and receives rows t0 .. t0 + 3 of channel c0 + i
     const int t0 = 4 * h + (i16 >> 2), c0 = (lane & 16) + 4 * (i16 & 3);
-    vo = tile_offset<T, G>(t0, c0 >> 3) + 2 * (c0 & 7);
+    vo = BF ? val_offset(t0, c0 >> 3) + 2 * (c0 & 7)
+            : val_offset(4 * h, l32 >> 2) + 4 * (l32 & 3);
+#pragma unroll
+    for (int b = 0; b < QW; ++b) {
+      mref[b] = limit[b] = -INFINITY;
+      nref[b] = l[b] = 0.f;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) O[b][d][i] = 0.f;
+    }
   }
 
-  // The lane's operand j of K in the block at LDS offset `at`: 16 bytes of its
-  // row, granule 2 j + h.
-  __device__ __forceinline__ u32x4 key(uint32_t at, int j) const {
-    return *(const __attribute__((address_space(3))) u32x4*)(size_t)((at + ko) ^ (32u * j));
+  // The lane's first operands in the block at LDS offset `at`.  (Opaque, so that
+  // the others are read at constant offsets from them and not from sums kept in
+  // registers.)
+  struct KeyBase {
+    uint32_t b[2];
+  };
+  __device__ __forceinline__ KeyBase key_base(uint32_t at) const {
+    KeyBase k = {{at + ko[0], at + ko[1]}};
+    asm volatile("" : "+v"(k.b[0]), "+v"(k.b[1]));
+    return k;
+  }
+  __device__ __forceinline__ uint32_t val_base(uint32_t at) const {
+    uint32_t v = at + vo;
+    asm volatile("" : "+v"(v));
+    return v;
+  }
+  // Operand j of K: 16 bytes of the lane's row, granule 2 j + h.
+  __device__ __forceinline__ static u32x4 key(const KeyBase& k, int j) {
+    return *(const __attribute__((address_space(3))) u32x4*)(size_t)(k.b[j & 1] +
+                                                                     (j >> 1) * kPiece);
   }
   __device__ __forceinline__ void keys(uint32_t at, u32x4 (&kf)[QS]) const {
+    const KeyBase k = key_base(at);
 #pragma unroll
-    for (int j = 0; j < QS; ++j) kf[j] = key(at, j);
+    for (int j = 0; j < QS; ++j) kf[j] = key(k, j);
   }
-  // Half of the lane's operand of V^T of 16 of the block's rows (bf16): rows 16
-  // kb + 8 k + 4 h .. + 3 of channel 32 d + l % 32.  (Eight rows on, the swizzle
-  // flips a granule's bit 1.)
-  __device__ __forceinline__ u32x2 val(uint32_t at, int kb, int d, int k) const {
+  // Half of the operand of V^T of 16 of the block's rows (bf16): rows 16 kb + 8 k
+  // + 4 h .. + 3 of channel 32 d + l % 32.
+  __device__ __forceinline__ static u32x2 val(uint32_t base, int kb, int d, int k) {
     return __builtin_bit_cast(
         u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                    (__attribute__((address_space(3))) v4i16p*)(size_t)(
-                       ((at + vo) ^ (64u * d + 32u * k)) + (2 * kb + k) * 128 * G)));
+                       base + d * kPiece + (2 * kb + k) * 512)));
   }
   // s = scores of 32 keys; lane: keys 8 (i / 4) + 4 h + i % 4 of query l % 32
   __device__ __forceinline__ void scores(const u32x4 (&kf)[QS], f32x16 (&s)[QW]) const {
@@ -130,95 +160,12 @@ struct PrefixWave {
       }
     }
   }
-  __device__ __forceinline__ static void maxima(const f32x16 (&s)[QW], float (&mx)[QW]) {
-#pragma unroll
-    for (int b = 0; b < QW; ++b) {
-      float m = fmaxf(s[b][0], s[b][1]);
-#pragma unroll
-      for (int i = 2; i < 16; i += 2) m = fmaxf(m, fmaxf(s[b][i], s[b][i + 1]));
-      mx[b] = m;
-    }
-  }
-  // The reference moves only when a score passes it by 2^8: weights then stay
-  // below 2^8, their sums far from the fp32 range, and a rescale of the outputs
-  // is rare.
-  __device__ __forceinline__ void raise(const float (&mx)[QW], float c2) {
-    bool grow = false;
-#pragma unroll
-    for (int b = 0; b < QW; ++b) grow |= mx[b] * c2 > mref[b] + 8.f;
-    if (__builtin_amdgcn_ballot_w64(grow) != 0) {
-#pragma unroll
-      for (int b = 0; b < QW; ++b) {
-        const float mn = fmaxf(mref[b], fmaxf(mx[b], partner32(mx[b])) * c2);
-        const float al = mref[b] > -INFINITY ? __builtin_amdgcn_exp2f(mref[b] - mn) : 0.f;
-        mref[b] = mn;
-        nref[b] = mn > -INFINITY ? -mn : 0.f;
-        l[b] *= al;
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) O[b][d][i] *= al;
-      }
-    }
-  }
-  // Weights of keys i0 .. i0 + 7 of the lane's, and their sum into l.  (The
-  // unrounded product less the reference: scores of thousands keep their
-  // differences.  While every score so far is -inf, their weights are 2^-inf =
-  // 0.)
-  __device__ __forceinline__ void weights(f32x16 (&s)[QW], int i0, float c2) {
-#pragma unroll
-    for (int b = 0; b < QW; ++b) {
-#pragma unroll
-      for (int i = i0; i < i0 + 8; ++i)
-        s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], c2, nref[b]));
-      l[b] += ((s[b][i0] + s[b][i0 + 1]) + (s[b][i0 + 2] + s[b][i0 + 3])) +
-              ((s[b][i0 + 4] + s[b][i0 + 5]) + (s[b][i0 + 6] + s[b][i0 + 7]));
-    }
-  }
-  // O^T += V^T P^T over 16 keys (bf16: the weights rounded to half a step of
-  // bf16, as the products' operands are)
-  __device__ __forceinline__ void add16(const f32x16 (&s)[QW], int kb, const u32x4 (&vf)[DT]) {
-    u32x4 pf[QW];
-#pragma unroll
-    for (int b = 0; b < QW; ++b)
-      pf[b] = u32x4{pack_bf16x2(s[b][8 * kb], s[b][8 * kb + 1]),
-                    pack_bf16x2(s[b][8 * kb + 2], s[b][8 * kb + 3]),
-                    pack_bf16x2(s[b][8 * kb + 4], s[b][8 * kb + 5]),
-                    pack_bf16x2(s[b][8 * kb + 6], s[b][8 * kb + 7])};
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-      for (int b = 0; b < QW; ++b)
-        O[b][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[d]),
-                                                          __builtin_bit_cast(bf16x8, pf[b]),
-                                                          O[b][d], 0, 0, 0);
-  }
-  // the same over the block's 32 keys in fp32
-  __device__ __forceinline__ void add32(const f32x16 (&s)[QW], const unsigned char* Vb, int sb) {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int r = sb + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3);
-#pragma unroll
-      for (int d = 0; d < DT; ++d) {
-        const int c = 32 * d + (lane & 31);
-        const float vf =
-            *reinterpret_cast<const float*>(Vb + tile_offset<T, G>(r, c >> 2) + 4 * (c & 3));
-#pragma unroll
-        for (int b = 0; b < QW; ++b)
-          O[b][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, s[b][i], O[b][d], 0, 0, 0);
-      }
-    }
-  }
 
-  // 32 keys (rows sb .. sb + 31 of the tile, nr of the tile's rows valid)
-  __device__ __forceinline__ void step(const unsigned char* Kb, const unsigned char* Vb, int sb,
-                                       int nr, float c2) {
-    const uint32_t kat = lds_offset(Kb) + sb * 16 * G, vat = lds_offset(Vb) + sb * 16 * G;
+  // 32 keys at LDS offsets kat, vat, the first nv of which are valid
+  __device__ __forceinline__ void step(uint32_t kat, uint32_t vat, int nv, float c2) {
     const int h = (threadIdx.x & 63) >> 5;
     u32x4 kf[QS];
     f32x16 s[QW];
-    float mx[QW];
     keys(kat, kf);
     scores(kf, s);
     if (neg) {
@@ -227,38 +174,107 @@ struct PrefixWave {
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[b][i] = -s[b][i];
     }
-    if (sb + 32 > nr) {
+    if (nv < 32) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const bool off = sb + 8 * (i >> 2) + 4 * h + (i & 3) >= nr;
+        const bool off = 8 * (i >> 2) + 4 * h + (i & 3) >= nv;
 #pragma unroll
         for (int b = 0; b < QW; ++b) s[b][i] = off ? -INFINITY : s[b][i];
       }
     }
-    maxima(s, mx);
-    raise(mx, c2);
-    weights(s, 0, c2);
-    weights(s, 8, c2);
+    // The reference moves only when a score passes it by 2^8: weights then stay
+    // below 2^8, their sums far from the fp32 range, and a rescale of the
+    // outputs is rare.
+    float mx[QW];
+    bool grow = false;
+#pragma unroll
+    for (int b = 0; b < QW; ++b) {
+      mx[b] = fmaxf(s[b][0], s[b][1]);
+#pragma unroll
+      for (int i = 2; i < 16; i += 2) mx[b] = fmaxf(mx[b], fmaxf(s[b][i], s[b][i + 1]));
+      grow |= mx[b] * c2 > mref[b] + 8.f;
+    }
+    if (__builtin_amdgcn_ballot_w64(grow) != 0) {
+#pragma unroll
+      for (int b = 0; b < QW; ++b) {
+        const float mn = fmaxf(mref[b], fmaxf(mx[b], partner32(mx[b])) * c2);
+        rescale(b, mn, mref[b] > -INFINITY ? __builtin_amdgcn_exp2f(mref[b] - mn) : 0.f);
+      }
+    }
+    // The weights: the unrounded product less the reference, so that scores of
+    // thousands keep their differences.  (While every score so far is -inf,
+    // their weights are 2^-inf = 0.)
+#pragma unroll
+    for (int b = 0; b < QW; ++b) {
+      float z = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], c2, nref[b]));
+        z += s[b][i];
+      }
+      l[b] += z;
+    }
+    const uint32_t vb = val_base(vat);
     if constexpr (BF) {
+      // (each weight rounded to bf16, as the products' operands are)
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
-        u32x4 vf[DT];
+        u32x4 pf[QW];
+#pragma unroll
+        for (int b = 0; b < QW; ++b)
+          pf[b] = u32x4{pack_bf16x2(s[b][8 * kb], s[b][8 * kb + 1]),
+                        pack_bf16x2(s[b][8 * kb + 2], s[b][8 * kb + 3]),
+                        pack_bf16x2(s[b][8 * kb + 4], s[b][8 * kb + 5]),
+                        pack_bf16x2(s[b][8 * kb + 6], s[b][8 * kb + 7])};
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
-          const u32x2 lo = val(vat, kb, d, 0), hi = val(vat, kb, d, 1);
-          vf[d] = u32x4{lo[0], lo[1], hi[0], hi[1]};
+          const u32x2 lo = val(vb, kb, d, 0), hi = val(vb, kb, d, 1);
+          const u32x4 vf = {lo[0], lo[1], hi[0], hi[1]};
+#pragma unroll
+          for (int b = 0; b < QW; ++b)
+            O[b][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf),
+                                                              __builtin_bit_cast(bf16x8, pf[b]),
+                                                              O[b][d], 0, 0, 0);
         }
-        add16(s, kb, vf);
       }
     } else {
-      add32(s, Vb, sb);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          const float vf = *(const __attribute__((address_space(3))) float*)(size_t)(
+              vb + 2 * d * kPiece + (8 * (i >> 2) + (i & 3)) * 64);
+#pragma unroll
+          for (int b = 0; b < QW; ++b)
+            O[b][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, s[b][i], O[b][d], 0, 0, 0);
+        }
+      }
     }
+  }
+  __device__ __forceinline__ void rescale(int b, float mn, float al) {
+    mref[b] = mn;
+    nref[b] = mn > -INFINITY ? -mn : 0.f;
+    limit[b] = mn > -INFINITY ? 8.f : -INFINITY;
+    l[b] *= al;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) O[b][d][i] *= al;
   }
 
   // The pipelined loop (bf16) keeps the next block's scores in log2 units less
   // the reference, t = s c2 - mref, and their maximum mx.  Before the block's
-  // weights are taken the reference is raised where t passes it (see raise).
-  float limit[QW];  // 8; -inf while the reference is -inf
+  // weights are taken the reference is raised where t passes it (as in step).
+  __device__ __forceinline__ void shift(f32x16 (&t)[QW], float (&mx)[QW], float c2) const {
+#pragma unroll
+    for (int b = 0; b < QW; ++b) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) t[b][i] = fmaf(t[b][i], c2, nref[b]);
+      mx[b] = fmaxf(t[b][0], t[b][1]);
+#pragma unroll
+      for (int i = 2; i < 16; i += 2) mx[b] = fmaxf(mx[b], fmaxf(t[b][i], t[b][i + 1]));
+    }
+  }
   __device__ __forceinline__ void raise_shifted(f32x16 (&t)[QW], const float (&mx)[QW]) {
     bool grow = false;
 #pragma unroll
@@ -270,45 +286,29 @@ struct PrefixWave {
         const bool first = mref[b] == -INFINITY;
         const float mn = first ? up : fmaxf(mref[b], mref[b] + up);
         const float by = mn > -INFINITY ? mn + nref[b] : 0.f;  // (nref: 0 or -mref)
-        const float al = first ? 0.f : __builtin_amdgcn_exp2f(-by);
-        mref[b] = mn;
-        nref[b] = mn > -INFINITY ? -mn : 0.f;
-        limit[b] = mn > -INFINITY ? 8.f : -INFINITY;
-        l[b] *= al;
 #pragma unroll
         for (int i = 0; i < 16; ++i) t[b][i] -= by;
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) O[b][d][i] *= al;
+        rescale(b, mn, first ? 0.f : __builtin_amdgcn_exp2f(-by));
       }
-    }
-  }
-  __device__ __forceinline__ void shift(f32x16 (&t)[QW], float (&mx)[QW], float c2) const {
-#pragma unroll
-    for (int b = 0; b < QW; ++b) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) t[b][i] = fmaf(t[b][i], c2, nref[b]);
-      mx[b] = fmaxf(t[b][0], t[b][1]);
-#pragma unroll
-      for (int i = 2; i < 16; i += 2) mx[b] = fmaxf(mx[b], fmaxf(t[b][i], t[b][i + 1]));
     }
   }
 
   // A block of that loop: weights of one block (shifted scores s) and their
   // product with V (at LDS offset vat) beside the scores sn of the next block
   // (its keys kf in registers; refilled with those at knext).  A wave issues in
-  // order and waits for the matrix pipe at its next product, so only what stands
-  // between two products runs beside them: every product (32 cycles) is followed
-  // by its share of the vector work, four to six instructions, and the barriers
-  // hold that order.
+  // order, an instruction in about five cycles, and waits for the matrix pipe at
+  // its next product: only what stands between two products runs beside them.
+  // Every product (32 cycles) is followed by its share of the vector work, LDS
+  // reads and tile loads (load(i), i < NL), and the barriers hold that order.
+  template <int NL, typename Load>
   __device__ __forceinline__ void block(uint32_t vat, uint32_t knext, u32x4 (&kf)[QS],
                                         f32x16 (&s)[QW], f32x16 (&sn)[QW], float (&mx)[QW],
-                                        float c2) {
-    raise_shifted(s, mx);
+                                        float c2, const Load& load) {
     float z[QW];
 #pragma unroll
     for (int b = 0; b < QW; ++b) z[b] = 0.f;
+    const uint32_t vb = val_base(vat);
+    const KeyBase kn = key_base(knext);
     u32x4 p0[QW], p1[QW], v0[DT], v1[DT];
     // weight e of 16 keys (of the block's first or second half)
     auto weight = [&](int half, int e) __attribute__((always_inline)) {
@@ -324,7 +324,7 @@ struct PrefixWave {
     };
     auto value = [&](int r) __attribute__((always_inline)) {
       const int kb = r / (2 * DT), d = (r >> 1) % DT, k = r & 1;
-      const u32x2 y = val(vat, kb, d, k);
+      const u32x2 y = val(vb, kb, d, k);
       (kb ? v1 : v0)[d][2 * k] = y[0];
       (kb ? v1 : v0)[d][2 * k + 1] = y[1];
     };
@@ -340,8 +340,20 @@ struct PrefixWave {
                                                       0);
 #pragma unroll
       for (int r = n * 4 * DT / NQ; r < (n + 1) * 4 * DT / NQ; ++r) value(r);
+      if (n < QW) {  // (the first products run beside this)
+        if (n == QW - 1) {
+          __builtin_amdgcn_sched_barrier(0);
+          raise_shifted(s, mx);
 #pragma unroll
-      for (int e = n * 8 * QW / NQ; e < (n + 1) * 8 * QW / NQ; ++e) weight(0, e);
+          for (int e = 0; e < QW * 8 * QW / NQ; ++e) weight(0, e);
+        }
+      } else {
+#pragma unroll
+        for (int e = n * 8 * QW / NQ; e < (n + 1) * 8 * QW / NQ; ++e) weight(0, e);
+      }
+      if constexpr (NL > 0) {
+        if ((n + 1) * NL / NQ > n * NL / NQ) load(n * NL / NQ, (n + 1) * NL / NQ);
+      }
       __builtin_amdgcn_sched_barrier(0);
     }
 #pragma unroll
@@ -361,7 +373,7 @@ struct PrefixWave {
                                                         __builtin_bit_cast(bf16x8, p1[b]), O[b][d],
                                                         0, 0, 0);
 #pragma unroll
-      for (int j = n * QS / NV; j < (n + 1) * QS / NV; ++j) kf[j] = key(knext, j);
+      for (int j = n * QS / NV; j < (n + 1) * QS / NV; ++j) kf[j] = key(kn, j);
 #pragma unroll
       for (int e = n * 8 * QW / NV; e < (n + 1) * 8 * QW / NV; ++e) {
         const int g = e >> 3, i = 2 * (e & 7);
@@ -381,63 +393,146 @@ struct PrefixWave {
   }
 };
 
-// 16 bytes per lane from base + off straight to LDS (lane l's at `lds` + 16 l).
-// Waited for as async_load16's.
+// 16 bytes per lane from base + off + OFF straight to LDS (lane l's at `lds` + AT
+// + 16 l; the instruction adds OFF to both addresses).  Waited for as
+// async_load16's.
+template <int OFF, int AT>
 __device__ __forceinline__ void tile_load(const void* base, uint32_t off, uint32_t lds) {
   asm volatile(
-      "s_mov_b32 m0, %2\n\t"
+      "s_add_u32 m0, %2, %4\n\t"
       "s_nop 0\n\t"
-      "global_load_lds_dwordx4 %0, %1"
+      "global_load_lds_dwordx4 %0, %1 offset:%3"
       :
-      : "v"(off), "s"(base), "s"(lds)
+      : "v"(off), "s"(base), "s"(lds), "n"(OFF), "n"(AT - OFF)
+      : "memory", "m0", "scc");
+}
+template <int OFF>
+__device__ __forceinline__ void row_load(const void* g, uint32_t lds) {
+  asm volatile(
+      "s_mov_b32 m0, %1\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %0, off offset:%2"
+      :
+      : "v"(g), "s"(lds - OFF), "n"(OFF)
       : "memory", "m0");
 }
 
+// Tiles by direct loads.  Wave w loads rows 16 w .. + 15 of a tile, one 64-byte
+// piece of each in an instruction (four lanes a row).
+template <typename T, int D>
+struct TileLoads {
+  using Geom = TileGeom<T, D>;
+  static constexpr int N = Geom::NP;  // instructions per wave and matrix
+  const unsigned char* K;             // the unit's rows
+  const unsigned char* V;
+  uint32_t off[2];                    // the lane's byte offsets in a tile of consecutive rows
+  uint32_t lds;                       // LDS offset of the wave's rows in tile slot 0
+  int row;                            // the lane's row in a tile
+
+  __device__ __forceinline__ void init(const void* Ku, const void* Vu, uint32_t lds0) {
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    K = static_cast<const unsigned char*>(Ku);
+    V = static_cast<const unsigned char*>(Vu);
+    row = 16 * wave + (lane >> 2);
+    off[0] = row * Geom::RB + 16 * ((lane & 3) ^ ((lane >> 4) & 3));
+    off[1] = row * Geom::RB + 16 * (lane & 3);
+    lds = lds0 + 1024 * wave;
+  }
+  // instruction i of 2 N (K's, then V's) of a tile of consecutive rows
+  struct Tile {
+    const unsigned char *k, *v;  // its first rows
+    uint32_t to;                 // LDS offset of the wave's rows in its slot
+    int go;                      // whether it is loaded
+  };
+  __device__ __forceinline__ Tile at(long r0, uint32_t slot, bool go) const {
+    return Tile{K + r0 * Geom::RB, V + r0 * Geom::RB, lds + slot * 2 * Geom::MB,
+                __builtin_amdgcn_readfirstlane(go ? 1 : 0)};
+  }
+  template <int I>
+  __device__ __forceinline__ void one(const Tile& t) const {
+    tile_load<(I % N) * 64, (I / N) * Geom::MB + (I % N) * kPiece>(I < N ? t.k : t.v, off[I / N],
+                                                                   t.to);
+  }
+  template <int I, int E>
+  __device__ __forceinline__ void some(const Tile& t) const {
+    if constexpr (I < E) {
+      one<I>(t);
+      some<I + 1, E>(t);
+    }
+  }
+  // a whole tile whose row i is `at`(i)
+  template <int I = 0>
+  __device__ __forceinline__ void rows(const unsigned char* k, const unsigned char* v,
+                                       uint32_t to) const {
+    if constexpr (I < N) {
+      row_load<I * 64>(k, to + I * kPiece);
+      row_load<I * 64>(v, to + Geom::MB + I * kPiece);
+      rows<I + 1>(k, v, to);
+    }
+  }
+  __device__ __forceinline__ void tile(const KeyRows& at, int first, bool straight,
+                                       uint32_t slot) const {
+    if (straight) {  // uniform
+      some<0, 2 * N>(this->at(at.k0 + first, slot, true));
+    } else {
+      const long r = at(first + row) - row;  // (the offsets hold the row in the tile)
+      rows(K + r * Geom::RB + off[0], V + r * Geom::RB + off[1], lds + slot * 2 * Geom::MB);
+    }
+  }
+};
+
 template <typename T>
-__device__ __forceinline__ void put4(T* p, float a, float b, float c, float d);
+__device__ __forceinline__ void put4(T* p, const f32x4& v);
 template <>
-__device__ __forceinline__ void put4<bf16_t>(bf16_t* p, float a, float b, float c, float d) {
-  *reinterpret_cast<u32x2*>(p) = u32x2{pack_bf16x2(a, b), pack_bf16x2(c, d)};
+__device__ __forceinline__ void put4<bf16_t>(bf16_t* p, const f32x4& v) {
+  *reinterpret_cast<u32x2*>(p) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
 }
 template <>
-__device__ __forceinline__ void put4<float>(float* p, float a, float b, float c, float d) {
-  *reinterpret_cast<f32x4*>(p) = f32x4{a, b, c, d};
+__device__ __forceinline__ void put4<float>(float* p, const f32x4& v) {
+  *reinterpret_cast<f32x4*>(p) = v;
 }
 
-// One row of a cache as a thread stages it: 16 codes (E4M3) or 32 (E2M1) in
-// 16 bytes, and their block's exponent byte.
+// A tile of a cache as a thread stages it: pieces of 16 codes (E4M3) or 32
+// (E2M1), 16 bytes, and their block's exponent byte.  Four threads in a row take
+// four rows, so that what eight of them write to LDS at once meets all banks.
 template <typename T, int D, int FMT>
 struct QuantStage {
+  using Geom = TileGeom<T, D>;
   static constexpr int CPP = FMT == WF_CACHE_E2M1 ? 32 : 16;  // channels per piece
   static constexpr int PPR = D / CPP;                         // pieces per row
-  static constexpr int PT = kTile<T> * PPR;                   // pieces of a tile and matrix
+  static constexpr int PT = kTileRows * PPR;                  // pieces of a tile and matrix
   static constexpr int N = (PT + kPrefixBlock - 1) / kPrefixBlock;  // per thread
-  static constexpr int G = D * (int)sizeof(T) / 16;
   u32x4 w[2][N];
   uint32_t x[2][N];
 
+  __device__ __forceinline__ static int row(int i) {
+    return (i * kPrefixBlock + threadIdx.x) / (4 * PPR) * 4 + (threadIdx.x & 3);
+  }
+  __device__ __forceinline__ static int piece() { return (threadIdx.x >> 2) % PPR; }
+
   __device__ __forceinline__ void load(const PrefixArgs& a, const KeyRows& rows, long unit,
-                                       int t0) {
+                                       int first) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int p = i * kPrefixBlock + threadIdx.x, pc = p % PPR;
-      if (PT % kPrefixBlock != 0 && p >= PT) break;
-      const long row = unit * a.cap + rows(t0 + p / PPR);
-      w[0][i] = reinterpret_cast<const u32x4*>(a.K)[row * PPR + pc];
-      w[1][i] = reinterpret_cast<const u32x4*>(a.V)[row * PPR + pc];
-      x[0][i] = a.Kx[row * (D / 32) + pc * CPP / 32];
-      x[1][i] = a.Vx[row * (D / 32) + pc * CPP / 32];
+      if (PT < kPrefixBlock && (int)threadIdx.x >= PT) break;
+      const long r = unit * a.cap + rows(first + row(i));
+      w[0][i] = reinterpret_cast<const u32x4*>(a.K)[r * PPR + piece()];
+      w[1][i] = reinterpret_cast<const u32x4*>(a.V)[r * PPR + piece()];
+      x[0][i] = a.Kx[r * (D / 32) + piece() * CPP / 32];
+      x[1][i] = a.Vx[r * (D / 32) + piece() * CPP / 32];
     }
   }
-  __device__ __forceinline__ void commit(unsigned char* Kb, unsigned char* Vb) const {
+  __device__ __forceinline__ void commit(unsigned char* tile) const {
 #pragma unroll
     for (int m = 0; m < 2; ++m)
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const int p = i * kPrefixBlock + threadIdx.x, r = p / PPR, pc = p % PPR;
-        if (PT % kPrefixBlock != 0 && p >= PT) break;
+        if (PT < kPrefixBlock && (int)threadIdx.x >= PT) break;
+        const int r = row(i), pc = piece();
         const float s = block_scale(x[m][i]);
-        unsigned char* dst = m ? Vb : Kb;
+        unsigned char* dst = tile + m * Geom::MB;
+        auto at = [&](int k) { return dst + (m ? val_offset(r, k) : key_offset(r, k)); };
         if constexpr (sizeof(T) == 2) {
           // v_cvt_scalef32_pk_bf16: two codes times the power of two, rounded to
           // nearest even (equal to decode8 and pack_bf16x2 for every code and
@@ -464,7 +559,7 @@ struct QuantStage {
               g[3] = __builtin_bit_cast(uint32_t,
                                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[k], s, 3));
             }
-            *reinterpret_cast<u32x4*>(dst + tile_offset<T, G>(r, pc * (CPP / 8) + k)) = g;
+            *reinterpret_cast<u32x4*>(at(pc * (CPP / 8) + k)) = g;
           }
         } else {
 #pragma unroll
@@ -474,80 +569,172 @@ struct QuantStage {
                                                  : u32x2{w[m][i][k], 0u};
             decode8<FMT>(c, s, v);
             const int g = 2 * (pc * (CPP / 8) + k);
-            *reinterpret_cast<f32x4*>(dst + tile_offset<T, G>(r, g)) = f32x4{v[0], v[1], v[2], v[3]};
-            *reinterpret_cast<f32x4*>(dst + tile_offset<T, G>(r, g + 1)) =
-                f32x4{v[4], v[5], v[6], v[7]};
+            *reinterpret_cast<f32x4*>(at(g)) = f32x4{v[0], v[1], v[2], v[3]};
+            *reinterpret_cast<f32x4*>(at(g + 1)) = f32x4{v[4], v[5], v[6], v[7]};
           }
         }
       }
   }
 };
 
+// Rows nr .. 63 of the tile's V cleared: they repeat the range's last row or hold
+// what was there before, and 0 times an infinite value is NaN.  Ends with a
+// barrier.
+template <typename T, int D>
+__device__ __forceinline__ void clear_rows(unsigned char* tile, int nr) {
+  using Geom = TileGeom<T, D>;
+  unsigned char* V = tile + Geom::MB;
+  const int n = (kTileRows - nr) * 4;  // granules of a piece's rows
+  for (int i = threadIdx.x; i < n * Geom::NP; i += kPrefixBlock)
+    *reinterpret_cast<u32x4*>(V + i / n * kPiece + nr * 64 + i % n * 16) = u32x4{0u, 0u, 0u, 0u};
+  lds_barrier();
+}
+
+// Running merge of partials (reference, sum, four channels).
+struct Merge4 {
+  float M = -INFINITY, z = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  __device__ __forceinline__ void add(float m, float zs, const f32x4& x) {
+    if (m == -INFINITY && zs == 0.f) return;  // an empty range: it has no output
+    const float mn = fmaxf(M, m);
+    // (all scores -inf or NaN: zs says it)
+    const float f = m > -INFINITY ? __builtin_amdgcn_exp2f(m - mn) : 1.f;
+    const float g = M > -INFINITY ? __builtin_amdgcn_exp2f(M - mn) : 1.f;
+    M = mn;
+    z = z * g + f * zs;
+    o = o * g + x * f;
+  }
+  template <typename T>
+  __device__ __forceinline__ void finish(T* O, float* lse, bool first) const {
+    put4<T>(O, o * (z == 0.f ? 0.f : 1.f / z));
+    if (lse && first) *lse = z == 0.f ? -INFINITY : (M + __log2f(z)) * kLn2;
+  }
+};
+
+// The workgroup's outputs in LDS, so that they leave it in whole rows: wave w's
+// row r at (w 32 QW + r), unnormalised, and its reference and sum behind them.
+template <int D, int QW>
+struct OutRows {
+  static constexpr int STRIDE = D + 4;  // floats (eight rows at one channel meet all banks)
+  static constexpr int ROWS = kPrefixWaves * 32 * QW;
+  static constexpr size_t BYTES = (size_t)ROWS * (STRIDE + 2) * sizeof(float);
+  float* o;
+  float* st;
+  __device__ __forceinline__ explicit OutRows(unsigned char* smem)
+      : o(reinterpret_cast<float*>(smem)), st(o + ROWS * STRIDE) {}
+  // (the tiles are idle: the caller has passed a barrier)
+  template <typename T>
+  __device__ __forceinline__ void put(PrefixWave<T, D, QW>& w, int wave) {
+    const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31;
+#pragma unroll
+    for (int b = 0; b < QW; ++b) {
+      const float l = w.l[b] + partner32(w.l[b]);
+      const int r = (wave * QW + b) * 32 + l32;
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+          *reinterpret_cast<f32x4*>(o + r * STRIDE + 32 * d + 2 * i + 4 * h) =
+              f32x4{w.O[b][d][i], w.O[b][d][i + 1], w.O[b][d][i + 2], w.O[b][d][i + 3]};
+      if (h == 0) {
+        st[2 * r] = w.mref[b];
+        st[2 * r + 1] = l;
+      }
+    }
+    lds_barrier();
+  }
+  // four channels of a row, merged over the KW waves that have it (the first in
+  // row v)
+  __device__ __forceinline__ Merge4 merged(int v, int KW, int c) const {
+    Merge4 g;
+    for (int k = 0; k < KW; ++k) {
+      const int x = v + k * 32 * QW;
+      g.add(st[2 * x], st[2 * x + 1], *reinterpret_cast<const f32x4*>(o + x * STRIDE + 4 * c));
+    }
+    return g;
+  }
+};
+
+// Tile loads I0 + i .. I0 + e - 1 (the bounds are constants after unrolling).
+template <typename T, int D, int I0, int I = 0>
+__device__ __forceinline__ void load_some(const TileLoads<T, D>& dma, int i, int e,
+                                          const typename TileLoads<T, D>::Tile& t) {
+  if constexpr (I0 + I < 2 * TileLoads<T, D>::N) {
+    if (I >= i && I < e) dma.template one<I0 + I>(t);
+    if (I + 1 < e) load_some<T, D, I0, I + 1>(dma, i, e, t);
+  }
+}
+
+// Partials first, first + step, ... of a query row into g, eight in flight.
+template <int D>
+__device__ __forceinline__ void merge_partials(const PrefixArgs& a, long row, int c, int first,
+                                               int step, Merge4& g) {
+  const float* st = a.pstat + row * a.slots * 2;
+  const float* src = a.part + row * a.slots * D + 4 * c;
+  constexpr int F = 8;
+  for (int s0 = first; s0 < a.slots; s0 += F * step) {
+    float m[F], z[F];
+    f32x4 x[F];
+#pragma unroll
+    for (int k = 0; k < F; ++k) {  // (all queued; those past the last are dropped)
+      const int s = min(s0 + k * step, a.slots - 1);
+      const hw_f32x2 mz = *reinterpret_cast<const hw_f32x2*>(st + 2 * s);
+      m[k] = s0 + k * step < a.slots ? mz[0] : -INFINITY;
+      z[k] = s0 + k * step < a.slots ? mz[1] : 0.f;
+      x[k] = *reinterpret_cast<const f32x4*>(src + (long)s * D);
+    }
+#pragma unroll
+    for (int k = 0; k < F; ++k) g.add(m[k], z[k], x[k]);
+  }
+}
+
+// The prefix: query rows of all sequences of a (prefix, head) over a range of its
+// keys.
 template <typename T, int D, int FMT, int QW>
 __global__ __launch_bounds__(kPrefixBlock, 1) void prefix_attn_kernel(PrefixArgs a) {
-  using W = PrefixWave<T, D, FMT, QW>;
-  constexpr int KT = W::KT, G = W::G, MB = W::MB, DT = W::DT, QS = W::QS;
-  extern __shared__ __align__(16) unsigned char smem[];  // [2][K, V] tiles, then row ids
-  int32_t* ids = reinterpret_cast<int32_t*>(smem + 4 * MB);
+  using W = PrefixWave<T, D, QW>;
+  using Geom = TileGeom<T, D>;
+  constexpr int MB = Geom::MB, SLOTS = Geom::SLOTS, QS = W::QS;
+  constexpr bool QUANT = FMT != WF_CACHE_PLAIN;
+  extern __shared__ __align__(16) unsigned char smem[];  // [SLOTS][K, V] tiles, row ids
+  int32_t* ids = reinterpret_cast<int32_t*>(smem + SLOTS * 2 * MB);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = lane >> 5, l32 = lane & 31;
 
-  // The workgroup's item.  Prefix items first, their blocks of query rows
-  // innermost, so that those reading the same keys run at once on one XCD.
-  const int np8 = (a.p.items + 7) & ~7;  // (the grid holds whole eights of them)
-  const bool own = (int)blockIdx.x >= np8;
-  const int item = own ? (int)blockIdx.x - np8 : xcd_swizzle(blockIdx.x, np8);
-  if (item >= (own ? a.t.items : a.p.items)) return;
-  const int mblocks = own ? a.t.mblocks : a.p.mblocks;
-  const int splits = own ? a.t.splits : a.p.splits;
-  const int rps = own ? a.t.rps : a.p.rps;
-  const int M = own ? a.t.M : a.p.M;
-  const int KW = own ? a.t.kw : a.p.kw;
-  const int mb = item % mblocks, sp = item / mblocks % splits;
-  const int unit = item / (mblocks * splits);  // (prefix or sequence, head)
+  // The workgroup's item, blocks of query rows innermost, so that those reading
+  // the same keys run at once on one XCD.
+  const int item = xcd_swizzle(blockIdx.x, gridDim.x);
+  if (item >= a.p.items) return;  // (the grid holds whole eights of them)
+  const int mb = item % a.p.mblocks, sp = item / a.p.mblocks % a.p.splits;
+  const int unit = item / (a.p.mblocks * a.p.splits);  // (prefix, head)
   const int group = unit / a.heads, head = unit % a.heads;
-  const int slot = own ? a.p.splits + sp : sp;
-  int len = own ? a.T : a.rows;
-  if (own ? a.tlen != nullptr : a.plen != nullptr)
-    len = min(max((own ? a.tlen : a.plen)[group], 0), len);
-  const int k0 = sp * rps, nk = min(rps, len - k0);  // the range's keys (none: nk <= 0)
-
+  const int M = a.p.M, KW = a.p.kw;
+  const int len = a.plen ? min(max(a.plen[group], 0), a.rows) : a.rows;
+  const int k0 = sp * a.p.rps, nk = min(a.p.rps, len - k0);  // the range's keys (none: nk <= 0)
   const int kw = wave % KW, qw = wave / KW;
-  const int m0 = (mb * (kPrefixWaves / KW) + qw) * 32 * QW;
-  // query row m of the unit -> row of Q, O
+  const int mrows = kPrefixWaves / KW * 32 * QW;  // query rows of the workgroup
+  // query row m of the unit -> row of Q, O (at most 2^30 in all)
   auto row_of = [&](int m) {
-    const int n = own ? group : group * a.share + m / a.R;
-    return ((long)n * a.heads + head) * a.R + (own ? m : m % a.R);
+    const int n = a.by_R(m);
+    return ((group * a.share + n) * a.heads + head) * a.R + (m - n * a.R);
   };
   W w;
-  w.offsets();
+  w.init(a.scale);
   const float c2 = fabsf(a.scale) * kLog2e;
-  w.neg = a.scale < 0.f;
-#pragma unroll
-  for (int b = 0; b < QW; ++b) {
-    const T* src = reinterpret_cast<const T*>(a.Q) + row_of(min(m0 + 32 * b + l32, M - 1)) * D;
-#pragma unroll
-    for (int j = 0; j < QS; ++j)
-      w.q[b][j] = reinterpret_cast<const u32x4*>(src)[2 * j + h];
-    w.mref[b] = -INFINITY;
-    w.limit[b] = -INFINITY;
-    w.nref[b] = w.l[b] = 0.f;
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) w.O[b][d][i] = 0.f;
-  }
-  const bool active = m0 < M;
 
   if (nk > 0) {
+    // tiles: one 64-key tile, or two where four waves take the keys in turn
+    const int us = KW == 4 ? 2 : 1;
+    const int ns = SLOTS / us, KT = us * kTileRows;
     const int nt = (nk + KT - 1) / KT;
     KeyRows rows;
-    rows.ids = !own && a.list ? ids : nullptr;
-    rows.cap = own ? a.T : a.cap;
+    rows.ids = a.list ? ids : nullptr;
+    rows.cap = a.cap;
     rows.k0 = k0;
     rows.last = k0 + nk - 1;
     rows.id0 = k0;
+    auto slot_of = [&](int t) { return t % ns * us; };
     // the next kPrefixIds ids of a list, from tile t on, when tile t starts them
     // (no wave reads older ones: tile t - 1 has been queued by all)
     auto stage_ids = [&](int t) __attribute__((always_inline)) {
@@ -558,313 +745,284 @@ __global__ __launch_bounds__(kPrefixBlock, 1) void prefix_attn_kernel(PrefixArgs
         ids[i] = a.list[(long)unit * a.rows + rows.id0 + i];
       __syncthreads();
     };
-    // The query operands, loaded above: here, so that the compiler's wait for them
-    // is no wait for a tile later on.  Those of 64 rows of 128 channels are put
-    // into the accumulation half of the registers, from where the products take
-    // them: in the other half they were copied there and back in every block.
-    auto queries = [&]() __attribute__((always_inline)) {
-      __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
-      if constexpr (W::BF && QW * QS >= 16) {
-#pragma unroll
-        for (int b = 0; b < QW; ++b)
-#pragma unroll
-          for (int j = 0; j < QS; ++j) asm volatile("" : "+a"(w.q[b][j]));
+    TileLoads<T, D> dma;
+    QuantStage<T, D, QUANT ? FMT : WF_CACHE_E4M3> st[2];
+    if constexpr (!QUANT)
+      dma.init(static_cast<const T*>(a.K) + (long)unit * a.cap * D,
+               static_cast<const T*>(a.V) + (long)unit * a.cap * D, lds_offset(smem));
+    // tile t queued: on its way to its slot, or to registers
+    int queued = 0;
+    auto straight = [&](int t) { return !rows.ids && nk - t * KT >= KT; };
+    auto queue = [&](int t) __attribute__((always_inline)) {
+      stage_ids(t);
+      queued = t + 1;
+      if constexpr (QUANT) {
+        st[0].load(a, rows, unit, t * KT);
+        if (us > 1) st[1].load(a, rows, unit, t * KT + kTileRows);
+      } else {
+        dma.tile(rows, t * KT, straight(t), slot_of(t));
+        if (us > 1) dma.tile(rows, t * KT + kTileRows, straight(t), slot_of(t) + 1);
       }
     };
-    // The tiles in turn, through two LDS slots.  arrive(t): tile t is in its slot
-    // for every wave; leave(t): no wave reads tile t any more.
-    auto run = [&](auto&& arrive, auto&& leave) __attribute__((always_inline)) {
-      // whole tiles in the pipelined loop (bf16)
-      const int nf = !W::BF || w.neg ? 0 : nk / KT;
-      auto slot_of = [&](int t) { return smem + (t & 1) * 2 * MB; };
-      arrive(0);
-      if constexpr (W::BF) {
-        if (nf > 0) {
-          const int nb = KT / 32 / KW;  // blocks of a tile that are the wave's
-          // LDS offset of the wave's i-th block in tile t
-          const uint32_t lds0 = lds_offset(smem) + kw * 512 * G;
-          const int stride = KW * 512 * G;
-          auto at = [&](int t, int i) { return lds0 + (t & 1) * 2 * MB + i * stride; };
-          u32x4 kf[QS];
-          f32x16 s0[QW], s1[QW];
-          float mx[QW];
-          w.keys(at(0, 0), kf);
-          w.scores(kf, s0);
-          w.shift(s0, mx, c2);
-          if (nb > 1) w.keys(at(0, 1), kf);
-          const int n = nf * nb;
-          int t = 0, i = 0;
-          auto one = [&](f32x16(&s)[QW], f32x16(&sn)[QW]) __attribute__((always_inline)) {
-            const bool last = i == nb - 1;
-            if (last && t + 1 < nt) {
-              arrive(t + 1);
-              w.keys(at(t + 1, 0), kf);  // (a partial tile's: not used)
-            }
-            // the keys after next, where they are in the next block's tile
-            const bool two = last ? nb > 1 && t + 1 < nt : i + 2 < nb;
-            const uint32_t next = last ? at(t + two, two) : at(t, two ? i + 2 : i);
-            // (also for query rows past the last: they repeat it)
-            w.block(at(t, i) + MB, next, kf, s, sn, mx, c2);
-            if (last) leave(t);
-            t += last ? 1 : 0;
-            i = last ? 0 : i + 1;
-          };
-          for (int j = 0; j < n; j += 2) {
-            one(s0, s1);
-            if (j + 1 < n) one(s1, s0);
+    auto commit = [&](int t) __attribute__((always_inline)) {
+      st[0].commit(smem + slot_of(t) * 2 * MB);
+      if (us > 1) st[1].commit(smem + (slot_of(t) + 1) * 2 * MB);
+    };
+    // tile t is in its slot once every wave has passed the barrier behind this
+    auto landed = [&](int t) __attribute__((always_inline)) {
+      wait_vmcnt_chunks<2 * TileLoads<T, D>::N>((queued - 1 - t) * us);
+    };
+    // The query operands: loaded beside the first tile, and waited for here, so
+    // that the compiler's wait for them is no wait for a tile later on.  Those of
+    // 64 rows of 128 channels are put into the accumulation half of the
+    // registers, from where the products take them: in the other half they were
+    // copied there and back in every block.
+    queue(0);
+#pragma unroll
+    for (int b = 0; b < QW; ++b) {
+      const int m = mb * mrows + (qw * QW + b) * 32 + l32;
+      const u32x4* src = reinterpret_cast<const u32x4*>(static_cast<const T*>(a.Q) +
+                                                        (long)row_of(min(m, M - 1)) * D);
+#pragma unroll
+      for (int j = 0; j < QS; ++j) w.q[b][j] = src[2 * j + h];
+    }
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+    if constexpr (W::BF && QW * QS >= 16) {
+#pragma unroll
+      for (int b = 0; b < QW; ++b)
+#pragma unroll
+        for (int j = 0; j < QS; ++j) asm volatile("" : "+a"(w.q[b][j]));
+    }
+
+    // LDS offset of the wave's first block in tile t
+    const uint32_t lds0 = lds_offset(smem) + (us > 1 ? (kw >> 1) * 2 * MB : 0) +
+                          (us > 1 ? kw & 1 : kw) * 2048;
+    auto tile_at = [&](int t) { return lds0 + slot_of(t) * 2 * MB; };
+    // whole tiles in the pipelined loop (bf16)
+    const int nf = !W::BF || KW == 4 || w.neg ? 0 : nk / KT;
+    if constexpr (W::BF) {
+      if (nf > 0) {
+        // Before tile t: tile t + 1 visible, t - 1 left by all; t + 2 in flight
+        // and t + 3 queued over the tile's blocks.
+        if constexpr (QUANT) {
+          commit(0);
+          if (nt > 1) {
+            queue(1);
+            commit(1);
           }
-        }
-      }
-      for (int t = nf; t < nt; ++t) {
-        if (t > nf) arrive(t);
-        const int nr = min(KT, nk - t * KT);
-        unsigned char* Vb = slot_of(t) + MB;
-        if (nr < KT) {  // rows past the range repeat its last one: 0 there, as 0
-                        // times an infinite value is NaN
-          for (int i = nr * G + threadIdx.x; i < KT * G; i += kPrefixBlock)
-            reinterpret_cast<u32x4*>(Vb)[i] = u32x4{0u, 0u, 0u, 0u};
-          lds_barrier();
-        }
-        if (active)
-          for (int sb = 32 * kw; sb < nr; sb += 32 * KW) w.step(slot_of(t), Vb, sb, nr, c2);
-        leave(t);
-      }
-    };
-    if (FMT == WF_CACHE_PLAIN || own) {
-      // direct loads to LDS, up to two tiles ahead
-      const T* Kg = reinterpret_cast<const T*>(own ? a.Kt : a.K) + (long)unit * rows.cap * D;
-      const T* Vg = reinterpret_cast<const T*>(own ? a.Vt : a.V) + (long)unit * rows.cap * D;
-      constexpr int IPW = KT * G / (64 * kPrefixWaves);  // loads per wave and matrix
-      constexpr int RPI = 64 / G;
-      constexpr int RB = D * W::ES;                      // bytes of a row
-      const uint32_t lds0 = lds_offset(smem) + 1024u * IPW * wave;
-      // byte offsets of the lane's loads in a tile of consecutive rows
-      uint32_t off[IPW];
-#pragma unroll
-      for (int i = 0; i < IPW; ++i) {
-        const int r = (wave * IPW + i) * RPI + lane / G;
-        off[i] = r * RB + 16 * ((lane % G) ^ tile_swz<T, G>(r));
-      }
-      int issued = 0;  // tiles queued so far
-      auto issue = [&](int t) __attribute__((always_inline)) {
-        stage_ids(t);
-        issued = t + 1;
-        const uint32_t at = lds0 + (t & 1) * 2 * MB;
-        if (!rows.ids && nk - t * KT >= KT) {  // uniform
-          const T* kt = Kg + (long)(k0 + t * KT) * D;
-          const T* vt = Vg + (long)(k0 + t * KT) * D;
-#pragma unroll
-          for (int i = 0; i < IPW; ++i) tile_load(kt, off[i], at + 1024u * i);
-#pragma unroll
-          for (int i = 0; i < IPW; ++i) tile_load(vt, off[i], at + MB + 1024u * i);
+          if (nt > 2) queue(2);
         } else {
-#pragma unroll 1
-          for (int i = 0; i < IPW; ++i) {
-            const int r = (wave * IPW + i) * RPI + lane / G;
-            const long o = rows(t * KT + r) * D + W::EPV * ((lane % G) ^ tile_swz<T, G>(r));
-            async_load16<false>(Kg + o, __builtin_amdgcn_readfirstlane(at + 1024u * i));
-            async_load16<false>(Vg + o, __builtin_amdgcn_readfirstlane(at + MB + 1024u * i));
+          if (nt > 1) queue(1);
+          if (nt > 2) queue(2);
+          landed(0);
+        }
+        lds_barrier();
+        u32x4 kf[QS];
+        f32x16 s0[QW], s1[QW];
+        float mx[QW];
+        w.keys(tile_at(0), kf);
+        w.scores(kf, s0);
+        w.shift(s0, mx, c2);
+        if (KW == 1) w.keys(tile_at(0) + 2048, kf);
+        auto begin = [&](int t) __attribute__((always_inline)) {
+          if (t + 1 >= nt) return;
+          if constexpr (!QUANT) landed(t + 1);
+          lds_barrier();
+          if constexpr (QUANT) {
+            if (t + 2 < nt) commit(t + 2);
+            if (t + 3 < nt) queue(t + 3);
+          }
+        };
+        // Whether the loads of tile t + 3 go between the products of tile t; else
+        // they are queued at once, if there are any.
+        auto spread = [&](int t) __attribute__((always_inline)) {
+          if (QUANT || t + 3 >= nt) return false;
+          if (!straight(t + 3)) {
+            queue(t + 3);
+            return false;
+          }
+          queued = t + 4;
+          return true;
+        };
+        constexpr int N = TileLoads<T, D>::N;  // tile loads of K, of V
+        if (KW == 1) {
+          for (int t = 0; t < nf; ++t) {
+            begin(t);
+            const auto ahead = dma.at(k0 + (long)(t + 3) * KT, slot_of(t + 3), spread(t));
+            const uint32_t now = tile_at(t) + MB, next = tile_at(t + 1 < nt ? t + 1 : t);
+            w.template block<QUANT ? 0 : N>(now, next, kf, s0, s1, mx, c2,
+                                            [&](int i, int e) __attribute__((always_inline)) {
+                                              if (ahead.go) load_some<T, D, 0>(dma, i, e, ahead);
+                                            });
+            w.template block<QUANT ? 0 : N>(now + 2048, next + 2048, kf, s1, s0, mx, c2,
+                                            [&](int i, int e) __attribute__((always_inline)) {
+                                              if (ahead.go) load_some<T, D, N>(dma, i, e, ahead);
+                                            });
+          }
+        } else {
+          auto one = [&](int t, f32x16(&s)[QW], f32x16(&sn)[QW]) __attribute__((always_inline)) {
+            begin(t);
+            const auto ahead = dma.at(k0 + (long)(t + 3) * KT, slot_of(t + 3), spread(t));
+            w.keys(tile_at(t + 1 < nt ? t + 1 : t), kf);
+            w.template block<QUANT ? 0 : 2 * N>(
+                tile_at(t) + MB, tile_at(t), kf, s, sn, mx, c2,
+                [&](int i, int e) __attribute__((always_inline)) {
+                  if (ahead.go) load_some<T, D, 0>(dma, i, e, ahead);
+                });
+          };
+          for (int t = 0; t < nf; t += 2) {
+            one(t, s0, s1);
+            if (t + 1 < nf) one(t + 1, s1, s0);
           }
         }
-      };
-      issue(0);
-      queries();
-      if (nt > 1) issue(1);
-      run(
-          [&](int t) __attribute__((always_inline)) {
-            // tile t + 1 may be in flight: it is queued when tile t - 1 is left,
-            // after tile t arrives in the pipelined loop, before in the other
-            wait_vmcnt_chunks<2 * IPW>(issued > t + 1 ? 1 : 0);
-            lds_barrier();
-          },
-          [&](int t) __attribute__((always_inline)) {
-            lds_barrier();
-            if (t + 2 < nt) issue(t + 2);
-          });
-    } else {
-      // codes are loaded to registers a tile ahead, and decoded into LDS
-      if constexpr (FMT != WF_CACHE_PLAIN) {
-        QuantStage<T, D, FMT> st;
-        stage_ids(0);
-        st.load(a, rows, unit, 0);
-        queries();
-        run(
-            [&](int t) __attribute__((always_inline)) {
-              unsigned char* Kb = smem + (t & 1) * 2 * MB;
-              st.commit(Kb, Kb + MB);
-              if (t + 1 < nt) {
-                stage_ids(t + 1);
-                st.load(a, rows, unit, (t + 1) * KT);
-              }
-              lds_barrier();
-            },
-            [&](int) __attribute__((always_inline)) { lds_barrier(); });
       }
     }
+    // The other tiles: tile t visible, then computed, with up to ns - 1 tiles
+    // behind it on their way.
+    if (nf == 0 && !QUANT)
+      for (int t = 1; t < min(nt, ns - 1); ++t) queue(t);
+    for (int t = nf; t < nt; ++t) {
+      if (nf == 0) {  // (else the tile has been visible since the last whole one)
+        if constexpr (QUANT) {
+          commit(t);
+          if (t + 1 < nt) queue(t + 1);
+        } else {
+          landed(t);
+        }
+        lds_barrier();
+        if (!QUANT && t + ns - 1 < nt) queue(t + ns - 1);
+      }
+      const int nr = nk - t * KT;  // rows of the tile that are in the range
+      if (nr < KT) {
+        const int last = (nr - 1) / kTileRows;  // its last 64 rows
+        if (nr % kTileRows)
+          clear_rows<T, D>(smem + (slot_of(t) + last) * 2 * MB, nr - last * kTileRows);
+      }
+      for (int r = 32 * kw; r < min(nr, KT); r += 32 * KW) {
+        const uint32_t at = lds_offset(smem) + (slot_of(t) + r / kTileRows) * 2 * MB +
+                            r % kTileRows * 64;
+        w.step(at, at + MB, min(32, nr - r), c2);
+      }
+    }
+    lds_barrier();  // the tiles are idle
   }
 
-  // merge the waves that took keys in turn: each adds up a share of the
-  // channels (the tiles are idle: every wave passed the barrier after the loop)
-#pragma unroll
-  for (int b = 0; b < QW; ++b) w.l[b] += partner32(w.l[b]);
-  constexpr int OW = QW * DT * 16 * 64;  // floats of a wave's output
-  float* oo = reinterpret_cast<float*>(smem);
-  float* sm = oo + kPrefixWaves * OW;    // [waves][QW][32] references, then sums
-  float* sl = sm + kPrefixWaves * QW * 32;
-  int dshare = DT, d0 = 0;               // the wave's output tiles
-  if (KW > 1) {
-    if (nk > 0 && active) {
-#pragma unroll
-      for (int b = 0; b < QW; ++b) {
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            oo[wave * OW + ((b * DT + d) * 16 + i) * 64 + lane] = w.O[b][d][i];
-        if (h == 0) {
-          sm[(wave * QW + b) * 32 + l32] = w.mref[b];
-          sl[(wave * QW + b) * 32 + l32] = w.l[b];
-        }
-      }
-    }
-    lds_barrier();
-    dshare = max(1, DT / KW);
-    d0 = kw * dshare;
-    if (nk > 0 && active) {
-#pragma unroll
-      for (int b = 0; b < QW; ++b) {
-        float M2 = -INFINITY, z = 0.f;
-        for (int k = 0; k < KW; ++k) M2 = fmaxf(M2, sm[((wave - kw + k) * QW + b) * 32 + l32]);
-        float acc[DT][16];
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
-        for (int k = 0; k < KW; ++k) {
-          const int v = wave - kw + k;
-          const float mk = sm[(v * QW + b) * 32 + l32];
-          const float f = mk > -INFINITY ? __builtin_amdgcn_exp2f(mk - M2) : 0.f;
-          z += f * sl[(v * QW + b) * 32 + l32];
-#pragma unroll
-          for (int d = 0; d < DT; ++d)
-            if (d >= d0 && d < d0 + dshare)
-#pragma unroll
-              for (int i = 0; i < 16; ++i)
-                acc[d][i] += f * oo[v * OW + ((b * DT + d) * 16 + i) * 64 + lane];
-        }
-        w.mref[b] = M2;
-        w.l[b] = z;
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) w.O[b][d][i] = acc[d][i];
-      }
-    }
-  }
-  if (!active) return;
-#pragma unroll
-  for (int b = 0; b < QW; ++b) {
-    const int m = m0 + 32 * b + l32;
-    if (m >= M) continue;
-    const long row = row_of(m);
-    const float inv = w.l[b] == 0.f ? 0.f : 1.f / w.l[b];
-    if (a.slots == 1) {
-      T* dst = reinterpret_cast<T*>(a.O) + row * D;
-#pragma unroll
-      for (int d = 0; d < DT; ++d)
-        if (d >= d0 && d < d0 + dshare)
-#pragma unroll
-          for (int i = 0; i < 16; i += 4)
-            put4<T>(dst + 32 * d + 2 * i + 4 * h, w.O[b][d][i] * inv, w.O[b][d][i + 1] * inv,
-                    w.O[b][d][i + 2] * inv, w.O[b][d][i + 3] * inv);
-      if (a.lse && kw == 0 && h == 0)
-        a.lse[row] = w.l[b] == 0.f ? -INFINITY : (w.mref[b] + __log2f(w.l[b])) * kLn2;
+  OutRows<D, QW> out(smem);
+  out.put(w, wave);
+  constexpr int C4 = D / 4, RPP = kPrefixBlock / C4;  // rows per round
+  const int c = threadIdx.x % C4;
+#pragma unroll 4
+  for (int r = threadIdx.x / C4; r < mrows; r += RPP) {
+    const int m = mb * mrows + r;
+    if (m >= M) break;
+    // row r of the workgroup is in row r % (32 QW) of the KW waves of its rows
+    const Merge4 g = out.merged(r / (32 * QW) * KW * 32 * QW + r % (32 * QW), KW, c);
+    const int row = row_of(m);
+    if (a.whole) {
+      g.finish(static_cast<T*>(a.O) + (long)row * D + 4 * c, a.lse ? a.lse + row : nullptr, c == 0);
     } else {
-      float* dst = a.part + (row * a.slots + slot) * D;
-      if (nk > 0) {
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-          if (d >= d0 && d < d0 + dshare)
-#pragma unroll
-            for (int i = 0; i < 16; i += 4)
-              put4<float>(dst + 32 * d + 2 * i + 4 * h, w.O[b][d][i], w.O[b][d][i + 1],
-                          w.O[b][d][i + 2], w.O[b][d][i + 3]);
-      }
-      if (kw == 0 && h == 0) {
-        a.pstat[(row * a.slots + slot) * 2] = w.mref[b];
-        a.pstat[(row * a.slots + slot) * 2 + 1] = w.l[b];
-      }
+      const long s = (long)row * a.slots + sp;
+      if (nk > 0) *reinterpret_cast<f32x4*>(a.part + s * D + 4 * c) = g.o;
+      if (c == 0) *reinterpret_cast<hw_f32x2*>(a.pstat + 2 * s) = hw_f32x2{g.M, g.z};
     }
   }
 }
 
-// Merges the partials of each query row.  A thread takes eight channels of every
-// SG-th partial of a row, four of them in flight; the SG threads of a row's
-// channels meet in LDS.  (33 partials of 256 rows: 24 us with SG = 1.)
-template <typename T, int SG>
-__global__ __launch_bounds__(kBlock) void prefix_merge_kernel(PrefixArgs a, long rows, int D) {
-  const int tpr = D / 8, rpb = kBlock / (tpr * SG);
-  const int c = threadIdx.x % tpr, sg = threadIdx.x / tpr % SG, rl = threadIdx.x / (tpr * SG);
-  const long row = (long)blockIdx.x * rpb + rl;
-  float M = -INFINITY, z = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  // one partial into the running ones; an empty range (-inf, 0) has no output
-  auto add = [&](float m, float zs, const float* x) {
-    if (m == -INFINITY && zs == 0.f) return;
-    const float mn = fmaxf(M, m);
-    // (all scores -inf or NaN: zs says it)
-    const float f = m > -INFINITY ? __builtin_amdgcn_exp2f(m - mn) : 1.f;
-    const float g = M > -INFINITY ? __builtin_amdgcn_exp2f(M - mn) : 1.f;
-    M = mn;
-    z = z * g + f * zs;
+// A sequence's rows over its own keys, merged with the partials of the prefix.
+// The keys are few (a block, a generated tail): a workgroup takes all of them,
+// and 32 rows per wave that does not share its rows' keys with others.
+template <typename T, int D>
+__global__ __launch_bounds__(kPrefixBlock, 2) void prefix_own_kernel(PrefixArgs a) {
+  using W = PrefixWave<T, D, 1>;
+  using Geom = TileGeom<T, D>;
+  constexpr int MB = Geom::MB, QS = W::QS, N = TileLoads<T, D>::N;
+  extern __shared__ __align__(16) unsigned char smem[];  // [2][K, V] tiles
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h = lane >> 5, l32 = lane & 31;
+  const int mb = blockIdx.x % a.t.mblocks, unit = blockIdx.x / a.t.mblocks;  // (sequence, head)
+  const int KW = a.t.kw, kw = wave % KW, qw = wave / KW;
+  const int mrows = a.t.qw * 32;  // query rows of the workgroup
+  const int m0 = mb * mrows;
+  const int n = a.tlen ? min(max(a.tlen[unit / a.heads], 0), a.T) : a.T;
+  const long row0 = (long)unit * a.R;
+  W w;
+  w.init(a.scale);
+  const float c2 = fabsf(a.scale) * kLog2e;
+  if (n > 0) {
+    const int nt = (n + kTileRows - 1) / kTileRows;
+    TileLoads<T, D> dma;
+    dma.init(static_cast<const T*>(a.Kt) + (long)unit * a.T * D,
+             static_cast<const T*>(a.Vt) + (long)unit * a.T * D, lds_offset(smem));
+    KeyRows rows;
+    rows.ids = nullptr;
+    rows.cap = a.T;
+    rows.k0 = rows.id0 = 0;
+    rows.last = n - 1;
+    auto queue = [&](int t) __attribute__((always_inline)) {
+      dma.tile(rows, t * kTileRows, n - t * kTileRows >= kTileRows, t & 1);
+    };
+    queue(0);
+    const u32x4* src = reinterpret_cast<const u32x4*>(
+        static_cast<const T*>(a.Q) + (row0 + min(m0 + qw * 32 + l32, a.R - 1)) * D);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] = o[e] * g + f * x[e];
-  };
-  if (row < rows) {
-    const float* st = a.pstat + row * a.slots * 2;
-    const float* src = a.part + row * a.slots * D + 8 * c;
-    constexpr int F = 4;
-    for (int s0 = sg; s0 < a.slots; s0 += F * SG) {
-      float m[F], zs[F];
-      f32x4 x[F][2];
-#pragma unroll
-      for (int k = 0; k < F; ++k) {
-        const int s = min(s0 + k * SG, a.slots - 1);
-        m[k] = s0 + k * SG < a.slots ? st[2 * s] : -INFINITY;
-        zs[k] = s0 + k * SG < a.slots ? st[2 * s + 1] : 0.f;
-        x[k][0] = reinterpret_cast<const f32x4*>(src + (long)s * D)[0];
-        x[k][1] = reinterpret_cast<const f32x4*>(src + (long)s * D)[1];
-      }
-#pragma unroll
-      for (int k = 0; k < F; ++k) {
-        const float v[8] = {x[k][0][0], x[k][0][1], x[k][0][2], x[k][0][3],
-                            x[k][1][0], x[k][1][1], x[k][1][2], x[k][1][3]};
-        add(m[k], zs[k], v);
-      }
+    for (int j = 0; j < QS; ++j) w.q[0][j] = src[2 * j + h];
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): the queries, and tile 0
+    for (int t = 0; t < nt; ++t) {
+      wait_vmcnt_chunks<2 * N>(0);
+      lds_barrier();  // tile t visible, everyone is past tile t - 1
+      if (t + 1 < nt) queue(t + 1);
+      const int nr = n - t * kTileRows;
+      unsigned char* tile = smem + (t & 1) * 2 * MB;
+      if (nr < kTileRows) clear_rows<T, D>(tile, nr);
+      if (qw < a.t.qw)
+        for (int r = 32 * kw; r < min(nr, kTileRows); r += 32 * KW) {
+          const uint32_t at = lds_offset(tile) + r * 64;
+          w.step(at, at + MB, min(32, nr - r), c2);
+        }
     }
+    lds_barrier();
   }
+  OutRows<D, 1> out(smem);
+  out.put(w, wave);
+  constexpr int C4 = D / 4, RPP = kPrefixBlock / C4;  // rows per round
+  const int c = threadIdx.x % C4;
+  const int mend = min(mrows, a.R - m0);
+#pragma unroll 2
+  for (int r = threadIdx.x / C4; r < mend; r += RPP) {
+    Merge4 g = out.merged(r / 32 * KW * 32 + r % 32, KW, c);
+    const long row = row0 + m0 + r;
+    if (a.slots > 0) merge_partials<D>(a, row, c, 0, 1, g);
+    g.finish(static_cast<T*>(a.O) + row * D + 4 * c, a.lse ? a.lse + row : nullptr, c == 0);
+  }
+}
+
+// Merges the partials of each query row.  A thread takes four channels of every
+// SG-th partial of a row; the SG threads of a row's channels meet in LDS.
+template <typename T, int D, int SG>
+__global__ __launch_bounds__(kBlock) void prefix_merge_kernel(PrefixArgs a, long nrows) {
+  constexpr int C4 = D / 4, RPB = kBlock / (C4 * SG);
+  const int c = threadIdx.x % C4, sg = threadIdx.x / C4 % SG;
+  const long row = (long)blockIdx.x * RPB + threadIdx.x / (C4 * SG);
+  Merge4 g;
+  if (row < nrows) merge_partials<D>(a, row, c, sg, SG, g);
   if constexpr (SG > 1) {
-    __shared__ float sh[kBlock][11];  // (odd stride: no bank met twice)
+    __shared__ float sh[kBlock][7];  // (odd stride: no bank met twice)
     float* mine = sh[threadIdx.x];
-    mine[0] = M;
-    mine[1] = z;
+    mine[0] = g.M;
+    mine[1] = g.z;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) mine[2 + e] = o[e];
+    for (int e = 0; e < 4; ++e) mine[2 + e] = g.o[e];
     __syncthreads();
     if (sg != 0) return;  // no barrier follows
 #pragma unroll
     for (int k = 1; k < SG; ++k) {
-      const float* other = sh[threadIdx.x + k * tpr];
-      add(other[0], other[1], other + 2);
+      const float* x = sh[threadIdx.x + k * C4];
+      g.add(x[0], x[1], f32x4{x[2], x[3], x[4], x[5]});
     }
   }
-  if (row >= rows) return;
-  const float inv = z == 0.f ? 0.f : 1.f / z;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) o[e] *= inv;
-  T* dst = reinterpret_cast<T*>(a.O) + row * D + 8 * c;
-  put4<T>(dst, o[0], o[1], o[2], o[3]);
-  put4<T>(dst + 4, o[4], o[5], o[6], o[7]);
-  if (a.lse && c == 0) a.lse[row] = z == 0.f ? -INFINITY : (M + __log2f(z)) * kLn2;
+  if (row < nrows)
+    g.finish(static_cast<T*>(a.O) + row * D + 4 * c, a.lse ? a.lse + row : nullptr, c == 0);
 }
 
 // ------------------------------------------------------------ host side
@@ -872,134 +1030,142 @@ __global__ __launch_bounds__(kBlock) void prefix_merge_kernel(PrefixArgs a, long
 PrefixPlan plan_prefix(const wf_prefix_params& p) {
   PrefixPlan l{};
   const bool bf = p.dtype == WF_BF16;
-  const int es = bf ? 2 : 4, KT = bf ? 128 : 64, nblk = KT / 32;
+  const int D = p.head_dim;
   const long R = (long)p.group * p.q_len, M = R * p.share, U = (long)p.prefixes * p.heads;
-  const long rows = M * U;
-  const long slots_at_once = device_cu_count();
-  const long most = p.prefix_rows > 0 ? M : R;
-  l.qw = bf && most > 32 ? 2 : 1;
-  // waves over query rows (the others over keys), blocks of query rows
-  auto shape = [&](long m, int* kw, int* mblocks) {
-    const long blocks = (m + 32 * l.qw - 1) / (32 * l.qw);
-    int qwaves = 1;
+  const long rows = M * U, cus = device_cu_count();
+  const int mb = kTileRows * D * (bf ? 2 : 4);  // bytes of a K (or V) tile
+  const int slots = 8 * mb > 131072 ? 2 : 4;
+  if (p.prefix_rows > 0) {
+    // 64 query rows per wave halve the LDS reads of 32; waves over query rows as
+    // far as there are any, the others over the keys
+    l.qw = bf && M > 32 ? 2 : 1;
+    const long blocks = (M + 32 * l.qw - 1) / (32 * l.qw);
+    int qwaves = bf ? 1 : 2;
     while (qwaves < kPrefixWaves && qwaves < blocks) qwaves *= 2;
-    while (kPrefixWaves / qwaves > nblk) qwaves *= 2;
-    *kw = kPrefixWaves / qwaves;
-    *mblocks = (int)((blocks + qwaves - 1) / qwaves);
-  };
-  // Key ranges per unit: whole rounds of workgroups, each with a fixed part of
-  // about a tile, against the partials that every range adds.
-  auto split = [&](long units, long keys, int mblocks, int* splits, int* rps) {
-    const long tiles = (keys + KT - 1) / KT;
-    const long top = std::min(tiles, 2 * slots_at_once / (units * mblocks) + 1);
+    l.kw = kPrefixWaves / qwaves;
+    l.mblocks = (int)((blocks + qwaves - 1) / qwaves);
+    // Key ranges per unit: whole rounds of workgroups, each with a fixed part of
+    // about two tiles, against the partials that every range adds (a write and a
+    // read of D floats a row at about 5 TB/s, a tile of 64 keys in about 1.2 us).
+    const long KT = l.kw == 4 ? 2 * kTileRows : kTileRows;
+    const long tiles = (p.prefix_rows + KT - 1) / KT;
+    const long top = std::min(tiles, 2 * cus / (U * l.mblocks) + 1);
+    const double fixed = KT == kTileRows ? 2.5 : 1.2, partial = (double)rows * D * 8 /
+                                                              (KT == kTileRows ? 6e6 : 11e6);
     long best = 1;
     double best_cost = 0;
     for (long s = 1; s <= top; ++s) {
       const long per = (tiles + s - 1) / s;
       if ((tiles + per - 1) / per != s) continue;
-      const long n = units * mblocks * s;
-      const double cost = (double)((n + slots_at_once - 1) / slots_at_once) * ((double)per + 1.2) +
-                          (double)s * rows * p.head_dim * 8 / 11e6;
+      const long n = U * l.mblocks * s;
+      const double cost =
+          (double)((n + cus - 1) / cus) * ((double)per + fixed) + (double)s * partial;
       if (best_cost == 0 || cost < best_cost) {
         best_cost = cost;
         best = s;
       }
     }
-    const long per = (tiles + best - 1) / best;
-    *rps = (int)(per * KT);
-    *splits = (int)((tiles + per - 1) / per);
-  };
-  if (p.prefix_rows > 0) {
-    shape(M, &l.kw, &l.mblocks);
-    split(U, p.prefix_rows, l.mblocks, &l.splits, &l.rps);
+    l.rps = (int)((tiles + best - 1) / best * KT);
+    l.splits = (int)((p.prefix_rows + l.rps - 1) / l.rps);
     l.items = U * l.mblocks * l.splits;
+    const size_t out = l.qw == 2 ? (size_t)kPrefixWaves * 64 * (D + 6) * sizeof(float)
+                                 : (size_t)kPrefixWaves * 32 * (D + 6) * sizeof(float);
+    l.lds_bytes = std::max((size_t)slots * 2 * mb, out);
+    l.ids_bytes = (size_t)slots * 2 * mb + std::min(l.rps, kPrefixIds) * sizeof(int32_t);
   }
   if (p.tail_cap > 0) {
-    shape(R, &l.tkw, &l.tmblocks);
-    split(U * p.share, p.tail_cap, l.tmblocks, &l.tsplits, &l.trps);
-    l.titems = U * p.share * l.tmblocks * l.tsplits;
+    // 32 rows per wave; a workgroup takes up to 128 of a sequence's rows, fewer
+    // where that leaves CUs without one
+    const long units = U * p.share, blocks = (R + 31) / 32;
+    l.tqw = (int)std::min(4L, blocks);
+    if (l.tqw == 3) l.tqw = 4;
+    while (l.tqw > 1 && units * ((blocks + l.tqw - 1) / l.tqw) < cus) l.tqw /= 2;
+    l.tkw = l.tqw == 4 ? 1 : 2;
+    l.tmblocks = (int)((blocks + l.tqw - 1) / l.tqw);
+    l.titems = units * l.tmblocks;
+    l.tlds_bytes = std::max((size_t)4 * mb, (size_t)kPrefixWaves * 32 * (D + 6) * sizeof(float));
   }
-  l.slots = l.splits + l.tsplits;
-  l.ids = std::min(l.rps, kPrefixIds);
-  if (l.slots > 1) {
-    l.part_bytes = (size_t)rows * l.slots * p.head_dim * sizeof(float);
+  l.slots = l.splits;
+  if (l.splits > 1 || (l.splits == 1 && l.titems > 0)) {
+    l.part_bytes = (size_t)rows * l.slots * D * sizeof(float);
     l.pstat_bytes = (size_t)rows * l.slots * 2 * sizeof(float);
   }
-  const size_t tiles = (size_t)4 * KT * es * p.head_dim;
-  const size_t merge = (size_t)kPrefixWaves * l.qw * (p.head_dim * 32 + 64) * sizeof(float);
-  l.lds_bytes = std::max(tiles + (size_t)l.ids * sizeof(int32_t), merge);
   return l;
 }
 
-template <typename T, int D, int FMT, int QW>
-static hipError_t prefix_launch(const PrefixArgs& a, size_t lds, hipStream_t s) {
-  auto kern = prefix_attn_kernel<T, D, FMT, QW>;
+template <typename Kernel>
+static hipError_t launch_lds(Kernel kern, long grid, size_t lds, const PrefixArgs& a,
+                             hipStream_t s) {
   if (lds > 65536) {
     hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern),
                                        hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
   }
-  const unsigned grid = (unsigned)(((a.p.items + 7) & ~7) + a.t.items);
-  hipLaunchKernelGGL(kern, dim3(grid), dim3(kPrefixBlock), lds, s, a);
+  hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(kPrefixBlock), lds, s, a);
   return hipGetLastError();
 }
 
-// Threads per row and channels in the merge: enough for every partial of a row to
-// be in flight.
-template <typename T>
-static hipError_t merge_launch(const PrefixArgs& a, long rows, int D, hipStream_t s) {
-  const int sg = a.slots <= 4 ? 1 : a.slots <= 16 ? 4 : 16;
+template <typename T, int D>
+static hipError_t merge_launch(const PrefixArgs& a, long rows, hipStream_t s) {
+  // threads per row and channels: enough for every partial of a row to be in flight
   auto go = [&](auto n) {
     constexpr int SG = decltype(n)::value;
-    const int rpb = kBlock / (D / 8 * SG);
-    hipLaunchKernelGGL((prefix_merge_kernel<T, SG>), dim3((unsigned)((rows + rpb - 1) / rpb)),
-                       dim3(kBlock), 0, s, a, rows, D);
+    constexpr int RPB = kBlock / (D / 4 * SG);
+    hipLaunchKernelGGL((prefix_merge_kernel<T, D, SG>), dim3((unsigned)((rows + RPB - 1) / RPB)),
+                       dim3(kBlock), 0, s, a, rows);
   };
-  if (sg == 1)
+  if (a.slots <= 8)
     go(std::integral_constant<int, 1>{});
-  else if (sg == 4)
+  else if (a.slots <= 32)
     go(std::integral_constant<int, 4>{});
   else
-    go(std::integral_constant<int, 16>{});
+    go(std::integral_constant<int, 8>{});
   return hipGetLastError();
 }
 
-hipError_t launch_prefix(const wf_prefix_params& p, PrefixArgs& a, hipStream_t s) {
-  const PrefixPlan l = plan_prefix(p);
+hipError_t launch_prefix(const wf_prefix_params& p, const PrefixPlan& l, PrefixArgs& a,
+                         hipStream_t s) {
   a.heads = p.heads;
   a.share = p.share;
   a.R = p.group * p.q_len;
+  a.by_R = FastDiv::by(a.R);
   a.cap = p.prefix_cap;
   a.rows = p.prefix_rows;
   a.T = p.tail_cap;
   a.slots = l.slots;
-  a.ids = l.ids;
+  a.whole = l.part_bytes == 0;
   a.scale = p.scale != 0.f ? p.scale : (float)(1.0 / std::sqrt((double)p.head_dim));
-  a.p = PrefixPart{(int)l.items, l.splits, l.rps, l.mblocks, a.R * p.share, l.kw};
-  a.t = PrefixPart{(int)l.titems, l.tsplits, l.trps, l.tmblocks, a.R, l.tkw};
-  auto go = [&](auto t, auto d, auto f) {
+  a.p = PrefixPart{(int)l.items, l.splits, l.rps, l.mblocks, a.R * p.share, l.kw, l.qw};
+  a.t = PrefixPart{(int)l.titems, 1, p.tail_cap, l.tmblocks, a.R, l.tkw, l.tqw};
+  auto run = [&](auto t, auto d) {
     using T = decltype(t);
-    constexpr int D = decltype(d)::value, F = decltype(f)::value;
-    if constexpr (sizeof(T) == 2)
-      if (l.qw == 2) return prefix_launch<T, D, F, 2>(a, l.lds_bytes, s);
-    return prefix_launch<T, D, F, 1>(a, l.lds_bytes, s);
+    constexpr int D = decltype(d)::value;
+    if (l.items > 0) {
+      const long grid = (l.items + 7) & ~7L;
+      const size_t lds = a.list ? std::max(l.lds_bytes, l.ids_bytes) : l.lds_bytes;
+      auto go = [&](auto f) {
+        constexpr int F = decltype(f)::value;
+        if constexpr (sizeof(T) == 2)
+          if (l.qw == 2) return launch_lds(prefix_attn_kernel<T, D, F, 2>, grid, lds, a, s);
+        return launch_lds(prefix_attn_kernel<T, D, F, 1>, grid, lds, a, s);
+      };
+      const hipError_t e =
+          p.format == WF_CACHE_E4M3   ? go(std::integral_constant<int, WF_CACHE_E4M3>{})
+          : p.format == WF_CACHE_E2M1 ? go(std::integral_constant<int, WF_CACHE_E2M1>{})
+                                      : go(std::integral_constant<int, WF_CACHE_PLAIN>{});
+      if (e != hipSuccess) return e;
+    }
+    if (l.titems > 0)
+      return launch_lds(prefix_own_kernel<T, D>, l.titems, l.tlds_bytes, a, s);
+    if (!a.whole)
+      return merge_launch<T, D>(a, (long)p.prefixes * p.share * p.heads * a.R, s);
+    return hipSuccess;
   };
-  auto by_format = [&](auto t, auto d) {
-    if (p.format == WF_CACHE_E4M3)
-      return go(t, d, std::integral_constant<int, WF_CACHE_E4M3>{});
-    if (p.format == WF_CACHE_E2M1)
-      return go(t, d, std::integral_constant<int, WF_CACHE_E2M1>{});
-    return go(t, d, std::integral_constant<int, WF_CACHE_PLAIN>{});
-  };
-  auto by_dim = [&](auto t) {
-    return p.head_dim == 128 ? by_format(t, std::integral_constant<int, 128>{})
-                             : by_format(t, std::integral_constant<int, 64>{});
-  };
-  hipError_t e = p.dtype == WF_BF16 ? by_dim(bf16_t{}) : by_dim(float{});
-  if (e != hipSuccess || l.slots == 1) return e;
-  const long rows = (long)p.prefixes * p.share * p.heads * a.R;
-  return p.dtype == WF_BF16 ? merge_launch<bf16_t>(a, rows, p.head_dim, s)
-                            : merge_launch<float>(a, rows, p.head_dim, s);
+  using D64 = std::integral_constant<int, 64>;
+  using D128 = std::integral_constant<int, 128>;
+  if (p.dtype == WF_BF16)
+    return p.head_dim == 128 ? run(bf16_t{}, D128{}) : run(bf16_t{}, D64{});
+  return p.head_dim == 128 ? run(float{}, D128{}) : run(float{}, D64{});
 }
 
 hipError_t load_prefix_kernels() {

@@ -123,9 +123,9 @@ def test_binding_refuses_what_the_parameters_do_not_describe():
             wf.wf_prefix_attn(q, *{**ok, **bad}.values(), None)
 
 
-def test_plans_over_the_range_cover_every_key():
-    """The workspace holds (d + 2) floats per query row and partial, whatever
-    the sizes: whole partials, and none where a row has one."""
+def test_workspaces_over_the_range_hold_whole_partials():
+    """A partial is (d + 2) floats per query row; a call has as many as ranges
+    of its prefix, and none where one range and no own rows are all."""
     import random
     rng = random.Random(4)
     for _ in range(300):
@@ -139,4 +139,6 @@ def test_plans_over_the_range_cover_every_key():
         nb = wf.prefix_workspace_bytes(p)
         assert nb % (rows * (p.head_dim + 2) * 4) == 0
         slots = nb // (rows * (p.head_dim + 2) * 4)
-        assert slots != 1 and (slots or p.tail_cap == 0)
+        assert slots > (1 if p.tail_cap == 0 else 0) or (slots == 0 and p.tail_cap == 0)
+        p.prefix_rows = 0
+        assert wf.prefix_workspace_bytes(p) == 0
