@@ -511,16 +511,32 @@ struct QuantStage {
   }
   __device__ __forceinline__ static int piece() { return (threadIdx.x >> 2) % PPR; }
 
+  // the tile whose first row is `first` of the range; straight: whole and of
+  // consecutive rows
   __device__ __forceinline__ void load(const PrefixArgs& a, const KeyRows& rows, long unit,
-                                       int first) {
+                                       int first, bool straight) {
+    const uint8_t* K = static_cast<const uint8_t*>(a.K);
+    const uint8_t* V = static_cast<const uint8_t*>(a.V);
+    if (PT < kPrefixBlock && (int)threadIdx.x >= PT) return;
+    if (straight) {  // uniform: the lanes' offsets are constant
+      const long r0 = unit * a.cap + rows.k0 + first;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      if (PT < kPrefixBlock && (int)threadIdx.x >= PT) break;
-      const long r = unit * a.cap + rows(first + row(i));
-      w[0][i] = reinterpret_cast<const u32x4*>(a.K)[r * PPR + piece()];
-      w[1][i] = reinterpret_cast<const u32x4*>(a.V)[r * PPR + piece()];
-      x[0][i] = a.Kx[r * (D / 32) + piece() * CPP / 32];
-      x[1][i] = a.Vx[r * (D / 32) + piece() * CPP / 32];
+      for (int i = 0; i < N; ++i) {
+        const uint32_t o = (row(i) * PPR + piece()) * 16, e = row(i) * (D / 32) + piece() * CPP / 32;
+        w[0][i] = *reinterpret_cast<const u32x4*>(K + r0 * (PPR * 16) + o);
+        w[1][i] = *reinterpret_cast<const u32x4*>(V + r0 * (PPR * 16) + o);
+        x[0][i] = (a.Kx + r0 * (D / 32))[e];
+        x[1][i] = (a.Vx + r0 * (D / 32))[e];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const long r = unit * a.cap + rows(first + row(i));
+        w[0][i] = *reinterpret_cast<const u32x4*>(K + (r * PPR + piece()) * 16);
+        w[1][i] = *reinterpret_cast<const u32x4*>(V + (r * PPR + piece()) * 16);
+        x[0][i] = a.Kx[r * (D / 32) + piece() * CPP / 32];
+        x[1][i] = a.Vx[r * (D / 32) + piece() * CPP / 32];
+      }
     }
   }
   __device__ __forceinline__ void commit(unsigned char* tile) const {
@@ -594,15 +610,17 @@ __device__ __forceinline__ void clear_rows(unsigned char* tile, int nr) {
 struct Merge4 {
   float M = -INFINITY, z = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  // (no branches: the loads of several partials stay in flight together)
   __device__ __forceinline__ void add(float m, float zs, const f32x4& x) {
-    if (m == -INFINITY && zs == 0.f) return;  // an empty range: it has no output
+    const bool none = m == -INFINITY && zs == 0.f;  // an empty range: it has no output
     const float mn = fmaxf(M, m);
     // (all scores -inf or NaN: zs says it)
     const float f = m > -INFINITY ? __builtin_amdgcn_exp2f(m - mn) : 1.f;
     const float g = M > -INFINITY ? __builtin_amdgcn_exp2f(M - mn) : 1.f;
     M = mn;
     z = z * g + f * zs;
-    o = o * g + x * f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = o[e] * g + f * (none ? 0.f : x[e]);
   }
   template <typename T>
   __device__ __forceinline__ void finish(T* O, float* lse, bool first) const {
@@ -643,15 +661,22 @@ struct OutRows {
     }
     lds_barrier();
   }
-  // four channels of a row, merged over the KW waves that have it (the first in
-  // row v)
-  __device__ __forceinline__ Merge4 merged(int v, int KW, int c) const {
-    Merge4 g;
+  // four channels of NR rows, each merged over the KW waves that have it (the
+  // first in row v)
+  template <int NR>
+  __device__ __forceinline__ void merged(const int (&v)[NR], int KW, int c, Merge4 (&g)[NR]) const {
     for (int k = 0; k < KW; ++k) {
-      const int x = v + k * 32 * QW;
-      g.add(st[2 * x], st[2 * x + 1], *reinterpret_cast<const f32x4*>(o + x * STRIDE + 4 * c));
+      hw_f32x2 mz[NR];
+      f32x4 x[NR];
+#pragma unroll
+      for (int i = 0; i < NR; ++i) {
+        const int r = v[i] + k * 32 * QW;
+        mz[i] = *reinterpret_cast<const hw_f32x2*>(st + 2 * r);
+        x[i] = *reinterpret_cast<const f32x4*>(o + r * STRIDE + 4 * c);
+      }
+#pragma unroll
+      for (int i = 0; i < NR; ++i) g[i].add(mz[i][0], mz[i][1], x[i]);
     }
-    return g;
   }
 };
 
@@ -665,26 +690,28 @@ __device__ __forceinline__ void load_some(const TileLoads<T, D>& dma, int i, int
   }
 }
 
-// Partials first, first + step, ... of a query row into g, eight in flight.
-template <int D>
-__device__ __forceinline__ void merge_partials(const PrefixArgs& a, long row, int c, int first,
-                                               int step, Merge4& g) {
-  const float* st = a.pstat + row * a.slots * 2;
-  const float* src = a.part + row * a.slots * D + 4 * c;
-  constexpr int F = 8;
+// Partials first, first + step, ... of NR query rows into g, F of each in flight.
+template <int D, int NR, int F>
+__device__ __forceinline__ void merge_partials(const PrefixArgs& a, const long (&row)[NR], int c,
+                                               int first, int step, Merge4 (&g)[NR]) {
   for (int s0 = first; s0 < a.slots; s0 += F * step) {
-    float m[F], z[F];
-    f32x4 x[F];
+    hw_f32x2 mz[NR][F];
+    f32x4 x[NR][F];
 #pragma unroll
-    for (int k = 0; k < F; ++k) {  // (all queued; those past the last are dropped)
-      const int s = min(s0 + k * step, a.slots - 1);
-      const hw_f32x2 mz = *reinterpret_cast<const hw_f32x2*>(st + 2 * s);
-      m[k] = s0 + k * step < a.slots ? mz[0] : -INFINITY;
-      z[k] = s0 + k * step < a.slots ? mz[1] : 0.f;
-      x[k] = *reinterpret_cast<const f32x4*>(src + (long)s * D);
-    }
+    for (int i = 0; i < NR; ++i)
 #pragma unroll
-    for (int k = 0; k < F; ++k) g.add(m[k], z[k], x[k]);
+      for (int k = 0; k < F; ++k) {  // (all queued; those past the last are dropped)
+        const long s = row[i] * a.slots + min(s0 + k * step, a.slots - 1);
+        mz[i][k] = *reinterpret_cast<const hw_f32x2*>(a.pstat + 2 * s);
+        x[i][k] = *reinterpret_cast<const f32x4*>(a.part + s * D + 4 * c);
+      }
+#pragma unroll
+    for (int i = 0; i < NR; ++i)
+#pragma unroll
+      for (int k = 0; k < F; ++k) {
+        const bool in = s0 + k * step < a.slots;
+        g[i].add(in ? mz[i][k][0] : -INFINITY, in ? mz[i][k][1] : 0.f, x[i][k]);
+      }
   }
 }
 
@@ -757,8 +784,8 @@ __global__ __launch_bounds__(kPrefixBlock, 1) void prefix_attn_kernel(PrefixArgs
       stage_ids(t);
       queued = t + 1;
       if constexpr (QUANT) {
-        st[0].load(a, rows, unit, t * KT);
-        if (us > 1) st[1].load(a, rows, unit, t * KT + kTileRows);
+        st[0].load(a, rows, unit, t * KT, straight(t));
+        if (us > 1) st[1].load(a, rows, unit, t * KT + kTileRows, straight(t));
       } else {
         dma.tile(rows, t * KT, straight(t), slot_of(t));
         if (us > 1) dma.tile(rows, t * KT + kTileRows, straight(t), slot_of(t) + 1);
@@ -911,19 +938,31 @@ __global__ __launch_bounds__(kPrefixBlock, 1) void prefix_attn_kernel(PrefixArgs
   out.put(w, wave);
   constexpr int C4 = D / 4, RPP = kPrefixBlock / C4;  // rows per round
   const int c = threadIdx.x % C4;
-#pragma unroll 4
-  for (int r = threadIdx.x / C4; r < mrows; r += RPP) {
-    const int m = mb * mrows + r;
-    if (m >= M) break;
+  constexpr int NR = 4;
+  const int mend = min(mrows, M - mb * mrows);
+  for (int r0 = threadIdx.x / C4; r0 < mend; r0 += NR * RPP) {
+    int v[NR];
+    Merge4 g[NR];
     // row r of the workgroup is in row r % (32 QW) of the KW waves of its rows
-    const Merge4 g = out.merged(r / (32 * QW) * KW * 32 * QW + r % (32 * QW), KW, c);
-    const int row = row_of(m);
-    if (a.whole) {
-      g.finish(static_cast<T*>(a.O) + (long)row * D + 4 * c, a.lse ? a.lse + row : nullptr, c == 0);
-    } else {
-      const long s = (long)row * a.slots + sp;
-      if (nk > 0) *reinterpret_cast<f32x4*>(a.part + s * D + 4 * c) = g.o;
-      if (c == 0) *reinterpret_cast<hw_f32x2*>(a.pstat + 2 * s) = hw_f32x2{g.M, g.z};
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+      const int r = min(r0 + i * RPP, mend - 1);
+      v[i] = r / (32 * QW) * KW * 32 * QW + r % (32 * QW);
+    }
+    out.merged(v, KW, c, g);
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+      const int r = r0 + i * RPP;
+      if (r >= mend) break;
+      const int row = row_of(mb * mrows + r);
+      if (a.whole) {
+        g[i].finish(static_cast<T*>(a.O) + (long)row * D + 4 * c, a.lse ? a.lse + row : nullptr,
+                    c == 0);
+      } else {
+        const long s = (long)row * a.slots + sp;
+        if (nk > 0) *reinterpret_cast<f32x4*>(a.part + s * D + 4 * c) = g[i].o;
+        if (c == 0) *reinterpret_cast<hw_f32x2*>(a.pstat + 2 * s) = hw_f32x2{g[i].M, g[i].z};
+      }
     }
   }
 }
@@ -988,13 +1027,31 @@ __global__ __launch_bounds__(kPrefixBlock, 2) void prefix_own_kernel(PrefixArgs 
   constexpr int C4 = D / 4, RPP = kPrefixBlock / C4;  // rows per round
   const int c = threadIdx.x % C4;
   const int mend = min(mrows, a.R - m0);
-#pragma unroll 2
-  for (int r = threadIdx.x / C4; r < mend; r += RPP) {
-    Merge4 g = out.merged(r / 32 * KW * 32 + r % 32, KW, c);
-    const long row = row0 + m0 + r;
-    if (a.slots > 0) merge_partials<D>(a, row, c, 0, 1, g);
-    g.finish(static_cast<T*>(a.O) + row * D + 4 * c, a.lse ? a.lse + row : nullptr, c == 0);
-  }
+  auto rows_of = [&](auto nr) {
+    constexpr int NR = decltype(nr)::value;
+    for (int r0 = threadIdx.x / C4; r0 < mend; r0 += NR * RPP) {
+      int v[NR];
+      long row[NR];
+      Merge4 g[NR];
+#pragma unroll
+      for (int i = 0; i < NR; ++i) {
+        const int r = min(r0 + i * RPP, mend - 1);
+        v[i] = r / 32 * KW * 32 + r % 32;
+        row[i] = row0 + m0 + r;
+      }
+      out.merged(v, KW, c, g);
+      if (a.slots > 0) merge_partials<D, NR, 16 / NR>(a, row, c, 0, 1, g);
+#pragma unroll
+      for (int i = 0; i < NR; ++i)
+        if (r0 + i * RPP < mend)
+          g[i].finish(static_cast<T*>(a.O) + row[i] * D + 4 * c, a.lse ? a.lse + row[i] : nullptr,
+                      c == 0);
+    }
+  };
+  if (mend <= RPP)
+    rows_of(std::integral_constant<int, 1>{});
+  else
+    rows_of(std::integral_constant<int, 4>{});
 }
 
 // Merges the partials of each query row.  A thread takes four channels of every
@@ -1004,8 +1061,10 @@ __global__ __launch_bounds__(kBlock) void prefix_merge_kernel(PrefixArgs a, long
   constexpr int C4 = D / 4, RPB = kBlock / (C4 * SG);
   const int c = threadIdx.x % C4, sg = threadIdx.x / C4 % SG;
   const long row = (long)blockIdx.x * RPB + threadIdx.x / (C4 * SG);
-  Merge4 g;
-  if (row < nrows) merge_partials<D>(a, row, c, sg, SG, g);
+  const long one[1] = {min(row, nrows - 1)};
+  Merge4 gs[1];
+  merge_partials<D, 1, 8>(a, one, c, sg, SG, gs);
+  Merge4& g = gs[0];
   if constexpr (SG > 1) {
     __shared__ float sh[kBlock][7];  // (odd stride: no bank met twice)
     float* mine = sh[threadIdx.x];
