@@ -267,8 +267,15 @@ def _ws(t) -> tuple[int | None, int]:
     return _ptr(t), t.numel() * t.element_size()
 
 
+# the current stream's handle without the Python object around it, where torch
+# has it (2.5 us of a call's host time)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream) -> int | None:
     if stream is None:
+        if _raw_stream is not None:
+            return _raw_stream(torch.cuda.current_device())
         return torch.cuda.current_stream().cuda_stream
     if isinstance(stream, torch.cuda.Stream):
         return stream.cuda_stream
@@ -673,38 +680,54 @@ def alloc_cache(p: WfCacheParams, device) -> tuple[torch.Tensor, ...]:
                  for s in shapes)
 
 
-def _expect_device(*tensors) -> None:
-    """Every tensor on the current device, which the kernels run on."""
-    for t in tensors:
-        if t is not None and t.device.type == "cuda" \
-                and t.device.index != torch.cuda.current_device():
-            raise ValueError(f"a tensor on {t.device}, the current device is "
-                             f"cuda:{torch.cuda.current_device()}")
+def _args(tensors) -> list[int | None]:
+    """The pointers of (name, tensor, dtype, elements, nullable) entries: each
+    checked as _expect and _ptr do, and all on the current device, which the
+    kernels run on."""
+    out = []
+    for name, t, dtype, numel, nullable in tensors:
+        if t is None and nullable:
+            out.append(None)
+            continue
+        if t.__class__ is not torch.Tensor or t.dtype is not dtype \
+                or t.numel() != numel:
+            _expect(t, name, dtype, numel)
+        out.append(t.data_ptr())
+    dev = -1
+    for name, t, _, _, _ in tensors:
+        if t is not None:
+            if not (t.is_cuda and t.is_contiguous()):
+                _ptr(t)
+            i = t.get_device()
+            if dev < 0:
+                dev = torch.cuda.current_device()
+            if i != dev:
+                raise ValueError(f"{name} is on cuda:{i}, the current device "
+                                 f"is cuda:{dev}")
+    return out
 
 
-def _expect_cache(p, K, V, row_idx, idx_rows, Kc, Kx, Vc, Vx) -> None:
-    U, d = _units(p), p.head_dim
-    for name, t in (("K", K), ("V", V)):
-        _expect(t, name, torch_dtype(p), U * p.rows * d)
-    _expect(row_idx, "row_idx", torch.int32, idx_rows * p.rows, nullable=True)
-    for name, t, n in (("Kc", Kc, _code_bytes(d, p.format)), ("Kx", Kx, d // 32),
-                       ("Vc", Vc, _code_bytes(d, p.format)), ("Vx", Vx, d // 32)):
-        _expect(t, name, torch.uint8, U * p.capacity * n)
-    _expect_device(K, V, row_idx, Kc, Kx, Vc, Vx)
+def _cache_args(p, K, V, row_idx, idx_rows, Kc, Kx, Vc, Vx) -> list:
+    d, units = p.head_dim, p.batch * p.heads
+    rows, cap = units * p.rows * d, units * p.capacity
+    dt, codes, u8 = torch_dtype(p), cap * _code_bytes(d, p.format), torch.uint8
+    return _args((("K", K, dt, rows, False), ("V", V, dt, rows, False),
+                  ("row_idx", row_idx, torch.int32, idx_rows * p.rows, True),
+                  ("Kc", Kc, u8, codes, False),
+                  ("Kx", Kx, u8, cap * (d // 32), False),
+                  ("Vc", Vc, u8, codes, False),
+                  ("Vx", Vx, u8, cap * (d // 32), False)))
 
 
 def wf_cache_store(p, K, V, row_idx, Kc, Kx, Vc, Vx, stream=None):
-    _expect_cache(p, K, V, row_idx, p.batch, Kc, Kx, Vc, Vx)
-    _check(_lib.wf_cache_store(ctypes.byref(p), _ptr(K), _ptr(V),
-                               _ptr(row_idx), _ptr(Kc), _ptr(Kx), _ptr(Vc),
-                               _ptr(Vx), _stream(stream)))
+    a = _cache_args(p, K, V, row_idx, p.batch, Kc, Kx, Vc, Vx)
+    _check(_lib.wf_cache_store(p, *a, _stream(stream)))
 
 
 def wf_cache_load(p, Kc, Kx, Vc, Vx, row_idx, K, V, stream=None):
-    _expect_cache(p, K, V, row_idx, _units(p), Kc, Kx, Vc, Vx)
-    _check(_lib.wf_cache_load(ctypes.byref(p), _ptr(Kc), _ptr(Kx), _ptr(Vc),
-                              _ptr(Vx), _ptr(row_idx), _ptr(K), _ptr(V),
-                              _stream(stream)))
+    k, v, i, kc, kx, vc, vx = _cache_args(p, K, V, row_idx, _units(p), Kc, Kx,
+                                          Vc, Vx)
+    _check(_lib.wf_cache_load(p, kc, kx, vc, vx, i, k, v, _stream(stream)))
 
 
 def cache_load(p: WfCacheParams, cache, row_idx=None, stream=None):
@@ -747,43 +770,29 @@ def alloc_prefix_workspace(p: WfPrefixParams, device) -> torch.Tensor | None:
     return torch.empty(nb, dtype=torch.uint8, device=device) if nb else None
 
 
-def _expect_prefix(p, Q, K, Kx, V, Vx, row_idx, prefix_len, Kt, Vt, tail_len,
-                   O, lse) -> None:
-    dt, d = torch_dtype(p), p.head_dim
-    seqs, units = p.prefixes * p.share, p.prefixes * p.heads
-    rows = seqs * p.heads * p.group * p.q_len
-    plain = p.format == CACHE_PLAIN
-    for name, t in (("Q", Q), ("O", O)):
-        _expect(t, name, dt, rows * d)
-    _expect(lse, "lse", torch.float32, rows, nullable=True)
-    for name, t in (("K", K), ("V", V)):
-        _expect(t, name, dt if plain else torch.uint8, units * p.prefix_cap *
-                (d if plain else _code_bytes(d, p.format)),
-                nullable=p.prefix_rows == 0)
-    for name, t in (("Kx", Kx), ("Vx", Vx)):
-        _expect(t, name, torch.uint8, 0 if plain else
-                units * p.prefix_cap * (d // 32),
-                nullable=plain or p.prefix_rows == 0)
-    _expect(row_idx, "row_idx", torch.int32, units * p.prefix_rows,
-            nullable=True)
-    _expect(prefix_len, "prefix_len", torch.int32, p.prefixes, nullable=True)
-    for name, t in (("Kt", Kt), ("Vt", Vt)):
-        _expect(t, name, dt, seqs * p.heads * p.tail_cap * d,
-                nullable=p.tail_cap == 0)
-    _expect(tail_len, "tail_len", torch.int32, seqs, nullable=True)
-    _expect_device(Q, K, Kx, V, Vx, row_idx, prefix_len, Kt, Vt, tail_len, O,
-                   lse)
-
-
 def wf_prefix_attn(p, Q, K, Kx, V, Vx, row_idx, prefix_len, Kt, Vt, tail_len,
                    O, lse, workspace, stream=None):
-    _expect_prefix(p, Q, K, Kx, V, Vx, row_idx, prefix_len, Kt, Vt, tail_len,
-                   O, lse)
+    dt, i32, d, fmt = torch_dtype(p), torch.int32, p.head_dim, p.format
+    seqs, cap = p.prefixes * p.share, p.prefixes * p.heads * p.prefix_cap
+    rows = seqs * p.heads * p.group * p.q_len
+    none, plain = p.prefix_rows == 0, fmt == CACHE_PLAIN
+    kv = dt if plain else torch.uint8
+    codes = cap * (d if plain else _code_bytes(d, fmt))
+    exps, tail = 0 if plain else cap * (d // 32), seqs * p.heads * p.tail_cap * d
+    a = _args((("Q", Q, dt, rows * d, False), ("K", K, kv, codes, none),
+               ("Kx", Kx, torch.uint8, exps, plain or none),
+               ("V", V, kv, codes, none),
+               ("Vx", Vx, torch.uint8, exps, plain or none),
+               ("row_idx", row_idx, i32,
+                p.prefixes * p.heads * p.prefix_rows, True),
+               ("prefix_len", prefix_len, i32, p.prefixes, True),
+               ("Kt", Kt, dt, tail, p.tail_cap == 0),
+               ("Vt", Vt, dt, tail, p.tail_cap == 0),
+               ("tail_len", tail_len, i32, seqs, True),
+               ("O", O, dt, rows * d, False),
+               ("lse", lse, torch.float32, rows, True)))
     ws, nb = _ws(workspace)
-    _check(_lib.wf_prefix_attn(
-        ctypes.byref(p), _ptr(Q), _ptr(K), _ptr(Kx), _ptr(V), _ptr(Vx),
-        _ptr(row_idx), _ptr(prefix_len), _ptr(Kt), _ptr(Vt), _ptr(tail_len),
-        _ptr(O), _ptr(lse), ws, nb, _stream(stream)))
+    _check(_lib.wf_prefix_attn(p, *a, ws, nb, _stream(stream)))
 
 
 def prefix_attend(p: WfPrefixParams, Q, K, V, Kx=None, Vx=None, row_idx=None,

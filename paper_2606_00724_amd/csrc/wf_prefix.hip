@@ -494,8 +494,9 @@ __device__ __forceinline__ void put4<float>(float* p, const f32x4& v) {
 }
 
 // A tile of a cache as a thread stages it: pieces of 16 codes (E4M3) or 32
-// (E2M1), 16 bytes, and their block's exponent byte.  Four threads in a row take
-// four rows, so that what eight of them write to LDS at once meets all banks.
+// (E2M1), 16 bytes, and their block's exponent byte.  Four lanes load 64 bytes in
+// a row; they write their granules in an order of their own each (by x below), so
+// that eight lanes meet all banks.
 template <typename T, int D, int FMT>
 struct QuantStage {
   using Geom = TileGeom<T, D>;
@@ -506,10 +507,16 @@ struct QuantStage {
   u32x4 w[2][N];
   uint32_t x[2][N];
 
+  // a wave's 64 pieces: 8 rows of 8 (two halves of a row's pieces after each
+  // other), 16 rows of 4 or 32 rows of 2
   __device__ __forceinline__ static int row(int i) {
-    return (i * kPrefixBlock + threadIdx.x) / (4 * PPR) * 4 + (threadIdx.x & 3);
+    const int lane = threadIdx.x & 63, w64 = i * kPrefixWaves + (threadIdx.x >> 6);
+    return PPR == 8 ? w64 * 8 + ((lane >> 2) & 7) : w64 * (64 / PPR) + lane / PPR;
   }
-  __device__ __forceinline__ static int piece() { return (threadIdx.x >> 2) % PPR; }
+  __device__ __forceinline__ static int piece() {
+    const int lane = threadIdx.x & 63;
+    return PPR == 8 ? (lane & 3) + 4 * (lane >> 5) : lane % PPR;
+  }
 
   // the tile whose first row is `first` of the range; straight: whole and of
   // consecutive rows
@@ -549,44 +556,62 @@ struct QuantStage {
         const float s = block_scale(x[m][i]);
         unsigned char* dst = tile + m * Geom::MB;
         auto at = [&](int k) { return dst + (m ? val_offset(r, k) : key_offset(r, k)); };
-        if constexpr (sizeof(T) == 2) {
-          // v_cvt_scalef32_pk_bf16: two codes times the power of two, rounded to
-          // nearest even (equal to decode8 and pack_bf16x2 for every code and
-          // exponent byte 1 .. 255; byte 0 means 0 and not 2^-127)
-          const u32x4 c = x[m][i] ? w[m][i] : u32x4{0u, 0u, 0u, 0u};
+        // v_cvt_scalef32_pk_bf16: two codes times the power of two, rounded to
+        // nearest even (equal to decode8 and pack_bf16x2 for every code and
+        // exponent byte 1 .. 255; byte 0 means 0 and not 2^-127)
+        u32x4 c = x[m][i] || sizeof(T) == 4 ? w[m][i] : u32x4{0u, 0u, 0u, 0u};
+        constexpr bool TWO = FMT == WF_CACHE_E4M3 && sizeof(T) == 2;   // two granules a piece
+        constexpr bool FOUR = !TWO && (sizeof(T) == 2 || FMT == WF_CACHE_E4M3);  // four, a word each
+        const int o = TWO ? (pc >> 1) & 1 : FOUR ? pc & 3 : 0;
+        if constexpr (TWO)
+          c = o ? u32x4{c[2], c[3], c[0], c[1]} : c;
+        if constexpr (FOUR) {
+          c = o & 1 ? u32x4{c[1], c[0], c[3], c[2]} : c;
+          c = o & 2 ? u32x4{c[2], c[3], c[0], c[1]} : c;
+        }
+        if constexpr (TWO) {
 #pragma unroll
-          for (int k = 0; k < CPP / 8; ++k) {  // eight channels, one granule each
+          for (int k = 0; k < 2; ++k) {
             u32x4 g;
-            if constexpr (FMT == WF_CACHE_E4M3) {
 #pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                g[2 * e] = __builtin_bit_cast(
-                    uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[2 * k + e], s, false));
-                g[2 * e + 1] = __builtin_bit_cast(
-                    uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[2 * k + e], s, true));
-              }
-            } else {
-              g[0] = __builtin_bit_cast(uint32_t,
-                                        __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[k], s, 0));
-              g[1] = __builtin_bit_cast(uint32_t,
-                                        __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[k], s, 1));
-              g[2] = __builtin_bit_cast(uint32_t,
-                                        __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[k], s, 2));
-              g[3] = __builtin_bit_cast(uint32_t,
-                                        __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[k], s, 3));
+            for (int e = 0; e < 2; ++e) {
+              g[2 * e] = __builtin_bit_cast(
+                  uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[2 * k + e], s, false));
+              g[2 * e + 1] = __builtin_bit_cast(
+                  uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[2 * k + e], s, true));
             }
-            *reinterpret_cast<u32x4*>(at(pc * (CPP / 8) + k)) = g;
+            *reinterpret_cast<u32x4*>(at(2 * pc + (k ^ o))) = g;
+          }
+        } else if constexpr (sizeof(T) == 2) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            u32x4 g;
+            g[0] = __builtin_bit_cast(uint32_t,
+                                      __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[k], s, 0));
+            g[1] = __builtin_bit_cast(uint32_t,
+                                      __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[k], s, 1));
+            g[2] = __builtin_bit_cast(uint32_t,
+                                      __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[k], s, 2));
+            g[3] = __builtin_bit_cast(uint32_t,
+                                      __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[k], s, 3));
+            *reinterpret_cast<u32x4*>(at(4 * pc + (k ^ o))) = g;
+          }
+        } else if constexpr (FOUR) {
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            float v[8];
+            decode8<FMT>(u32x2{c[2 * k], c[2 * k + 1]}, s, v);
+            *reinterpret_cast<f32x4*>(at(4 * pc + ((2 * k) ^ o))) = f32x4{v[0], v[1], v[2], v[3]};
+            *reinterpret_cast<f32x4*>(at(4 * pc + ((2 * k + 1) ^ o))) =
+                f32x4{v[4], v[5], v[6], v[7]};
           }
         } else {
 #pragma unroll
-          for (int k = 0; k < CPP / 8; ++k) {  // eight channels, two granules each
+          for (int k = 0; k < 4; ++k) {
             float v[8];
-            const u32x2 c = FMT == WF_CACHE_E4M3 ? u32x2{w[m][i][2 * k % 4], w[m][i][(2 * k + 1) % 4]}
-                                                 : u32x2{w[m][i][k], 0u};
-            decode8<FMT>(c, s, v);
-            const int g = 2 * (pc * (CPP / 8) + k);
-            *reinterpret_cast<f32x4*>(at(g)) = f32x4{v[0], v[1], v[2], v[3]};
-            *reinterpret_cast<f32x4*>(at(g + 1)) = f32x4{v[4], v[5], v[6], v[7]};
+            decode8<FMT>(u32x2{c[k], 0u}, s, v);
+            *reinterpret_cast<f32x4*>(at(8 * pc + 2 * k)) = f32x4{v[0], v[1], v[2], v[3]};
+            *reinterpret_cast<f32x4*>(at(8 * pc + 2 * k + 1)) = f32x4{v[4], v[5], v[6], v[7]};
           }
         }
       }
@@ -805,6 +830,13 @@ __global__ __launch_bounds__(kPrefixBlock, 1) void prefix_attn_kernel(PrefixArgs
     // registers, from where the products take them: in the other half they were
     // copied there and back in every block.
     queue(0);
+    // whole tiles in the pipelined loop (bf16)
+    const int nf = !W::BF || KW == 4 || w.neg ? 0 : nk / KT;
+    if (QUANT && nf > 0 && nt > 1) {  // (the second stage is free: us = 1)
+      stage_ids(1);
+      st[1].load(a, rows, unit, KT, straight(1));
+      queued = 2;
+    }
 #pragma unroll
     for (int b = 0; b < QW; ++b) {
       const int m = mb * mrows + (qw * QW + b) * 32 + l32;
@@ -825,18 +857,13 @@ __global__ __launch_bounds__(kPrefixBlock, 1) void prefix_attn_kernel(PrefixArgs
     const uint32_t lds0 = lds_offset(smem) + (us > 1 ? (kw >> 1) * 2 * MB : 0) +
                           (us > 1 ? kw & 1 : kw) * 2048;
     auto tile_at = [&](int t) { return lds0 + slot_of(t) * 2 * MB; };
-    // whole tiles in the pipelined loop (bf16)
-    const int nf = !W::BF || KW == 4 || w.neg ? 0 : nk / KT;
     if constexpr (W::BF) {
       if (nf > 0) {
         // Before tile t: tile t + 1 visible, t - 1 left by all; t + 2 in flight
         // and t + 3 queued over the tile's blocks.
         if constexpr (QUANT) {
           commit(0);
-          if (nt > 1) {
-            queue(1);
-            commit(1);
-          }
+          if (nt > 1) st[1].commit(smem + slot_of(1) * 2 * MB);
           if (nt > 2) queue(2);
         } else {
           if (nt > 1) queue(1);
@@ -1050,6 +1077,8 @@ __global__ __launch_bounds__(kPrefixBlock, 2) void prefix_own_kernel(PrefixArgs 
   };
   if (mend <= RPP)
     rows_of(std::integral_constant<int, 1>{});
+  else if (mend <= 2 * RPP)
+    rows_of(std::integral_constant<int, 2>{});
   else
     rows_of(std::integral_constant<int, 4>{});
 }
@@ -1097,7 +1126,7 @@ PrefixPlan plan_prefix(const wf_prefix_params& p) {
   if (p.prefix_rows > 0) {
     // 64 query rows per wave halve the LDS reads of 32; waves over query rows as
     // far as there are any, the others over the keys
-    l.qw = bf && M > 32 ? 2 : 1;
+    l.qw = bf && M > 128 ? 2 : 1;
     const long blocks = (M + 32 * l.qw - 1) / (32 * l.qw);
     int qwaves = bf ? 1 : 2;
     while (qwaves < kPrefixWaves && qwaves < blocks) qwaves *= 2;
