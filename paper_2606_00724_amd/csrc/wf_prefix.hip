@@ -557,9 +557,10 @@ struct QuantStage {
         unsigned char* dst = tile + m * Geom::MB;
         auto at = [&](int k) { return dst + (m ? val_offset(r, k) : key_offset(r, k)); };
         // v_cvt_scalef32_pk_bf16: two codes times the power of two, rounded to
-        // nearest even (equal to decode8 and pack_bf16x2 for every code and
-        // exponent byte 1 .. 255; byte 0 means 0 and not 2^-127)
-        u32x4 c = x[m][i] || sizeof(T) == 4 ? w[m][i] : u32x4{0u, 0u, 0u, 0u};
+        // nearest even: equal to decode8 and pack_bf16x2 for every code and
+        // exponent byte 1 .. 255 (byte 0 is 2^-127 here, and the store gives it to
+        // no block: it stands in cleared rows, whose codes are 0)
+        u32x4 c = w[m][i];
         constexpr bool TWO = FMT == WF_CACHE_E4M3 && sizeof(T) == 2;   // two granules a piece
         constexpr bool FOUR = !TWO && (sizeof(T) == 2 || FMT == WF_CACHE_E4M3);  // four, a word each
         const int o = TWO ? (pc >> 1) & 1 : FOUR ? pc & 3 : 0;
@@ -820,6 +821,15 @@ __global__ __launch_bounds__(kPrefixBlock, 1) void prefix_attn_kernel(PrefixArgs
       st[0].commit(smem + slot_of(t) * 2 * MB);
       if (us > 1) st[1].commit(smem + (slot_of(t) + 1) * 2 * MB);
     };
+    // (pipelined) tile t from its stage to its slot, and tile `then` on its way to
+    // the stage: two tiles are
+    auto fill = [&](int t, auto& stage, int then) __attribute__((always_inline)) {
+      stage.commit(smem + slot_of(t) * 2 * MB);
+      if (then < nt) {
+        stage_ids(then);
+        stage.load(a, rows, unit, then * KT, straight(then));
+      }
+    };
     // tile t is in its slot once every wave has passed the barrier behind this
     auto landed = [&](int t) __attribute__((always_inline)) {
       wait_vmcnt_chunks<2 * TileLoads<T, D>::N>((queued - 1 - t) * us);
@@ -835,7 +845,6 @@ __global__ __launch_bounds__(kPrefixBlock, 1) void prefix_attn_kernel(PrefixArgs
     if (QUANT && nf > 0 && nt > 1) {  // (the second stage is free: us = 1)
       stage_ids(1);
       st[1].load(a, rows, unit, KT, straight(1));
-      queued = 2;
     }
 #pragma unroll
     for (int b = 0; b < QW; ++b) {
@@ -862,9 +871,8 @@ __global__ __launch_bounds__(kPrefixBlock, 1) void prefix_attn_kernel(PrefixArgs
         // Before tile t: tile t + 1 visible, t - 1 left by all; t + 2 in flight
         // and t + 3 queued over the tile's blocks.
         if constexpr (QUANT) {
-          commit(0);
-          if (nt > 1) st[1].commit(smem + slot_of(1) * 2 * MB);
-          if (nt > 2) queue(2);
+          fill(0, st[0], 2);
+          if (nt > 1) fill(1, st[1], 3);
         } else {
           if (nt > 1) queue(1);
           if (nt > 2) queue(2);
@@ -878,14 +886,12 @@ __global__ __launch_bounds__(kPrefixBlock, 1) void prefix_attn_kernel(PrefixArgs
         w.scores(kf, s0);
         w.shift(s0, mx, c2);
         if (KW == 1) w.keys(tile_at(0) + 2048, kf);
-        auto begin = [&](int t) __attribute__((always_inline)) {
+        auto begin = [&](int t, auto& stage) __attribute__((always_inline)) {
           if (t + 1 >= nt) return;
           if constexpr (!QUANT) landed(t + 1);
           lds_barrier();
-          if constexpr (QUANT) {
-            if (t + 2 < nt) commit(t + 2);
-            if (t + 3 < nt) queue(t + 3);
-          }
+          if constexpr (QUANT)
+            if (t + 2 < nt) fill(t + 2, stage, t + 4);
         };
         // Whether the loads of tile t + 3 go between the products of tile t; else
         // they are queued at once, if there are any.
@@ -900,8 +906,8 @@ __global__ __launch_bounds__(kPrefixBlock, 1) void prefix_attn_kernel(PrefixArgs
         };
         constexpr int N = TileLoads<T, D>::N;  // tile loads of K, of V
         if (KW == 1) {
-          for (int t = 0; t < nf; ++t) {
-            begin(t);
+          auto two = [&](int t, auto& stage) __attribute__((always_inline)) {
+            begin(t, stage);
             const auto ahead = dma.at(k0 + (long)(t + 3) * KT, slot_of(t + 3), spread(t));
             const uint32_t now = tile_at(t) + MB, next = tile_at(t + 1 < nt ? t + 1 : t);
             w.template block<QUANT ? 0 : N>(now, next, kf, s0, s1, mx, c2,
@@ -912,21 +918,31 @@ __global__ __launch_bounds__(kPrefixBlock, 1) void prefix_attn_kernel(PrefixArgs
                                             [&](int i, int e) __attribute__((always_inline)) {
                                               if (ahead.go) load_some<T, D, N>(dma, i, e, ahead);
                                             });
+          };
+          if constexpr (QUANT) {
+            for (int t = 0; t < nf; t += 2) {
+              two(t, st[0]);
+              if (t + 1 < nf) two(t + 1, st[1]);
+            }
+          } else {
+            for (int t = 0; t < nf; ++t) two(t, st[0]);
           }
         } else {
-          auto one = [&](int t, f32x16(&s)[QW], f32x16(&sn)[QW]) __attribute__((always_inline)) {
-            begin(t);
-            const auto ahead = dma.at(k0 + (long)(t + 3) * KT, slot_of(t + 3), spread(t));
-            w.keys(tile_at(t + 1 < nt ? t + 1 : t), kf);
-            w.template block<QUANT ? 0 : 2 * N>(
-                tile_at(t) + MB, tile_at(t), kf, s, sn, mx, c2,
-                [&](int i, int e) __attribute__((always_inline)) {
-                  if (ahead.go) load_some<T, D, 0>(dma, i, e, ahead);
-                });
-          };
+          auto one = [&](int t, auto& stage, f32x16(&s)[QW], f32x16(&sn)[QW])
+                         __attribute__((always_inline)) {
+                           begin(t, stage);
+                           const auto ahead =
+                               dma.at(k0 + (long)(t + 3) * KT, slot_of(t + 3), spread(t));
+                           w.keys(tile_at(t + 1 < nt ? t + 1 : t), kf);
+                           w.template block<QUANT ? 0 : 2 * N>(
+                               tile_at(t) + MB, tile_at(t), kf, s, sn, mx, c2,
+                               [&](int i, int e) __attribute__((always_inline)) {
+                                 if (ahead.go) load_some<T, D, 0>(dma, i, e, ahead);
+                               });
+                         };
           for (int t = 0; t < nf; t += 2) {
-            one(t, s0, s1);
-            if (t + 1 < nf) one(t + 1, s1, s0);
+            one(t, st[0], s0, s1);
+            if (t + 1 < nf) one(t + 1, st[1], s1, s0);
           }
         }
       }
@@ -1067,7 +1083,7 @@ __global__ __launch_bounds__(kPrefixBlock, 2) void prefix_own_kernel(PrefixArgs 
         row[i] = row0 + m0 + r;
       }
       out.merged(v, KW, c, g);
-      if (a.slots > 0) merge_partials<D, NR, 16 / NR>(a, row, c, 0, 1, g);
+      if (a.slots > 0) merge_partials<D, NR, NR == 1 ? 16 : 32 / NR>(a, row, c, 0, 1, g);
 #pragma unroll
       for (int i = 0; i < NR; ++i)
         if (r0 + i * RPP < mend)
@@ -1132,22 +1148,30 @@ PrefixPlan plan_prefix(const wf_prefix_params& p) {
     while (qwaves < kPrefixWaves && qwaves < blocks) qwaves *= 2;
     l.kw = kPrefixWaves / qwaves;
     l.mblocks = (int)((blocks + qwaves - 1) / qwaves);
-    // Key ranges per unit: whole rounds of workgroups, each with a fixed part of
-    // about two tiles, against the partials that every range adds (a write and a
-    // read of D floats a row at about 5 TB/s, a tile of 64 keys in about 1.2 us).
+    // Key ranges per unit: whole rounds of workgroups, each with a fixed part (5
+    // us: its first loads, its outputs), against the partials that every range
+    // adds (a write and a read of D floats a row at about 8 TB/s, for the most part
+    // in the Infinity Cache).  A tile costs its products or its bytes, as measured
+    // in long ranges.
     const long KT = l.kw == 4 ? 2 * kTileRows : kTileRows;
     const long tiles = (p.prefix_rows + KT - 1) / KT;
     const long top = std::min(tiles, 2 * cus / (U * l.mblocks) + 1);
-    const double fixed = KT == kTileRows ? 2.5 : 1.2, partial = (double)rows * D * 8 /
-                                                              (KT == kTileRows ? 6e6 : 11e6);
+    const bool quant = p.format != WF_CACHE_PLAIN;
+    const double row_bytes = quant ? D * (p.format == WF_CACHE_E4M3 ? 1.0 : 0.5) + D / 32 : D * (bf ? 2.0 : 4.0);
+    const double products = (double)(KT / 32) / l.kw * D / 128.0 *
+                                (!bf ? 4.2 : l.qw == 2 ? 0.85 : 0.45) +
+                            (quant ? 0.4 : 0.1);
+    const double partial = (double)rows * D * 8 / 8e6;
     long best = 1;
     double best_cost = 0;
     for (long s = 1; s <= top; ++s) {
       const long per = (tiles + s - 1) / s;
       if ((tiles + per - 1) / per != s) continue;
       const long n = U * l.mblocks * s;
-      const double cost =
-          (double)((n + cus - 1) / cus) * ((double)per + fixed) + (double)s * partial;
+      const double bytes = 2 * KT * row_bytes * std::min(n, cus) / l.mblocks / 5e6;
+      const double cost = (double)((n + cus - 1) / cus) *
+                              ((double)per * std::max(products, bytes) + 5.0) +
+                          (double)s * partial;
       if (best_cost == 0 || cost < best_cost) {
         best_cost = cost;
         best = s;
