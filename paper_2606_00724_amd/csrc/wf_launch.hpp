@@ -311,9 +311,10 @@ hipError_t load_cache_kernels();
 struct PrefixArgs;
 struct PrefixPlan {
   // the prefix: workgroups, ranges per unit, keys per range, blocks of query
-  // rows per unit, waves over the keys of a tile, 32-row blocks per wave
+  // rows per unit, waves of a workgroup, those over the keys of a tile, 32-row
+  // blocks per wave
   long items;
-  int splits, rps, mblocks, kw, qw;
+  int splits, rps, mblocks, nw, kw, qw;
   size_t lds_bytes, ids_bytes;  // LDS, with a list of rows
   // the sequences' own rows: workgroups, blocks of query rows, waves over the
   // keys, waves over the query rows

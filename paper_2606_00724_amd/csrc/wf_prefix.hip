@@ -21,8 +21,14 @@
 
 namespace wf {
 
-constexpr int kPrefixBlock = 256;
-constexpr int kPrefixWaves = kPrefixBlock / kWave;
+// Waves of a workgroup.  bf16 rows that are read as codes take two per SIMD in a
+// plain loop, one beside the other's waits, decodes and softmax; the others take
+// one per SIMD, in bf16 with a loop that pipelines itself.
+template <typename T, int FMT>
+constexpr int prefix_waves() {
+  return sizeof(T) == 2 && FMT != WF_CACHE_PLAIN ? 8 : 4;
+}
+constexpr int kOwnWaves = 4;      // waves of a workgroup over a sequence's own keys
 constexpr int kPrefixIds = 4096;  // row ids in LDS at once (whole tiles)
 constexpr int kTileRows = 64;     // keys of an LDS tile
 
@@ -167,7 +173,9 @@ struct PrefixWave {
     u32x4 kf[QS];
     f32x16 s[QW];
     keys(kat, kf);
+    __builtin_amdgcn_s_setprio(1);  // products before the other wave's softmax
     scores(kf, s);
+    __builtin_amdgcn_s_setprio(0);
     if (neg) {
 #pragma unroll
       for (int b = 0; b < QW; ++b)
@@ -215,6 +223,7 @@ struct PrefixWave {
       l[b] += z;
     }
     const uint32_t vb = val_base(vat);
+    __builtin_amdgcn_s_setprio(1);
     if constexpr (BF) {
       // (each weight rounded to bf16, as the products' operands are)
 #pragma unroll
@@ -250,6 +259,7 @@ struct PrefixWave {
         }
       }
     }
+    __builtin_amdgcn_s_setprio(0);
   }
   __device__ __forceinline__ void rescale(int b, float mn, float al) {
     mref[b] = mn;
@@ -497,20 +507,20 @@ __device__ __forceinline__ void put4<float>(float* p, const f32x4& v) {
 // (E2M1), 16 bytes, and their block's exponent byte.  Four lanes load 64 bytes in
 // a row; they write their granules in an order of their own each (by x below), so
 // that eight lanes meet all banks.
-template <typename T, int D, int FMT>
+template <typename T, int D, int FMT, int NW>
 struct QuantStage {
   using Geom = TileGeom<T, D>;
   static constexpr int CPP = FMT == WF_CACHE_E2M1 ? 32 : 16;  // channels per piece
   static constexpr int PPR = D / CPP;                         // pieces per row
   static constexpr int PT = kTileRows * PPR;                  // pieces of a tile and matrix
-  static constexpr int N = (PT + kPrefixBlock - 1) / kPrefixBlock;  // per thread
+  static constexpr int N = (PT + 64 * NW - 1) / (64 * NW);  // per thread
   u32x4 w[2][N];
   uint32_t x[2][N];
 
   // a wave's 64 pieces: 8 rows of 8 (two halves of a row's pieces after each
   // other), 16 rows of 4 or 32 rows of 2
   __device__ __forceinline__ static int row(int i) {
-    const int lane = threadIdx.x & 63, w64 = i * kPrefixWaves + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, w64 = i * NW + (threadIdx.x >> 6);
     return PPR == 8 ? w64 * 8 + ((lane >> 2) & 7) : w64 * (64 / PPR) + lane / PPR;
   }
   __device__ __forceinline__ static int piece() {
@@ -524,7 +534,7 @@ struct QuantStage {
                                        int first, bool straight) {
     const uint8_t* K = static_cast<const uint8_t*>(a.K);
     const uint8_t* V = static_cast<const uint8_t*>(a.V);
-    if (PT < kPrefixBlock && (int)threadIdx.x >= PT) return;
+    if (PT < 64 * NW && (int)threadIdx.x >= PT) return;
     if (straight) {  // uniform: the lanes' offsets are constant
       const long r0 = unit * a.cap + rows.k0 + first;
 #pragma unroll
@@ -551,7 +561,7 @@ struct QuantStage {
     for (int m = 0; m < 2; ++m)
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        if (PT < kPrefixBlock && (int)threadIdx.x >= PT) break;
+        if (PT < 64 * NW && (int)threadIdx.x >= PT) break;
         const int r = row(i), pc = piece();
         const float s = block_scale(x[m][i]);
         unsigned char* dst = tile + m * Geom::MB;
@@ -622,12 +632,12 @@ struct QuantStage {
 // Rows nr .. 63 of the tile's V cleared: they repeat the range's last row or hold
 // what was there before, and 0 times an infinite value is NaN.  Ends with a
 // barrier.
-template <typename T, int D>
+template <typename T, int D, int NW>
 __device__ __forceinline__ void clear_rows(unsigned char* tile, int nr) {
   using Geom = TileGeom<T, D>;
   unsigned char* V = tile + Geom::MB;
   const int n = (kTileRows - nr) * 4;  // granules of a piece's rows
-  for (int i = threadIdx.x; i < n * Geom::NP; i += kPrefixBlock)
+  for (int i = threadIdx.x; i < n * Geom::NP; i += 64 * NW)
     *reinterpret_cast<u32x4*>(V + i / n * kPiece + nr * 64 + i % n * 16) = u32x4{0u, 0u, 0u, 0u};
   lds_barrier();
 }
@@ -657,10 +667,10 @@ struct Merge4 {
 
 // The workgroup's outputs in LDS, so that they leave it in whole rows: wave w's
 // row r at (w 32 QW + r), unnormalised, and its reference and sum behind them.
-template <int D, int QW>
+template <int D, int QW, int NW>
 struct OutRows {
   static constexpr int STRIDE = D + 4;  // floats (eight rows at one channel meet all banks)
-  static constexpr int ROWS = kPrefixWaves * 32 * QW;
+  static constexpr int ROWS = NW * 32 * QW;
   static constexpr size_t BYTES = (size_t)ROWS * (STRIDE + 2) * sizeof(float);
   float* o;
   float* st;
@@ -744,7 +754,9 @@ __device__ __forceinline__ void merge_partials(const PrefixArgs& a, const long (
 // The prefix: query rows of all sequences of a (prefix, head) over a range of its
 // keys.
 template <typename T, int D, int FMT, int QW>
-__global__ __launch_bounds__(kPrefixBlock, 1) void prefix_attn_kernel(PrefixArgs a) {
+__global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void prefix_attn_kernel(
+    PrefixArgs a) {
+  constexpr int NW = prefix_waves<T, FMT>();
   using W = PrefixWave<T, D, QW>;
   using Geom = TileGeom<T, D>;
   constexpr int MB = Geom::MB, SLOTS = Geom::SLOTS, QS = W::QS;
@@ -766,7 +778,7 @@ __global__ __launch_bounds__(kPrefixBlock, 1) void prefix_attn_kernel(PrefixArgs
   const int len = a.plen ? min(max(a.plen[group], 0), a.rows) : a.rows;
   const int k0 = sp * a.p.rps, nk = min(a.p.rps, len - k0);  // the range's keys (none: nk <= 0)
   const int kw = wave % KW, qw = wave / KW;
-  const int mrows = kPrefixWaves / KW * 32 * QW;  // query rows of the workgroup
+  const int mrows = NW / KW * 32 * QW;  // query rows of the workgroup
   // query row m of the unit -> row of Q, O (at most 2^30 in all)
   auto row_of = [&](int m) {
     const int n = a.by_R(m);
@@ -777,8 +789,9 @@ __global__ __launch_bounds__(kPrefixBlock, 1) void prefix_attn_kernel(PrefixArgs
   const float c2 = fabsf(a.scale) * kLog2e;
 
   if (nk > 0) {
-    // tiles: one 64-key tile, or two where four waves take the keys in turn
-    const int us = KW == 4 ? 2 : 1;
+    // tiles: one 64-key tile, or two where four waves take the keys in turn or
+    // eight waves pass half as many barriers
+    const int us = KW == 4 || NW == 8 ? 2 : 1;
     const int ns = SLOTS / us, KT = us * kTileRows;
     const int nt = (nk + KT - 1) / KT;
     KeyRows rows;
@@ -794,12 +807,12 @@ __global__ __launch_bounds__(kPrefixBlock, 1) void prefix_attn_kernel(PrefixArgs
       if (!rows.ids || t * KT % kPrefixIds != 0) return;  // uniform
       rows.id0 = k0 + t * KT;
       lds_barrier();
-      for (int i = threadIdx.x; i < min(kPrefixIds, nk - t * KT); i += kPrefixBlock)
+      for (int i = threadIdx.x; i < min(kPrefixIds, nk - t * KT); i += 64 * NW)
         ids[i] = a.list[(long)unit * a.rows + rows.id0 + i];
       __syncthreads();
     };
     TileLoads<T, D> dma;
-    QuantStage<T, D, QUANT ? FMT : WF_CACHE_E4M3> st[2];
+    QuantStage<T, D, QUANT ? FMT : WF_CACHE_E4M3, NW> st[2];
     if constexpr (!QUANT)
       dma.init(static_cast<const T*>(a.K) + (long)unit * a.cap * D,
                static_cast<const T*>(a.V) + (long)unit * a.cap * D, lds_offset(smem));
@@ -821,15 +834,6 @@ __global__ __launch_bounds__(kPrefixBlock, 1) void prefix_attn_kernel(PrefixArgs
       st[0].commit(smem + slot_of(t) * 2 * MB);
       if (us > 1) st[1].commit(smem + (slot_of(t) + 1) * 2 * MB);
     };
-    // (pipelined) tile t from its stage to its slot, and tile `then` on its way to
-    // the stage: two tiles are
-    auto fill = [&](int t, auto& stage, int then) __attribute__((always_inline)) {
-      stage.commit(smem + slot_of(t) * 2 * MB);
-      if (then < nt) {
-        stage_ids(then);
-        stage.load(a, rows, unit, then * KT, straight(then));
-      }
-    };
     // tile t is in its slot once every wave has passed the barrier behind this
     auto landed = [&](int t) __attribute__((always_inline)) {
       wait_vmcnt_chunks<2 * TileLoads<T, D>::N>((queued - 1 - t) * us);
@@ -840,12 +844,8 @@ __global__ __launch_bounds__(kPrefixBlock, 1) void prefix_attn_kernel(PrefixArgs
     // registers, from where the products take them: in the other half they were
     // copied there and back in every block.
     queue(0);
-    // whole tiles in the pipelined loop (bf16)
-    const int nf = !W::BF || KW == 4 || w.neg ? 0 : nk / KT;
-    if (QUANT && nf > 0 && nt > 1) {  // (the second stage is free: us = 1)
-      stage_ids(1);
-      st[1].load(a, rows, unit, KT, straight(1));
-    }
+    // whole tiles in the pipelined loop
+    const int nf = !W::BF || QUANT || KW == 4 || w.neg ? 0 : nk / KT;
 #pragma unroll
     for (int b = 0; b < QW; ++b) {
       const int m = mb * mrows + (qw * QW + b) * 32 + l32;
@@ -866,18 +866,13 @@ __global__ __launch_bounds__(kPrefixBlock, 1) void prefix_attn_kernel(PrefixArgs
     const uint32_t lds0 = lds_offset(smem) + (us > 1 ? (kw >> 1) * 2 * MB : 0) +
                           (us > 1 ? kw & 1 : kw) * 2048;
     auto tile_at = [&](int t) { return lds0 + slot_of(t) * 2 * MB; };
-    if constexpr (W::BF) {
+    if constexpr (W::BF && !QUANT) {
       if (nf > 0) {
         // Before tile t: tile t + 1 visible, t - 1 left by all; t + 2 in flight
         // and t + 3 queued over the tile's blocks.
-        if constexpr (QUANT) {
-          fill(0, st[0], 2);
-          if (nt > 1) fill(1, st[1], 3);
-        } else {
-          if (nt > 1) queue(1);
-          if (nt > 2) queue(2);
-          landed(0);
-        }
+        if (nt > 1) queue(1);
+        if (nt > 2) queue(2);
+        landed(0);
         lds_barrier();
         u32x4 kf[QS];
         f32x16 s0[QW], s1[QW];
@@ -886,17 +881,15 @@ __global__ __launch_bounds__(kPrefixBlock, 1) void prefix_attn_kernel(PrefixArgs
         w.scores(kf, s0);
         w.shift(s0, mx, c2);
         if (KW == 1) w.keys(tile_at(0) + 2048, kf);
-        auto begin = [&](int t, auto& stage) __attribute__((always_inline)) {
+        auto begin = [&](int t) __attribute__((always_inline)) {
           if (t + 1 >= nt) return;
-          if constexpr (!QUANT) landed(t + 1);
+          landed(t + 1);
           lds_barrier();
-          if constexpr (QUANT)
-            if (t + 2 < nt) fill(t + 2, stage, t + 4);
         };
         // Whether the loads of tile t + 3 go between the products of tile t; else
         // they are queued at once, if there are any.
         auto spread = [&](int t) __attribute__((always_inline)) {
-          if (QUANT || t + 3 >= nt) return false;
+          if (t + 3 >= nt) return false;
           if (!straight(t + 3)) {
             queue(t + 3);
             return false;
@@ -906,43 +899,35 @@ __global__ __launch_bounds__(kPrefixBlock, 1) void prefix_attn_kernel(PrefixArgs
         };
         constexpr int N = TileLoads<T, D>::N;  // tile loads of K, of V
         if (KW == 1) {
-          auto two = [&](int t, auto& stage) __attribute__((always_inline)) {
-            begin(t, stage);
+          for (int t = 0; t < nf; ++t) {
+            begin(t);
             const auto ahead = dma.at(k0 + (long)(t + 3) * KT, slot_of(t + 3), spread(t));
             const uint32_t now = tile_at(t) + MB, next = tile_at(t + 1 < nt ? t + 1 : t);
-            w.template block<QUANT ? 0 : N>(now, next, kf, s0, s1, mx, c2,
-                                            [&](int i, int e) __attribute__((always_inline)) {
-                                              if (ahead.go) load_some<T, D, 0>(dma, i, e, ahead);
-                                            });
-            w.template block<QUANT ? 0 : N>(now + 2048, next + 2048, kf, s1, s0, mx, c2,
-                                            [&](int i, int e) __attribute__((always_inline)) {
-                                              if (ahead.go) load_some<T, D, N>(dma, i, e, ahead);
-                                            });
-          };
-          if constexpr (QUANT) {
-            for (int t = 0; t < nf; t += 2) {
-              two(t, st[0]);
-              if (t + 1 < nf) two(t + 1, st[1]);
-            }
-          } else {
-            for (int t = 0; t < nf; ++t) two(t, st[0]);
+            w.template block<N>(now, next, kf, s0, s1, mx, c2,
+                                [&](int i, int e) __attribute__((always_inline)) {
+                                  if (ahead.go) load_some<T, D, 0>(dma, i, e, ahead);
+                                });
+            w.template block<N>(now + 2048, next + 2048, kf, s1, s0, mx, c2,
+                                [&](int i, int e) __attribute__((always_inline)) {
+                                  if (ahead.go) load_some<T, D, N>(dma, i, e, ahead);
+                                });
           }
         } else {
-          auto one = [&](int t, auto& stage, f32x16(&s)[QW], f32x16(&sn)[QW])
+          auto one = [&](int t, f32x16(&s)[QW], f32x16(&sn)[QW])
                          __attribute__((always_inline)) {
-                           begin(t, stage);
+                           begin(t);
                            const auto ahead =
                                dma.at(k0 + (long)(t + 3) * KT, slot_of(t + 3), spread(t));
                            w.keys(tile_at(t + 1 < nt ? t + 1 : t), kf);
-                           w.template block<QUANT ? 0 : 2 * N>(
+                           w.template block<2 * N>(
                                tile_at(t) + MB, tile_at(t), kf, s, sn, mx, c2,
                                [&](int i, int e) __attribute__((always_inline)) {
                                  if (ahead.go) load_some<T, D, 0>(dma, i, e, ahead);
                                });
                          };
           for (int t = 0; t < nf; t += 2) {
-            one(t, st[0], s0, s1);
-            if (t + 1 < nf) one(t + 1, st[1], s1, s0);
+            one(t, s0, s1);
+            if (t + 1 < nf) one(t + 1, s1, s0);
           }
         }
       }
@@ -966,7 +951,7 @@ __global__ __launch_bounds__(kPrefixBlock, 1) void prefix_attn_kernel(PrefixArgs
       if (nr < KT) {
         const int last = (nr - 1) / kTileRows;  // its last 64 rows
         if (nr % kTileRows)
-          clear_rows<T, D>(smem + (slot_of(t) + last) * 2 * MB, nr - last * kTileRows);
+          clear_rows<T, D, NW>(smem + (slot_of(t) + last) * 2 * MB, nr - last * kTileRows);
       }
       for (int r = 32 * kw; r < min(nr, KT); r += 32 * KW) {
         const uint32_t at = lds_offset(smem) + (slot_of(t) + r / kTileRows) * 2 * MB +
@@ -977,9 +962,9 @@ __global__ __launch_bounds__(kPrefixBlock, 1) void prefix_attn_kernel(PrefixArgs
     lds_barrier();  // the tiles are idle
   }
 
-  OutRows<D, QW> out(smem);
+  OutRows<D, QW, NW> out(smem);
   out.put(w, wave);
-  constexpr int C4 = D / 4, RPP = kPrefixBlock / C4;  // rows per round
+  constexpr int C4 = D / 4, RPP = 64 * NW / C4;  // rows per round
   const int c = threadIdx.x % C4;
   constexpr int NR = 4;
   const int mend = min(mrows, M - mb * mrows);
@@ -1014,7 +999,7 @@ __global__ __launch_bounds__(kPrefixBlock, 1) void prefix_attn_kernel(PrefixArgs
 // The keys are few (a block, a generated tail): a workgroup takes all of them,
 // and 32 rows per wave that does not share its rows' keys with others.
 template <typename T, int D>
-__global__ __launch_bounds__(kPrefixBlock, 2) void prefix_own_kernel(PrefixArgs a) {
+__global__ __launch_bounds__(64 * kOwnWaves, 2) void prefix_own_kernel(PrefixArgs a) {
   using W = PrefixWave<T, D, 1>;
   using Geom = TileGeom<T, D>;
   constexpr int MB = Geom::MB, QS = W::QS, N = TileLoads<T, D>::N;
@@ -1056,7 +1041,7 @@ __global__ __launch_bounds__(kPrefixBlock, 2) void prefix_own_kernel(PrefixArgs 
       if (t + 1 < nt) queue(t + 1);
       const int nr = n - t * kTileRows;
       unsigned char* tile = smem + (t & 1) * 2 * MB;
-      if (nr < kTileRows) clear_rows<T, D>(tile, nr);
+      if (nr < kTileRows) clear_rows<T, D, kOwnWaves>(tile, nr);
       if (qw < a.t.qw)
         for (int r = 32 * kw; r < min(nr, kTileRows); r += 32 * KW) {
           const uint32_t at = lds_offset(tile) + r * 64;
@@ -1065,9 +1050,9 @@ __global__ __launch_bounds__(kPrefixBlock, 2) void prefix_own_kernel(PrefixArgs 
     }
     lds_barrier();
   }
-  OutRows<D, 1> out(smem);
+  OutRows<D, 1, kOwnWaves> out(smem);
   out.put(w, wave);
-  constexpr int C4 = D / 4, RPP = kPrefixBlock / C4;  // rows per round
+  constexpr int C4 = D / 4, RPP = 64 * kOwnWaves / C4;  // rows per round
   const int c = threadIdx.x % C4;
   const int mend = min(mrows, a.R - m0);
   auto rows_of = [&](auto nr) {
@@ -1140,26 +1125,28 @@ PrefixPlan plan_prefix(const wf_prefix_params& p) {
   const int mb = kTileRows * D * (bf ? 2 : 4);  // bytes of a K (or V) tile
   const int slots = 8 * mb > 131072 ? 2 : 4;
   if (p.prefix_rows > 0) {
-    // 64 query rows per wave halve the LDS reads of 32; waves over query rows as
-    // far as there are any, the others over the keys
-    l.qw = bf && M > 128 ? 2 : 1;
+    // Waves over query rows as far as there are any, the others over the keys.  64
+    // rows per wave halve the LDS reads of 32, and are taken where the loop
+    // pipelines itself and there are more than the four waves have at 32.
+    const bool quant = p.format != WF_CACHE_PLAIN;
+    l.nw = bf && quant ? 8 : 4;
+    l.qw = bf && !quant && M > 128 ? 2 : 1;
     const long blocks = (M + 32 * l.qw - 1) / (32 * l.qw);
-    int qwaves = bf ? 1 : 2;
-    while (qwaves < kPrefixWaves && qwaves < blocks) qwaves *= 2;
-    l.kw = kPrefixWaves / qwaves;
+    int qwaves = l.nw == 8 || !bf ? 2 : 1;
+    while (qwaves < l.nw && qwaves < blocks) qwaves *= 2;
+    l.kw = l.nw / qwaves;
     l.mblocks = (int)((blocks + qwaves - 1) / qwaves);
     // Key ranges per unit: whole rounds of workgroups, each with a fixed part (5
     // us: its first loads, its outputs), against the partials that every range
     // adds (a write and a read of D floats a row at about 8 TB/s, for the most part
     // in the Infinity Cache).  A tile costs its products or its bytes, as measured
     // in long ranges.
-    const long KT = l.kw == 4 ? 2 * kTileRows : kTileRows;
+    const long KT = l.kw == 4 || l.nw == 8 ? 2 * kTileRows : kTileRows;
     const long tiles = (p.prefix_rows + KT - 1) / KT;
     const long top = std::min(tiles, 2 * cus / (U * l.mblocks) + 1);
-    const bool quant = p.format != WF_CACHE_PLAIN;
     const double row_bytes = quant ? D * (p.format == WF_CACHE_E4M3 ? 1.0 : 0.5) + D / 32 : D * (bf ? 2.0 : 4.0);
     const double products = (double)(KT / 32) / l.kw * D / 128.0 *
-                                (!bf ? 4.2 : l.qw == 2 ? 0.85 : 0.45) +
+                                (!bf ? 4.2 : l.qw == 2 ? 0.85 : l.nw == 8 ? 0.8 : 0.45) +
                             (quant ? 0.4 : 0.1);
     const double partial = (double)rows * D * 8 / 8e6;
     long best = 1;
@@ -1180,8 +1167,7 @@ PrefixPlan plan_prefix(const wf_prefix_params& p) {
     l.rps = (int)((tiles + best - 1) / best * KT);
     l.splits = (int)((p.prefix_rows + l.rps - 1) / l.rps);
     l.items = U * l.mblocks * l.splits;
-    const size_t out = l.qw == 2 ? (size_t)kPrefixWaves * 64 * (D + 6) * sizeof(float)
-                                 : (size_t)kPrefixWaves * 32 * (D + 6) * sizeof(float);
+    const size_t out = (size_t)l.nw * 32 * l.qw * (D + 6) * sizeof(float);
     l.lds_bytes = std::max((size_t)slots * 2 * mb, out);
     l.ids_bytes = (size_t)slots * 2 * mb + std::min(l.rps, kPrefixIds) * sizeof(int32_t);
   }
@@ -1195,7 +1181,7 @@ PrefixPlan plan_prefix(const wf_prefix_params& p) {
     l.tkw = l.tqw == 4 ? 1 : 2;
     l.tmblocks = (int)((blocks + l.tqw - 1) / l.tqw);
     l.titems = units * l.tmblocks;
-    l.tlds_bytes = std::max((size_t)4 * mb, (size_t)kPrefixWaves * 32 * (D + 6) * sizeof(float));
+    l.tlds_bytes = std::max((size_t)4 * mb, (size_t)kOwnWaves * 32 * (D + 6) * sizeof(float));
   }
   l.slots = l.splits;
   if (l.splits > 1 || (l.splits == 1 && l.titems > 0)) {
@@ -1206,14 +1192,14 @@ PrefixPlan plan_prefix(const wf_prefix_params& p) {
 }
 
 template <typename Kernel>
-static hipError_t launch_lds(Kernel kern, long grid, size_t lds, const PrefixArgs& a,
+static hipError_t launch_lds(Kernel kern, long grid, int waves, size_t lds, const PrefixArgs& a,
                              hipStream_t s) {
   if (lds > 65536) {
     hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern),
                                        hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(kPrefixBlock), lds, s, a);
+  hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(64 * waves), lds, s, a);
   return hipGetLastError();
 }
 
@@ -1257,9 +1243,9 @@ hipError_t launch_prefix(const wf_prefix_params& p, const PrefixPlan& l, PrefixA
       const size_t lds = a.list ? std::max(l.lds_bytes, l.ids_bytes) : l.lds_bytes;
       auto go = [&](auto f) {
         constexpr int F = decltype(f)::value;
-        if constexpr (sizeof(T) == 2)
-          if (l.qw == 2) return launch_lds(prefix_attn_kernel<T, D, F, 2>, grid, lds, a, s);
-        return launch_lds(prefix_attn_kernel<T, D, F, 1>, grid, lds, a, s);
+        if constexpr (sizeof(T) == 2 && F == WF_CACHE_PLAIN)
+          if (l.qw == 2) return launch_lds(prefix_attn_kernel<T, D, F, 2>, grid, l.nw, lds, a, s);
+        return launch_lds(prefix_attn_kernel<T, D, F, 1>, grid, l.nw, lds, a, s);
       };
       const hipError_t e =
           p.format == WF_CACHE_E4M3   ? go(std::integral_constant<int, WF_CACHE_E4M3>{})
@@ -1268,7 +1254,7 @@ hipError_t launch_prefix(const wf_prefix_params& p, const PrefixPlan& l, PrefixA
       if (e != hipSuccess) return e;
     }
     if (l.titems > 0)
-      return launch_lds(prefix_own_kernel<T, D>, l.titems, l.tlds_bytes, a, s);
+      return launch_lds(prefix_own_kernel<T, D>, l.titems, kOwnWaves, l.tlds_bytes, a, s);
     if (!a.whole)
       return merge_launch<T, D>(a, (long)p.prefixes * p.share * p.heads * a.R, s);
     return hipSuccess;
