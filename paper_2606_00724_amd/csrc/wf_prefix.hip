@@ -789,10 +789,9 @@ __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void prefix_attn_ker
   const float c2 = fabsf(a.scale) * kLog2e;
 
   if (nk > 0) {
-    // tiles: one 64-key tile, or two where four waves take the keys in turn or
-    // eight waves pass half as many barriers
-    const int us = KW == 4 || NW == 8 ? 2 : 1;
-    const int ns = SLOTS / us, KT = us * kTileRows;
+    // a tile: the keys of one slot, or with eight waves of two, for half the
+    // barriers
+    constexpr int US = NW == 8 ? 2 : 1, NS = SLOTS / US, KT = US * kTileRows;
     const int nt = (nk + KT - 1) / KT;
     KeyRows rows;
     rows.ids = a.list ? ids : nullptr;
@@ -800,7 +799,7 @@ __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void prefix_attn_ker
     rows.k0 = k0;
     rows.last = k0 + nk - 1;
     rows.id0 = k0;
-    auto slot_of = [&](int t) { return t % ns * us; };
+    auto slot_of = [&](int t) { return t % NS * US; };
     // the next kPrefixIds ids of a list, from tile t on, when tile t starts them
     // (no wave reads older ones: tile t - 1 has been queued by all)
     auto stage_ids = [&](int t) __attribute__((always_inline)) {
@@ -812,7 +811,7 @@ __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void prefix_attn_ker
       __syncthreads();
     };
     TileLoads<T, D> dma;
-    QuantStage<T, D, QUANT ? FMT : WF_CACHE_E4M3, NW> st[2];
+    QuantStage<T, D, QUANT ? FMT : WF_CACHE_E4M3, NW> st[US];
     if constexpr (!QUANT)
       dma.init(static_cast<const T*>(a.K) + (long)unit * a.cap * D,
                static_cast<const T*>(a.V) + (long)unit * a.cap * D, lds_offset(smem));
@@ -823,20 +822,20 @@ __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void prefix_attn_ker
       stage_ids(t);
       queued = t + 1;
       if constexpr (QUANT) {
-        st[0].load(a, rows, unit, t * KT, straight(t));
-        if (us > 1) st[1].load(a, rows, unit, t * KT + kTileRows, straight(t));
+#pragma unroll
+        for (int i = 0; i < US; ++i)
+          st[i].load(a, rows, unit, t * KT + i * kTileRows, straight(t));
       } else {
         dma.tile(rows, t * KT, straight(t), slot_of(t));
-        if (us > 1) dma.tile(rows, t * KT + kTileRows, straight(t), slot_of(t) + 1);
       }
     };
     auto commit = [&](int t) __attribute__((always_inline)) {
-      st[0].commit(smem + slot_of(t) * 2 * MB);
-      if (us > 1) st[1].commit(smem + (slot_of(t) + 1) * 2 * MB);
+#pragma unroll
+      for (int i = 0; i < US; ++i) st[i].commit(smem + (slot_of(t) + i) * 2 * MB);
     };
     // tile t is in its slot once every wave has passed the barrier behind this
     auto landed = [&](int t) __attribute__((always_inline)) {
-      wait_vmcnt_chunks<2 * TileLoads<T, D>::N>((queued - 1 - t) * us);
+      wait_vmcnt_chunks<2 * TileLoads<T, D>::N>(queued - 1 - t);
     };
     // The query operands: loaded beside the first tile, and waited for here, so
     // that the compiler's wait for them is no wait for a tile later on.  Those of
@@ -845,7 +844,7 @@ __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void prefix_attn_ker
     // copied there and back in every block.
     queue(0);
     // whole tiles in the pipelined loop
-    const int nf = !W::BF || QUANT || KW == 4 || w.neg ? 0 : nk / KT;
+    const int nf = !W::BF || QUANT || w.neg ? 0 : nk / KT;
 #pragma unroll
     for (int b = 0; b < QW; ++b) {
       const int m = mb * mrows + (qw * QW + b) * 32 + l32;
@@ -863,8 +862,7 @@ __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void prefix_attn_ker
     }
 
     // LDS offset of the wave's first block in tile t
-    const uint32_t lds0 = lds_offset(smem) + (us > 1 ? (kw >> 1) * 2 * MB : 0) +
-                          (us > 1 ? kw & 1 : kw) * 2048;
+    const uint32_t lds0 = lds_offset(smem) + kw * 2048;
     auto tile_at = [&](int t) { return lds0 + slot_of(t) * 2 * MB; };
     if constexpr (W::BF && !QUANT) {
       if (nf > 0) {
@@ -932,10 +930,10 @@ __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void prefix_attn_ker
         }
       }
     }
-    // The other tiles: tile t visible, then computed, with up to ns - 1 tiles
+    // The other tiles: tile t visible, then computed, with up to NS - 1 tiles
     // behind it on their way.
     if (nf == 0 && !QUANT)
-      for (int t = 1; t < min(nt, ns - 1); ++t) queue(t);
+      for (int t = 1; t < min(nt, NS - 1); ++t) queue(t);
     for (int t = nf; t < nt; ++t) {
       if (nf == 0) {  // (else the tile has been visible since the last whole one)
         if constexpr (QUANT) {
@@ -945,7 +943,7 @@ __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void prefix_attn_ker
           landed(t);
         }
         lds_barrier();
-        if (!QUANT && t + ns - 1 < nt) queue(t + ns - 1);
+        if (!QUANT && t + NS - 1 < nt) queue(t + NS - 1);
       }
       const int nr = nk - t * KT;  // rows of the tile that are in the range
       if (nr < KT) {
@@ -1125,23 +1123,24 @@ PrefixPlan plan_prefix(const wf_prefix_params& p) {
   const int mb = kTileRows * D * (bf ? 2 : 4);  // bytes of a K (or V) tile
   const int slots = 8 * mb > 131072 ? 2 : 4;
   if (p.prefix_rows > 0) {
-    // Waves over query rows as far as there are any, the others over the keys.  64
-    // rows per wave halve the LDS reads of 32, and are taken where the loop
-    // pipelines itself and there are more than the four waves have at 32.
+    // Waves over query rows as far as there are any, at least two (two over the
+    // keys of a tile; four of eight), the others over the keys.  64 rows per wave
+    // halve the LDS reads of 32, and are taken where the loop pipelines itself and
+    // there are more than the four waves have at 32.
     const bool quant = p.format != WF_CACHE_PLAIN;
     l.nw = bf && quant ? 8 : 4;
     l.qw = bf && !quant && M > 128 ? 2 : 1;
     const long blocks = (M + 32 * l.qw - 1) / (32 * l.qw);
-    int qwaves = l.nw == 8 || !bf ? 2 : 1;
+    int qwaves = 2;
     while (qwaves < l.nw && qwaves < blocks) qwaves *= 2;
     l.kw = l.nw / qwaves;
     l.mblocks = (int)((blocks + qwaves - 1) / qwaves);
     // Key ranges per unit: whole rounds of workgroups, each with a fixed part (5
     // us: its first loads, its outputs), against the partials that every range
     // adds (a write and a read of D floats a row at about 8 TB/s, for the most part
-    // in the Infinity Cache).  A tile costs its products or its bytes, as measured
-    // in long ranges.
-    const long KT = l.kw == 4 || l.nw == 8 ? 2 * kTileRows : kTileRows;
+    // in the Infinity Cache).  A tile costs its products or its bytes, which come
+    // at 5 TB/s to all CUs and at 32 GB/s to one; all as measured in long ranges.
+    const long KT = l.nw == 8 ? 2 * kTileRows : kTileRows;
     const long tiles = (p.prefix_rows + KT - 1) / KT;
     const long top = std::min(tiles, 2 * cus / (U * l.mblocks) + 1);
     const double row_bytes = quant ? D * (p.format == WF_CACHE_E4M3 ? 1.0 : 0.5) + D / 32 : D * (bf ? 2.0 : 4.0);
@@ -1155,7 +1154,8 @@ PrefixPlan plan_prefix(const wf_prefix_params& p) {
       const long per = (tiles + s - 1) / s;
       if ((tiles + per - 1) / per != s) continue;
       const long n = U * l.mblocks * s;
-      const double bytes = 2 * KT * row_bytes * std::min(n, cus) / l.mblocks / 5e6;
+      const double bytes =
+          2 * KT * row_bytes * std::max(std::min(n, cus) / l.mblocks / 5e6, 1 / 32e3);
       const double cost = (double)((n + cus - 1) / cus) *
                               ((double)per * std::max(products, bytes) + 5.0) +
                           (double)s * partial;
