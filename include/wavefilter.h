@@ -430,8 +430,10 @@ const char* wf_filter_attend_recursive_kernel_name(const wf_params* p,
  *                 exponent, 3 mantissa), [..][d / 2] for E2M1 (sign, 2
  *                 exponent, 1 mantissa; channel 2 i in the low half of byte i)
  *   exps  Kx, Vx  [batch][heads][capacity][d / 32] bytes
- * A value reads back as its code times the float whose bits are x << 23: 0
- * for x = 0 (rows of a cache cleared to zero bytes), NaN for x = 255.
+ * A value reads back as its code times the float whose bits are x << 23, NaN
+ * for x = 255.  x = 0 stands in rows of a cache cleared to zero bytes, which
+ * read 0; no stored block has it, and beside codes other than 0 it has no
+ * meaning.
  * --------------------------------------------------------------------- */
 enum { WF_CACHE_PLAIN = 0, /* no quantisation: rows of the call's dtype
                               (wf_prefix_attn only)                      */

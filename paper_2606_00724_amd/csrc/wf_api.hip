@@ -848,7 +848,7 @@ static wf_status check_cache(const wf_cache_params* p) {
     return fail(WF_ERR_INVALID_ARG, "unknown cache format %d", p->format);
   if ((long)p->batch * p->heads > (1L << 24))
     return fail(WF_ERR_UNSUPPORTED, "batch*heads = %ld exceeds 2^24", (long)p->batch * p->heads);
-  if (cache_groups(*p) > INT32_MAX)
+  if (cache_groups(*p) * kBlock > UINT32_MAX)  // a launch has fewer than 2^32 threads
     return fail(WF_ERR_UNSUPPORTED, "%ld rows in one call are too many",
                 (long)p->batch * p->heads * p->rows);
   return WF_OK;
@@ -907,7 +907,8 @@ static wf_status check_prefix(const wf_prefix_params* p, PrefixPlan* plan) {
       return fail(WF_ERR_UNSUPPORTED, "more than 2^30 query rows in one call");
   }
   *plan = plan_prefix(*p);
-  if (plan->items + 7 > INT32_MAX || plan->titems > INT32_MAX)
+  // a launch has fewer than 2^32 threads
+  if ((plan->items + 7) * 64 * plan->nw > UINT32_MAX || plan->titems * kBlock > UINT32_MAX)
     return fail(WF_ERR_UNSUPPORTED, "too many workgroups in one call");
   return WF_OK;
 }

@@ -142,3 +142,16 @@ def test_workspaces_over_the_range_hold_whole_partials():
         assert slots > (1 if p.tail_cap == 0 else 0) or (slots == 0 and p.tail_cap == 0)
         p.prefix_rows = 0
         assert wf.prefix_workspace_bytes(p) == 0
+
+
+def test_launches_of_two_to_the_32_threads_are_refused():
+    lib = wf.library()
+    # 2^24 units, a workgroup of 256 threads each
+    p = cache_params(batch=1 << 12, heads=1 << 12, rows=1, capacity=1)
+    assert lib.wf_cache_store(ctypes.byref(p), GOOD, GOOD, None, *[GOOD] * 4, None) == 2
+    assert lib.wf_cache_load(ctypes.byref(p), *[GOOD] * 4, None, GOOD, GOOD, None) == 2
+    for change in (dict(prefix_cap=16, tail_cap=0), dict(prefix_cap=0, tail_cap=4)):
+        q = prefix_params(prefixes=1 << 12, share=1, heads=1 << 12, q_len=1, **change)
+        args = [GOOD, GOOD, None, GOOD, None, None, None, GOOD, GOOD, None, GOOD, None, GOOD,
+                1 << 50]
+        assert lib.wf_prefix_attn(ctypes.byref(q), *args, None) == 2, change
