@@ -878,7 +878,7 @@ __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void prefix_attn_ker
         w.keys(tile_at(0), kf);
         w.scores(kf, s0);
         w.shift(s0, mx, c2);
-        if (KW == 1) w.keys(tile_at(0) + 2048, kf);
+        if (QW > 1 || KW == 1) w.keys(tile_at(0) + 2048, kf);
         auto begin = [&](int t) __attribute__((always_inline)) {
           if (t + 1 >= nt) return;
           landed(t + 1);
@@ -896,7 +896,7 @@ __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void prefix_attn_ker
           return true;
         };
         constexpr int N = TileLoads<T, D>::N;  // tile loads of K, of V
-        if (KW == 1) {
+        if (QW > 1 || KW == 1) {  // (64 rows per wave: no waves share them)
           for (int t = 0; t < nf; ++t) {
             begin(t);
             const auto ahead = dma.at(k0 + (long)(t + 3) * KT, slot_of(t + 3), spread(t));

@@ -271,3 +271,83 @@ def test_filtered_step_on_a_quantised_shared_prompt(wf):
         Q, Kr.cpu(), Vr.cpu(), prefixes=1, share=share, heads=h, group=1, scale=d ** -0.5,
         rows=k, row_idx=tok.cpu(), Kt=Kt, Vt=Vt)
     assert bool(((O.cpu().double() - ref).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("dtype,fmt,d", [("bf16", None, 128), ("bf16", None, 64),
+                                         ("bf16", "e4m3", 128), ("bf16", "e2m1", 64),
+                                         ("f32", None, 128), ("f32", "e2m1", 128)])
+@pytest.mark.parametrize("listed", [False, True], ids=["dense", "list"])
+@pytest.mark.parametrize("share,group,B", [(1, 1, 7), (2, 2, 15), (2, 2, 25), (2, 2, 75)],
+                         ids=["7", "60", "100", "300"])
+def test_long_ranges(wf, dtype, fmt, d, listed, share, group, B):
+    """Units enough that a range has many tiles, at every split of a
+    workgroup's waves over query rows and keys; one prefix ends inside a tile,
+    one inside a range."""
+    check(wf, *make(wf, dtype=dtype, fmt=fmt, d=d, prefixes=2, share=share, heads=32, group=group,
+                    B=B, P=1100, n=1090 if listed else 0, T=3, plen=[1090, 777]))
+
+
+def test_late_maxima_in_long_ranges(wf):
+    """Scores that rise along the keys, so that the reference of the softmax is
+    raised in many blocks, and a first block far below the others."""
+    for M in (60, 100, 300):
+        p, c = make(wf, prefixes=2, share=1, heads=32, B=M, d=128, P=1100, gain=0.05)
+        ramp = torch.linspace(-60, 60, 1100)
+        ramp[:32] = -300
+        c["K"][..., 0] = ramp.to(torch.bfloat16)
+        c["Q"][..., 0] = 4.0
+        check(wf, p, c)
+
+
+def test_two_calls_at_once(wf):
+    """Two streams with a workspace each."""
+    calls = []
+    for k, fmt in enumerate((None, "e4m3")):
+        p, c = make(wf, seed=k, fmt=fmt, P=5000, T=20, share=4, heads=4, group=2, B=8, d=128)
+        dev = {a: None if c[a] is None else c[a].cuda() for a in ARGS}
+        calls.append((p, dev, wf.prefix_attend(p, **dev), wf.alloc_prefix_workspace(p, "cuda"),
+                      torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    outs = [[wf.prefix_attend(p, **dev, workspace=ws, stream=s) for p, dev, _, ws, s in calls]
+            for _ in range(5)]
+    torch.cuda.synchronize()
+    for pair in outs:
+        for O, (_, _, want, _, _) in zip(pair, calls):
+            assert torch.equal(O, want)
+
+
+@pytest.mark.parametrize("fmt", [None, "e2m1"])
+def test_offsets_past_32_bits(wf, fmt):
+    """Rows behind 2^32 bytes of K and V: the last ones of a long prefix, by a
+    list and by their place, equal to the same rows in a short one."""
+    d, n, B = 128, 200, 8
+    cap = (1 << 24) + 4096 if fmt is None else (1 << 26) + 4096
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("less than 24 GB of device memory free")
+    p, c = make(wf, fmt=fmt, P=n, B=B, share=2, d=d)
+    want = call(wf, p, c)
+    dev = {k: None if c[k] is None else c[k].cuda() for k in ARGS}
+    for m in ("K", "V", "Kx", "Vx"):
+        if dev[m] is not None:
+            long = torch.zeros((1, 1, cap, dev[m].shape[-1]), dtype=dev[m].dtype, device="cuda")
+            long[:, :, -n:] = dev[m]
+            dev[m] = long
+    dev["row_idx"] = torch.arange(cap - n, cap, dtype=torch.int32, device="cuda").view(1, 1, n)
+    q = wf.make_prefix_params(share=2, heads=1, q_len=B, head_dim=d, prefix_cap=cap,
+                              prefix_rows=n, format=fmt)
+    got = wf.prefix_attend(q, **dev, want_lse=True)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    # all rows: the cleared ones have score 0 and value 0
+    dev["row_idx"] = None
+    q = wf.make_prefix_params(share=2, heads=1, q_len=B, head_dim=d, prefix_cap=cap,
+                              prefix_rows=cap, format=fmt)
+    O, lse = wf.prefix_attend(q, **dev, want_lse=True)
+    z = want[1].double().exp()
+    ref = want[0].double() * (z / (z + cap - n))[..., None]
+    # both outputs rounded to bf16 and their weights too (half a step 2^-8 each, the
+    # weights' of sum w |v| <= max |v|); fp32 sums of at most cap / 256 terms each
+    sums = cap / 256 * 2.0 ** -24
+    share_ = (z / (z + cap - n))[..., None]
+    tol = (2 * 2.0 ** -8 * 1.01 + sums) * ref.abs() + 2 * 2.0 ** -8 * float(c["Vv"].abs().max()) * share_
+    assert bool(((O.double() - ref).abs() <= tol).all())
+    assert bool(((lse.double() - (z + cap - n).log()).abs() <= 20 * 2.0 ** -20 + sums).all())
