@@ -198,6 +198,7 @@ struct PrefixPart {
   int splits;           // key ranges per unit
   int rps;              // keys per range (multiple of the tile)
   int mblocks;          // blocks of query rows per unit
+  int mrows;            // query rows per workgroup
   int M;                // query rows per unit
   int kw;               // waves that take the keys of a tile in turn
   int qw;               // 32-row blocks per wave (prefix), waves over rows (own keys)

@@ -316,10 +316,10 @@ struct PrefixPlan {
   long items;
   int splits, rps, mblocks, nw, kw, qw;
   size_t lds_bytes, ids_bytes;  // LDS, with a list of rows
-  // the sequences' own rows: workgroups, blocks of query rows, waves over the
-  // keys, waves over the query rows
+  // the sequences' own rows: workgroups, blocks of query rows, query rows per
+  // workgroup, waves over the keys, waves over the query rows
   long titems;
-  int tmblocks, tkw, tqw;
+  int tmblocks, trows, tkw, tqw;
   size_t tlds_bytes;
   int slots;                       // partials per query row
   size_t part_bytes, pstat_bytes;  // workspace (0: no partials)

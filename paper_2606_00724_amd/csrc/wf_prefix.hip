@@ -778,7 +778,7 @@ __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void prefix_attn_ker
   const int len = a.plen ? min(max(a.plen[group], 0), a.rows) : a.rows;
   const int k0 = sp * a.p.rps, nk = min(a.p.rps, len - k0);  // the range's keys (none: nk <= 0)
   const int kw = wave % KW, qw = wave / KW;
-  const int mrows = NW / KW * 32 * QW;  // query rows of the workgroup
+  const int mrows = a.p.mrows;  // NW / KW * 32 QW
   // query row m of the unit -> row of Q, O (at most 2^30 in all)
   auto row_of = [&](int m) {
     const int n = a.by_R(m);
@@ -995,7 +995,8 @@ __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void prefix_attn_ker
 
 // A sequence's rows over its own keys, merged with the partials of the prefix.
 // The keys are few (a block, a generated tail): a workgroup takes all of them,
-// and 32 rows per wave that does not share its rows' keys with others.
+// and 32 rows per wave that does not share its rows' keys with others, or fewer
+// where the partials of the rows are the work.
 template <typename T, int D>
 __global__ __launch_bounds__(64 * kOwnWaves, 2) void prefix_own_kernel(PrefixArgs a) {
   using W = PrefixWave<T, D, 1>;
@@ -1007,7 +1008,7 @@ __global__ __launch_bounds__(64 * kOwnWaves, 2) void prefix_own_kernel(PrefixArg
   const int h = lane >> 5, l32 = lane & 31;
   const int mb = blockIdx.x % a.t.mblocks, unit = blockIdx.x / a.t.mblocks;  // (sequence, head)
   const int KW = a.t.kw, kw = wave % KW, qw = wave / KW;
-  const int mrows = a.t.qw * 32;  // query rows of the workgroup
+  const int mrows = a.t.mrows;
   const int m0 = mb * mrows;
   const int n = a.tlen ? min(max(a.tlen[unit / a.heads], 0), a.T) : a.T;
   const long row0 = (long)unit * a.R;
@@ -1053,6 +1054,34 @@ __global__ __launch_bounds__(64 * kOwnWaves, 2) void prefix_own_kernel(PrefixArg
   constexpr int C4 = D / 4, RPP = 64 * kOwnWaves / C4;  // rows per round
   const int c = threadIdx.x % C4;
   const int mend = min(mrows, a.R - m0);
+  if (2 * mend <= RPP && a.slots > 16) {
+    // SG groups of threads take a row's partials in turn and meet in LDS
+    int SG = 2;
+    while (2 * SG * mend <= RPP) SG *= 2;
+    const int r = (int)threadIdx.x / C4 / SG, sg = (int)threadIdx.x / C4 % SG;
+    const int v[1] = {min(r, mend - 1)};
+    const long row[1] = {row0 + m0 + v[0]};
+    Merge4 g[1];
+    if (sg == 0) out.merged(v, KW, c, g);
+    merge_partials<D, 1, 16>(a, row, c, sg, SG, g);
+    lds_barrier();  // the outputs have been read
+    float* sh = reinterpret_cast<float*>(smem);
+    constexpr int ST = 7;  // (odd: no bank met twice)
+    float* mine = sh + threadIdx.x * ST;
+    mine[0] = g[0].M;
+    mine[1] = g[0].z;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) mine[2 + e] = g[0].o[e];
+    lds_barrier();
+    if (sg != 0 || r >= mend) return;  // no barrier follows
+    for (int k = 1; k < SG; ++k) {
+      const float* x = mine + k * C4 * ST;
+      g[0].add(x[0], x[1], f32x4{x[2], x[3], x[4], x[5]});
+    }
+    g[0].finish(static_cast<T*>(a.O) + row[0] * D + 4 * c, a.lse ? a.lse + row[0] : nullptr,
+                c == 0);
+    return;
+  }
   auto rows_of = [&](auto nr) {
     constexpr int NR = decltype(nr)::value;
     for (int r0 = threadIdx.x / C4; r0 < mend; r0 += NR * RPP) {
@@ -1123,48 +1152,54 @@ PrefixPlan plan_prefix(const wf_prefix_params& p) {
   const int mb = kTileRows * D * (bf ? 2 : 4);  // bytes of a K (or V) tile
   const int slots = 8 * mb > 131072 ? 2 : 4;
   if (p.prefix_rows > 0) {
-    // Waves over query rows as far as there are any, at least two (two over the
-    // keys of a tile; four of eight), the others over the keys.  64 rows per wave
-    // halve the LDS reads of 32, and are taken where the loop pipelines itself and
-    // there are more than the four waves have at 32.
+    // A workgroup's waves are over query rows (two at least, more as far as there
+    // are any) and over the keys of a tile.  64 rows per wave halve the LDS reads of
+    // 32, where the loop pipelines itself.  Fewer rows per workgroup give as many
+    // workgroups with fewer ranges of the keys, and so fewer partials.  The cost of
+    // a choice in us, as measured in long ranges: whole rounds of workgroups, each
+    // with a fixed part (its first loads, its outputs) and its tiles, and a write
+    // and a read of D floats a row and range at about 8 TB/s (for the most part in
+    // the Infinity Cache).  A tile costs its products or its bytes, which come at 5
+    // TB/s to all CUs and at 32 GB/s to one; its products cost `block` for each 32
+    // keys of a wave (at 128 channels) and `fixed` once.
     const bool quant = p.format != WF_CACHE_PLAIN;
     l.nw = bf && quant ? 8 : 4;
-    l.qw = bf && !quant && M > 128 ? 2 : 1;
-    const long blocks = (M + 32 * l.qw - 1) / (32 * l.qw);
-    int qwaves = 2;
-    while (qwaves < l.nw && qwaves < blocks) qwaves *= 2;
-    l.kw = l.nw / qwaves;
-    l.mblocks = (int)((blocks + qwaves - 1) / qwaves);
-    // Key ranges per unit: whole rounds of workgroups, each with a fixed part (5
-    // us: its first loads, its outputs), against the partials that every range
-    // adds (a write and a read of D floats a row at about 8 TB/s, for the most part
-    // in the Infinity Cache).  A tile costs its products or its bytes, which come
-    // at 5 TB/s to all CUs and at 32 GB/s to one; all as measured in long ranges.
     const long KT = l.nw == 8 ? 2 * kTileRows : kTileRows;
     const long tiles = (p.prefix_rows + KT - 1) / KT;
-    const long top = std::min(tiles, 2 * cus / (U * l.mblocks) + 1);
-    const double row_bytes = quant ? D * (p.format == WF_CACHE_E4M3 ? 1.0 : 0.5) + D / 32 : D * (bf ? 2.0 : 4.0);
-    const double products = (double)(KT / 32) / l.kw * D / 128.0 *
-                                (!bf ? 4.2 : l.qw == 2 ? 0.85 : l.nw == 8 ? 0.8 : 0.45) +
-                            (quant ? 0.4 : 0.1);
+    const double row_bytes = quant ? D * (p.format == WF_CACHE_E4M3 ? 1.0 : 0.5) + D / 32
+                                   : D * (bf ? 2.0 : 4.0);
     const double partial = (double)rows * D * 8 / 8e6;
-    long best = 1;
-    double best_cost = 0;
-    for (long s = 1; s <= top; ++s) {
-      const long per = (tiles + s - 1) / s;
-      if ((tiles + per - 1) / per != s) continue;
-      const long n = U * l.mblocks * s;
-      const double bytes =
-          2 * KT * row_bytes * std::max(std::min(n, cus) / l.mblocks / 5e6, 1 / 32e3);
-      const double cost = (double)((n + cus - 1) / cus) *
-                              ((double)per * std::max(products, bytes) + 5.0) +
-                          (double)s * partial;
-      if (best_cost == 0 || cost < best_cost) {
-        best_cost = cost;
-        best = s;
-      }
-    }
-    l.rps = (int)((tiles + best - 1) / best * KT);
+    double least = 0;
+    auto consider = [&](int qw, int qwaves, double block, double fixed) {
+      const long mblocks = (M + 32 * qw * qwaves - 1) / (32 * qw * qwaves);
+      const int kw = l.nw / qwaves;
+      const double products = (double)(KT / 32) / kw * D / 128.0 * block + fixed;
+      const long one = std::max(1L, cus / (U * mblocks));  // ranges that fill the chip once
+      auto ranges = [&](long n) {
+        const long per = (tiles + n - 1) / n, s = (tiles + per - 1) / per;
+        const double groups = (double)(U * mblocks * s), at_once = std::min(groups, (double)cus);
+        const double bytes = 2 * KT * row_bytes * std::max(at_once / mblocks / 5e6, 1 / 32e3);
+        const double cost = std::ceil(groups / cus) * (per * std::max(products, bytes) + 5.0) +
+                            (s > 1 || p.tail_cap > 0 ? s * partial : 0.0);
+        if (least != 0 && cost >= least) return;
+        least = cost;
+        l.qw = qw;
+        l.kw = kw;
+        l.mblocks = (int)mblocks;
+        l.rps = (int)(per * KT);
+      };
+      for (long n = 1; n < std::min(one, tiles); n += 1 + n / 16) ranges(n);
+      ranges(std::min(one, tiles));
+      ranges(std::min(2 * one, tiles));
+    };
+    for (int qwaves = 2; qwaves <= l.nw && (qwaves == 2 || 16 * qwaves < M); qwaves *= 2)
+      if (!bf)
+        consider(1, qwaves, 4.2, quant ? 0.4 : 0.1);
+      else if (quant)
+        consider(1, qwaves, 0.95, 0.3);
+      else
+        consider(1, qwaves, 0.45, 0.1);
+    if (bf && !quant && M > 128) consider(2, l.nw, 0.85, 0.1);
     l.splits = (int)((p.prefix_rows + l.rps - 1) / l.rps);
     l.items = U * l.mblocks * l.splits;
     const size_t out = (size_t)l.nw * 32 * l.qw * (D + 6) * sizeof(float);
@@ -1173,13 +1208,24 @@ PrefixPlan plan_prefix(const wf_prefix_params& p) {
   }
   if (p.tail_cap > 0) {
     // 32 rows per wave; a workgroup takes up to 128 of a sequence's rows, fewer
-    // where that leaves CUs without one
+    // where that leaves CUs without one.  Below 32 rows the workgroups of a block
+    // compute the same scores, and share the partials of its rows: worth it while
+    // those are more bytes than the own keys, down to a row for each group of
+    // threads that reads them, or where a thread has them in flight at once anyway
+    // (two heads, four sequences of 32 rows over 16K keys: 7.4 us, and 32 with 32
+    // rows each).
     const long units = U * p.share, blocks = (R + 31) / 32;
     l.tqw = (int)std::min(4L, blocks);
     if (l.tqw == 3) l.tqw = 4;
     while (l.tqw > 1 && units * ((blocks + l.tqw - 1) / l.tqw) < cus) l.tqw /= 2;
     l.tkw = l.tqw == 4 ? 1 : 2;
-    l.tmblocks = (int)((blocks + l.tqw - 1) / l.tqw);
+    l.trows = l.tqw == 1 ? (int)std::min(32L, R) : 32 * l.tqw;
+    const int groups = 4 * kOwnWaves * kWave / D;
+    while (l.tqw == 1 && l.trows > 1 && units * ((R + l.trows - 1) / l.trows) < cus &&
+           (l.trows > groups || l.splits > 16) &&
+           l.trows * l.splits * 4L > 2L * p.tail_cap * (bf ? 2 : 4))
+      l.trows = (l.trows + 1) / 2;
+    l.tmblocks = (int)((R + l.trows - 1) / l.trows);
     l.titems = units * l.tmblocks;
     l.tlds_bytes = std::max((size_t)4 * mb, (size_t)kOwnWaves * 32 * (D + 6) * sizeof(float));
   }
@@ -1233,8 +1279,10 @@ hipError_t launch_prefix(const wf_prefix_params& p, const PrefixPlan& l, PrefixA
   a.slots = l.slots;
   a.whole = l.part_bytes == 0;
   a.scale = p.scale != 0.f ? p.scale : (float)(1.0 / std::sqrt((double)p.head_dim));
-  a.p = PrefixPart{(int)l.items, l.splits, l.rps, l.mblocks, a.R * p.share, l.kw, l.qw};
-  a.t = PrefixPart{(int)l.titems, 1, p.tail_cap, l.tmblocks, a.R, l.tkw, l.tqw};
+  const int M = a.R * p.share;
+  if (l.items > 0)
+    a.p = PrefixPart{(int)l.items, l.splits, l.rps, l.mblocks, l.nw / l.kw * 32 * l.qw, M, l.kw, l.qw};
+  a.t = PrefixPart{(int)l.titems, 1, p.tail_cap, l.tmblocks, l.trows, a.R, l.tkw, l.tqw};
   auto run = [&](auto t, auto d) {
     using T = decltype(t);
     constexpr int D = decltype(d)::value;
