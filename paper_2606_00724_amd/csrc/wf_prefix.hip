@@ -84,13 +84,11 @@ struct PrefixWave {
   float mref[QW], l[QW];
   float nref[QW];   // -mref, 0 while that is -inf
   float limit[QW];  // 8; -inf while the reference is -inf
-  bool neg;  // a negative scale: the scores change sign (and c2 is positive)
   // LDS byte offsets of the lane's first operands in a 32-row block of a tile
   uint32_t ko[2], vo;
 
-  __device__ __forceinline__ void init(float scale) {
+  __device__ __forceinline__ void init() {
     const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, i16 = lane & 15;
-    neg = scale < 0.f;
     ko[0] = key_offset(l32, h);
     ko[1] = key_offset(l32, 2 + h);
     // bf16: in each 16-lane group lane i points at row t0 + i / 4, channels c0 +
@@ -176,49 +174,34 @@ struct PrefixWave {
     __builtin_amdgcn_s_setprio(1);  // products before the other wave's softmax
     scores(kf, s);
     __builtin_amdgcn_s_setprio(0);
-    if (neg) {
-#pragma unroll
-      for (int b = 0; b < QW; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[b][i] = -s[b][i];
-    }
-    if (nv < 32) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const bool off = 8 * (i >> 2) + 4 * h + (i & 3) >= nv;
-#pragma unroll
-        for (int b = 0; b < QW; ++b) s[b][i] = off ? -INFINITY : s[b][i];
-      }
-    }
-    // The reference moves only when a score passes it by 2^8: weights then stay
-    // below 2^8, their sums far from the fp32 range, and a rescale of the
-    // outputs is rare.
+    f32x16 t[QW];
     float mx[QW];
-    bool grow = false;
+    auto shifted = [&](int b) __attribute__((always_inline)) {
+      shift_one(b, s[b], t[b], c2);
+      if (nv < 32) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          t[b][i] = 8 * (i >> 2) + 4 * h + (i & 3) >= nv ? -INFINITY : t[b][i];
+      }
+    };
 #pragma unroll
     for (int b = 0; b < QW; ++b) {
-      mx[b] = fmaxf(s[b][0], s[b][1]);
-#pragma unroll
-      for (int i = 2; i < 16; i += 2) mx[b] = fmaxf(mx[b], fmaxf(s[b][i], s[b][i + 1]));
-      grow |= mx[b] * c2 > mref[b] + 8.f;
+      shifted(b);
+      mx[b] = largest(t[b]);
     }
-    if (__builtin_amdgcn_ballot_w64(grow) != 0) {
-#pragma unroll
-      for (int b = 0; b < QW; ++b) {
-        const float mn = fmaxf(mref[b], fmaxf(mx[b], partner32(mx[b])) * c2);
-        rescale(b, mn, mref[b] > -INFINITY ? __builtin_amdgcn_exp2f(mref[b] - mn) : 0.f);
-      }
-    }
-    // The weights: the unrounded product less the reference, so that scores of
-    // thousands keep their differences.  (While every score so far is -inf,
-    // their weights are 2^-inf = 0.)
+    raise(mx, [&](int b, float by) __attribute__((always_inline)) {
+      if constexpr (BF)
+        drop(t[b], by);
+      else
+        shifted(b);  // (fp32: large scores keep their differences)
+    });
 #pragma unroll
     for (int b = 0; b < QW; ++b) {
       float z = 0.f;
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], c2, nref[b]));
-        z += s[b][i];
+        t[b][i] = __builtin_amdgcn_exp2f(t[b][i]);
+        z += t[b][i];
       }
       l[b] += z;
     }
@@ -231,10 +214,10 @@ struct PrefixWave {
         u32x4 pf[QW];
 #pragma unroll
         for (int b = 0; b < QW; ++b)
-          pf[b] = u32x4{pack_bf16x2(s[b][8 * kb], s[b][8 * kb + 1]),
-                        pack_bf16x2(s[b][8 * kb + 2], s[b][8 * kb + 3]),
-                        pack_bf16x2(s[b][8 * kb + 4], s[b][8 * kb + 5]),
-                        pack_bf16x2(s[b][8 * kb + 6], s[b][8 * kb + 7])};
+          pf[b] = u32x4{pack_bf16x2(t[b][8 * kb], t[b][8 * kb + 1]),
+                        pack_bf16x2(t[b][8 * kb + 2], t[b][8 * kb + 3]),
+                        pack_bf16x2(t[b][8 * kb + 4], t[b][8 * kb + 5]),
+                        pack_bf16x2(t[b][8 * kb + 6], t[b][8 * kb + 7])};
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
           const u32x2 lo = val(vb, kb, d, 0), hi = val(vb, kb, d, 1);
@@ -255,7 +238,7 @@ struct PrefixWave {
               vb + 2 * d * kPiece + (8 * (i >> 2) + (i & 3)) * 64);
 #pragma unroll
           for (int b = 0; b < QW; ++b)
-            O[b][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, s[b][i], O[b][d], 0, 0, 0);
+            O[b][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, t[b][i], O[b][d], 0, 0, 0);
         }
       }
     }
@@ -272,20 +255,27 @@ struct PrefixWave {
       for (int i = 0; i < 16; ++i) O[b][d][i] *= al;
   }
 
-  // The pipelined loop (bf16) keeps the next block's scores in log2 units less
-  // the reference, t = s c2 - mref, and their maximum mx.  Before the block's
-  // weights are taken the reference is raised where t passes it (as in step).
-  __device__ __forceinline__ void shift(f32x16 (&t)[QW], float (&mx)[QW], float c2) const {
+  // Scores in log2 units less the reference: t = s c2 - mref, the product
+  // unrounded (while every score so far is -inf, t is -inf and the weight 0).
+  __device__ __forceinline__ void shift_one(int b, const f32x16& s, f32x16& t, float c2) const {
 #pragma unroll
-    for (int b = 0; b < QW; ++b) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) t[b][i] = fmaf(t[b][i], c2, nref[b]);
-      mx[b] = fmaxf(t[b][0], t[b][1]);
-#pragma unroll
-      for (int i = 2; i < 16; i += 2) mx[b] = fmaxf(mx[b], fmaxf(t[b][i], t[b][i + 1]));
-    }
+    for (int i = 0; i < 16; ++i) t[i] = fmaf(s[i], c2, nref[b]);
   }
-  __device__ __forceinline__ void raise_shifted(f32x16 (&t)[QW], const float (&mx)[QW]) {
+  __device__ __forceinline__ static void drop(f32x16& t, float by) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) t[i] -= by;
+  }
+  __device__ __forceinline__ static float largest(const f32x16& t) {
+    float mx = fmaxf(t[0], t[1]);
+#pragma unroll
+    for (int i = 2; i < 16; i += 2) mx = fmaxf(mx, fmaxf(t[i], t[i + 1]));
+    return mx;
+  }
+  // The reference moves only when a score passes it by 2^8: weights then stay
+  // below 2^8, their sums far from the fp32 range, and a rescale of the outputs
+  // is rare.  again(b, by): the scores less the new reference, by above the old.
+  template <typename Again>
+  __device__ __forceinline__ void raise(const float (&mx)[QW], const Again& again) {
     bool grow = false;
 #pragma unroll
     for (int b = 0; b < QW; ++b) grow |= mx[b] > limit[b];
@@ -296,14 +286,13 @@ struct PrefixWave {
         const bool first = mref[b] == -INFINITY;
         const float mn = first ? up : fmaxf(mref[b], mref[b] + up);
         const float by = mn > -INFINITY ? mn + nref[b] : 0.f;  // (nref: 0 or -mref)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) t[b][i] -= by;
         rescale(b, mn, first ? 0.f : __builtin_amdgcn_exp2f(-by));
+        again(b, by);
       }
     }
   }
 
-  // A block of that loop: weights of one block (shifted scores s) and their
+  // A block of the pipelined loop (bf16): weights of one block (shifted scores s) and their
   // product with V (at LDS offset vat) beside the scores sn of the next block
   // (its keys kf in registers; refilled with those at knext).  A wave issues in
   // order, an instruction in about five cycles, and waits for the matrix pipe at
@@ -353,7 +342,7 @@ struct PrefixWave {
       if (n < QW) {  // (the first products run beside this)
         if (n == QW - 1) {
           __builtin_amdgcn_sched_barrier(0);
-          raise_shifted(s, mx);
+          raise(mx, [&](int g, float by) __attribute__((always_inline)) { drop(s[g], by); });
 #pragma unroll
           for (int e = 0; e < QW * 8 * QW / NQ; ++e) weight(0, e);
         }
@@ -785,8 +774,8 @@ __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void prefix_attn_ker
     return ((group * a.share + n) * a.heads + head) * a.R + (m - n * a.R);
   };
   W w;
-  w.init(a.scale);
-  const float c2 = fabsf(a.scale) * kLog2e;
+  w.init();
+  const float c2 = a.scale * kLog2e;
 
   if (nk > 0) {
     // a tile: the keys of one slot, or with eight waves of two, for half the
@@ -844,7 +833,7 @@ __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void prefix_attn_ker
     // copied there and back in every block.
     queue(0);
     // whole tiles in the pipelined loop
-    const int nf = !W::BF || QUANT || w.neg ? 0 : nk / KT;
+    const int nf = W::BF && !QUANT ? nk / KT : 0;
 #pragma unroll
     for (int b = 0; b < QW; ++b) {
       const int m = mb * mrows + (qw * QW + b) * 32 + l32;
@@ -877,7 +866,11 @@ __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void prefix_attn_ker
         float mx[QW];
         w.keys(tile_at(0), kf);
         w.scores(kf, s0);
-        w.shift(s0, mx, c2);
+#pragma unroll
+        for (int b = 0; b < QW; ++b) {
+          w.shift_one(b, s0[b], s0[b], c2);
+          mx[b] = w.largest(s0[b]);
+        }
         if (QW > 1 || KW == 1) w.keys(tile_at(0) + 2048, kf);
         auto begin = [&](int t) __attribute__((always_inline)) {
           if (t + 1 >= nt) return;
@@ -998,7 +991,8 @@ __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void prefix_attn_ker
 // and 32 rows per wave that does not share its rows' keys with others, or fewer
 // where the partials of the rows are the work.
 template <typename T, int D>
-__global__ __launch_bounds__(64 * kOwnWaves, 2) void prefix_own_kernel(PrefixArgs a) {
+__global__ __launch_bounds__(64 * kOwnWaves, (TileGeom<T, D>::SLOTS / 2)) void prefix_own_kernel(
+    PrefixArgs a) {  // (workgroups per CU: as its two tiles fit)
   using W = PrefixWave<T, D, 1>;
   using Geom = TileGeom<T, D>;
   constexpr int MB = Geom::MB, QS = W::QS, N = TileLoads<T, D>::N;
@@ -1013,8 +1007,8 @@ __global__ __launch_bounds__(64 * kOwnWaves, 2) void prefix_own_kernel(PrefixArg
   const int n = a.tlen ? min(max(a.tlen[unit / a.heads], 0), a.T) : a.T;
   const long row0 = (long)unit * a.R;
   W w;
-  w.init(a.scale);
-  const float c2 = fabsf(a.scale) * kLog2e;
+  w.init();
+  const float c2 = a.scale * kLog2e;
   if (n > 0) {
     const int nt = (n + kTileRows - 1) / kTileRows;
     TileLoads<T, D> dma;
