@@ -1150,19 +1150,22 @@ PrefixPlan plan_prefix(const wf_prefix_params& p) {
     // are any) and over the keys of a tile.  64 rows per wave halve the LDS reads of
     // 32, where the loop pipelines itself.  Fewer rows per workgroup give as many
     // workgroups with fewer ranges of the keys, and so fewer partials.  The cost of
-    // a choice in us, as measured in long ranges: whole rounds of workgroups, each
+    // a choice in us, fitted to measured times: whole rounds of workgroups, each
     // with a fixed part (its first loads, its outputs) and its tiles, and a write
-    // and a read of D floats a row and range at about 8 TB/s (for the most part in
-    // the Infinity Cache).  A tile costs its products or its bytes, which come at 5
-    // TB/s to all CUs and at 32 GB/s to one; its products cost `block` for each 32
-    // keys of a wave (at 128 channels) and `fixed` once.
+    // and a read of D floats a row and range at 5 TB/s.  A tile costs its products
+    // (`block` for each 32 keys of a wave at 128 channels, `fixed` once) or its
+    // bytes, which come at 8 TB/s to all CUs (in part from the Infinity Cache) and
+    // at 32 GB/s to one.  E.g. 128 rows over 16K keys of 32 heads take 69.5 us in
+    // ranges for all CUs and 76 in fewer; 256 rows of two heads over 4K keys 17.6 in
+    // blocks of 128 rows and 24 in one of 256, of 32 heads over 16K 89 in one of 256
+    // and 98 in two.
     const bool quant = p.format != WF_CACHE_PLAIN;
     l.nw = bf && quant ? 8 : 4;
     const long KT = l.nw == 8 ? 2 * kTileRows : kTileRows;
     const long tiles = (p.prefix_rows + KT - 1) / KT;
     const double row_bytes = quant ? D * (p.format == WF_CACHE_E4M3 ? 1.0 : 0.5) + D / 32
                                    : D * (bf ? 2.0 : 4.0);
-    const double partial = (double)rows * D * 8 / 8e6;
+    const double partial = (double)rows * D * 8 / 5e6;
     double least = 0;
     auto consider = [&](int qw, int qwaves, double block, double fixed) {
       const long mblocks = (M + 32 * qw * qwaves - 1) / (32 * qw * qwaves);
@@ -1172,7 +1175,7 @@ PrefixPlan plan_prefix(const wf_prefix_params& p) {
       auto ranges = [&](long n) {
         const long per = (tiles + n - 1) / n, s = (tiles + per - 1) / per;
         const double groups = (double)(U * mblocks * s), at_once = std::min(groups, (double)cus);
-        const double bytes = 2 * KT * row_bytes * std::max(at_once / mblocks / 5e6, 1 / 32e3);
+        const double bytes = 2 * KT * row_bytes * std::max(at_once / mblocks / 8e6, 1 / 32e3);
         const double cost = std::ceil(groups / cus) * (per * std::max(products, bytes) + 5.0) +
                             (s > 1 || p.tail_cap > 0 ? s * partial : 0.0);
         if (least != 0 && cost >= least) return;
@@ -1190,10 +1193,10 @@ PrefixPlan plan_prefix(const wf_prefix_params& p) {
       if (!bf)
         consider(1, qwaves, 4.2, quant ? 0.4 : 0.1);
       else if (quant)
-        consider(1, qwaves, 0.95, 0.3);
+        consider(1, qwaves, 0.875, 0.7);
       else
         consider(1, qwaves, 0.45, 0.1);
-    if (bf && !quant && M > 128) consider(2, l.nw, 0.85, 0.1);
+    if (bf && !quant && M > 128) consider(2, l.nw, 0.82, 0.1);
     l.splits = (int)((p.prefix_rows + l.rps - 1) / l.rps);
     l.items = U * l.mblocks * l.splits;
     const size_t out = (size_t)l.nw * 32 * l.qw * (D + 6) * sizeof(float);
