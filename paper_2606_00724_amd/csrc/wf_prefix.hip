@@ -15,6 +15,12 @@
 // with the lane of the other 16, and its weights are in place as the B operand
 // of O^T = V^T P^T (the order of the keys inside that product is free, and V^T
 // is read from LDS in the order of the scores).
+//
+// Few query rows are bound by the cache's bytes, more than about 250 rows a
+// K/V head by the products.  bf16, d = 128, 8 K/V heads, on one MI355X: 2048
+// query rows a head over 32K keys take 247 us, 1.12 PFLOP/s (a product of 8192
+// x 8192 matrices reaches 1.21); 256 rows over 128K keys in 4 bits 138 us, 1.0
+// PFLOP/s; 32 rows over 32K bf16 keys 30 us, 4.5 TB/s with the merge.
 #include "wf_cache.hpp"
 #include "wf_kernels.hpp"
 #include "wf_launch.hpp"
@@ -22,8 +28,13 @@
 namespace wf {
 
 // Waves of a workgroup.  bf16 rows that are read as codes take two per SIMD in a
-// plain loop, one beside the other's waits, decodes and softmax; the others take
-// one per SIMD, in bf16 with a loop that pipelines itself.
+// plain loop, one beside the other's waits, decodes and softmax (128 query rows
+// over 32K keys in 8 bits: 40 us, and 49 with four waves that pipeline
+// themselves, whose registers the codes on their way overfill); bf16 rows take one
+// per SIMD with a loop that pipelines itself (2048 rows over 32K keys: 253 us, and
+// 293 with eight waves in the plain loop, which read every key from LDS twice as
+// often); fp32 rows one per SIMD in the plain loop,
+// whose products, at an eighth of the rate, are the bound.
 template <typename T, int FMT>
 constexpr int prefix_waves() {
   return sizeof(T) == 2 && FMT != WF_CACHE_PLAIN ? 8 : 4;
@@ -741,7 +752,12 @@ __device__ __forceinline__ void merge_partials(const PrefixArgs& a, const long (
 }
 
 // The prefix: query rows of all sequences of a (prefix, head) over a range of its
-// keys.
+// keys.  Whole tiles of bf16 rows go through the pipelined loop, three tiles
+// ahead in LDS; without its tile loads it is 14% faster, the products alone would
+// take 70% of it (2048 rows over 32K keys).  Rows kept as codes are loaded to
+// registers one tile ahead, decoded into LDS and multiplied from there: 128 keys
+// take about 4.2 us for 256 query rows, 2.5 for 128 and 1.6 for 64, half of it
+// products at 256 rows, and the decode and the LDS reads below.
 template <typename T, int D, int FMT, int QW>
 __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void prefix_attn_kernel(
     PrefixArgs a) {
@@ -1049,7 +1065,9 @@ __global__ __launch_bounds__(64 * kOwnWaves, (TileGeom<T, D>::SLOTS / 2)) void p
   const int c = threadIdx.x % C4;
   const int mend = min(mrows, a.R - m0);
   if (2 * mend <= RPP && a.slots > 16) {
-    // SG groups of threads take a row's partials in turn and meet in LDS
+    // SG groups of threads take a row's partials in turn and meet in LDS (one row
+    // a workgroup: 128 ranges 7.0 us and 18.2 without, 32 ranges 7.0 and 7.9; 16
+    // ranges, which a thread has in flight at once, 6.8 and 6.2)
     int SG = 2;
     while (2 * SG * mend <= RPP) SG *= 2;
     const int r = (int)threadIdx.x / C4 / SG, sg = (int)threadIdx.x / C4 % SG;
@@ -1105,8 +1123,11 @@ __global__ __launch_bounds__(64 * kOwnWaves, (TileGeom<T, D>::SLOTS / 2)) void p
     rows_of(std::integral_constant<int, 4>{});
 }
 
-// Merges the partials of each query row.  A thread takes four channels of every
-// SG-th partial of a row; the SG threads of a row's channels meet in LDS.
+// Merges the partials of each query row where there are no own keys.  A thread
+// takes four channels of every SG-th partial of a row; the SG threads of a row's
+// channels meet in LDS.  Bound by the latency of the loads with few rows, by the
+// partials' bytes with many (8192 rows of four ranges: 7.0 us, 2.4 TB/s with the
+// launch).
 template <typename T, int D, int SG>
 __global__ __launch_bounds__(kBlock) void prefix_merge_kernel(PrefixArgs a, long nrows) {
   constexpr int C4 = D / 4, RPB = kBlock / (C4 * SG);
@@ -1248,7 +1269,9 @@ static hipError_t launch_lds(Kernel kern, long grid, int waves, size_t lds, cons
 
 template <typename T, int D>
 static hipError_t merge_launch(const PrefixArgs& a, long rows, hipStream_t s) {
-  // threads per row and channels: enough for every partial of a row to be in flight
+  // threads per row and channels: as many as have every partial of a row in flight
+  // (32 rows, 1, 4 and 8 threads: 8 ranges 2.8, 3.6, 3.8 us; 16 ranges 3.8, 3.4, 3.8;
+  // 32 ranges 5.6, 3.6, 3.8; 128 ranges and 8 rows 17.5, 5.7, 4.7)
   auto go = [&](auto n) {
     constexpr int SG = decltype(n)::value;
     constexpr int RPB = kBlock / (D / 4 * SG);
