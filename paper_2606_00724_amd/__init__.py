@@ -792,6 +792,9 @@ def wf_prefix_attn(p, Q, K, Kx, V, Vx, row_idx, prefix_len, Kt, Vt, tail_len,
                ("O", O, dt, rows * d, False),
                ("lse", lse, torch.float32, rows, True)))
     ws, nb = _ws(workspace)
+    if workspace is not None and workspace.get_device() != Q.get_device():
+        raise ValueError(f"workspace is on cuda:{workspace.get_device()}, Q "
+                         f"on cuda:{Q.get_device()}")
     _check(_lib.wf_prefix_attn(p, *a, ws, nb, _stream(stream)))
 
 

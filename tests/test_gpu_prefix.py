@@ -351,3 +351,16 @@ def test_offsets_past_32_bits(wf, fmt):
     tol = (2 * 2.0 ** -8 * 1.01 + sums) * ref.abs() + 2 * 2.0 ** -8 * float(c["Vv"].abs().max()) * share_
     assert bool(((O.double() - ref).abs() <= tol).all())
     assert bool(((lse.double() - (z + cap - n).log()).abs() <= 20 * 2.0 ** -20 + sums).all())
+
+
+@pytest.mark.parametrize("dtype,fmt,d", [("bf16", None, 128), ("bf16", "e4m3", 64),
+                                         ("f32", None, 128), ("f32", None, 64)])
+@pytest.mark.parametrize("share,group,B,T", [(1, 1, 1, 1), (2, 1, 1, 300), (1, 5, 1, 20),
+                                             (2, 1, 33, 20), (3, 4, 10, 300), (1, 1, 200, 64)])
+def test_few_units_of_a_long_prefix(wf, dtype, fmt, d, share, group, B, T):
+    """Many ranges of the keys for few query rows, whose partials are merged by
+    several workgroups of a sequence and several threads of a row; the same
+    without own keys."""
+    check(wf, *make(wf, dtype=dtype, fmt=fmt, d=d, share=share, heads=1, group=group, B=B,
+                    P=7001, T=T, tlen=[T - i for i in range(share)]))
+    check(wf, *make(wf, dtype=dtype, fmt=fmt, d=d, share=share, heads=1, group=group, B=B, P=7001))
