@@ -1095,8 +1095,8 @@ __global__ __launch_bounds__(64 * kOwnWaves, (TileGeom<T, D>::SLOTS / 2)) void p
                 c == 0);
     return;
   }
-  auto rows_of = [&](auto nr) {
-    constexpr int NR = decltype(nr)::value;
+  auto rows_of = [&](auto nr, auto f) {
+    constexpr int NR = decltype(nr)::value, F = decltype(f)::value;
     for (int r0 = threadIdx.x / C4; r0 < mend; r0 += NR * RPP) {
       int v[NR];
       long row[NR];
@@ -1108,7 +1108,7 @@ __global__ __launch_bounds__(64 * kOwnWaves, (TileGeom<T, D>::SLOTS / 2)) void p
         row[i] = row0 + m0 + r;
       }
       out.merged(v, KW, c, g);
-      if (a.slots > 0) merge_partials<D, NR, NR == 1 ? 16 : 32 / NR>(a, row, c, 0, 1, g);
+      if (a.slots > 0) merge_partials<D, NR, F>(a, row, c, 0, 1, g);
 #pragma unroll
       for (int i = 0; i < NR; ++i)
         if (r0 + i * RPP < mend)
@@ -1116,12 +1116,29 @@ __global__ __launch_bounds__(64 * kOwnWaves, (TileGeom<T, D>::SLOTS / 2)) void p
                       c == 0);
     }
   };
+  // Partials of a row in flight: about those it has, up to 32 of a thread's rows
+  // together.  (Places past the last one are loaded too: 1024 rows of 32 heads over
+  // 1K keys, one range, 39 us, and 50 with eight places a row; 128 rows over 4K,
+  // eight ranges, 29.6, and 31.3 with 16.)
+  auto rows_by = [&](auto nr) {
+    constexpr int NR = decltype(nr)::value;
+    if (a.slots <= 1)
+      rows_of(nr, std::integral_constant<int, 1>{});
+    else if (a.slots <= 2)
+      rows_of(nr, std::integral_constant<int, 2>{});
+    else if (a.slots <= 4)
+      rows_of(nr, std::integral_constant<int, 4>{});
+    else if (NR == 4 || a.slots <= 8)
+      rows_of(nr, std::integral_constant<int, 8>{});
+    else
+      rows_of(nr, std::integral_constant<int, 16>{});
+  };
   if (mend <= RPP)
-    rows_of(std::integral_constant<int, 1>{});
+    rows_by(std::integral_constant<int, 1>{});
   else if (mend <= 2 * RPP)
-    rows_of(std::integral_constant<int, 2>{});
+    rows_by(std::integral_constant<int, 2>{});
   else
-    rows_of(std::integral_constant<int, 4>{});
+    rows_by(std::integral_constant<int, 4>{});
 }
 
 // Merges the partials of each query row where there are no own keys.  A thread
