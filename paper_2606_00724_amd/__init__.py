@@ -684,26 +684,31 @@ def _args(tensors) -> list[int | None]:
     """The pointers of (name, tensor, dtype, elements, nullable) entries: each
     checked as _expect and _ptr do, and all on the current device, which the
     kernels run on."""
+    # one pass that asks each tensor once, 3 us of a small call's 7.5; what it
+    # refuses is looked at again for the message
+    dev = torch.cuda.current_device() if torch.cuda.is_initialized() else -2
+    out = []
+    for _, t, dtype, numel, nullable in tensors:
+        if t is None:
+            if not nullable:
+                break
+            out.append(None)
+        elif (t.__class__ is torch.Tensor and t.dtype is dtype
+              and t.numel() == numel and t.get_device() == dev
+              and t.is_contiguous()):
+            out.append(t.data_ptr())
+        else:
+            break
+    else:
+        return out
     out = []
     for name, t, dtype, numel, nullable in tensors:
-        if t is None and nullable:
-            out.append(None)
-            continue
-        if t.__class__ is not torch.Tensor or t.dtype is not dtype \
-                or t.numel() != numel:
-            _expect(t, name, dtype, numel)
-        out.append(t.data_ptr())
-    dev = -1
+        _expect(t, name, dtype, numel, nullable)
     for name, t, _, _, _ in tensors:
-        if t is not None:
-            if not (t.is_cuda and t.is_contiguous()):
-                _ptr(t)
-            i = t.get_device()
-            if dev < 0:
-                dev = torch.cuda.current_device()
-            if i != dev:
-                raise ValueError(f"{name} is on cuda:{i}, the current device "
-                                 f"is cuda:{dev}")
+        out.append(_ptr(t))
+        if t is not None and t.get_device() != torch.cuda.current_device():
+            raise ValueError(f"{name} is on cuda:{t.get_device()}, the current "
+                             f"device is cuda:{torch.cuda.current_device()}")
     return out
 
 
