@@ -509,8 +509,14 @@ typedef struct wf_prefix_params {
     float scale;         /* softmax scale; 0 selects 1/sqrt(d)              */
 } wf_prefix_params;
 
-/* Workspace bytes wf_prefix_attn needs (0 if it needs none or the parameters
- * are invalid). */
+/* Workspace bytes of the split of the prefix into key ranges that
+ * wf_prefix_attn takes when it can (0 if that needs none or the parameters are
+ * invalid).  Each range has (d + 2) floats for each query row.  With fewer bytes
+ * the call takes fewer ranges, one at least: (d + 2) floats for each query row
+ * where it has prefix rows and own rows, nothing otherwise.  A workspace of this
+ * size is thus enough for every call with a shorter prefix or fewer query rows
+ * too, whose own preferred size may be larger.  Outputs of different splits
+ * differ by rounding; equal parameters and bytes give equal bits. */
 size_t wf_prefix_workspace_bytes(const wf_prefix_params* p);
 
 /*
@@ -531,7 +537,8 @@ size_t wf_prefix_workspace_bytes(const wf_prefix_params* p);
  *               past a length may hold anything)
  *   O           [prefixes share][heads group][B][d]        dtype out
  *   lse         nullable [prefixes share][heads group][B]  fp32 out
- *   workspace   >= wf_prefix_workspace_bytes(p), 256-byte aligned
+ *   workspace   wf_prefix_workspace_bytes(p) bytes (fewer: see there), 256-byte
+ *               aligned
  * K, V (and Kx, Vx) may be NULL where prefix_rows == 0; at least one of
  * prefix_rows and tail_cap is above 0.
  */

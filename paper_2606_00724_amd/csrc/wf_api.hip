@@ -877,7 +877,7 @@ static wf_status cache_impl(const wf_cache_params* p, bool store, const void* K,
 
 // ------------------------------------------------------------ shared prefix
 
-static wf_status check_prefix(const wf_prefix_params* p, PrefixPlan* plan) {
+static wf_status check_prefix(const wf_prefix_params* p, size_t have, PrefixPlan* plan) {
   if (!p) return fail(WF_ERR_INVALID_ARG, "params is NULL");
   if (p->prefixes < 1 || p->share < 1 || p->heads < 1 || p->group < 1 || p->q_len < 1)
     return fail(WF_ERR_INVALID_ARG,
@@ -906,7 +906,7 @@ static wf_status check_prefix(const wf_prefix_params* p, PrefixPlan* plan) {
     if (rows > (1L << 30))
       return fail(WF_ERR_UNSUPPORTED, "more than 2^30 query rows in one call");
   }
-  *plan = plan_prefix(*p);
+  *plan = plan_prefix(*p, have);
   // a launch has fewer than 2^32 threads
   if ((plan->items + 7) * 64 * plan->nw > UINT32_MAX || plan->titems * kBlock > UINT32_MAX)
     return fail(WF_ERR_UNSUPPORTED, "too many workgroups in one call");
@@ -919,7 +919,7 @@ static wf_status prefix_impl(const wf_prefix_params* p, const void* Q, const voi
                              const void* Vt, const int32_t* tail_len, void* O, float* lse,
                              void* ws, size_t ws_bytes, void* stream) {
   PrefixPlan plan;
-  WF_TRY(check_prefix(p, &plan));
+  WF_TRY(check_prefix(p, ws ? ws_bytes : 0, &plan));
   WF_TRY(check_ptr(Q, "Q", false));
   WF_TRY(check_ptr(O, "O", false));
   WF_TRY(check_ptr(lse, "lse", true));
@@ -1250,7 +1250,7 @@ wf_status wf_cache_load(const wf_cache_params* p, const void* Kc, const void* Kx
 
 size_t wf_prefix_workspace_bytes(const wf_prefix_params* p) {
   PrefixPlan plan;
-  if (check_prefix(p, &plan) != WF_OK) return 0;
+  if (check_prefix(p, SIZE_MAX, &plan) != WF_OK) return 0;
   return plan.part_bytes + plan.pstat_bytes;
 }
 

@@ -324,7 +324,7 @@ struct PrefixPlan {
   int slots;                       // partials per query row
   size_t part_bytes, pstat_bytes;  // workspace (0: no partials)
 };
-PrefixPlan plan_prefix(const wf_prefix_params& p);
+PrefixPlan plan_prefix(const wf_prefix_params& p, size_t have);  // have: workspace bytes
 hipError_t launch_prefix(const wf_prefix_params& p, const PrefixPlan& plan, PrefixArgs& a,
                          hipStream_t s);
 hipError_t load_prefix_kernels();

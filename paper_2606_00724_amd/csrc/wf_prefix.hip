@@ -1178,7 +1178,7 @@ __global__ __launch_bounds__(kBlock) void prefix_merge_kernel(PrefixArgs a, long
 
 // ------------------------------------------------------------ host side
 
-PrefixPlan plan_prefix(const wf_prefix_params& p) {
+PrefixPlan plan_prefix(const wf_prefix_params& p, size_t have) {
   PrefixPlan l{};
   const bool bf = p.dtype == WF_BF16;
   const int D = p.head_dim;
@@ -1207,6 +1207,10 @@ PrefixPlan plan_prefix(const wf_prefix_params& p) {
     const double row_bytes = quant ? D * (p.format == WF_CACHE_E4M3 ? 1.0 : 0.5) + D / 32
                                    : D * (bf ? 2.0 : 4.0);
     const double partial = (double)rows * D * 8 / 5e6;
+    // Ranges are as many as the workspace holds partials for, and one at least:
+    // they need not grow with the rows (2304 rows of the prefix may take fewer than
+    // 2048), and a caller keeps one workspace while its prompts and batches change.
+    const long most = (long)std::min<size_t>(have / (rows * (D + 2) * sizeof(float)), 1L << 30);
     double least = 0;
     auto consider = [&](int qw, int qwaves, double block, double fixed) {
       const long mblocks = (M + 32 * qw * qwaves - 1) / (32 * qw * qwaves);
@@ -1215,6 +1219,7 @@ PrefixPlan plan_prefix(const wf_prefix_params& p) {
       const long one = std::max(1L, cus / (U * mblocks));  // ranges that fill the chip once
       auto ranges = [&](long n) {
         const long per = (tiles + n - 1) / n, s = (tiles + per - 1) / per;
+        if (s > 1 && s > most) return;
         const double groups = (double)(U * mblocks * s), at_once = std::min(groups, (double)cus);
         const double bytes = 2 * KT * row_bytes * std::max(at_once / mblocks / 8e6, 1 / 32e3);
         const double cost = std::ceil(groups / cus) * (per * std::max(products, bytes) + 5.0) +
