@@ -506,7 +506,8 @@ typedef struct wf_prefix_params {
     int32_t dtype;       /* WF_BF16 or WF_F32: Q, Kt, Vt, O                 */
     int32_t format;      /* K, V: WF_CACHE_PLAIN (dtype) or as stored by
                             wf_cache_store with batch = prefixes            */
-    float scale;         /* softmax scale; 0 selects 1/sqrt(d)              */
+    float scale;         /* softmax scale, of either sign, times log2(e)
+                            finite; 0 selects 1/sqrt(d)                     */
 } wf_prefix_params;
 
 /* Workspace bytes of the split of the prefix into key ranges that

@@ -898,7 +898,9 @@ static wf_status check_prefix(const wf_prefix_params* p, size_t have, PrefixPlan
     return fail(WF_ERR_INVALID_ARG, "unknown dtype %d", p->dtype);
   if (p->format != WF_CACHE_PLAIN && p->format != WF_CACHE_E4M3 && p->format != WF_CACHE_E2M1)
     return fail(WF_ERR_INVALID_ARG, "unknown cache format %d", p->format);
-  if (!std::isfinite(p->scale)) return fail(WF_ERR_INVALID_ARG, "scale is not finite");
+  // the kernels scale scores in log2 units: an infinite factor would make a score of 0 NaN
+  if (!std::isfinite(p->scale * 1.44269504f))
+    return fail(WF_ERR_INVALID_ARG, "scale times log2(e) is not finite in fp32");
   // every product below stays in 64 bits: each factor is held to 2^31 in turn
   long rows = 1;
   for (long f : {(long)p->prefixes, (long)p->share, (long)p->heads, (long)p->group, (long)p->q_len}) {
