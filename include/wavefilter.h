@@ -520,6 +520,18 @@ typedef struct wf_prefix_params {
  * differ by rounding; equal parameters and bytes give equal bits. */
 size_t wf_prefix_workspace_bytes(const wf_prefix_params* p);
 
+/* How wf_prefix_attn works on the prefix with a workspace of that many bytes
+ * (for tests and measurements; the choice may change between builds). */
+typedef struct wf_prefix_split {
+    int32_t ranges;     /* key ranges; 0 where prefix_rows == 0              */
+    int32_t range_rows; /* keys of a range (the last one may have fewer)     */
+    int32_t group_rows; /* query rows of a workgroup                         */
+    int32_t wave_rows;  /* query rows of a wave: 32 or 64                    */
+    int32_t key_waves;  /* waves of a workgroup that take keys in turn       */
+} wf_prefix_split;
+wf_status wf_prefix_plan(const wf_prefix_params* p, size_t workspace_bytes,
+                         wf_prefix_split* split);
+
 /*
  *   Q           [prefixes share][heads group][B][d]       dtype
  *   K, V        [prefixes][heads][prefix_cap][d]           dtype, or codes

@@ -44,7 +44,7 @@ EXPORTED = ("wf_workspace_bytes", "wf_effective_budget", "wf_dwt_keys",
             "wf_filter_attend_recursive_kernels",
             "wf_filter_attend_recursive_kernel_name",
             "wf_cache_store", "wf_cache_load", "wf_prefix_workspace_bytes",
-            "wf_prefix_attn", "wf_init", "wf_status_str", "wf_last_error")
+            "wf_prefix_plan", "wf_prefix_attn", "wf_init", "wf_status_str", "wf_last_error")
 
 
 class WfParams(ctypes.Structure):
@@ -68,6 +68,11 @@ class WfPrefixParams(ctypes.Structure):
         "prefixes", "share", "heads", "group", "q_len", "head_dim",
         "prefix_cap", "prefix_rows", "tail_cap", "dtype", "format")] + [
         ("scale", ctypes.c_float)]
+
+
+class WfPrefixSplit(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "ranges", "range_rows", "group_rows", "wave_rows", "key_waves")]
 
 
 class WfError(RuntimeError):
@@ -136,6 +141,7 @@ def _load() -> ctypes.CDLL:
         "wf_cache_store": (ctypes.c_int, [CP, vp, vp, vp, vp, vp, vp, vp, vp]),
         "wf_cache_load": (ctypes.c_int, [CP, vp, vp, vp, vp, vp, vp, vp, vp]),
         "wf_prefix_workspace_bytes": (sz, [PP]),
+        "wf_prefix_plan": (ctypes.c_int, [PP, sz, ctypes.POINTER(WfPrefixSplit)]),
         "wf_prefix_attn": (ctypes.c_int,
                            [PP, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp,
                             vp, sz, vp]),
@@ -768,6 +774,16 @@ def make_prefix_params(*, prefixes: int = 1, share: int, heads: int,
 
 def prefix_workspace_bytes(p: WfPrefixParams) -> int:
     return int(_lib.wf_prefix_workspace_bytes(ctypes.byref(p)))
+
+
+def prefix_plan(p: WfPrefixParams, nbytes: int | None = None) -> WfPrefixSplit:
+    """How wf_prefix_attn splits the prefix with a workspace of nbytes (None:
+    of prefix_workspace_bytes)."""
+    s = WfPrefixSplit()
+    _check(_lib.wf_prefix_plan(
+        ctypes.byref(p), prefix_workspace_bytes(p) if nbytes is None else nbytes,
+        ctypes.byref(s)))
+    return s
 
 
 def alloc_prefix_workspace(p: WfPrefixParams, device) -> torch.Tensor | None:

@@ -1256,6 +1256,18 @@ size_t wf_prefix_workspace_bytes(const wf_prefix_params* p) {
   return plan.part_bytes + plan.pstat_bytes;
 }
 
+wf_status wf_prefix_plan(const wf_prefix_params* p, size_t workspace_bytes,
+                         wf_prefix_split* split) {
+  PrefixPlan plan;
+  WF_TRY(check_prefix(p, workspace_bytes, &plan));
+  if (!split) return fail(WF_ERR_INVALID_ARG, "split is NULL");
+  *split = wf_prefix_split{};
+  if (p->prefix_rows > 0)
+    *split = wf_prefix_split{plan.splits, plan.rps, plan.nw / plan.kw * 32 * plan.qw,
+                             32 * plan.qw, plan.kw};
+  return ok();
+}
+
 wf_status wf_prefix_attn(const wf_prefix_params* p, const void* Q, const void* K, const void* Kx,
                          const void* V, const void* Vx, const int32_t* row_idx,
                          const int32_t* prefix_len, const void* Kt, const void* Vt,
