@@ -474,7 +474,8 @@ wf_status wf_cache_store(const wf_cache_params* p, const void* K, const void* V,
  *            as wanted (wf_scan_select's tok_idx, the tokens of regions);
  *            an index outside [0, capacity) gives a row of zeros
  *   K, V     [batch][heads][rows][d]   dtype out (rounded to nearest even;
- *            exact where the value is no subnormal of bf16)
+ *            exact where the value is no subnormal of bf16; a magnitude stored
+ *            within half a code's step of 2^128 reads infinite)
  * rows = 0 queues nothing.
  */
 wf_status wf_cache_load(const wf_cache_params* p, const void* Kc, const void* Kx,

@@ -95,10 +95,14 @@ struct PrefixWave {
   float mref[QW], l[QW];
   float nref[QW];   // -mref, 0 while that is -inf
   float limit[QW];  // 8; -inf while the reference is -inf
+  float f[QW];      // what scores are multiplied by: c2, or with a far reference c2p
+  float c2, c2p;    // scale log2(e); its power of two
   // LDS byte offsets of the lane's first operands in a 32-row block of a tile
   uint32_t ko[2], vo;
 
-  __device__ __forceinline__ void init() {
+  __device__ __forceinline__ void init(float scale) {
+    c2 = scale * kLog2e;
+    c2p = __uint_as_float(__float_as_uint(c2) & 0xff800000u);
     const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, i16 = lane & 15;
     ko[0] = key_offset(l32, h);
     ko[1] = key_offset(l32, 2 + h);
@@ -111,6 +115,7 @@ struct PrefixWave {
     for (int b = 0; b < QW; ++b) {
       mref[b] = limit[b] = -INFINITY;
       nref[b] = l[b] = 0.f;
+      f[b] = c2;
 #pragma unroll
       for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -177,7 +182,7 @@ struct PrefixWave {
   }
 
   // 32 keys at LDS offsets kat, vat, the first nv of which are valid
-  __device__ __forceinline__ void step(uint32_t kat, uint32_t vat, int nv, float c2) {
+  __device__ __forceinline__ void step(uint32_t kat, uint32_t vat, int nv) {
     const int h = (threadIdx.x & 63) >> 5;
     u32x4 kf[QS];
     f32x16 s[QW];
@@ -190,7 +195,7 @@ struct PrefixWave {
     f32x16 t[QW];
     float mx[QW];
     auto shifted = [&](int b) __attribute__((always_inline)) {
-      shift_one(b, s[b], t[b], c2);
+      shift_one(b, s[b], t[b]);
       if (nv < 32) {
 #pragma unroll
         for (int i = 0; i < 16; ++i)
@@ -202,12 +207,27 @@ struct PrefixWave {
       shifted(b);
       mx[b] = largest(t[b]);
     }
-    raise(mx, [&](int b, float by) __attribute__((always_inline)) {
-      if constexpr (BF)
-        drop(t[b], by);
-      else
-        shifted(b);  // (fp32: large scores keep their differences)
-    });
+    raise(
+        mx,
+        [&](int b, float by) __attribute__((always_inline)) {
+          if constexpr (BF)
+            drop(t[b], by);
+          else
+            shifted(b);  // (fp32: large scores keep their differences)
+        },
+        [&](int b, float& mn, float& al) __attribute__((always_inline)) {
+          // (a count of its own: the comparisons are not kept for this)
+          int n = nv;
+          asm volatile("" : "+s"(n));
+          if constexpr (BF)
+            score_one(b, key_base(kat), t[b]);  // (s is not kept for this)
+          else
+            t[b] = s[b];
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            t[b][i] = 8 * (i >> 2) + 4 * h + (i & 3) >= n ? -c2 * INFINITY : t[b][i];
+          anew(b, t[b], mn, al);
+        });
 #pragma unroll
     for (int b = 0; b < QW; ++b) {
       float z = 0.f;
@@ -268,11 +288,11 @@ struct PrefixWave {
       for (int i = 0; i < 16; ++i) O[b][d][i] *= al;
   }
 
-  // Scores in log2 units less the reference: t = s c2 - mref, the product
+  // Scores in log2 units less the reference: t = s f - mref, the product
   // unrounded (while every score so far is -inf, t is -inf and the weight 0).
-  __device__ __forceinline__ void shift_one(int b, const f32x16& s, f32x16& t, float c2) const {
+  __device__ __forceinline__ void shift_one(int b, const f32x16& s, f32x16& t) const {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) t[i] = fmaf(s[i], c2, nref[b]);
+    for (int i = 0; i < 16; ++i) t[i] = fmaf(s[i], f[b], nref[b]);
   }
   __device__ __forceinline__ static void drop(f32x16& t, float by) {
 #pragma unroll
@@ -284,24 +304,87 @@ struct PrefixWave {
     for (int i = 2; i < 16; i += 2) mx = fmaxf(mx, fmaxf(t[i], t[i + 1]));
     return mx;
   }
+  __device__ __forceinline__ float ratio() const {  // c2 / c2p
+    return __uint_as_float((__float_as_uint(c2) & 0x7fffffu) | 0x3f800000u);
+  }
+  // The reference in log2 units.
+  __device__ __forceinline__ float reference(int b) const {
+    return f[b] == c2 ? mref[b] : mref[b] * ratio();
+  }
   // The reference moves only when a score passes it by 2^8: weights then stay
   // below 2^8, their sums far from the fp32 range, and a rescale of the outputs
   // is rare.  again(b, by): the scores less the new reference, by above the old.
-  template <typename Again>
-  __device__ __forceinline__ void raise(const float (&mx)[QW], const Again& again) {
+  // Scores less a reference that is far below them have lost their differences:
+  // where a reference moves far, or to a far place, afresh(b, its place, the factor
+  // of the sums) makes them anew.  (The factor in a register of its own and the code
+  // that is not reached cost 1%: 2048 rows over 32K keys 240.5 -> 242.8 us.)
+  template <typename Again, typename Afresh>
+  __device__ __forceinline__ void raise(const float (&mx)[QW], const Again& again,
+                                        const Afresh& afresh) {
     bool grow = false;
 #pragma unroll
     for (int b = 0; b < QW; ++b) grow |= mx[b] > limit[b];
     if (__builtin_amdgcn_ballot_w64(grow) != 0) {
+      float mn[QW], by[QW], al[QW];
+      bool far = false;
 #pragma unroll
       for (int b = 0; b < QW; ++b) {
         const float up = fmaxf(mx[b], partner32(mx[b]));
         const bool first = mref[b] == -INFINITY;
-        const float mn = first ? up : fmaxf(mref[b], mref[b] + up);
-        const float by = mn > -INFINITY ? mn + nref[b] : 0.f;  // (nref: 0 or -mref)
-        rescale(b, mn, first ? 0.f : __builtin_amdgcn_exp2f(-by));
-        again(b, by);
+        mn[b] = first ? up : fmaxf(mref[b], mref[b] + up);
+        by[b] = mn[b] > -INFINITY ? mn[b] + nref[b] : 0.f;  // (nref: 0 or -mref)
+        al[b] = first ? 0.f : __builtin_amdgcn_exp2f(-by[b]);
+        far |= fabsf(by[b]) > 1024.f || (mn[b] > -INFINITY && fabsf(mn[b]) >= kFar);
       }
+      if (__builtin_amdgcn_ballot_w64(far) != 0) {
+#pragma unroll
+        for (int b = 0; b < QW; ++b) {
+          afresh(b, mn[b], al[b]);
+          by[b] = 0.f;
+        }
+      }
+#pragma unroll
+      for (int b = 0; b < QW; ++b) {
+        rescale(b, mn[b], al[b]);
+        again(b, by[b]);
+      }
+    }
+  }
+  // A block's scores t made scores less the reference mn, which moves to their
+  // maximum where that is above the old one; al: the factor of the sums so far.  The
+  // unrounded product and the reference, a rounded one, differ by up to half a unit
+  // in the last place: 32 below 2^30, and beyond it weights would leave the fp32
+  // range.  There a row multiplies its scores by a power of two, which is exact, in
+  // place of c2.  Two scores of that size that differ do so by 32 at least then: the
+  // lower one's weight is nothing with either factor.
+  static constexpr float kFar = 0x1p30f;
+  __device__ __forceinline__ void anew(int b, f32x16& t, float& mn, float& al) {
+    float x = t[0] * c2p;  // (c2p: in the order of the products with c2, and exact)
+#pragma unroll
+    for (int i = 1; i < 16; ++i) x = fmaxf(x, t[i] * c2p);
+    x = fmaxf(x, partner32(x));
+    const float was = reference(b), m = x * ratio();
+    const bool up = m > was;
+    const float g = !up ? f[b] : fabsf(m) >= kFar ? c2p : c2;
+    mn = !up ? mref[b] : g == c2 ? m : x;
+    // (equal factors: the difference of the references themselves)
+    al = !up ? 1.f
+         : mref[b] == -INFINITY ? 0.f
+                                : __builtin_amdgcn_exp2f(g == f[b] ? mref[b] - mn : was - m);
+    f[b] = g;
+    const float n = mn > -INFINITY ? -mn : 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) t[i] = fmaf(t[i], g, n);
+  }
+  // The scores of 32 keys of one block of query rows, an operand at a time (bf16).
+  __device__ __forceinline__ void score_one(int b, const KeyBase& k, f32x16& s) const {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+    for (int j = 0; j < QS; ++j) {
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, key(k, j)),
+                                                  __builtin_bit_cast(bf16x8, q[b][j]), s, 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
 
@@ -315,7 +398,7 @@ struct PrefixWave {
   template <int NL, typename Load>
   __device__ __forceinline__ void block(uint32_t vat, uint32_t knext, u32x4 (&kf)[QS],
                                         f32x16 (&s)[QW], f32x16 (&sn)[QW], float (&mx)[QW],
-                                        float c2, const Load& load) {
+                                        const Load& load) {
     float z[QW];
 #pragma unroll
     for (int b = 0; b < QW; ++b) z[b] = 0.f;
@@ -355,7 +438,13 @@ struct PrefixWave {
       if (n < QW) {  // (the first products run beside this)
         if (n == QW - 1) {
           __builtin_amdgcn_sched_barrier(0);
-          raise(mx, [&](int g, float by) __attribute__((always_inline)) { drop(s[g], by); });
+          raise(
+              mx, [&](int g, float by) __attribute__((always_inline)) { drop(s[g], by); },
+              [&](int g, float& mn, float& al) __attribute__((always_inline)) {
+                // (the block's keys are still in LDS, before its values)
+                score_one(g, key_base(vat - Geom::MB), s[g]);
+                anew(g, s[g], mn, al);
+              });
 #pragma unroll
           for (int e = 0; e < QW * 8 * QW / NQ; ++e) weight(0, e);
         }
@@ -389,8 +478,8 @@ struct PrefixWave {
 #pragma unroll
       for (int e = n * 8 * QW / NV; e < (n + 1) * 8 * QW / NV; ++e) {
         const int g = e >> 3, i = 2 * (e & 7);
-        sn[g][i] = fmaf(sn[g][i], c2, nref[g]);
-        sn[g][i + 1] = fmaf(sn[g][i + 1], c2, nref[g]);
+        sn[g][i] = fmaf(sn[g][i], f[g], nref[g]);
+        sn[g][i + 1] = fmaf(sn[g][i + 1], f[g], nref[g]);
         const float two = fmaxf(sn[g][i], sn[g][i + 1]);
         mx[g] = i ? fmaxf(mx[g], two) : two;
         asm volatile("" : "+v"(mx[g]));
@@ -694,7 +783,7 @@ struct OutRows {
           *reinterpret_cast<f32x4*>(o + r * STRIDE + 32 * d + 2 * i + 4 * h) =
               f32x4{w.O[b][d][i], w.O[b][d][i + 1], w.O[b][d][i + 2], w.O[b][d][i + 3]};
       if (h == 0) {
-        st[2 * r] = w.mref[b];
+        st[2 * r] = w.reference(b);
         st[2 * r + 1] = l;
       }
     }
@@ -793,8 +882,7 @@ __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void prefix_attn_ker
     return ((group * a.share + n) * a.heads + head) * a.R + (m - n * a.R);
   };
   W w;
-  w.init();
-  const float c2 = a.scale * kLog2e;
+  w.init(a.scale);
 
   if (nk > 0) {
     // a tile: the keys of one slot, or with eight waves of two, for half the
@@ -887,7 +975,7 @@ __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void prefix_attn_ker
         w.scores(kf, s0);
 #pragma unroll
         for (int b = 0; b < QW; ++b) {
-          w.shift_one(b, s0[b], s0[b], c2);
+          w.shift_one(b, s0[b], s0[b]);
           mx[b] = w.largest(s0[b]);
         }
         if (QW > 1 || KW == 1) w.keys(tile_at(0) + 2048, kf);
@@ -913,11 +1001,11 @@ __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void prefix_attn_ker
             begin(t);
             const auto ahead = dma.at(k0 + (long)(t + 3) * KT, slot_of(t + 3), spread(t));
             const uint32_t now = tile_at(t) + MB, next = tile_at(t + 1 < nt ? t + 1 : t);
-            w.template block<N>(now, next, kf, s0, s1, mx, c2,
+            w.template block<N>(now, next, kf, s0, s1, mx,
                                 [&](int i, int e) __attribute__((always_inline)) {
                                   if (ahead.go) load_some<T, D, 0>(dma, i, e, ahead);
                                 });
-            w.template block<N>(now + 2048, next + 2048, kf, s1, s0, mx, c2,
+            w.template block<N>(now + 2048, next + 2048, kf, s1, s0, mx,
                                 [&](int i, int e) __attribute__((always_inline)) {
                                   if (ahead.go) load_some<T, D, N>(dma, i, e, ahead);
                                 });
@@ -930,7 +1018,7 @@ __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void prefix_attn_ker
                                dma.at(k0 + (long)(t + 3) * KT, slot_of(t + 3), spread(t));
                            w.keys(tile_at(t + 1 < nt ? t + 1 : t), kf);
                            w.template block<2 * N>(
-                               tile_at(t) + MB, tile_at(t), kf, s, sn, mx, c2,
+                               tile_at(t) + MB, tile_at(t), kf, s, sn, mx,
                                [&](int i, int e) __attribute__((always_inline)) {
                                  if (ahead.go) load_some<T, D, 0>(dma, i, e, ahead);
                                });
@@ -966,7 +1054,7 @@ __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void prefix_attn_ker
       for (int r = 32 * kw; r < min(nr, KT); r += 32 * KW) {
         const uint32_t at = lds_offset(smem) + (slot_of(t) + r / kTileRows) * 2 * MB +
                             r % kTileRows * 64;
-        w.step(at, at + MB, min(32, nr - r), c2);
+        w.step(at, at + MB, min(32, nr - r));
       }
     }
     lds_barrier();  // the tiles are idle
@@ -1026,8 +1114,7 @@ __global__ __launch_bounds__(64 * kOwnWaves, (TileGeom<T, D>::SLOTS / 2)) void p
   const int n = a.tlen ? min(max(a.tlen[unit / a.heads], 0), a.T) : a.T;
   const long row0 = (long)unit * a.R;
   W w;
-  w.init();
-  const float c2 = a.scale * kLog2e;
+  w.init(a.scale);
   if (n > 0) {
     const int nt = (n + kTileRows - 1) / kTileRows;
     TileLoads<T, D> dma;
@@ -1057,7 +1144,7 @@ __global__ __launch_bounds__(64 * kOwnWaves, (TileGeom<T, D>::SLOTS / 2)) void p
       if (qw < a.t.qw)
         for (int r = 32 * kw; r < min(nr, kTileRows); r += 32 * KW) {
           const uint32_t at = lds_offset(tile) + r * 64;
-          w.step(at, at + MB, min(32, nr - r), c2);
+          w.step(at, at + MB, min(32, nr - r));
         }
     }
     lds_barrier();
