@@ -34,7 +34,8 @@ HIPCC_FLAGS = [
 # register file, whichever they are allocated to; by default they would all be
 # in the accumulation half, and the softmax between two products moves them
 # (prefix attention, 64 query rows a wave: 240 moves for 32 products).  The
-# warning left out says at each of its tile loads that m0 is a reserved register.
+# warning left out says at each of its tile loads that m0 is a reserved register
+# (tests/test_build_m0.py holds that the compiler does not use it there).
 EXTRA_FLAGS = {"wf_prefix.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1",
                                  "-Wno-inline-asm"]}
 

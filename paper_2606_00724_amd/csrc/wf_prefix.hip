@@ -497,7 +497,7 @@ struct PrefixWave {
 // 16 bytes per lane from base + off + OFF straight to LDS (lane l's at `lds` + AT
 // + 16 l; the instruction adds OFF to both addresses).  Waited for as
 // async_load16's.  m0 is named as overwritten, not saved and restored as there:
-// nothing else in this file's kernels uses it.
+// nothing else in this file's kernels uses it (a test reads the built code for that).
 template <int OFF, int AT>
 __device__ __forceinline__ void tile_load(const void* base, uint32_t off, uint32_t lds) {
   asm volatile(
