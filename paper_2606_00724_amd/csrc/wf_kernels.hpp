@@ -191,8 +191,8 @@ struct CacheArgs {
   int blocks;           // workgroups per unit
 };
 
-// Work of one kernel of the prefix attention: units x ranges of their keys x
-// blocks of their query rows.
+// Work of the prefix kernel: units x ranges of their keys x blocks of their query
+// rows.
 struct PrefixPart {
   int items;            // workgroups
   int splits;           // key ranges per unit
@@ -201,7 +201,11 @@ struct PrefixPart {
   int mrows;            // query rows per workgroup
   int M;                // query rows per unit
   int kw;               // waves that take the keys of a tile in turn
-  int qw;               // 32-row blocks per wave (prefix), waves over rows (own keys)
+};
+// Work of the kernel of the own keys: units x blocks of their query rows.
+struct OwnPart {
+  int mblocks, mrows;   // blocks per unit, query rows per workgroup
+  int kw, qw;           // waves over the keys of a tile, waves over the query rows
 };
 
 // Division of 0 <= n < 2^31 by a constant d >= 1: with 2^(l-1) < d <= 2^l, n times
@@ -235,7 +239,8 @@ struct PrefixArgs {
   float* lse;           // nullable [sequences][heads][R]
   float* part;          // [query rows][slots][D] unnormalised partial outputs
   float* pstat;         // [query rows][slots][2] reference (log2 units), sum
-  PrefixPart p, t;      // the prefix; the sequences' own rows
+  PrefixPart p;
+  OwnPart t;
   int heads, share, R;  // R: group * q_len
   FastDiv by_R;
   int cap, rows, T;

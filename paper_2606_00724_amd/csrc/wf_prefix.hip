@@ -1413,8 +1413,8 @@ hipError_t launch_prefix(const wf_prefix_params& p, const PrefixPlan& l, PrefixA
   a.scale = p.scale != 0.f ? p.scale : (float)(1.0 / std::sqrt((double)p.head_dim));
   const int M = a.R * p.share;
   if (l.items > 0)
-    a.p = PrefixPart{(int)l.items, l.splits, l.rps, l.mblocks, l.nw / l.kw * 32 * l.qw, M, l.kw, l.qw};
-  a.t = PrefixPart{(int)l.titems, 1, p.tail_cap, l.tmblocks, l.trows, a.R, l.tkw, l.tqw};
+    a.p = PrefixPart{(int)l.items, l.splits, l.rps, l.mblocks, l.nw / l.kw * 32 * l.qw, M, l.kw};
+  a.t = OwnPart{l.tmblocks, l.trows, l.tkw, l.tqw};
   auto run = [&](auto t, auto d) {
     using T = decltype(t);
     constexpr int D = decltype(d)::value;
