@@ -540,7 +540,8 @@ wf_status wf_prefix_plan(const wf_prefix_params* p, size_t workspace_bytes,
  *   row_idx     nullable [prefixes][heads][prefix_rows]    int32 list of
  *               prefix rows (wf_scan_select's tok_idx of the shared prompt),
  *               each in [0, prefix_cap): ids outside are taken as the nearest
- *               row inside
+ *               row inside, as wf_gather_kv's are (a list is not padded with
+ *               them as the store's may be: prefix_len says how many count)
  *   prefix_len  nullable [prefixes] int32: only the first prefix_len[i] rows
  *               (or list entries) of prefix i are seen
  *   Kt, Vt      [prefixes share][heads][T][d]              dtype; NULL iff T

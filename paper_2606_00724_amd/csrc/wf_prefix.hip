@@ -18,9 +18,10 @@
 //
 // Few query rows are bound by the cache's bytes, more than about 250 rows a
 // K/V head by the products.  bf16, d = 128, 8 K/V heads, on one MI355X: 2048
-// query rows a head over 32K keys take 247 us, 1.12 PFLOP/s (a product of 8192
-// x 8192 matrices reaches 1.21); 256 rows over 128K keys in 4 bits 138 us, 1.0
-// PFLOP/s; 32 rows over 32K bf16 keys 30 us, 4.5 TB/s with the merge.
+// query rows a head over 32K keys take 243 to 253 us by the card, 1.1 PFLOP/s (a
+// product of 8192 x 8192 matrices reaches 1.21, groups of four 1.34); 256 rows over
+// 128K keys in 4 bits 138 to 143 us, 1.0 PFLOP/s; 32 rows over 32K bf16 keys 30 us,
+// 4.5 TB/s with the merge.
 #include "wf_cache.hpp"
 #include "wf_kernels.hpp"
 #include "wf_launch.hpp"
@@ -31,9 +32,9 @@ namespace wf {
 // plain loop, one beside the other's waits, decodes and softmax (128 query rows
 // over 32K keys in 8 bits: 40 us, and 49 with four waves that pipeline
 // themselves, whose registers the codes on their way overfill); bf16 rows take one
-// per SIMD with a loop that pipelines itself (2048 rows over 32K keys: 253 us, and
-// 293 with eight waves in the plain loop, which read every key from LDS twice as
-// often); fp32 rows one per SIMD in the plain loop,
+// per SIMD with a loop that pipelines itself (2048 rows over 32K keys: 253 us, and on
+// the same card 293 with eight waves in the plain loop, which read every key from LDS
+// twice as often); fp32 rows one per SIMD in the plain loop,
 // whose products, at an eighth of the rate, are the bound.
 template <typename T, int FMT>
 constexpr int prefix_waves() {
