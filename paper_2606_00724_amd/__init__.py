@@ -5,7 +5,7 @@ tensors (pointers) and a HIP stream to the C entry point of the same name
 declared in include/wavefilter.h, and raises :class:`WfError` on a non-OK
 status.  Torch supplies device memory and streams; all arithmetic runs in the
 library's HIP kernels.  There is no fallback: importing this package fails if
-the library has not been built (``python -m paper_2606_00724_amd.build``).
+the library has not been built (``python paper_2606_00724_amd/build.py``).
 """
 from __future__ import annotations
 
@@ -86,7 +86,7 @@ def _load() -> ctypes.CDLL:
     if not os.path.exists(LIB_PATH):
         raise ImportError(
             f"{LIB_PATH} is missing: build it with "
-            "`python -m paper_2606_00724_amd.build` (hipcc, gfx950)")
+            f"`python {os.path.join(_HERE, 'build.py')}` (hipcc, gfx950)")
     lib = ctypes.CDLL(LIB_PATH)
     P = ctypes.POINTER(WfParams)
     vp, sz, i32 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int32
@@ -150,7 +150,11 @@ def _load() -> ctypes.CDLL:
         "wf_last_error": (ctypes.c_char_p, []),
     }
     for name, (res, args) in sig.items():
-        fn = getattr(lib, name)
+        fn = getattr(lib, name, None)
+        if fn is None:
+            raise ImportError(
+                f"{LIB_PATH} has no {name}, an older build: build it again with "
+                f"`python {os.path.join(_HERE, 'build.py')}` (hipcc, gfx950)")
         fn.restype = res
         fn.argtypes = args
     return lib

@@ -1,6 +1,6 @@
 """Builds libwavefilter.so (gfx950 only) next to this file.
 
-    python -m paper_2606_00724_amd.build
+    python paper_2606_00724_amd/build.py
 
 Every HIP source under csrc/ is compiled with hipcc in parallel into _build/
 at the repository root, then linked into one shared library.  The build
