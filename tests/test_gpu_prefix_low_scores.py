@@ -41,8 +41,8 @@ def compare(wf, p, c, cut):  # noqa: F811
 @pytest.mark.parametrize("low", [LOWEST, -1e7])
 @pytest.mark.parametrize("dtype,fmt,rows,waves,M,P", LONG, ids=NAMES)
 def test_prefix(wf, dtype, fmt, rows, waves, M, P, low):  # noqa: F811
-    """The low keys end inside a block of 32, between two and in a tile of their
-    own; what they leave of a range has many blocks."""
+    """The low keys end inside a block of 32 keys or between two; what they leave
+    of a range has many blocks."""
     for cut in (300, 320) if M == 150 else (300,):
         p, c = make(wf, **shape(M, dtype=dtype, fmt=fmt, d=64, prefixes=2, heads=24, P=P, T=3))
         expect(wf, p, rows, waves)
