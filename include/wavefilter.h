@@ -435,8 +435,8 @@ const char* wf_filter_attend_recursive_kernel_name(const wf_params* p,
  * read 0; no stored block has it, and beside codes other than 0 it has no
  * meaning.
  * --------------------------------------------------------------------- */
-enum { WF_CACHE_PLAIN = 0, /* no quantisation: rows of the call's dtype
-                              (wf_prefix_attn only)                      */
+enum { WF_CACHE_PLAIN = 0, /* no quantisation: rows of the call's dtype (not
+                              for wf_cache_store and wf_cache_load)      */
        WF_CACHE_E4M3 = 1, WF_CACHE_E2M1 = 2 };
 
 typedef struct wf_cache_params {
@@ -563,6 +563,122 @@ wf_status wf_prefix_attn(const wf_prefix_params* p, const void* Q, const void* K
                          const void* Kt, const void* Vt, const int32_t* tail_len,
                          void* O, float* lse, void* workspace,
                          size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------
+ * Rotary positions.  A row at position (t_0 .. t_{axes-1}) (one axis for
+ * text; time, height and width for images and video) has its first rot_dim
+ * channels rotated in pairs: pair i, channels (i, i + rot_dim / 2) or
+ * (2 i, 2 i + 1), by the angle t_a f_i with a = axis[i] and f the caller's
+ * frequencies:
+ *   y1 = x1 c - x2 s,  y2 = x2 c + x1 s,  c, s = factor cos, factor sin
+ * Angles are formed in 64 bits (exact below 2^53; |t f| < 2^31), c and s are
+ * rounded once to fp32, products and sums are fp32, each rounded by itself
+ * (no contraction), and the result is rounded to the type.  Channels from
+ * rot_dim on are copied.  Negated positions give the transpose, which takes
+ * gradients of the rotated rows back.
+ * --------------------------------------------------------------------- */
+enum { WF_ROPE_HALVES = 0, WF_ROPE_PAIRS = 1 };
+#define WF_MAX_ROPE_AXES 4
+
+typedef struct wf_rope_params {
+    int32_t batch;    /* >= 1                                              */
+    int32_t heads;    /* >= 1                                              */
+    int32_t rows;     /* rows per (batch, head), >= 0                      */
+    int32_t head_dim; /* d: 64 or 128                                      */
+    int32_t dtype;    /* WF_BF16 or WF_F32: X and Y                        */
+    int32_t rot_dim;  /* channels rotated: a multiple of 16 in [16, d]     */
+    int32_t layout;   /* WF_ROPE_HALVES or WF_ROPE_PAIRS                   */
+    int32_t axes;     /* 1 .. WF_MAX_ROPE_AXES                             */
+    float factor;     /* of cosine and sine; 0 selects 1                   */
+    uint8_t axis[64]; /* axis of pair i < rot_dim / 2, below axes          */
+    int64_t x_strides[3], y_strides[3]; /* elements from batch to batch,
+                         head to head, row to row (channels are adjacent):
+                         multiples of 16 bytes; all three 0: contiguous    */
+} wf_rope_params;
+
+/*
+ *   X         [batch][heads][rows][d] of x_strides   dtype
+ *   pos       [axes][batch][rows]                    int32
+ *   inv_freq  [rot_dim / 2]                          fp32: f
+ *   Y         like X, of y_strides: X itself with equal strides, or elements
+ *             apart from X's, no two at one place
+ * rows = 0 queues nothing.
+ */
+wf_status wf_rope(const wf_rope_params* p, const void* X, const int32_t* pos,
+                  const float* inv_freq, void* Y, void* stream);
+
+/* ---------------------------------------------------------------------
+ * A cache in pages.  K and V rows of all sequences stand in one pool of
+ * pages of page_rows rows each; row t of a sequence is row t % page_rows of
+ * page table[t / page_rows].
+ *   Kc, Vc   [pages][heads][page_rows][d] dtype (WF_CACHE_PLAIN), bytes
+ *            (WF_CACHE_E4M3) or [..][d / 2] bytes (WF_CACHE_E2M1)
+ *   Kx, Vx   [pages][heads][page_rows][d / 32] exponent bytes; NULL for
+ *            WF_CACHE_PLAIN
+ * Codes and exponent bytes are as of wf_cache_store.
+ * --------------------------------------------------------------------- */
+typedef struct wf_append_params {
+    int32_t pages;     /* of the pool, >= 1                                */
+    int32_t page_rows; /* a power of two, 16 .. 1024                       */
+    int32_t heads;     /* K/V heads, >= 1                                  */
+    int32_t head_dim;  /* d: 64 or 128                                     */
+    int32_t dtype;     /* WF_BF16 or WF_F32: Q, K, V, Qr                   */
+    int32_t format;    /* WF_CACHE_PLAIN (dtype), _E4M3 or _E2M1           */
+    int32_t tokens;    /* >= 0                                             */
+    int32_t group;     /* query heads per K/V head; 0: no queries          */
+    int32_t rot_dim;   /* as in wf_rope, or 0: nothing is rotated          */
+    int32_t layout, axes;
+    float factor;
+    uint8_t axis[64];
+    int64_t q_row, k_row, v_row, qr_row; /* elements from token to token
+                          (heads and channels are adjacent): multiples of 16
+                          bytes, at least a token's; 0: contiguous         */
+} wf_append_params;
+
+/*
+ * The rows of new tokens, each to its place in the pool: keys rotated, values
+ * as they are, both rounded once, to dtype or to the format.  The tokens'
+ * queries are rotated beside.
+ *   Q         nullable [tokens][heads group][d] of q_row   dtype
+ *   K, V      [tokens][heads][d] of k_row, v_row           dtype
+ *   pos       [axes][tokens]      int32 (not looked at where rot_dim = 0)
+ *   inv_freq  [rot_dim / 2]       fp32 (likewise)
+ *   slot      [tokens]            int32: page * page_rows + row in the page.
+ *             A token with a slot outside [0, pages page_rows) (padding) is
+ *             not stored; its query is rotated all the same.  The slots inside
+ *             must differ: what a row named twice holds is undefined.
+ *   Qr        [tokens][heads group][d] of qr_row  dtype out; Q itself with
+ *             equal strides, or apart from it.  NULL iff Q is (group = 0)
+ * All other rows of the pool keep their bytes.  tokens = 0 queues nothing.
+ */
+wf_status wf_page_append(const wf_append_params* p, const void* Q, const void* K,
+                         const void* V, const int32_t* pos, const float* inv_freq,
+                         const int32_t* slot, void* Kc, void* Kx, void* Vc,
+                         void* Vx, void* Qr, void* stream);
+
+typedef struct wf_move_params {
+    int32_t pages, page_rows, heads, head_dim; /* the pool: as above        */
+    int32_t dtype, format;
+    int32_t batch;       /* sequences, >= 1                                 */
+    int32_t table_pages; /* entries of a sequence's table, >= 1             */
+    int32_t moves;       /* rows a sequence may move: 0 .. WF_MAX_Q_LEN     */
+} wf_move_params;
+
+/*
+ * Rows brought together, as the accepted branch of a tree of drafted rows is
+ * behind its context: row first[b] + i of sequence b becomes what its row
+ * first[b] + source[b][i] was before the call (in any order, a row as often
+ * as wanted).  A source below 0 moves nothing, nor does a row or source that
+ * lies outside [0, table_pages page_rows) or in a page outside [0, pages).
+ *   table   [batch][table_pages]  int32
+ *   first   [batch]               int32
+ *   source  [batch][moves]        int32
+ * Rows that are written belong to one sequence: a page that several share
+ * may be read from by its sequences, and written by none.
+ */
+wf_status wf_page_move(const wf_move_params* p, const int32_t* table,
+                       const int32_t* first, const int32_t* source, void* Kc,
+                       void* Kx, void* Vc, void* Vx, void* stream);
 
 /* Loads the library's kernels onto the current device and sets up its
  * per-device state, so that no later call stalls for it (otherwise the

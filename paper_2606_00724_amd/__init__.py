@@ -22,6 +22,7 @@ EXT_SYMMETRIC, EXT_PERIODIC = 0, 1
 BF16, F32 = 0, 1
 OP_SKIM, OP_SCAN, OP_ATTN, OP_FUSED, OP_CACHED, OP_SHARED = 0, 1, 2, 3, 4, 5
 CACHE_PLAIN, CACHE_E4M3, CACHE_E2M1 = 0, 1, 2
+ROPE_HALVES, ROPE_PAIRS = 0, 1
 MAX_LEVELS, MAX_Q_LEN = 10, 256
 NOALLOC_SCRATCH_BYTES = 32 << 20
 
@@ -44,7 +45,8 @@ EXPORTED = ("wf_workspace_bytes", "wf_effective_budget", "wf_dwt_keys",
             "wf_filter_attend_recursive_kernels",
             "wf_filter_attend_recursive_kernel_name",
             "wf_cache_store", "wf_cache_load", "wf_prefix_workspace_bytes",
-            "wf_prefix_plan", "wf_prefix_attn", "wf_init", "wf_status_str", "wf_last_error")
+            "wf_prefix_plan", "wf_prefix_attn", "wf_rope", "wf_page_append",
+            "wf_page_move", "wf_init", "wf_status_str", "wf_last_error")
 
 
 class WfParams(ctypes.Structure):
@@ -75,6 +77,29 @@ class WfPrefixSplit(ctypes.Structure):
         "ranges", "range_rows", "group_rows", "wave_rows", "key_waves")]
 
 
+class WfRopeParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "batch", "heads", "rows", "head_dim", "dtype", "rot_dim", "layout",
+        "axes")] + [("factor", ctypes.c_float), ("axis", ctypes.c_uint8 * 64),
+                    ("x_strides", ctypes.c_int64 * 3),
+                    ("y_strides", ctypes.c_int64 * 3)]
+
+
+_POOL = ("pages", "page_rows", "heads", "head_dim", "dtype", "format")
+
+
+class WfAppendParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in _POOL + (
+        "tokens", "group", "rot_dim", "layout", "axes")] + [
+        ("factor", ctypes.c_float), ("axis", ctypes.c_uint8 * 64)] + [
+        (n, ctypes.c_int64) for n in ("q_row", "k_row", "v_row", "qr_row")]
+
+
+class WfMoveParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in _POOL + (
+        "batch", "table_pages", "moves")]
+
+
 class WfError(RuntimeError):
     def __init__(self, status: int, message: str):
         self.status = status
@@ -92,6 +117,8 @@ def _load() -> ctypes.CDLL:
     vp, sz, i32 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int32
     fp, ip = ctypes.POINTER(ctypes.c_float), ctypes.POINTER(ctypes.c_int32)
     CP, PP = ctypes.POINTER(WfCacheParams), ctypes.POINTER(WfPrefixParams)
+    RP, AP = ctypes.POINTER(WfRopeParams), ctypes.POINTER(WfAppendParams)
+    MP = ctypes.POINTER(WfMoveParams)
     sig = {
         "wf_workspace_bytes": (sz, [P, i32]),
         "wf_effective_budget": (i32, [P]),
@@ -145,6 +172,10 @@ def _load() -> ctypes.CDLL:
         "wf_prefix_attn": (ctypes.c_int,
                            [PP, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp,
                             vp, sz, vp]),
+        "wf_rope": (ctypes.c_int, [RP, vp, vp, vp, vp, vp]),
+        "wf_page_append": (ctypes.c_int, [AP, vp, vp, vp, vp, vp, vp, vp, vp,
+                                          vp, vp, vp, vp]),
+        "wf_page_move": (ctypes.c_int, [MP, vp, vp, vp, vp, vp, vp, vp, vp]),
         "wf_init": (ctypes.c_int, []),
         "wf_status_str": (ctypes.c_char_p, [ctypes.c_int]),
         "wf_last_error": (ctypes.c_char_p, []),
@@ -838,6 +869,194 @@ def prefix_attend(p: WfPrefixParams, Q, K, V, Kx=None, Vx=None, row_idx=None,
     wf_prefix_attn(p, Q, K, Kx, V, Vx, row_idx, prefix_len, Kt, Vt, tail_len,
                    O, lse, workspace, stream)
     return (O, lse) if want_lse else O
+
+
+# ------------------------------------------------------------ rotary positions
+# Pairs of a row's first channels rotated by their angles: the row's position
+# along the pair's axis times the pair's frequency.
+
+_LAYOUTS = {"halves": ROPE_HALVES, "pairs": ROPE_PAIRS}
+
+
+def _turn_fields(rot_dim, sections, axis, layout, factor) -> tuple:
+    """(rot_dim, layout, axes, factor, axis) of the parameters: pair by pair in
+    axis, or consecutive pairs of each axis in sections."""
+    if axis is None:
+        if sections is None:
+            sections = [rot_dim // 2]
+        axis = [a for a, n in enumerate(sections) for _ in range(n)]
+    axis = [int(a) for a in axis]
+    if len(axis) != rot_dim // 2 or len(axis) > 64 or any(
+            not 0 <= a < 256 for a in axis):
+        raise ValueError(f"{len(axis)} pairs have an axis, rot_dim {rot_dim} "
+                         f"has {rot_dim // 2}")
+    axes = len(sections) if sections is not None else max(axis, default=0) + 1
+    return (rot_dim, _LAYOUTS.get(layout, layout), axes, factor,
+            (ctypes.c_uint8 * 64)(*axis))
+
+
+def make_rope_params(*, batch: int, heads: int, rows: int, head_dim: int,
+                     rot_dim: int | None = None, sections=None, axis=None,
+                     layout: str | int = "halves", factor: float = 0.0,
+                     dtype: str | int = "bf16", x_strides=(0, 0, 0),
+                     y_strides=(0, 0, 0)) -> WfRopeParams:
+    """rot_dim: all of head_dim by default; sections: pairs of each axis, one
+    after the other (or axis: that of each pair); the strides of X and Y from
+    batch to batch, head to head and row to row, in elements (0s:
+    contiguous)."""
+    i64 = ctypes.c_int64 * 3
+    return WfRopeParams(batch, heads, rows, head_dim, _DTYPES.get(dtype, dtype),
+                        *_turn_fields(head_dim if rot_dim is None else rot_dim,
+                                      sections, axis, layout, factor),
+                        i64(*x_strides), i64(*y_strides))
+
+
+def _rows_ptr(name: str, t, dtype: torch.dtype, shape: tuple,
+              strides) -> int:
+    """The pointer of a tensor of this shape whose outer strides are those of
+    the parameters (all 0: contiguous), what is inside of them adjacent."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch tensor, got {type(t).__name__}")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name}: dtype {t.dtype}, expected {dtype}")
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {shape} "
+                         f"for these parameters")
+    if not any(strides):
+        good = t.is_contiguous()
+    else:
+        want, inner = list(strides), 1
+        for n in reversed(shape[len(want):]):
+            want.insert(len(strides), inner)
+            inner *= n
+        good = all(n <= 1 or h == w for n, h, w in zip(shape, t.stride(), want))
+    if not good:
+        raise ValueError(f"{name}: strides {t.stride()} are not those of the "
+                         f"parameters, {tuple(strides)} (0: contiguous)")
+    return t.data_ptr()
+
+
+def _on_current(tensors) -> None:
+    dev = torch.cuda.current_device() if torch.cuda.is_initialized() else -2
+    for name, t in tensors:
+        if t.get_device() != dev:
+            raise ValueError(f"{name} is on {t.device}, not on the current GPU")
+
+
+def wf_rope(p, X, pos, inv_freq, Y, stream=None):
+    dt, shape = torch_dtype(p), (p.batch, p.heads, p.rows, p.head_dim)
+    x = _rows_ptr("X", X, dt, shape, p.x_strides)
+    y = _rows_ptr("Y", Y, dt, shape, p.y_strides)
+    a = _args((("pos", pos, torch.int32, p.axes * p.batch * p.rows, False),
+               ("inv_freq", inv_freq, torch.float32, p.rot_dim // 2, False)))
+    _on_current((("X", X), ("Y", Y)))
+    _check(_lib.wf_rope(p, x, *a, y, _stream(stream)))
+
+
+def rope(X, pos, inv_freq, *, out=None, stream=None, **kw):
+    """Rotates the rows of X [batch, heads, rows, d], of any strides with
+    adjacent channels, at positions pos [axes, batch, rows] (or [batch, rows]);
+    kw: rot_dim, sections, axis, layout and factor of make_rope_params.
+    Returns out, allocated like X where it is None (X itself: in place)."""
+    if out is None:
+        with torch.cuda.stream(_torch_stream(stream)):
+            out = torch.empty_like(X)
+    b, h, n, d = X.shape
+    p = make_rope_params(batch=b, heads=h, rows=n, head_dim=d, dtype=X.dtype,
+                         x_strides=() if X.is_contiguous() else X.stride()[:3],
+                         y_strides=() if out.is_contiguous()
+                         else out.stride()[:3], **kw)
+    wf_rope(p, X, pos, inv_freq, out, stream)
+    return out
+
+
+# ------------------------------------------------------------ a cache in pages
+# K and V rows of all sequences in one pool, [pages][heads][page_rows][d] each;
+# row t of a sequence is row t % page_rows of page table[t // page_rows].
+
+def make_append_params(*, pages: int, page_rows: int, heads: int,
+                       head_dim: int, tokens: int, group: int = 1,
+                       dtype: str | int = "bf16",
+                       format: str | int | None = None,
+                       rot_dim: int | None = None, sections=None, axis=None,
+                       layout: str | int = "halves", factor: float = 0.0,
+                       q_row: int = 0, k_row: int = 0, v_row: int = 0,
+                       qr_row: int = 0) -> WfAppendParams:
+    """group: query heads per K/V head whose rows are rotated beside (0: none);
+    format: None for rows of dtype, "e4m3" or "e2m1"; the rotation as in
+    make_rope_params (rot_dim 0: none); *_row: elements from token to token
+    (0: contiguous)."""
+    return WfAppendParams(pages, page_rows, heads, head_dim,
+                          _DTYPES.get(dtype, dtype),
+                          _FORMATS.get(format, format), tokens, group,
+                          *_turn_fields(head_dim if rot_dim is None else rot_dim,
+                                        sections, axis, layout, factor),
+                          q_row, k_row, v_row, qr_row)
+
+
+def alloc_pages(p, device) -> tuple[torch.Tensor | None, ...]:
+    """A pool (Kc, Kx, Vc, Vx) for append, move or tree parameters, whose rows
+    all read back as zeros (Kx and Vx are None where rows are of dtype)."""
+    unit = (p.pages, p.heads, p.page_rows)
+    if p.format == CACHE_PLAIN:
+        K, V = (torch.zeros(unit + (p.head_dim,), dtype=torch_dtype(p),
+                            device=device) for _ in range(2))
+        return K, None, V, None
+    shapes = [unit + (_code_bytes(p.head_dim, p.format),),
+              unit + (p.head_dim // 32,)] * 2
+    return tuple(torch.zeros(s, dtype=torch.uint8, device=device)
+                 for s in shapes)
+
+
+def _pool_entries(p, Kc, Kx, Vc, Vx) -> tuple:
+    plain = p.format == CACHE_PLAIN
+    dt = torch_dtype(p) if plain else torch.uint8
+    rows = p.pages * p.heads * p.page_rows
+    codes = rows * (p.head_dim if plain else _code_bytes(p.head_dim, p.format))
+    exps = 0 if plain else rows * (p.head_dim // 32)
+    return (("Kc", Kc, dt, codes, False), ("Kx", Kx, torch.uint8, exps, plain),
+            ("Vc", Vc, dt, codes, False), ("Vx", Vx, torch.uint8, exps, plain))
+
+
+def wf_page_append(p, Q, K, V, pos, inv_freq, slot, Kc, Kx, Vc, Vx, Qr,
+                   stream=None):
+    dt, i32 = torch_dtype(p), torch.int32
+    n, h, d = p.tokens, p.heads, p.head_dim
+    k = _rows_ptr("K", K, dt, (n, h, d), (p.k_row,))
+    v = _rows_ptr("V", V, dt, (n, h, d), (p.v_row,))
+    q = qr = None
+    rows = [("K", K), ("V", V)]
+    if p.group:
+        q = _rows_ptr("Q", Q, dt, (n, h * p.group, d), (p.q_row,))
+        qr = _rows_ptr("Qr", Qr, dt, (n, h * p.group, d), (p.qr_row,))
+        rows += [("Q", Q), ("Qr", Qr)]
+    elif Q is not None or Qr is not None:
+        raise ValueError("Q or Qr with a group of 0")
+    turned = p.rot_dim > 0
+    a = _args((("pos", pos, i32, p.axes * n, not turned),
+               ("inv_freq", inv_freq, torch.float32, p.rot_dim // 2,
+                not turned),
+               ("slot", slot, i32, n, False), *_pool_entries(p, Kc, Kx, Vc, Vx)))
+    _on_current(rows)
+    _check(_lib.wf_page_append(p, q, k, v, *a, qr, _stream(stream)))
+
+
+def make_move_params(*, pages: int, page_rows: int, heads: int, head_dim: int,
+                     batch: int, table_pages: int, moves: int,
+                     dtype: str | int = "bf16",
+                     format: str | int | None = None) -> WfMoveParams:
+    return WfMoveParams(pages, page_rows, heads, head_dim,
+                        _DTYPES.get(dtype, dtype), _FORMATS.get(format, format),
+                        batch, table_pages, moves)
+
+
+def wf_page_move(p, table, first, source, Kc, Kx, Vc, Vx, stream=None):
+    i32 = torch.int32
+    a = _args((("table", table, i32, p.batch * p.table_pages, False),
+               ("first", first, i32, p.batch, False),
+               ("source", source, i32, p.batch * p.moves, False),
+               *_pool_entries(p, Kc, Kx, Vc, Vx)))
+    _check(_lib.wf_page_move(p, *a, _stream(stream)))
 
 
 # ------------------------------------------------------------ allocation

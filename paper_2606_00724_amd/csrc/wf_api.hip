@@ -875,6 +875,187 @@ static wf_status cache_impl(const wf_cache_params* p, bool store, const void* K,
   return ok();
 }
 
+// ------------------------------------------------------------ a cache in pages
+
+// Arrays of 32-bit words, which the kernels read one at a time.
+static wf_status check_words(const void* ptr, const char* name, bool nullable) {
+  if (!ptr) return nullable ? WF_OK : fail(WF_ERR_INVALID_ARG, "%s is NULL", name);
+  if (((uintptr_t)ptr & 3u) != 0)
+    return fail(WF_ERR_INVALID_ARG, "%s is not 4-byte aligned", name);
+  return WF_OK;
+}
+
+static wf_status check_rows(int dtype, int head_dim) {
+  if (head_dim != 64 && head_dim != 128)
+    return fail(WF_ERR_UNSUPPORTED, "head_dim %d: only 64 and 128 are built", head_dim);
+  if (dtype != WF_BF16 && dtype != WF_F32)
+    return fail(WF_ERR_INVALID_ARG, "unknown dtype %d", dtype);
+  return WF_OK;
+}
+
+// The pool of a params struct that begins with it.
+template <typename P>
+static wf_status check_pool(const P* p) {
+  if (!p) return fail(WF_ERR_INVALID_ARG, "params is NULL");
+  if (p->pages < 1 || p->heads < 1)
+    return fail(WF_ERR_INVALID_ARG, "pages (%d) and heads (%d) must be >= 1", p->pages, p->heads);
+  if (p->page_rows < 16 || p->page_rows > 1024 || (p->page_rows & (p->page_rows - 1)) != 0)
+    return fail(WF_ERR_UNSUPPORTED, "page_rows %d: powers of two from 16 to 1024 are built",
+                p->page_rows);
+  WF_TRY(check_rows(p->dtype, p->head_dim));
+  if (p->format != WF_CACHE_PLAIN && p->format != WF_CACHE_E4M3 && p->format != WF_CACHE_E2M1)
+    return fail(WF_ERR_INVALID_ARG, "unknown cache format %d", p->format);
+  if ((long)p->pages * p->page_rows > (1L << 30))
+    return fail(WF_ERR_UNSUPPORTED, "more than 2^30 rows in the pool");
+  if (p->heads > (1 << 20)) return fail(WF_ERR_UNSUPPORTED, "heads %d exceeds 2^20", p->heads);
+  return WF_OK;
+}
+
+template <typename P>
+static wf_status check_pool_ptrs(const P* p, const void* Kc, const void* Kx, const void* Vc,
+                                 const void* Vx) {
+  WF_TRY(check_ptr(Kc, "Kc", false));
+  WF_TRY(check_ptr(Vc, "Vc", false));
+  WF_TRY(check_ptr(Kx, "Kx", p->format == WF_CACHE_PLAIN));
+  WF_TRY(check_ptr(Vx, "Vx", p->format == WF_CACHE_PLAIN));
+  return WF_OK;
+}
+
+template <typename P>
+static wf_status check_rotation(const P* p) {
+  if (p->rot_dim < 16 || p->rot_dim > p->head_dim || p->rot_dim % 16 != 0)
+    return fail(WF_ERR_UNSUPPORTED, "rot_dim %d: multiples of 16 up to head_dim are built",
+                p->rot_dim);
+  if (p->layout != WF_ROPE_HALVES && p->layout != WF_ROPE_PAIRS)
+    return fail(WF_ERR_INVALID_ARG, "unknown layout of pairs %d", p->layout);
+  if (p->axes < 1 || p->axes > WF_MAX_ROPE_AXES)
+    return fail(WF_ERR_INVALID_ARG, "axes %d outside [1, %d]", p->axes, WF_MAX_ROPE_AXES);
+  if (!std::isfinite(p->factor)) return fail(WF_ERR_INVALID_ARG, "factor is not finite");
+  for (int i = 0; i < p->rot_dim / 2; ++i)
+    if (p->axis[i] >= p->axes)
+      return fail(WF_ERR_INVALID_ARG, "axis %d of pair %d: there are %d", p->axis[i], i, p->axes);
+  return WF_OK;
+}
+
+// A stride of n > 1 places, in elements, of which 16 bytes have `unit`.
+static wf_status check_stride(const char* name, int64_t stride, int64_t least, int unit) {
+  if (stride < least || stride > (1L << 40) || stride % unit != 0)
+    return fail(WF_ERR_INVALID_ARG, "%s %ld: a multiple of %d, at least %ld", name, (long)stride,
+                unit, (long)least);
+  return WF_OK;
+}
+
+static wf_status rope_impl(const wf_rope_params* p, const void* X, const int32_t* pos,
+                           const float* freq, void* Y, void* stream) {
+  if (!p) return fail(WF_ERR_INVALID_ARG, "params is NULL");
+  if (p->batch < 1 || p->heads < 1 || p->rows < 0)
+    return fail(WF_ERR_INVALID_ARG, "batch (%d) and heads (%d) must be >= 1, rows (%d) >= 0",
+                p->batch, p->heads, p->rows);
+  WF_TRY(check_rows(p->dtype, p->head_dim));
+  WF_TRY(check_rotation(p));
+  if (p->heads > (1 << 20) || (long)p->batch * p->rows > (1L << 30))
+    return fail(WF_ERR_UNSUPPORTED, "heads above 2^20 or batch*rows above 2^30");
+  const int unit = p->dtype == WF_BF16 ? 8 : 4;
+  long xs[3], ys[3];
+  const long n[3] = {p->batch, p->heads, p->rows};
+  static const char* const xn[3] = {"x_strides[0]", "x_strides[1]", "x_strides[2]"};
+  static const char* const yn[3] = {"y_strides[0]", "y_strides[1]", "y_strides[2]"};
+  auto whole = [&](const int64_t* s) { return s[0] == 0 && s[1] == 0 && s[2] == 0; };
+  const long dense[3] = {(long)p->heads * p->rows * p->head_dim, (long)p->rows * p->head_dim,
+                         p->head_dim};
+  const bool xw = whole(p->x_strides), yw = whole(p->y_strides);
+  for (int i = 0; i < 3; ++i) {
+    xs[i] = xw ? dense[i] : n[i] > 1 ? p->x_strides[i] : 0;
+    ys[i] = yw ? dense[i] : n[i] > 1 ? p->y_strides[i] : 0;
+    if (!xw && n[i] > 1) WF_TRY(check_stride(xn[i], xs[i], 0, unit));
+    if (!yw && n[i] > 1) WF_TRY(check_stride(yn[i], ys[i], p->head_dim, unit));
+    if (n[i] <= 1) xs[i] = ys[i] = 0;
+  }
+  if (p->rows == 0) return ok();
+  if (rope_groups(*p) * kBlock > UINT32_MAX)
+    return fail(WF_ERR_UNSUPPORTED, "too many rows in one call");
+  WF_TRY(check_ptr(X, "X", false));
+  WF_TRY(check_words(pos, "pos", false));
+  WF_TRY(check_words(freq, "inv_freq", false));
+  WF_TRY(check_ptr(Y, "Y", false));
+  if (X == Y && (xs[0] != ys[0] || xs[1] != ys[1] || xs[2] != ys[2]))
+    return fail(WF_ERR_INVALID_ARG, "Y is X, with other strides");
+  (void)hipGetLastError();
+  WF_HIP(launch_rope(*p, X, pos, freq, Y, xs, ys, static_cast<hipStream_t>(stream)), "rope");
+  return ok();
+}
+
+static wf_status append_impl(const wf_append_params* p, const void* Q, const void* K,
+                             const void* V, const int32_t* pos, const float* freq,
+                             const int32_t* slot, void* Kc, void* Kx, void* Vc, void* Vx, void* Qr,
+                             void* stream) {
+  WF_TRY(check_pool(p));
+  if (p->tokens < 0 || p->group < 0)
+    return fail(WF_ERR_INVALID_ARG, "tokens (%d) and group (%d) must be >= 0", p->tokens, p->group);
+  if (p->rot_dim != 0) WF_TRY(check_rotation(p));
+  if (p->tokens > (1 << 30) || (long)p->heads * ((long)p->group + 2) > (1L << 20))
+    return fail(WF_ERR_UNSUPPORTED, "tokens above 2^30 or heads*(group + 2) above 2^20");
+  const int unit = p->dtype == WF_BF16 ? 8 : 4;
+  const long kv = (long)p->heads * p->head_dim, hq = kv * p->group;
+  AppendArgs a{};
+  auto stride = [&](const char* name, int64_t given, long least, long& out) {
+    out = given ? given : least;
+    return check_stride(name, out, least, unit);
+  };
+  WF_TRY(stride("k_row", p->k_row, kv, a.ks));
+  WF_TRY(stride("v_row", p->v_row, kv, a.vs));
+  WF_TRY(stride("q_row", p->q_row, hq, a.qs));
+  WF_TRY(stride("qr_row", p->qr_row, hq, a.os));
+  if (p->tokens == 0) return ok();
+  if (append_groups(*p) * kBlock > UINT32_MAX)
+    return fail(WF_ERR_UNSUPPORTED, "too many rows in one call");
+  WF_TRY(check_ptr(Q, "Q", p->group == 0));
+  WF_TRY(check_ptr(K, "K", false));
+  WF_TRY(check_ptr(V, "V", false));
+  WF_TRY(check_words(pos, "pos", p->rot_dim == 0));
+  WF_TRY(check_words(freq, "inv_freq", p->rot_dim == 0));
+  WF_TRY(check_words(slot, "slot", false));
+  WF_TRY(check_pool_ptrs(p, Kc, Kx, Vc, Vx));
+  WF_TRY(check_ptr(Qr, "Qr", p->group == 0));
+  if (p->group > 0 && Q == Qr && a.qs != a.os)
+    return fail(WF_ERR_INVALID_ARG, "Qr is Q, with another stride");
+  a.Q = Q;
+  a.K = K;
+  a.V = V;
+  a.Qr = Qr;
+  a.slot = slot;
+  a.Kc = Kc;
+  a.Kx = static_cast<uint8_t*>(Kx);
+  a.Vc = Vc;
+  a.Vx = static_cast<uint8_t*>(Vx);
+  (void)hipGetLastError();
+  WF_HIP(launch_append(*p, a, pos, freq, static_cast<hipStream_t>(stream)), "page_append");
+  return ok();
+}
+
+static wf_status move_impl(const wf_move_params* p, const int32_t* table, const int32_t* first,
+                           const int32_t* source, void* Kc, void* Kx, void* Vc, void* Vx,
+                           void* stream) {
+  WF_TRY(check_pool(p));
+  if (p->batch < 1 || p->table_pages < 1 || p->moves < 0)
+    return fail(WF_ERR_INVALID_ARG,
+                "batch (%d) and table_pages (%d) must be >= 1, moves (%d) >= 0", p->batch,
+                p->table_pages, p->moves);
+  if (p->moves > WF_MAX_Q_LEN)
+    return fail(WF_ERR_UNSUPPORTED, "moves %d exceeds %d", p->moves, (int)WF_MAX_Q_LEN);
+  if (p->moves == 0) return ok();
+  if ((long)p->batch * p->heads > (1L << 24) || move_groups(*p) * kBlock > UINT32_MAX)
+    return fail(WF_ERR_UNSUPPORTED, "too many sequences and heads in one call");
+  WF_TRY(check_words(table, "table", false));
+  WF_TRY(check_words(first, "first", false));
+  WF_TRY(check_words(source, "source", false));
+  WF_TRY(check_pool_ptrs(p, Kc, Kx, Vc, Vx));
+  (void)hipGetLastError();
+  WF_HIP(launch_move(*p, table, first, source, Kc, Kx, Vc, Vx, static_cast<hipStream_t>(stream)),
+         "page_move");
+  return ok();
+}
+
 // ------------------------------------------------------------ shared prefix
 
 static wf_status check_prefix(const wf_prefix_params* p, size_t have, PrefixPlan* plan) {
@@ -1250,6 +1431,23 @@ wf_status wf_cache_load(const wf_cache_params* p, const void* Kc, const void* Kx
   return cache_impl(p, false, K, V, row_idx, Kc, Kx, Vc, Vx, stream);
 }
 
+wf_status wf_rope(const wf_rope_params* p, const void* X, const int32_t* pos,
+                  const float* inv_freq, void* Y, void* stream) {
+  return rope_impl(p, X, pos, inv_freq, Y, stream);
+}
+
+wf_status wf_page_append(const wf_append_params* p, const void* Q, const void* K, const void* V,
+                         const int32_t* pos, const float* inv_freq, const int32_t* slot, void* Kc,
+                         void* Kx, void* Vc, void* Vx, void* Qr, void* stream) {
+  return append_impl(p, Q, K, V, pos, inv_freq, slot, Kc, Kx, Vc, Vx, Qr, stream);
+}
+
+wf_status wf_page_move(const wf_move_params* p, const int32_t* table, const int32_t* first,
+                       const int32_t* source, void* Kc, void* Kx, void* Vc, void* Vx,
+                       void* stream) {
+  return move_impl(p, table, first, source, Kc, Kx, Vc, Vx, stream);
+}
+
 size_t wf_prefix_workspace_bytes(const wf_prefix_params* p) {
   PrefixPlan plan;
   if (check_prefix(p, SIZE_MAX, &plan) != WF_OK) return 0;
@@ -1285,6 +1483,7 @@ wf_status wf_init(void) {
   WF_HIP(load_dwt_kernels(), "loading the DWT kernels");
   WF_HIP(load_cache_kernels(), "loading the cache kernels");
   WF_HIP(load_prefix_kernels(), "loading the prefix-attention kernels");
+  WF_HIP(load_page_kernels(), "loading the kernels of a cache in pages");
   void* scratch_ptr = nullptr;  // this file's code object and its scratch array
   WF_TRY(scratch_of_current_device(&scratch_ptr));
   return ok();

@@ -23,39 +23,6 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t v) {
   return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4e, 0xf, 0xf, false));
 }
 
-template <typename T>
-__device__ __forceinline__ void load8(const T* p, float (&v)[8]);
-template <>
-__device__ __forceinline__ void load8<bf16_t>(const bf16_t* p, float (&v)[8]) {
-  const u32x4 w = *reinterpret_cast<const u32x4*>(p);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[2 * i] = bf16_lo(w[i]);
-    v[2 * i + 1] = bf16_hi(w[i]);
-  }
-}
-template <>
-__device__ __forceinline__ void load8<float>(const float* p, float (&v)[8]) {
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const f32x4 w = reinterpret_cast<const f32x4*>(p)[i];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[4 * i + e] = w[e];
-  }
-}
-template <typename T>
-__device__ __forceinline__ void put8(T* p, const float (&v)[8]);
-template <>
-__device__ __forceinline__ void put8<bf16_t>(bf16_t* p, const float (&v)[8]) {
-  *reinterpret_cast<u32x4*>(p) = u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
-                                       pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
-}
-template <>
-__device__ __forceinline__ void put8<float>(float* p, const float (&v)[8]) {
-  reinterpret_cast<f32x4*>(p)[0] = f32x4{v[0], v[1], v[2], v[3]};
-  reinterpret_cast<f32x4*>(p)[1] = f32x4{v[4], v[5], v[6], v[7]};
-}
-
 // Rows of a unit that a workgroup moves: two per thread group.
 template <int D>
 constexpr int kRowsPerGroup = 2 * kBlock / (D / 8);

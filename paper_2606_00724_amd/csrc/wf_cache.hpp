@@ -7,6 +7,40 @@
 
 namespace wf {
 
+// Eight channels of a row as fp32 numbers, and back (rounded to nearest even).
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float (&v)[8]);
+template <>
+__device__ __forceinline__ void load8<bf16_t>(const bf16_t* p, float (&v)[8]) {
+  const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = bf16_lo(w[i]);
+    v[2 * i + 1] = bf16_hi(w[i]);
+  }
+}
+template <>
+__device__ __forceinline__ void load8<float>(const float* p, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const f32x4 w = reinterpret_cast<const f32x4*>(p)[i];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[4 * i + e] = w[e];
+  }
+}
+template <typename T>
+__device__ __forceinline__ void put8(T* p, const float (&v)[8]);
+template <>
+__device__ __forceinline__ void put8<bf16_t>(bf16_t* p, const float (&v)[8]) {
+  *reinterpret_cast<u32x4*>(p) = u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
+                                       pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+}
+template <>
+__device__ __forceinline__ void put8<float>(float* p, const float (&v)[8]) {
+  reinterpret_cast<f32x4*>(p)[0] = f32x4{v[0], v[1], v[2], v[3]};
+  reinterpret_cast<f32x4*>(p)[1] = f32x4{v[4], v[5], v[6], v[7]};
+}
+
 // Exponent byte of a block whose largest magnitude has the fp32 bits amax:
 // the smallest x >= 1 with amax <= top 2^(x - 127).  With top = m 2^k the
 // exponent field of amax less k is that x, one more where its mantissa is

@@ -191,6 +191,56 @@ struct CacheArgs {
   int blocks;           // workgroups per unit
 };
 
+// Angles of rotated rows: positions of several axes times the pairs' frequencies.
+struct TurnArgs {
+  const int32_t* pos;   // [axes][rows in all]
+  const float* freq;    // [half]
+  long n;               // rows in all
+  int half;             // pairs (0: nothing is rotated)
+  int pairs;            // adjacent channels are a pair, not halves
+  uint32_t axis[4];     // axis of pair i: bits 2 (i % 16) of word i / 16
+  float factor;
+};
+
+struct RopeArgs {
+  TurnArgs turn;
+  const void* X;
+  void* Y;
+  long xs[3], ys[3];    // elements from batch to batch, head to head, row to row
+  int heads, rows;
+  int blocks;           // blocks of rows per batch
+  int hgroups, iters;   // workgroups over the heads, eights of heads in each
+};
+
+struct AppendArgs {
+  TurnArgs turn;
+  const void* Q;        // nullable [tokens][hq][D]
+  const void* K;        // [tokens][heads][D]
+  const void* V;
+  void* Qr;
+  const int32_t* slot;  // [tokens]
+  void* Kc;             // [pages][heads][page rows][D] or codes
+  uint8_t* Kx;          // exponent bytes (quantised)
+  void* Vc;
+  uint8_t* Vx;
+  long qs, ks, vs, os;  // elements from token to token
+  long slots;           // rows of the pool per head
+  int tokens, heads, hq;
+  int shift;            // log2 of a page's rows
+  int hgroups, iters;
+};
+
+struct MoveArgs {
+  const int32_t* table;  // [batch][tp]
+  const int32_t* first;  // [batch]
+  const int32_t* src;    // [batch][moves]
+  void* c[2];            // K, V: rows of rb bytes
+  uint8_t* x[2];         // exponent bytes, xb a row (quantised)
+  int pages, heads, tp, moves, shift;
+  int rb, xb;
+  int pc, cols;          // 16-byte pieces of a row in a workgroup, workgroups a row takes
+};
+
 // Work of the prefix kernel: units x ranges of their keys x blocks of their query
 // rows.
 struct PrefixPart {

@@ -307,6 +307,22 @@ hipError_t launch_cache(const wf_cache_params& p, bool store, const void* K, con
                         const void* Vx, hipStream_t s);
 hipError_t load_cache_kernels();
 
+// The cache in pages: rows rotated, appended, moved.  *_groups: the workgroups of
+// such a call.
+struct AppendArgs;
+long rope_groups(const wf_rope_params& p);
+long append_groups(const wf_append_params& p);
+long move_groups(const wf_move_params& p);
+hipError_t launch_rope(const wf_rope_params& p, const void* X, const int32_t* pos,
+                       const float* freq, void* Y, const long (&xs)[3], const long (&ys)[3],
+                       hipStream_t s);
+hipError_t launch_append(const wf_append_params& p, AppendArgs& a, const int32_t* pos,
+                         const float* freq, hipStream_t s);
+hipError_t launch_move(const wf_move_params& p, const int32_t* table, const int32_t* first,
+                       const int32_t* source, void* Kc, void* Kx, void* Vc, void* Vx,
+                       hipStream_t s);
+hipError_t load_page_kernels();
+
 // Attention over a shared prefix: its split into workgroups, and the launches.
 struct PrefixArgs;
 struct PrefixPlan {

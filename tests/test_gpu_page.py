@@ -1,0 +1,304 @@
+"""Rotary positions, and rows appended to and moved in a cache in pages, bit by
+bit against the CPU reference: every rounding is defined (cosines and sines of
+64-bit angles rounded once, products and sums each rounded by itself, one
+rounding to the type or format)."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+import torch
+
+import pageref
+
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+@pytest.fixture(scope="module")
+def wf():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU visible")
+    import paper_2606_00724_amd as wf
+    return wf
+
+
+def rows(seed, shape, dtype):
+    g = torch.Generator().manual_seed(seed)
+    return torch.randn(shape, generator=g).to(DT[dtype])
+
+
+def places(seed, shape, hi=200000):
+    g = torch.Generator().manual_seed(seed)
+    return torch.randint(-1000, hi, shape, generator=g).int()
+
+
+def same(name, got, want):
+    a, b = (x.cpu().contiguous() for x in (got, want))
+    bits = {2: torch.int16, 4: torch.int32, 1: torch.uint8}[a.element_size()]
+    bad = (a.view(bits) != b.view(bits)).nonzero()
+    assert len(bad) == 0, f"{name}: {len(bad)} differ, first {bad[0].tolist()}"
+
+
+SECTIONS = {1: lambda n: [n], 2: lambda n: [n // 3, n - n // 3],
+            3: lambda n: [n // 4, n // 3, n - n // 4 - n // 3], 4: lambda n: [1, n - 5, 4, 0]}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("layout", ["halves", "pairs"])
+@pytest.mark.parametrize("b,h,n,d,rot,axes", [
+    (1, 1, 1, 128, 128, 1), (2, 3, 17, 64, 64, 1), (3, 9, 5, 128, 48, 3), (1, 33, 31, 64, 16, 2),
+    (2, 8, 130, 128, 112, 4), (1, 17, 4, 128, 64, 1), (40, 1, 3, 64, 32, 3),
+])
+def test_rope(wf, dtype, layout, b, h, n, d, rot, axes):
+    X, pos = rows(1, (b, h, n, d), dtype), places(2, (axes, b, n))
+    sec, freq = SECTIONS[axes](rot // 2), pageref.frequencies(rot // 2)
+    axis = [a for a, k in enumerate(sec) for _ in range(k)]
+    c, s = pageref.turn(pos, freq, axis, 1.25)
+    want = pageref.rotate(X, c[:, None], s[:, None], layout).to(DT[dtype])
+    got = wf.rope(X.cuda(), pos.cuda(), freq.cuda(), rot_dim=rot, sections=sec, layout=layout,
+                  factor=1.25)
+    same("Y", got, want)
+
+
+def test_rope_strides_in_place_and_axis_by_axis(wf):
+    """Slices of a fused projection, written to another layout and in place;
+    axes that alternate from pair to pair; rows beside the slices are kept."""
+    b, n, h, d = 2, 19, 5, 128
+    x = rows(3, (b, n, h + 4, d), "bf16").cuda()
+    pos, freq = places(4, (3, b, n)), pageref.frequencies(64)
+    axis = [i % 3 for i in range(64)]
+    c, s = pageref.turn(pos, freq, axis)
+    X = x[:, :, 2:2 + h].transpose(1, 2)
+    want = pageref.rotate(X.cpu(), c[:, None], s[:, None]).to(torch.bfloat16)
+    same("Y", wf.rope(X, pos.cuda(), freq.cuda(), axis=axis), want)
+    out = torch.full((h, b, n + 1, d), 7.0, dtype=torch.bfloat16, device="cuda")
+    wf.rope(X, pos.cuda(), freq.cuda(), axis=axis, out=out[:, :, :n].transpose(0, 1))
+    same("Y", out[:, :, :n].transpose(0, 1), want)
+    assert (out[:, :, n] == 7).all()
+    before = x.clone()
+    assert wf.rope(X, pos.cuda(), freq.cuda(), axis=axis, out=X) is X
+    same("X", X, want)
+    same("beside", x[:, :, :2], before[:, :, :2])
+    same("beside", x[:, :, 2 + h:], before[:, :, 2 + h:])
+    # one row for all heads and sequences
+    one = rows(5, (1, 1, n, d), "bf16").cuda().expand(b, h, n, d)
+    same("broadcast", wf.rope(one, pos.cuda(), freq.cuda(), axis=axis,
+                              out=torch.empty_like(before[:, :, :h]).transpose(1, 2)),
+         pageref.rotate(one.cpu(), c[:, None], s[:, None]).to(torch.bfloat16))
+
+
+def test_rope_far_positions_and_back(wf):
+    """The largest positions: the angle's own 64-bit rounding is 2^-53 of it,
+    2^-22 at 2^31, beside the half step of the cosine and one of each product
+    and sum (2^-24 of the pair's magnitude each); turning back by the negated
+    positions gives the rows again."""
+    pos = torch.tensor([[[0, 1, -1, 2 ** 24 - 1, 2 ** 31 - 1, -2 ** 31, 1234567891]]]).int()
+    n, d = pos.shape[-1], 128
+    X, freq = rows(6, (1, 2, n, d), "f32"), pageref.frequencies(64)
+    Y = wf.rope(X.cuda(), pos.cuda(), freq.cuda())
+    c, s = pageref.turn(pos, freq, [0] * 64)
+    want = pageref.rotate(X, c[:, None], s[:, None], exact=True)
+    mag = (X[..., :64].abs() + X[..., 64:].abs()).double().repeat(1, 1, 1, 2)
+    assert ((Y.cpu().double() - want).abs() <= mag * (2.0 ** -22 + 4 * 2.0 ** -24)).all()
+    back = wf.rope(Y, (-pos).cuda(), freq.cuda())   # (-2^31 has no negative)
+    keep = [i for i in range(n) if int(pos[0, 0, i]) != -2 ** 31]
+    assert ((back.cpu() - X).abs()[:, :, keep].double()
+            <= mag[:, :, keep] * 2 * (4 * 2.0 ** -24)).all()
+
+
+def test_rope_gradient(wf):
+    """The gradient of sum(w y) by negated positions against differences of
+    the 64-bit formula."""
+    b, h, n, d, rot = 1, 2, 3, 64, 48
+    X, W = rows(7, (b, h, n, d), "f32"), rows(8, (b, h, n, d), "f32")
+    pos, freq = places(9, (2, b, n)), pageref.frequencies(rot // 2)
+    sec = [10, 14]
+    axis = [0] * 10 + [1] * 14
+    dX = wf.rope(W.cuda(), (-pos).cuda(), freq.cuda(), rot_dim=rot, sections=sec, factor=0.75)
+    c, s = pageref.turn(pos, freq, axis, 0.75)
+
+    def f(x):
+        return (pageref.rotate(x, c[:, None], s[:, None], exact=True) * W.double()).sum()
+
+    for at in [(0, 0, 0, 0), (0, 1, 2, 5), (0, 1, 1, 24), (0, 0, 2, 47), (0, 1, 0, 48)]:
+        e = torch.zeros(X.shape, dtype=torch.float64)
+        e[at] = 0.5     # (f is linear: any step)
+        diff = float(f(X.double() + e) - f(X.double() - e))
+        assert abs(diff - float(dX.cpu()[at])) <= 8 * 2.0 ** -24 * 8
+
+
+# ------------------------------------------------------------ append
+
+def append_case(wf, *, tokens, heads, group, d, P, fmt, dtype, rot, axes=1, layout="halves",
+                fused=False, seed=11, pages=None):
+    hq = heads * group
+    x = rows(seed, (tokens, hq + 2 * heads, d), dtype)
+    parts = x.cuda().split([hq, heads, heads], dim=1)
+    if not fused:
+        parts = [t.contiguous() for t in parts]
+    q, k, v = parts
+    pos = places(seed + 1, (axes, tokens))
+    sec = SECTIONS[axes](rot // 2) if rot else None
+    freq = pageref.frequencies(max(1, rot // 2))
+    pages = pages or -(-tokens // P) + 3
+    p = wf.make_append_params(pages=pages, page_rows=P, heads=heads, head_dim=d, tokens=tokens,
+                              group=group, dtype=dtype, format=fmt, rot_dim=rot, sections=sec,
+                              layout=layout, q_row=q.stride(0) if fused and hq else 0,
+                              k_row=k.stride(0) if fused else 0, v_row=v.stride(0) if fused else 0)
+    pool = pageref.pool_like(wf, p, seed + 2)
+    g = torch.Generator().manual_seed(seed + 3)
+    slot = torch.randperm(pages * P, generator=g)[:tokens].int()
+    if tokens > 2:
+        outside = torch.tensor([-1, pages * P, 2 ** 31 - 1, -2 ** 31]).int()
+        slot[1::5] = outside[torch.arange(len(range(1, tokens, 5))) % 4]
+    K, Q = x[:, hq:hq + heads], x[:, :hq]
+    if rot:
+        axis = [a for a, n in enumerate(sec) for _ in range(n)]
+        c, s = pageref.turn(pos, freq, axis)
+        K, Q = (pageref.rotate(t, c[:, None], s[:, None], layout) for t in (K, Q))
+    want = pageref.append(pool, fmt, DT[dtype], K.float(), x[:, hq + heads:].float(), slot, P)
+    return p, (q, k, v), pos, freq, slot, pool, want, Q.to(DT[dtype])
+
+
+@pytest.mark.parametrize("fmt", [None, "e4m3", "e2m1"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("tokens,heads,group,d,P,rot,axes,layout,fused", [
+    (1, 1, 1, 128, 16, 128, 1, "halves", False), (3, 2, 4, 64, 16, 64, 1, "halves", True),
+    (65, 3, 1, 128, 32, 48, 3, "halves", True), (33, 5, 7, 64, 64, 48, 2, "pairs", False),
+    (131, 8, 0, 128, 16, 96, 1, "pairs", True), (17, 2, 2, 128, 1024, 0, 1, "halves", False),
+    (600, 8, 4, 128, 64, 128, 3, "halves", True), (9, 33, 1, 64, 128, 16, 1, "halves", False),
+])
+def test_append(wf, fmt, dtype, tokens, heads, group, d, P, rot, axes, layout, fused):
+    p, (q, k, v), pos, freq, slot, pool, want, wantq = append_case(
+        wf, tokens=tokens, heads=heads, group=group, d=d, P=P, fmt=fmt, dtype=dtype, rot=rot,
+        axes=axes, layout=layout, fused=fused)
+    dev = [None if t is None else t.cuda() for t in pool]
+    qr = torch.empty((tokens, heads * group, d), dtype=DT[dtype], device="cuda") if group else None
+    turned = (pos.cuda(), freq.cuda()) if rot else (None, None)
+    wf.wf_page_append(p, q if group else None, k, v, *turned, slot.cuda(), *dev, qr)
+    for name, x, y in zip(("Kc", "Kx", "Vc", "Vx"), dev, want):
+        if y is not None:
+            same(name, x, y)
+    if group:
+        same("Qr", qr, wantq)
+
+
+def test_append_keeps_bits_of_what_it_does_not_turn(wf):
+    """NaN, infinities and subnormals of values and of the channels behind the
+    rotated ones; blocks that hold one in 8 bits."""
+    p, (q, k, v), pos, freq, slot, pool, _, _ = append_case(
+        wf, tokens=4, heads=2, group=1, d=64, P=16, fmt=None, dtype="bf16", rot=32)
+    odd = torch.tensor([0x7fc1, 0x7f81, -0x80, 0x7f80, 1, -0x7fff], dtype=torch.int16)
+    bits = odd.repeat(100)[:4 * 2 * 64].view(4, 2, 64)
+    v.copy_(bits.view(torch.bfloat16))
+    k[:, :, 32:] = bits.view(torch.bfloat16)[:, :, 32:].cuda()
+    dev = [None if t is None else t.cuda() for t in pool]
+    slot = torch.tensor([5, 100, 40, 18]).int()
+    wf.wf_page_append(p, q, k, v, pos.cuda(), freq.cuda(), slot.cuda(), *dev, torch.empty_like(q))
+    for n, at in ((0, 5), (2, 40), (3, 18)):
+        if at >= p.pages * 16:
+            continue
+        same("V", dev[2][at // 16, :, at % 16], bits[n].view(torch.bfloat16))
+        same("K", dev[0][at // 16, :, at % 16, 32:], bits[n, :, 32:].view(torch.bfloat16))
+
+
+def test_append_in_place_and_past_two_to_the_31_bytes(wf):
+    """Queries rotated where they are; a pool whose last rows lie behind 2^32
+    bytes (2^21 rows of 8 heads of 128 channels: 4 GiB for K)."""
+    p, (q, k, v), pos, freq, slot, _, _, wantq = append_case(
+        wf, tokens=7, heads=8, group=2, d=128, P=16, fmt=None, dtype="bf16", rot=128, fused=True)
+    pages = (1 << 21) // 16 + 4
+    p.pages, p.qr_row = pages, q.stride(0)
+    K = torch.zeros((pages, 8, 16, 128), dtype=torch.bfloat16, device="cuda")
+    V = torch.zeros_like(K)
+    slot = torch.arange(7).int() * 9 + (pages * 16 - 60)
+    slot[3] = 5
+    want = (k.clone(), v.clone())
+    wf.wf_page_append(p, q, k, v, pos.cuda(), freq.cuda(), slot.cuda(), K, None, V, None, q)
+    same("Q", q, wantq)
+    c, s = pageref.turn(pos, freq, [0] * 64)
+    turned = pageref.rotate(want[0].cpu(), c[:, None], s[:, None]).to(torch.bfloat16)
+    for n, at in enumerate(slot.tolist()):
+        same("K", K[at // 16, :, at % 16], turned[n])
+        same("V", V[at // 16, :, at % 16], want[1][n])
+    assert int((V != 0).any(-1).sum()) == 7 * 8
+
+
+# ------------------------------------------------------------ move
+
+@pytest.mark.parametrize("fmt", [None, "e4m3", "e2m1"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("b,h,d,P,tp,moves", [
+    (1, 1, 128, 16, 3, 1), (3, 2, 64, 16, 9, 6), (5, 3, 128, 32, 5, 64), (2, 2, 128, 64, 9, 256),
+    (2, 1, 64, 1024, 2, 255),
+])
+def test_move(wf, fmt, dtype, b, h, d, P, tp, moves):
+    """Accepted branches, permutations, repeated and missing sources, rows past
+    the table's end and in no page."""
+    pages = b * tp + 2
+    p = wf.make_move_params(pages=pages, page_rows=P, heads=h, head_dim=d, batch=b,
+                            table_pages=tp, moves=moves, dtype=dtype, format=fmt)
+    pool = pageref.pool_like(wf, p)
+    g = torch.Generator().manual_seed(5)
+    table = torch.randperm(pages, generator=g)[:b * tp].view(b, tp).int()
+    first = torch.randint(0, tp * P - moves // 2, (b,), generator=g).int()
+    source = torch.randint(-1, 2 * moves, (b, moves), generator=g).int()
+    source[0] = torch.randperm(moves, generator=g).int()    # in a circle
+    if b > 1:
+        source[1] = torch.arange(moves).flip(0).int() * 2
+        table[1, -1] = pages if b > 2 else -1               # no page
+    if b > 2:
+        first[2] = -moves // 2
+    want = pageref.move(pool, table, first, source, P)
+    dev = [None if t is None else t.cuda() for t in pool]
+    wf.wf_page_move(p, table.cuda(), first.cuda(), source.cuda(), *dev)
+    for name, x, y in zip(("Kc", "Kx", "Vc", "Vx"), dev, want):
+        if y is not None:
+            same(name, x, y)
+
+
+# ------------------------------------------------------------ as a program uses them
+
+def test_graph_replays_on_another_stream(wf):
+    """A captured step (append, then a move) replayed with new rows, with eager
+    work between the replays."""
+    p, (q, k, v), pos, freq, slot, pool, _, _ = append_case(
+        wf, tokens=40, heads=3, group=2, d=64, P=16, fmt="e4m3", dtype="bf16", rot=64)
+    m = wf.make_move_params(pages=p.pages, page_rows=16, heads=3, head_dim=64, batch=1,
+                            table_pages=2, moves=5, format="e4m3")
+    table, first = torch.tensor([[1, 0]]).int(), torch.tensor([3]).int()
+    source = torch.tensor([[0, 4, 2, 9, -1]]).int()
+    dev = [t.cuda() for t in pool]
+    gt, gf, gs = table.cuda(), first.cuda(), source.cuda()
+    gpos, gfreq, gslot, qr = pos.cuda(), freq.cuda(), slot.cuda(), torch.empty_like(q)
+
+    def step():
+        wf.wf_page_append(p, q, k, v, gpos, gfreq, gslot, *dev, qr)
+        wf.wf_page_move(m, gt, gf, gs, *dev)
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        step()
+    s.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        step()
+    for i in range(4):
+        x = [rows(20 + 3 * i + j, t.shape, "bf16") for j, t in enumerate((q, k, v))]
+        for t, y in zip((q, k, v), x):
+            t.copy_(y)
+        for t, y in zip(dev, pool):
+            t.copy_(y)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        c, sn = pageref.turn(pos, freq, [0] * 32)
+        K = pageref.rotate(x[1], c[:, None], sn[:, None])
+        want = pageref.append(pool, "e4m3", torch.bfloat16, K, x[2].float(), slot, 16)
+        want = pageref.move(want, table, first, source, 16)
+        for name, a, y in zip(("Kc", "Kx", "Vc", "Vx"), dev, want):
+            same(name, a, y)
+        same("Qr", qr, pageref.rotate(x[0], c[:, None], sn[:, None]).to(torch.bfloat16))
+        (q.float() @ q.float().transpose(-1, -2)).sum()  # eager work between the replays
