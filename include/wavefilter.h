@@ -680,6 +680,72 @@ wf_status wf_page_move(const wf_move_params* p, const int32_t* table,
                        const int32_t* first, const int32_t* source, void* Kc,
                        void* Kx, void* Vc, void* Vx, void* stream);
 
+/* ---------------------------------------------------------------------
+ * Attention of new rows over a cache in pages: the rows of a tree of drafted
+ * tokens, of a block whose rows see each other, or single tokens.  Sequence b
+ * has len[b] = L rows in the cache, the last n of which (appended before) are
+ * those of its n query rows.  Query row i sees row t < L iff t < L - n, or new
+ * row j = t - (L - n) is one that it sees: bit j % 32 of word j / 32 of its
+ * mask, or without masks every new row (causal: j <= i).  Query head a reads
+ * K/V head a / group.
+ *   O   = sum_t w_t v_t, w = softmax(scale q k_t) over those rows
+ *   lse = log sum_t exp(scale q k_t)
+ * A row that sees nothing has O = 0 and lse = -inf; rows it does not see may
+ * hold anything, NaN and infinities too.
+ * --------------------------------------------------------------------- */
+typedef struct wf_tree_params {
+    int32_t pages, page_rows, heads, head_dim; /* the pool: as above        */
+    int32_t dtype, format;
+    int32_t group;       /* query heads per K/V head, >= 1                  */
+    int32_t batch;       /* sequences, >= 1                                 */
+    int32_t tokens;      /* rows of Q and O, >= 1                           */
+    int32_t max_rows;    /* most query rows of a sequence: 1 .. WF_MAX_Q_LEN */
+    int32_t table_pages; /* entries of a sequence's table, >= 1             */
+    int32_t max_len;     /* most cache rows of a sequence: 0 .. table_pages
+                            page_rows (the nearer to the lengths, the better
+                            the split fits them)                            */
+    int32_t causal;      /* without masks: 0 or 1                           */
+    float scale;         /* as in wf_prefix_attn; 0 selects 1/sqrt(d)       */
+    int64_t q_row, o_row; /* elements from token to token, as in
+                            wf_page_append                                  */
+} wf_tree_params;
+
+/* Workspace bytes of the split of the cache into key ranges that wf_tree_attn
+ * takes when it can (0 if that needs none or the parameters are invalid).
+ * With fewer bytes it takes fewer ranges, one at least, which needs none. */
+size_t wf_tree_workspace_bytes(const wf_tree_params* p);
+
+/* How wf_tree_attn works with a workspace of that many bytes (for tests and
+ * measurements; the choice may change between builds). */
+wf_status wf_tree_plan(const wf_tree_params* p, size_t workspace_bytes,
+                       wf_prefix_split* split);
+
+/*
+ *   Q          [tokens][heads group][d] of q_row   dtype
+ *   table      [batch][table_pages]  int32: pages (those outside [0, pages)
+ *              are taken as the nearest inside); entries behind a sequence's
+ *              last row are not read
+ *   len        [batch]               int32: L
+ *   row_start  nullable [batch + 1]  int32: sequence b's query rows are tokens
+ *              row_start[b] .. row_start[b + 1] - 1; NULL: tokens b max_rows
+ *              on, max_rows each (tokens = batch max_rows)
+ *              (lengths and counts outside [0, max_len] and [0, max_rows] are
+ *              taken as the nearest one inside; tokens outside [0, tokens)
+ *              are left out)
+ *   mask       nullable [tokens][(max_rows + 31) / 32]  32-bit words
+ *   O          [tokens][heads group][d] of o_row   dtype out, apart from Q
+ *   lse        nullable [tokens][heads group]      fp32 out
+ *   workspace  wf_tree_workspace_bytes(p) bytes (fewer: see there), 256-byte
+ *              aligned
+ * Tokens of no sequence keep what their rows of O and lse held.
+ */
+wf_status wf_tree_attn(const wf_tree_params* p, const void* Q, const void* Kc,
+                       const void* Kx, const void* Vc, const void* Vx,
+                       const int32_t* table, const int32_t* len,
+                       const int32_t* row_start, const void* mask, void* O,
+                       float* lse, void* workspace, size_t workspace_bytes,
+                       void* stream);
+
 /* Loads the library's kernels onto the current device and sets up its
  * per-device state, so that no later call stalls for it (otherwise the
  * first call on a device loads what it launches, a few milliseconds of host

@@ -46,7 +46,8 @@ EXPORTED = ("wf_workspace_bytes", "wf_effective_budget", "wf_dwt_keys",
             "wf_filter_attend_recursive_kernel_name",
             "wf_cache_store", "wf_cache_load", "wf_prefix_workspace_bytes",
             "wf_prefix_plan", "wf_prefix_attn", "wf_rope", "wf_page_append",
-            "wf_page_move", "wf_init", "wf_status_str", "wf_last_error")
+            "wf_page_move", "wf_tree_workspace_bytes", "wf_tree_plan",
+            "wf_tree_attn", "wf_init", "wf_status_str", "wf_last_error")
 
 
 class WfParams(ctypes.Structure):
@@ -100,6 +101,13 @@ class WfMoveParams(ctypes.Structure):
         "batch", "table_pages", "moves")]
 
 
+class WfTreeParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in _POOL + (
+        "group", "batch", "tokens", "max_rows", "table_pages", "max_len",
+        "causal")] + [("scale", ctypes.c_float), ("q_row", ctypes.c_int64),
+                      ("o_row", ctypes.c_int64)]
+
+
 class WfError(RuntimeError):
     def __init__(self, status: int, message: str):
         self.status = status
@@ -118,7 +126,7 @@ def _load() -> ctypes.CDLL:
     fp, ip = ctypes.POINTER(ctypes.c_float), ctypes.POINTER(ctypes.c_int32)
     CP, PP = ctypes.POINTER(WfCacheParams), ctypes.POINTER(WfPrefixParams)
     RP, AP = ctypes.POINTER(WfRopeParams), ctypes.POINTER(WfAppendParams)
-    MP = ctypes.POINTER(WfMoveParams)
+    MP, TP = ctypes.POINTER(WfMoveParams), ctypes.POINTER(WfTreeParams)
     sig = {
         "wf_workspace_bytes": (sz, [P, i32]),
         "wf_effective_budget": (i32, [P]),
@@ -176,6 +184,11 @@ def _load() -> ctypes.CDLL:
         "wf_page_append": (ctypes.c_int, [AP, vp, vp, vp, vp, vp, vp, vp, vp,
                                           vp, vp, vp, vp]),
         "wf_page_move": (ctypes.c_int, [MP, vp, vp, vp, vp, vp, vp, vp, vp]),
+        "wf_tree_workspace_bytes": (sz, [TP]),
+        "wf_tree_plan": (ctypes.c_int, [TP, sz, ctypes.POINTER(WfPrefixSplit)]),
+        "wf_tree_attn": (ctypes.c_int,
+                         [TP, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp,
+                          sz, vp]),
         "wf_init": (ctypes.c_int, []),
         "wf_status_str": (ctypes.c_char_p, [ctypes.c_int]),
         "wf_last_error": (ctypes.c_char_p, []),
@@ -1057,6 +1070,85 @@ def wf_page_move(p, table, first, source, Kc, Kx, Vc, Vx, stream=None):
                ("source", source, i32, p.batch * p.moves, False),
                *_pool_entries(p, Kc, Kx, Vc, Vx)))
     _check(_lib.wf_page_move(p, *a, _stream(stream)))
+
+
+# A sequence's new rows (a tree of drafted tokens, a block, a single token) are
+# the last of its len rows in the cache; they see what lies before them, and
+# those new rows that their masks name.
+
+def make_tree_params(*, pages: int, page_rows: int, heads: int, head_dim: int,
+                     batch: int, max_rows: int, table_pages: int,
+                     tokens: int | None = None, max_len: int | None = None,
+                     group: int = 1, causal: bool = False,
+                     dtype: str | int = "bf16",
+                     format: str | int | None = None, scale: float = 0.0,
+                     q_row: int = 0, o_row: int = 0) -> WfTreeParams:
+    """tokens: rows of Q (batch * max_rows by default); max_len: most rows of a
+    sequence's cache (all of its table's by default; the nearer to the lengths,
+    the better the split)."""
+    return WfTreeParams(pages, page_rows, heads, head_dim,
+                        _DTYPES.get(dtype, dtype), _FORMATS.get(format, format),
+                        group, batch,
+                        batch * max_rows if tokens is None else tokens,
+                        max_rows, table_pages,
+                        table_pages * page_rows if max_len is None else max_len,
+                        int(causal), scale, q_row, o_row)
+
+
+def tree_workspace_bytes(p: WfTreeParams) -> int:
+    return int(_lib.wf_tree_workspace_bytes(p))
+
+
+def tree_plan(p: WfTreeParams, nbytes: int | None = None) -> WfPrefixSplit:
+    """How wf_tree_attn splits the cache with a workspace of nbytes (None: of
+    tree_workspace_bytes)."""
+    s = WfPrefixSplit()
+    _check(_lib.wf_tree_plan(
+        p, tree_workspace_bytes(p) if nbytes is None else nbytes,
+        ctypes.byref(s)))
+    return s
+
+
+def alloc_tree_workspace(p: WfTreeParams, device) -> torch.Tensor | None:
+    nb = tree_workspace_bytes(p)
+    return torch.empty(nb, dtype=torch.uint8, device=device) if nb else None
+
+
+def wf_tree_attn(p, Q, Kc, Kx, Vc, Vx, table, length, row_start, mask, O, lse,
+                 workspace, stream=None):
+    dt, i32, hq = torch_dtype(p), torch.int32, p.heads * p.group
+    shape = (p.tokens, hq, p.head_dim)
+    q = _rows_ptr("Q", Q, dt, shape, (p.q_row,))
+    o = _rows_ptr("O", O, dt, shape, (p.o_row,))
+    kc, kx, vc, vx, *a, l = _args((
+        *_pool_entries(p, Kc, Kx, Vc, Vx),
+        ("table", table, i32, p.batch * p.table_pages, False),
+        ("length", length, i32, p.batch, False),
+        ("row_start", row_start, i32, p.batch + 1, True),
+        ("mask", mask, i32, p.tokens * ((p.max_rows + 31) // 32), True),
+        ("lse", lse, torch.float32, p.tokens * hq, True)))
+    ws, nb = _ws(workspace)
+    _on_current([("Q", Q), ("O", O)] + [("workspace", workspace)] * bool(nb))
+    _check(_lib.wf_tree_attn(p, q, kc, kx, vc, vx, *a, o, l, ws, nb,
+                             _stream(stream)))
+
+
+def tree_attend(p: WfTreeParams, Q, pool, table, length, row_start=None,
+                mask=None, workspace=None, want_lse: bool = False, stream=None):
+    """Allocates O (and lse), zeros and -inf for tokens of no sequence, and
+    runs wf_tree_attn over a pool (Kc, Kx, Vc, Vx).  Returns O, or (O, lse)
+    when want_lse.  What it allocates belongs to the stream the kernels run
+    on."""
+    with torch.cuda.stream(_torch_stream(stream)):
+        rows = (p.tokens, p.heads * p.group)
+        O = torch.zeros(rows + (p.head_dim,), dtype=Q.dtype, device=Q.device)
+        lse = (torch.full(rows, float("-inf"), device=Q.device)
+               if want_lse else None)
+        if workspace is None:
+            workspace = alloc_tree_workspace(p, Q.device)
+    wf_tree_attn(p, Q, *pool, table, length, row_start, mask, O, lse, workspace,
+                 stream)
+    return (O, lse) if want_lse else O
 
 
 # ------------------------------------------------------------ allocation

@@ -1056,6 +1056,80 @@ static wf_status move_impl(const wf_move_params* p, const int32_t* table, const 
   return ok();
 }
 
+static wf_status check_tree(const wf_tree_params* p, size_t have, TreePlan* plan) {
+  WF_TRY(check_pool(p));
+  if (p->group < 1 || p->batch < 1 || p->tokens < 1 || p->table_pages < 1 || p->max_rows < 1)
+    return fail(WF_ERR_INVALID_ARG,
+                "group (%d), batch (%d), tokens (%d), table_pages (%d) and max_rows (%d) must be "
+                ">= 1",
+                p->group, p->batch, p->tokens, p->table_pages, p->max_rows);
+  if (p->max_rows > WF_MAX_Q_LEN)
+    return fail(WF_ERR_UNSUPPORTED, "max_rows %d exceeds %d", p->max_rows, (int)WF_MAX_Q_LEN);
+  if (p->max_len < 0 || p->max_len > (long)p->table_pages * p->page_rows)
+    return fail(WF_ERR_INVALID_ARG, "max_len %d outside [0, %ld], the rows of a table", p->max_len,
+                (long)p->table_pages * p->page_rows);
+  if (p->causal != 0 && p->causal != 1)
+    return fail(WF_ERR_INVALID_ARG, "causal %d is neither 0 nor 1", p->causal);
+  // as for the prefix: an infinite factor would make a score of 0 NaN
+  if (!std::isfinite(p->scale * 1.44269504f))
+    return fail(WF_ERR_INVALID_ARG, "scale times log2(e) is not finite in fp32");
+  if (p->max_len > (1 << 30)) return fail(WF_ERR_UNSUPPORTED, "more than 2^30 rows");
+  // every product below stays in 64 bits: each factor is held to 2^31 in turn
+  const long hq = (long)p->heads * p->group;
+  if (hq > (1L << 20) || (long)p->tokens * hq > (1L << 30) ||
+      (long)p->batch * p->max_rows * hq > (1L << 30))
+    return fail(WF_ERR_UNSUPPORTED, "more than 2^20 query heads or 2^30 query rows in one call");
+  const int unit = p->dtype == WF_BF16 ? 8 : 4;
+  if (p->q_row) WF_TRY(check_stride("q_row", p->q_row, hq * p->head_dim, unit));
+  if (p->o_row) WF_TRY(check_stride("o_row", p->o_row, hq * p->head_dim, unit));
+  *plan = plan_tree(*p, have);
+  // a launch has fewer than 2^32 threads
+  if ((plan->items + 7) * 64 * plan->nw > UINT32_MAX || plan->merges * kBlock > UINT32_MAX)
+    return fail(WF_ERR_UNSUPPORTED, "too many workgroups in one call");
+  return WF_OK;
+}
+
+static wf_status tree_impl(const wf_tree_params* p, const void* Q, const void* Kc, const void* Kx,
+                           const void* Vc, const void* Vx, const int32_t* table,
+                           const int32_t* len, const int32_t* row_start, const void* mask, void* O,
+                           float* lse, void* ws, size_t ws_bytes, void* stream) {
+  TreePlan plan;
+  WF_TRY(check_tree(p, ws ? ws_bytes : 0, &plan));
+  if (!row_start && p->tokens != (long)p->batch * p->max_rows)
+    return fail(WF_ERR_INVALID_ARG, "tokens %d are not batch * max_rows = %ld, without row_start",
+                p->tokens, (long)p->batch * p->max_rows);
+  WF_TRY(check_ptr(Q, "Q", false));
+  WF_TRY(check_pool_ptrs(p, Kc, Kx, Vc, Vx));
+  WF_TRY(check_words(table, "table", false));
+  WF_TRY(check_words(len, "len", false));
+  WF_TRY(check_words(row_start, "row_start", true));
+  WF_TRY(check_words(mask, "mask", true));
+  WF_TRY(check_ptr(O, "O", false));
+  WF_TRY(check_words(lse, "lse", true));
+  if (Q == O) return fail(WF_ERR_INVALID_ARG, "O is Q");
+  WF_TRY(check_workspace(ws, ws_bytes, plan.part_bytes + plan.pstat_bytes));
+  TreeArgs a{};
+  a.Q = Q;
+  a.K = Kc;
+  a.V = Vc;
+  a.Kx = static_cast<const uint8_t*>(Kx);
+  a.Vx = static_cast<const uint8_t*>(Vx);
+  a.table = table;
+  a.len = len;
+  a.start = row_start;
+  a.mask = static_cast<const uint32_t*>(mask);
+  a.O = O;
+  a.lse = lse;
+  a.part = static_cast<float*>(ws);
+  a.pstat = ws ? reinterpret_cast<float*>(at(ws, plan.part_bytes)) : nullptr;
+  const long row = (long)p->heads * p->group * p->head_dim;
+  a.qs = p->q_row ? p->q_row : row;
+  a.os = p->o_row ? p->o_row : row;
+  (void)hipGetLastError();
+  WF_HIP(launch_tree(*p, plan, a, static_cast<hipStream_t>(stream)), "tree_attn");
+  return ok();
+}
+
 // ------------------------------------------------------------ shared prefix
 
 static wf_status check_prefix(const wf_prefix_params* p, size_t have, PrefixPlan* plan) {
@@ -1448,6 +1522,29 @@ wf_status wf_page_move(const wf_move_params* p, const int32_t* table, const int3
   return move_impl(p, table, first, source, Kc, Kx, Vc, Vx, stream);
 }
 
+size_t wf_tree_workspace_bytes(const wf_tree_params* p) {
+  TreePlan plan;
+  if (check_tree(p, SIZE_MAX, &plan) != WF_OK) return 0;
+  return plan.part_bytes + plan.pstat_bytes;
+}
+
+wf_status wf_tree_plan(const wf_tree_params* p, size_t workspace_bytes, wf_prefix_split* split) {
+  TreePlan plan;
+  WF_TRY(check_tree(p, workspace_bytes, &plan));
+  if (!split) return fail(WF_ERR_INVALID_ARG, "split is NULL");
+  *split = wf_prefix_split{plan.splits, plan.rps, plan.nw / plan.kw * 32 * plan.qw, 32 * plan.qw,
+                           plan.kw};
+  return ok();
+}
+
+wf_status wf_tree_attn(const wf_tree_params* p, const void* Q, const void* Kc, const void* Kx,
+                       const void* Vc, const void* Vx, const int32_t* table, const int32_t* len,
+                       const int32_t* row_start, const void* mask, void* O, float* lse,
+                       void* workspace, size_t workspace_bytes, void* stream) {
+  return tree_impl(p, Q, Kc, Kx, Vc, Vx, table, len, row_start, mask, O, lse, workspace,
+                   workspace_bytes, stream);
+}
+
 size_t wf_prefix_workspace_bytes(const wf_prefix_params* p) {
   PrefixPlan plan;
   if (check_prefix(p, SIZE_MAX, &plan) != WF_OK) return 0;
@@ -1484,6 +1581,7 @@ wf_status wf_init(void) {
   WF_HIP(load_cache_kernels(), "loading the cache kernels");
   WF_HIP(load_prefix_kernels(), "loading the prefix-attention kernels");
   WF_HIP(load_page_kernels(), "loading the kernels of a cache in pages");
+  WF_HIP(load_tree_kernels(), "loading the attention over a cache in pages");
   void* scratch_ptr = nullptr;  // this file's code object and its scratch array
   WF_TRY(scratch_of_current_device(&scratch_ptr));
   return ok();

@@ -299,4 +299,32 @@ struct PrefixArgs {
   float scale;
 };
 
+struct TreeArgs {
+  const void* Q;         // [tokens][hq][D]
+  const void* K;         // [pages][heads][page rows][D], or codes
+  const void* V;
+  const uint8_t* Kx;     // exponent bytes (quantised)
+  const uint8_t* Vx;
+  const int32_t* table;  // [batch][tp]
+  const int32_t* len;    // [batch]
+  const int32_t* start;  // nullable [batch + 1]
+  const uint32_t* mask;  // nullable [tokens][words]
+  void* O;               // [tokens][hq][D]
+  float* lse;            // nullable [tokens][hq]
+  float* part;           // [tokens][hq][splits][D] unnormalised partial outputs
+  float* pstat;          // [tokens][hq][splits][2] reference (log2 units), sum
+  long qs, os;           // elements from token to token
+  int items;             // workgroups: units x ranges x blocks of query rows
+  int splits, rps;       // key ranges per unit at most, keys of a range (whole tiles)
+  int mblocks, mrows;    // blocks per unit, query rows of a block
+  int kw;                // waves that take the keys of a tile in turn
+  int batch, heads, g, hq;
+  FastDiv by_g;
+  int pages, shift, tp;  // log2 of a page's rows
+  int tokens, max_rows, max_len, words;
+  int causal;
+  int whole;             // the kernel writes O itself
+  float scale;
+};
+
 }  // namespace wf

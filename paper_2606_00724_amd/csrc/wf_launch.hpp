@@ -345,4 +345,17 @@ hipError_t launch_prefix(const wf_prefix_params& p, const PrefixPlan& plan, Pref
                          hipStream_t s);
 hipError_t load_prefix_kernels();
 
+// Attention of new rows over a cache in pages: its split, and the launches.
+struct TreeArgs;
+struct TreePlan {
+  long items;                      // workgroups
+  int splits, rps, mblocks, nw, kw, qw;
+  long merges;                     // workgroups of the merge (0: none)
+  size_t lds_bytes;
+  size_t part_bytes, pstat_bytes;  // workspace (0: no partials)
+};
+TreePlan plan_tree(const wf_tree_params& p, size_t have);  // have: workspace bytes
+hipError_t launch_tree(const wf_tree_params& p, const TreePlan& plan, TreeArgs& a, hipStream_t s);
+hipError_t load_tree_kernels();
+
 }  // namespace wf

@@ -146,9 +146,15 @@ struct PrefixWave {
     }
   }
 
-  // 32 keys at LDS offsets kat, vat, the first nv of which are valid
-  __device__ __forceinline__ void step(uint32_t kat, uint32_t vat, int nv) {
+  // 32 keys at LDS offsets kat, vat, the first nv of which are valid; or MASK: those
+  // whose bits are set in the word of the lane's query row (for each block of rows)
+  template <bool MASK = false>
+  __device__ __forceinline__ void step(uint32_t kat, uint32_t vat, int nv,
+                                       const uint32_t* words = nullptr) {
     const int h = (threadIdx.x & 63) >> 5;
+    uint32_t seen[QW];  // the lane's keys: bits 8 (i / 4) + i % 4
+#pragma unroll
+    for (int b = 0; b < QW; ++b) seen[b] = MASK ? words[b] >> (4 * h) : 0u;
     u32x4 kf[QS];
     f32x16 s[QW];
     keys(kat, kf);
@@ -161,7 +167,11 @@ struct PrefixWave {
     float mx[QW];
     auto shifted = [&](int b) __attribute__((always_inline)) {
       shift_one(b, s[b], t[b]);
-      if (nv < 32) {
+      if constexpr (MASK) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          t[b][i] = seen[b] >> (8 * (i >> 2) + (i & 3)) & 1 ? t[b][i] : -INFINITY;
+      } else if (nv < 32) {
 #pragma unroll
         for (int i = 0; i < 16; ++i)
           t[b][i] = 8 * (i >> 2) + 4 * h + (i & 3) >= nv ? -INFINITY : t[b][i];
@@ -189,8 +199,11 @@ struct PrefixWave {
           else
             t[b] = s[b];
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
-            t[b][i] = 8 * (i >> 2) + 4 * h + (i & 3) >= n ? -c2 * INFINITY : t[b][i];
+          for (int i = 0; i < 16; ++i) {
+            const bool hidden = MASK ? !(seen[b] >> (8 * (i >> 2) + (i & 3)) & 1)
+                                     : 8 * (i >> 2) + 4 * h + (i & 3) >= n;
+            t[b][i] = hidden ? -c2 * INFINITY : t[b][i];
+          }
           anew(b, t[b], mn, al);
         });
 #pragma unroll

@@ -92,3 +92,94 @@ def move(pool, table, first, source, page_rows):
                 if o is not None:
                     o[to[0], :, to[1]] = x[of[0], :, of[1]]
     return out
+
+
+# ------------------------------------------------------------ attention
+
+def cached_rows(pool, table, b, head, L, page_rows, fmt):
+    """K and V rows 0 .. L - 1 of a sequence's head in float64."""
+    pages = pool[0].shape[0]
+    out = []
+    if L == 0:
+        return [torch.zeros((0, 1), dtype=torch.float64)] * 2
+    for c, x in ((pool[0], pool[1]), (pool[2], pool[3])):
+        at = table[b, :-(-L // page_rows)].long().clamp(0, pages - 1)
+        rows = c[at, head].flatten(0, 1)[:L]
+        if fmt is not None:
+            rows = cacheref.values(rows, x[at, head].flatten(0, 1)[:L], fmt)
+        out.append(rows.double())
+    return out
+
+
+def sees(i, n, L, mask=None, causal=False):
+    """Which of L rows query row i of n sees; mask: its words."""
+    t = torch.arange(L)
+    j = t - (L - n)
+    if mask is not None:
+        word = mask.long()[(j.clamp(min=0) // 32).clamp(max=len(mask) - 1)] & 0xffffffff
+        new = (word >> (j.clamp(min=0) % 32)) & 1 == 1
+    else:
+        new = j <= i if causal else torch.ones(L, dtype=torch.bool)
+    return (j < 0) | new
+
+
+def tree_attention(Q, pool, table, length, start, mask, *, page_rows, heads, group, max_rows,
+                   max_len, scale, causal=False, fmt=None):
+    """O, lse in float64 and how far the kernel may be off, elementwise (as in
+    cacheref.prefix_attention, whose tolerances are derived there), for the
+    tokens of a sequence; the others keep NaN.  A row's hidden keys take no
+    part, whatever they hold.  One more term: a weight below 2^-126 of the
+    largest one, or a product of it below 2^-126, may be taken as 0 (the fp32
+    range; the largest weight is 1 at least), which moves an output by up to
+    2^-126 (1 + max |v|) for each of n keys."""
+    tokens, hq, d = Q.shape
+    bf = Q.dtype == torch.bfloat16
+    half = 2.0 ** -8 if bf else 2.0 ** -24
+    O = torch.full((tokens, hq, d), float("nan"), dtype=torch.float64)
+    lse = torch.full((tokens, hq), float("nan"), dtype=torch.float64)
+    tol, ltol = torch.zeros_like(O), torch.zeros_like(lse)
+    for b in range(len(length)):
+        L = min(max(int(length[b]), 0), max_len)
+        first = b * max_rows if start is None else int(start[b])
+        n = max_rows if start is None else min(max(int(start[b + 1]) - first, 0), max_rows)
+        for h in range(heads):
+            K, V = cached_rows(pool, table, b, h, L, page_rows, fmt)
+            for i in range(n):
+                at = first + i
+                if not 0 <= at < tokens:
+                    continue
+                s = sees(i, n, L, None if mask is None else mask[at], causal)
+                k, v = K[s], V[s]
+                x = slice(h * group, (h + 1) * group)
+                if len(k) == 0:
+                    O[at, x], lse[at, x] = 0.0, -np.inf
+                    continue
+                q = Q[at, x].double()
+                sc = scale * q @ k.T.contiguous()
+                mag = (abs(scale) * q.abs() @ k.abs().T.contiguous()).amax(-1)
+                w = torch.softmax(sc, -1)
+                O[at, x], lse[at, x] = w @ v, torch.logsumexp(sc, -1)
+                A = w @ v.abs()
+                es = ((2 * d + 4) * mag + 4) * 2.0 ** -24
+                sums = (len(k) + 8) * 2.0 ** -24
+                tol[at, x] = A * (2 * es + 2 * sums + (half if bf else 0))[:, None] \
+                    + half * 1.01 * O[at, x].abs() \
+                    + len(k) * 2.0 ** -126 * (1 + v.abs().amax(0))
+                ltol[at, x] = es + sums + 2.0 ** -22 * (1 + lse[at, x].abs())
+    return O, lse, tol, ltol
+
+
+def ancestors(n, seed):
+    """Masks [n, words] of a random tree: a row sees itself and its ancestors."""
+    g = torch.Generator().manual_seed(seed)
+    seen = torch.zeros((n, -(-n // 32) * 32), dtype=torch.bool)
+    for i in range(n):
+        if i:
+            seen[i] = seen[int(torch.randint(0, i, (1,), generator=g))]
+        seen[i, i] = True
+    return words(seen)
+
+
+def words(seen):
+    w = (seen.unflatten(-1, (-1, 32)).long() << torch.arange(32)).sum(-1)
+    return torch.where(w >= 1 << 31, w - (1 << 32), w).int()

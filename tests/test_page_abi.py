@@ -171,3 +171,97 @@ def test_binding_refuses_what_the_parameters_do_not_describe():
                     Vx=None), **bad}
         with pytest.raises(ValueError):
             wf.wf_page_move(m, *a.values())
+
+
+# ------------------------------------------------------------ attention
+
+def tree_params(**kw):
+    return wf.make_tree_params(**{**dict(pages=4, page_rows=16, heads=2, head_dim=64, batch=2,
+                                         max_rows=3, table_pages=2, group=2), **kw})
+
+
+@pytest.mark.parametrize("change,code", POOL + [
+    (dict(group=0), 1), (dict(batch=0), 1), (dict(tokens=0), 1), (dict(table_pages=0), 1),
+    (dict(max_rows=0), 1), (dict(max_rows=257), 2), (dict(max_len=-1), 1), (dict(max_len=33), 1),
+    (dict(scale=float("nan")), 1), (dict(scale=float("-inf")), 1), (dict(scale=3e38), 1),
+    (dict(group=1 << 20), 2), (dict(batch=1 << 22, max_rows=128), 2), (dict(q_row=192), 1),
+    (dict(o_row=252), 1), (dict(o_row=260), 1),
+    (dict(batch=1 << 20, heads=1 << 8, max_rows=1, group=1, head_dim=128), 2),
+])
+def test_tree_parameters(change, code):
+    p = tree_params(**change)
+    args = [GOOD] * 9 + [ctypes.c_void_p(0x20000), GOOD, GOOD, 1 << 50]
+    lib = wf.library()
+    assert lib.wf_tree_attn(ctypes.byref(p), *args, None) == code, lib.wf_last_error()
+    assert lib.wf_last_error().decode()
+    assert wf.tree_workspace_bytes(p) == 0
+    with pytest.raises(wf.WfError):
+        wf.tree_plan(p, 0)
+
+
+def test_tree_pointers_and_workspace():
+    #       Q  Kc Kx Vc Vx table len start mask O lse
+    lib, nullable, words = wf.library(), {7, 8, 10}, {5, 6, 7, 8, 10}
+    p = tree_params(format="e4m3", page_rows=1024, table_pages=8)
+    need = wf.tree_workspace_bytes(p)
+    assert need > 0
+    args = [GOOD] * 9 + [ctypes.c_void_p(0x20000), GOOD, GOOD, need]
+    for i in range(11):
+        for bad in (None, ctypes.c_void_p(0x10002) if i in words else ODD):
+            if bad is None and i in nullable:
+                continue
+            a = list(args)
+            a[i] = bad
+            assert lib.wf_tree_attn(ctypes.byref(p), *a, None) == 1, i
+    assert lib.wf_tree_attn(ctypes.byref(p), *args[:9], GOOD, *args[10:], None) == 1  # O is Q
+    assert lib.wf_tree_attn(ctypes.byref(p), *args[:11], ctypes.c_void_p(0x10010), need, None) == 3
+    assert lib.wf_tree_attn(None, *args, None) == 1
+    p.causal = 2
+    assert lib.wf_tree_attn(ctypes.byref(p), *args, None) == 1
+    p = tree_params(tokens=5)
+    a = list(args)
+    a[7] = None
+    assert lib.wf_tree_attn(ctypes.byref(p), *a, None) == 1  # tokens need row_start
+    assert lib.wf_tree_plan(ctypes.byref(tree_params()), 0, None) == 1
+
+
+def test_tree_workspaces_hold_whole_partials():
+    import random
+    rng = random.Random(5)
+    for _ in range(300):
+        P = rng.choice([16, 64, 1024])
+        p = tree_params(page_rows=P, table_pages=rng.choice([1, 7, 300, 2048]),
+                        pages=1 << 16 if P < 1024 else 4096, heads=rng.choice([1, 3, 8, 32]),
+                        group=rng.choice([1, 4, 7]), batch=rng.choice([1, 3, 64, 300]),
+                        max_rows=rng.choice([1, 5, 32, 256]), head_dim=rng.choice([64, 128]),
+                        dtype=rng.choice(["bf16", "f32"]),
+                        format=rng.choice([None, "e4m3", "e2m1"]))
+        nb, rows = wf.tree_workspace_bytes(p), p.tokens * p.heads * p.group
+        s = wf.tree_plan(p)
+        assert nb == (rows * s.ranges * (p.head_dim + 2) * 4 if s.ranges > 1 else 0)
+        assert s.ranges * s.range_rows >= p.max_len > (s.ranges - 1) * s.range_rows
+        assert s.range_rows % 64 == 0
+        for have in (0, nb // 2, nb):
+            t = wf.tree_plan(p, have)
+            assert t.ranges == 1 or rows * t.ranges * (p.head_dim + 2) * 4 <= have
+        # a cache without rows
+        p.max_len = 0
+        assert wf.tree_workspace_bytes(p) == 0 and wf.tree_plan(p).ranges == 1
+
+
+def test_tree_binding_refuses_what_the_parameters_do_not_describe():
+    p = tree_params()
+    Kc, _, Vc, _ = wf.alloc_pages(p, "cpu")
+    Q = torch.zeros((6, 4, 64)).bfloat16()
+    i32 = torch.zeros(64).int()
+    ok = dict(Q=Q, Kc=Kc, Kx=None, Vc=Vc, Vx=None, table=i32[:4], length=i32[:2], row_start=None,
+              mask=None, O=Q.clone(), lse=None, workspace=None)
+    for bad, err in ((dict(Q=Q.float()), TypeError), (dict(O=Q[:5]), ValueError),
+                     (dict(Q=torch.zeros((6, 5, 64)).bfloat16()[:, 1:]), ValueError),
+                     (dict(Kc=Kc[:3]), ValueError), (dict(Vc=Vc.float()), TypeError),
+                     (dict(table=i32[:3]), ValueError), (dict(length=None), ValueError),
+                     (dict(row_start=i32[:2]), ValueError), (dict(mask=i32[:12]), ValueError),
+                     (dict(mask=i32[:6].long()), TypeError), (dict(lse=i32[:24]), TypeError),
+                     (dict(), ValueError)):
+        with pytest.raises(err):
+            wf.wf_tree_attn(p, *{**ok, **bad}.values())
