@@ -37,7 +37,8 @@ HIPCC_FLAGS = [
 # warning left out says at each of its tile loads that m0 is a reserved register
 # (tests/test_build_m0.py holds that the compiler does not use it there).
 _PRODUCTS = ["-mllvm", "-amdgpu-mfma-vgpr-form=1", "-Wno-inline-asm"]
-EXTRA_FLAGS = {"wf_prefix.hip": _PRODUCTS, "wf_tree.hip": _PRODUCTS}
+EXTRA_FLAGS = {"wf_prefix.hip": _PRODUCTS, "wf_tree.hip": _PRODUCTS,
+               "wf_tree_few.hip": _PRODUCTS}
 
 
 def hipcc() -> str:

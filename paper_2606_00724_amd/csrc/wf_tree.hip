@@ -9,28 +9,13 @@
 // sixteen rows of a tile lie in one page, whose number it takes from a part of the
 // table in LDS, and the last tiles, which hold keys that some of the new rows do
 // not see, are masked by a word of bits for each query row and 32 keys.
-#include "wf_tiles.hpp"
+#include "wf_tree.hpp"
 #include "wf_launch.hpp"
 
 namespace wf {
 
 constexpr int kPageKeys = 32768;                 // keys whose pages are in LDS at once
 constexpr int kPageIds = kPageKeys / 16 + 1;     // (pages of 16 rows at least)
-
-// A sequence: its rows in the cache, its query rows, and what hides keys from them.
-struct Sequence {
-  int L, n, base;  // keys, query rows, first key that is not seen by all
-  long first;      // token of query row 0
-  __device__ __forceinline__ Sequence(const TreeArgs& a, int b) {
-    L = min(max(a.len[b], 0), a.max_len);
-    first = a.start ? a.start[b] : (long)b * a.max_rows;
-    n = a.start ? (int)min(max((long)a.start[b + 1] - first, 0L), (long)a.max_rows) : a.max_rows;
-    base = L - n;
-  }
-  __device__ __forceinline__ static bool there(const TreeArgs& a, long token) {
-    return token >= 0 && token < a.tokens;
-  }
-};
 
 // The pages of a range's keys, kPageKeys of them at once.
 struct PageIds {
@@ -397,22 +382,10 @@ __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void tree_attn_kerne
         lds_barrier();
       }
       blocks([&](int key, uint32_t at, int nv) {
-        const int j0 = key - s.base;  // the first key as a new row (below 0: seen by all)
         uint32_t seen[QW];
 #pragma unroll
-        for (int b = 0; b < QW; ++b) {
-          if (a.mask) {
-            const uint32_t* words = masks + (row[b] - i0) * a.words;
-            auto word = [&](int i) { return i < 0 ? ~0u : i < a.words ? words[i] : 0u; };
-            seen[b] = (uint32_t)((((uint64_t)word((j0 >> 5) + 1) << 32) | word(j0 >> 5)) >> (j0 & 31));
-          } else if (a.causal) {
-            const int c = row[b] - j0;
-            seen[b] = c < 0 ? 0u : c >= 31 ? ~0u : (2u << c) - 1u;
-          } else {
-            seen[b] = ~0u;
-          }
-          if (nv < 32) seen[b] &= (1u << nv) - 1u;
-        }
+        for (int b = 0; b < QW; ++b)
+          seen[b] = seen_keys(a, s, row[b], masks + (row[b] - i0) * a.words, key, nv);
         w.template step<true>(at, at + MB, nv, seen);
         if (odd) {  // (rare: from memory again)
           for (int j = 0; j < nv; ++j) {
@@ -545,6 +518,7 @@ TreePlan plan_tree(const wf_tree_params& p, size_t have) {
   const double row_bytes = quant ? D * (p.format == WF_CACHE_E4M3 ? 1.0 : 0.5) + D / 32
                                  : D * (bf ? 2.0 : 4.0);
   const double partial = (double)rows * D * 8 / 5e6;
+  const bool few = bf && quant && M <= 32;
   const long most = (long)std::min<size_t>(have / (rows * (D + 2) * sizeof(float)), 1L << 30);
   double least = 0;
   auto consider = [&](int qw, int qwaves, double block, double fixed) {
@@ -570,7 +544,23 @@ TreePlan plan_tree(const wf_tree_params& p, size_t have) {
     ranges(std::min(one, tiles));
     ranges(std::min(2 * one, tiles));
   };
-  for (int qwaves = 2; qwaves <= l.nw && (qwaves == 2 || 16 * qwaves < M); qwaves *= 2)
+  if (few) {
+    l.few = true;
+    l.qw = l.mblocks = 1;
+    l.nw = l.kw = 4;
+    for (long n = 1; n <= tiles; n += 1 + n / 16) {
+      const long per = (tiles + n - 1) / n, s = (tiles + per - 1) / per;
+      if (s > 1 && s > most) break;
+      const double groups = (double)(U * s), at_once = std::min(groups, 2.0 * cus);
+      const double bytes = 2 * KT * row_bytes * std::max(at_once / 6e6, 1 / 20e3);
+      const double cost = std::ceil(groups / (2 * cus)) * (per * std::max(bytes, 0.7) + 5.0) +
+                          (s > 1 ? s * partial + 3.0 : 0.0);
+      if (least != 0 && cost >= least) continue;
+      least = cost;
+      l.rps = (int)(per * KT);
+    }
+  }
+  for (int qwaves = 2; !few && qwaves <= l.nw && (qwaves == 2 || 16 * qwaves < M); qwaves *= 2)
     if (!bf)
       consider(1, qwaves, 4.2, quant ? 0.4 : 0.1);
     else if (quant)
@@ -631,7 +621,9 @@ hipError_t launch_tree(const wf_tree_params& p, const TreePlan& l, TreeArgs& a, 
       return hipGetLastError();
     };
     hipError_t e = hipErrorInvalidValue;
-    if (p.format == WF_CACHE_E4M3)
+    if (l.few)
+      e = launch_tree_few(a, D, p.format, l.items, s);
+    else if (p.format == WF_CACHE_E4M3)
       e = go(tree_attn_kernel<T, D, WF_CACHE_E4M3, 1>);
     else if (p.format == WF_CACHE_E2M1)
       e = go(tree_attn_kernel<T, D, WF_CACHE_E2M1, 1>);

@@ -1,0 +1,452 @@
+// Attention of few query rows (32 of a sequence's K/V head at most) over the codes
+// of a cache in pages: bound by the cache's bytes.
+//
+// Each wave has keys, and a ring of blocks of 32 of them, of its own: it loads
+// their codes straight to LDS, waits for them by the count of its loads and meets
+// the workgroup's other waves only when its last block is done.  K's codes are
+// read row by row and decoded with the row's scale into the operand of S^T = K Q^T
+// (which channels make up one step of that product is free: here a lane has
+// consecutive ones of its row).  V's codes are read transposed, by the LDS loads
+// made for operands of 8 and 4 bits, and decoded without their scales; these, one
+// for each key and 32 channels, are put to the weights instead, which are the
+// other operand of O^T = V^T P^T for those 32 channels.
+#include "wf_tree.hpp"
+#include "wf_launch.hpp"
+
+namespace wf {
+
+constexpr int kFewWaves = 4;
+
+typedef int v2i_few __attribute__((ext_vector_type(2)));
+
+// A wave's ring.  Rows of a block stand after each other, their 16-byte chunks in an
+// order that lets eight rows at one chunk meet all banks.
+template <int D, int FMT>
+struct FewGeom {
+  static constexpr int RB = FMT == WF_CACHE_E4M3 ? D : D / 2;  // bytes of a row
+  static constexpr int C = RB / 16;                            // chunks of a row
+  static constexpr int KB = 32 * RB;                           // bytes of 32 rows
+  static constexpr int NI = KB / 1024;                         // loads of 32 rows
+  static constexpr int XB = D / 32;                            // exponent bytes of a row
+  static constexpr int R = KB >= 4096 ? 2 : 4;                 // blocks of the ring
+  static constexpr int XR = R + 1;  // a block's exponents outlive its keys
+  static constexpr int WAVE = R * 2 * KB + XR * 256;           // bytes of a wave
+  static constexpr int BI = 2 * NI + 1;                        // loads of a block
+  // place of row r's chunk c
+  __device__ __forceinline__ static constexpr int swz(int r) {
+    return C == 8 ? r & 7 : C == 4 ? (r >> 1) & 3 : (r >> 2) & 1;
+  }
+  __device__ __forceinline__ static int at(int r, int c) { return r * RB + 16 * (c ^ swz(r)); }
+};
+
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+// 4 bytes per lane straight to LDS (lane l's at `lds` + 4 l); m0 as in tile_load.
+__device__ __forceinline__ void word_load(const void* g, uint32_t lds) {
+  asm volatile(
+      "s_mov_b32 m0, %1\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dword %0, off"
+      :
+      : "v"(g), "s"(lds)
+      : "memory", "m0");
+}
+template <typename V>
+__device__ __forceinline__ V lds_read(uint32_t at) {
+  return *(const __attribute__((address_space(3))) V*)(size_t)at;
+}
+
+template <int D, int FMT>
+__global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(TreeArgs a) {
+  using G = FewGeom<D, FMT>;
+  using W = PrefixWave<bf16_t, D, 1>;
+  constexpr int NI = G::NI, R = G::R, RB = G::RB, KB = G::KB, XB = G::XB, DT = D / 32;
+  extern __shared__ __align__(16) unsigned char smem[];  // the waves' rings
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h = lane >> 5, l32 = lane & 31;
+
+  const int item = xcd_swizzle(blockIdx.x, gridDim.x);
+  if (item >= a.items) return;  // (the grid holds whole eights of them)
+  const int sp = item % a.splits, unit = item / a.splits;
+  const int head = unit % a.heads, seq = unit / a.heads;
+  const Sequence s(a, seq);
+  const int M = s.n * a.g;
+  const int k0 = sp * a.rps, nk = min(a.rps, s.L - k0);  // the range's keys
+  if (M <= 0 || (nk <= 0 && !a.whole)) return;
+  W w;
+  w.init(a.scale);
+
+  // the wave's blocks: wave, wave + 4, ... of the range
+  const int nb = nk > 0 ? (nk + 31) / 32 : 0;
+  const int mine = nb > wave ? (nb - wave + kFewWaves - 1) / kFewWaves : 0;
+  if (mine > 0) {
+    const int kend = k0 + nk, last = (s.L - 1) >> a.shift;
+    auto key_of = [&](int i) { return k0 + 32 * (wave + kFewWaves * i); };
+    // (a scalar load: uniform, and no kernel that runs beside this writes tables)
+    const __attribute__((address_space(4))) int32_t* table =
+        (const __attribute__((address_space(4))) int32_t*)(a.table + (long)seq * a.tp);
+    // row of the pool of key k, the first of sixteen (past the last: any that is there)
+    auto pool_row = [&](int k) -> long {
+      const int page = min(max(table[min(k >> a.shift, last)], 0), a.pages - 1);
+      return (((long)page * a.heads + head) << a.shift) + (k & ((1 << a.shift) - 1));
+    };
+    const uint32_t ring = lds_offset(smem) + wave * G::WAVE, exps = ring + R * 2 * KB;
+    // the lane's 16 bytes of a load: row of those that it holds, chunk
+    const int lrow = lane / G::C;
+    const uint32_t off = lrow * RB + 16 * (lane % G::C ^ G::swz(lrow));
+    // the lane's 4 bytes of the exponents: K's of the 32 rows, then V's (again in the
+    // lanes behind them)
+    constexpr int XD = 8 * XB;
+    const int xl = lane % (2 * XD), xg = xl % XD / (XD / 2);
+    const uint8_t* xbase = (xl / XD ? a.Vx : a.Kx) + 4 * (xl % (XD / 2));
+    // block i's loads: 32 rows of K or V from r0 and r1 on
+    auto load = [&](const void* P, long r0, long r1, uint32_t lds) __attribute__((always_inline)) {
+      const unsigned char* b0 = static_cast<const unsigned char*>(P) + r0 * RB;
+      const unsigned char* b1 = static_cast<const unsigned char*>(P) + r1 * RB;
+      if constexpr (G::C == 8) {
+        tile_load<0, 0>(b0, off, lds);
+        tile_load<1024, 1024>(b0, off, lds);
+        tile_load<0, 2048>(b1, off, lds);
+        tile_load<1024, 3072>(b1, off, lds);
+      } else if constexpr (G::C == 4) {
+        tile_load<0, 0>(b0, off, lds);
+        tile_load<0, 1024>(b1, off, lds);
+      } else {
+        row_load<0>((lane < 32 ? b0 : b1 - 16 * RB) + off, lds);
+      }
+    };
+    auto exp_load = [&](long r0, long r1, uint32_t lds) __attribute__((always_inline)) {
+      word_load(xbase + (xg ? r1 : r0) * XB, lds);
+    };
+    // the exponents' slot of the block that is next to be loaded, and of this one
+    int xin = 0, xout = 0;
+    auto next = [&](int x) { return x + 1 == G::XR ? 0 : x + 1; };
+    auto queue_keys = [&](int i, long r0, long r1) __attribute__((always_inline)) {
+      load(a.K, r0, r1, ring + i % R * 2 * KB);
+      exp_load(r0, r1, exps + xin * 256);
+      xin = next(xin);
+    };
+    auto queue_vals = [&](int i, long r0, long r1) __attribute__((always_inline)) {
+      load(a.V, r0, r1, ring + i % R * 2 * KB + KB);
+    };
+
+    {
+      const long r0 = pool_row(key_of(0)), r1 = pool_row(key_of(0) + 16);
+      queue_keys(0, r0, r1);
+      queue_vals(0, r0, r1);
+    }
+    // the lane's query row: channels h D / 2 + 8 j of step j
+    const int m = min(l32, M - 1), ti = a.by_g(m);
+    const long tok = min(max(s.first + ti, 0L), a.tokens - 1L);
+    {
+      const u32x4* src = reinterpret_cast<const u32x4*>(static_cast<const bf16_t*>(a.Q) + tok * a.qs +
+                                                        (long)(head * a.g + m - ti * a.g) * D);
+#pragma unroll
+      for (int j = 0; j < W::QS; ++j) w.q[0][j] = src[h * (D / 16) + j];
+    }
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): so that no later wait is for these
+    for (int i = 1; i < min(R, mine); ++i) {
+      const long r0 = pool_row(key_of(i)), r1 = pool_row(key_of(i) + 16);
+      queue_keys(i, r0, r1);
+      queue_vals(i, r0, r1);
+    }
+    const uint32_t* words = a.mask ? a.mask + tok * a.words : nullptr;
+
+    for (int i = 0; i < mine; ++i) {
+      const int key = key_of(i), nv = min(32, kend - key);
+      const uint32_t kat = ring + i % R * 2 * KB, vat = kat + KB, xat = exps + xout * 256;
+      xout = next(xout);
+      const int ahead = min(mine - 1 - i, R);  // blocks behind this one, R at most
+      long r0 = 0, r1 = 0;
+      if (ahead == R) {
+        r0 = pool_row(key_of(i + R));
+        r1 = pool_row(key_of(i + R) + 16);
+      }
+      if (ahead >= R - 1)
+        wait_loads<NI + (R - 1) * G::BI>();
+      else if (R == 4 && ahead == 2)
+        wait_loads<NI + 2 * G::BI>();
+      else if (R == 4 && ahead == 1)
+        wait_loads<NI + G::BI>();
+      else
+        wait_loads<NI>();
+      // scores: lane: keys 8 (i / 4) + 4 h + i % 4 of query l32
+      f32x16 sc, t;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sc[e] = 0.f;
+      {
+        constexpr int HC = G::C / 2 > 0 ? G::C / 2 : 1;  // chunks of a lane
+        u32x4 kc[HC];
+#pragma unroll
+        for (int c = 0; c < HC; ++c) kc[c] = lds_read<u32x4>(kat + G::at(l32, h * HC + c));
+        const uint32_t kx = XB == 4 ? lds_read<uint32_t>(xat + 4 * l32) >> (16 * h)
+                                    : lds_read<uint8_t>(xat + 2 * l32 + h);
+#pragma unroll
+        for (int j = 0; j < W::QS; ++j) {
+          const float scale = block_scale(j < 4 ? kx & 0xff : kx >> 8 & 0xff);
+          u32x4 kf;
+          if constexpr (FMT == WF_CACHE_E4M3) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const uint32_t c = kc[j / 2][2 * (j & 1) + e];
+              kf[2 * e] = __builtin_bit_cast(
+                  uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, scale, false));
+              kf[2 * e + 1] = __builtin_bit_cast(
+                  uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, scale, true));
+            }
+          } else {
+            const uint32_t c = kc[j / 4][j & 3];
+            kf[0] = __builtin_bit_cast(uint32_t,
+                                       __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 0));
+            kf[1] = __builtin_bit_cast(uint32_t,
+                                       __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 1));
+            kf[2] = __builtin_bit_cast(uint32_t,
+                                       __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 2));
+            kf[3] = __builtin_bit_cast(uint32_t,
+                                       __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 3));
+          }
+          sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf),
+                                                       __builtin_bit_cast(bf16x8, w.q[0][j]), sc,
+                                                       0, 0, 0);
+        }
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the codes have been read
+      if (ahead == R) queue_keys(i + R, r0, r1);
+
+      // softmax, with the keys that the row does not see taken out
+      const bool masked = key + 32 > min(s.base, kend);
+      uint32_t seen = ~0u;
+      if (masked) seen = seen_keys(a, s, ti, words, key, nv);
+      auto hide = [&](float by) __attribute__((always_inline)) {
+        if (!masked) return;
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          t[e] = seen >> (8 * (e >> 2) + 4 * h + (e & 3)) & 1 ? t[e] : by;
+      };
+      w.shift_one(0, sc, t);
+      hide(-INFINITY);
+      float mx[1] = {w.largest(t)};
+      w.raise(
+          mx, [&](int, float by) __attribute__((always_inline)) { w.drop(t, by); },
+          [&](int, float& mn, float& al) __attribute__((always_inline)) {
+            t = sc;
+            hide(-w.c2 * INFINITY);
+            w.anew(0, t, mn, al);
+          });
+      float z = 0.f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        t[e] = __builtin_amdgcn_exp2f(t[e]);
+        z += t[e];
+      }
+      w.l[0] += z;
+
+      if (ahead == R)
+        wait_loads<(R - 1) * G::BI + NI + 1>();
+      else if (R == 4 && ahead == 3)
+        wait_loads<3 * G::BI>();
+      else if (R == 4 && ahead == 2)
+        wait_loads<2 * G::BI>();
+      else if (ahead == 1)
+        wait_loads<G::BI>();
+      else
+        wait_loads<0>();
+      const uint32_t vx = xat + 32 * XB;  // V's exponents
+      if (nv < 32) {  // rows behind the last: they may hold codes that are no numbers
+        for (int c = lane; c < (32 - nv) * G::C; c += 64)
+          *(__attribute__((address_space(3))) u32x4*)(size_t)(vat + nv * RB + 16 * c) =
+              u32x4{0u, 0u, 0u, 0u};
+      }
+      // Values that are no numbers: a block of channels with the exponent byte 255, and
+      // in 8 bits codes of NaN.  They are put to the rows that see them here; codes of
+      // NaN that not all rows see are cleared.
+      bool odd;
+      {
+        uint32_t x = XB == 4 ? lds_read<uint32_t>(vx + 4 * l32) : lds_read<uint16_t>(vx + 2 * l32);
+        x = ~x & (XB == 4 ? ~0u : 0xffffu);
+        x |= XB == 4 ? 0u : 0xffff0000u;
+        odd = l32 < nv && ((x - 0x01010101u) & ~x & 0x80808080u) != 0;
+        if (FMT == WF_CACHE_E4M3 && masked)
+          for (int c = lane; c < nv * G::C; c += 64) {
+            const u32x4 v = lds_read<u32x4>(vat + 16 * c);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t y = ~v[e] & 0x7f7f7f7fu;
+              odd |= ((y - 0x01010101u) & ~y & 0x80808080u) != 0;
+            }
+          }
+      }
+      if (__builtin_amdgcn_ballot_w64(odd) != 0) {
+        for (int j = 0; j < nv; ++j) {
+#pragma unroll
+          for (int d = 0; d < DT; ++d) {
+            const float scale = block_scale(lds_read<uint8_t>(vx + j * XB + d));
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+              const int c = 32 * d + 2 * e + 4 * h;  // its channels c .. c + 3
+              u32x2 code = {0u, 0u};
+              if constexpr (FMT == WF_CACHE_E4M3)
+                code[0] = lds_read<uint32_t>(vat + G::at(j, c / 16) + c % 16);
+              else
+                code[0] = lds_read<uint16_t>(vat + G::at(j, c / 32) + c % 32 / 2);
+              float v[8];
+              decode8<FMT>(code, scale, v);
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                if (!(fabsf(v[k]) < INFINITY) && (seen >> j & 1)) w.O[0][d][e + k] += v[k];
+            }
+          }
+        }
+        if constexpr (FMT == WF_CACHE_E4M3)
+          for (int c = lane; c < 32 * G::C; c += 64) {
+            u32x4 v = lds_read<u32x4>(vat + 16 * c);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+              for (int k = 0; k < 32; k += 8)
+                if ((v[e] >> k & 0x7f) == 0x7f) v[e] &= ~(0xffu << k);
+            *(__attribute__((address_space(3))) u32x4*)(size_t)(vat + 16 * c) = v;
+          }
+      }
+      // exponents of the lane's 16 keys, less 128 (the weights are doubled for it)
+      uint32_t xs[16 * XB / 4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        if constexpr (XB == 4) {
+          const u32x4 x = lds_read<u32x4>(vx + (8 * q + 4 * h) * 4);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) xs[4 * q + e] = x[e] ^ 0x80808080u;
+        } else {
+          const u32x2 x = lds_read<u32x2>(vx + (8 * q + 4 * h) * 2);
+          xs[2 * q] = x[0] ^ 0x80808080u;
+          xs[2 * q + 1] = x[1] ^ 0x80808080u;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) t[e] += t[e];
+      // weight of key e (of the lane's 16) for channels 32 d ..: times 2^(x - 127)
+      auto weight = [&](int e, int d) __attribute__((always_inline)) {
+        const int b = e * XB + d;
+        return __builtin_amdgcn_ldexpf(t[e], (int)(xs[b / 4] << (24 - 8 * (b & 3))) >> 24);
+      };
+      // the lane's place in a transposed load: in 8 bits row e of eight and half of its 16
+      // channels, in 4 bits row e of sixteen
+      const int i16 = lane & 15, half = (lane >> 4) & 1;
+      const int p = FMT == WF_CACHE_E4M3 ? i16 >> 1 : i16;
+      const int vrow = 16 * (p >> 3) + 8 * (p >> 2 & 1) + 4 * h + (p & 3);
+      uint32_t vb = vat + (FMT == WF_CACHE_E4M3 ? G::at(vrow, half) + 8 * (i16 & 1)
+                                                : G::at(vrow, 0) + 8 * half);
+      asm volatile("" : "+v"(vb));
+      if constexpr (FMT == WF_CACHE_E4M3) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+          for (int d = 0; d < DT; ++d) {
+            const v2i_few c = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                (__attribute__((address_space(3))) v2i_few*)(size_t)((vb ^ (32 * d)) + kb * 16 * RB));
+            u32x4 vf, pf;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              vf[2 * e] = __builtin_bit_cast(
+                  uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[e], 1.0f, false));
+              vf[2 * e + 1] = __builtin_bit_cast(
+                  uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[e], 1.0f, true));
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              pf[e] = pack_bf16x2(weight(8 * kb + 2 * e, d), weight(8 * kb + 2 * e + 1, d));
+            w.O[0][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf),
+                                                                __builtin_bit_cast(bf16x8, pf),
+                                                                w.O[0][d], 0, 0, 0);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          const v2i_few c = __builtin_amdgcn_ds_read_tr4_b64_v2i32(
+              (__attribute__((address_space(3))) v2i_few*)(size_t)(vb ^ (16 * d)));
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb) {
+            u32x4 vf, pf;
+            vf[0] = __builtin_bit_cast(uint32_t,
+                                       __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[kb], 1.0f, 0));
+            vf[1] = __builtin_bit_cast(uint32_t,
+                                       __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[kb], 1.0f, 1));
+            vf[2] = __builtin_bit_cast(uint32_t,
+                                       __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[kb], 1.0f, 2));
+            vf[3] = __builtin_bit_cast(uint32_t,
+                                       __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[kb], 1.0f, 3));
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              pf[e] = pack_bf16x2(weight(8 * kb + 2 * e, d), weight(8 * kb + 2 * e + 1, d));
+            w.O[0][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf),
+                                                                __builtin_bit_cast(bf16x8, pf),
+                                                                w.O[0][d], 0, 0, 0);
+          }
+        }
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the codes have been read
+      if (ahead == R) queue_vals(i + R, r0, r1);
+    }
+  }
+
+  lds_barrier();  // the rings are idle
+  OutRows<D, 1, kFewWaves> out(smem);
+  out.put(w, wave);
+  constexpr int C4 = D / 4, RPP = 64 * kFewWaves / C4;  // rows per round
+  const int c = threadIdx.x % C4;
+  for (int r = threadIdx.x / C4; r < M; r += RPP) {
+    const int v[1] = {r};
+    Merge4 g[1];
+    out.merged(v, kFewWaves, c, g);
+    const int i = a.by_g(r);
+    const long tok = s.first + i;
+    if (!Sequence::there(a, tok)) continue;
+    const int hq = head * a.g + r - i * a.g;
+    const long row = tok * a.hq + hq;
+    if (a.whole) {
+      g[0].finish(static_cast<bf16_t*>(a.O) + tok * a.os + (long)hq * D + 4 * c,
+                  a.lse ? a.lse + row : nullptr, c == 0);
+    } else {
+      const long at = row * a.splits + sp;
+      *reinterpret_cast<f32x4*>(a.part + at * D + 4 * c) = g[0].o;
+      if (c == 0) *reinterpret_cast<hw_f32x2*>(a.pstat + 2 * at) = hw_f32x2{g[0].M, g[0].z};
+    }
+  }
+}
+
+// ------------------------------------------------------------ host side
+
+template <int D, int FMT>
+static constexpr size_t few_lds() {
+  const size_t rings = (size_t)kFewWaves * FewGeom<D, FMT>::WAVE;
+  const size_t out = OutRows<D, 1, kFewWaves>::BYTES;
+  return rings > out ? rings : out;
+}
+
+hipError_t launch_tree_few(const TreeArgs& a, int head_dim, int format, long items, hipStream_t s) {
+  auto go = [&](auto d, auto f) {
+    constexpr int D = decltype(d)::value, F = decltype(f)::value;
+    constexpr size_t lds = few_lds<D, F>();
+    auto kern = tree_few_kernel<D, F>;
+    if (lds > 65536) {
+      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern),
+                                               hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+      if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(kern, dim3((unsigned)((items + 7) & ~7L)), dim3(64 * kFewWaves), lds, s, a);
+    return hipGetLastError();
+  };
+  using D64 = std::integral_constant<int, 64>;
+  using D128 = std::integral_constant<int, 128>;
+  using E4 = std::integral_constant<int, WF_CACHE_E4M3>;
+  using E2 = std::integral_constant<int, WF_CACHE_E2M1>;
+  if (head_dim == 128)
+    return format == WF_CACHE_E4M3 ? go(D128{}, E4{}) : go(D128{}, E2{});
+  return format == WF_CACHE_E4M3 ? go(D64{}, E4{}) : go(D64{}, E2{});
+}
+
+}  // namespace wf
