@@ -146,8 +146,9 @@ struct PrefixWave {
     }
   }
 
-  // 32 keys at LDS offsets kat, vat, the first nv of which are valid; or MASK: those
-  // whose bits are set in the word of the lane's query row (for each block of rows)
+  // 32 keys at LDS offsets kat, vat, the first nv of which are valid; MASK: with nv
+  // < 32 those whose bits are set in the word of the lane's query row (for each block
+  // of rows)
   template <bool MASK = false>
   __device__ __forceinline__ void step(uint32_t kat, uint32_t vat, int nv,
                                        const uint32_t* words = nullptr) {
@@ -167,14 +168,13 @@ struct PrefixWave {
     float mx[QW];
     auto shifted = [&](int b) __attribute__((always_inline)) {
       shift_one(b, s[b], t[b]);
-      if constexpr (MASK) {
+      if (nv < 32) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          t[b][i] = seen[b] >> (8 * (i >> 2) + (i & 3)) & 1 ? t[b][i] : -INFINITY;
-      } else if (nv < 32) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          t[b][i] = 8 * (i >> 2) + 4 * h + (i & 3) >= nv ? -INFINITY : t[b][i];
+        for (int i = 0; i < 16; ++i) {
+          const bool hidden = MASK ? !(seen[b] >> (8 * (i >> 2) + (i & 3)) & 1)
+                                   : 8 * (i >> 2) + 4 * h + (i & 3) >= nv;
+          t[b][i] = hidden ? -INFINITY : t[b][i];
+        }
       }
     };
 #pragma unroll
@@ -200,7 +200,7 @@ struct PrefixWave {
             t[b] = s[b];
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            const bool hidden = MASK ? !(seen[b] >> (8 * (i >> 2) + (i & 3)) & 1)
+            const bool hidden = MASK ? n < 32 && !(seen[b] >> (8 * (i >> 2) + (i & 3)) & 1)
                                      : 8 * (i >> 2) + 4 * h + (i & 3) >= n;
             t[b][i] = hidden ? -c2 * INFINITY : t[b][i];
           }

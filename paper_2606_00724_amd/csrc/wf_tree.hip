@@ -86,9 +86,9 @@ struct PageLoads {
   }
 };
 
-// Whether V's rows 0 .. nr - 1 of a tile hold a NaN or an infinity, of the granules
-// that this thread looks at; CLEAR: and those are made 0.
-template <typename T, int D, int NW, bool CLEAR>
+// NaN and infinities in V's rows 0 .. nr - 1 of a tile are made 0; whether there are
+// any in the granules that this thread looks at.
+template <typename T, int D, int NW>
 __device__ __forceinline__ bool odd_values(unsigned char* tile, int nr) {
   using Geom = TileGeom<T, D>;
   bool odd = false;
@@ -108,34 +108,47 @@ __device__ __forceinline__ bool odd_values(unsigned char* tile, int nr) {
         w[e] = bad ? 0u : w[e];
       }
     }
-    if (CLEAR && here) *g = w;
+    if (here) *g = w;
     odd |= here;
   }
   return odd;
 }
 
-// Four channels from c on of row r of V as fp32 numbers.
-template <typename T, int D, int FMT>
-__device__ __forceinline__ f32x4 values4(const TreeArgs& a, long r, int c) {
-  f32x4 v;
-  if constexpr (FMT == WF_CACHE_PLAIN) {
-    const T* p = static_cast<const T*>(a.V) + r * D + c;
+// A tile's codes as a thread stages them.  The rows of a wave's load lie in one page
+// (or, two pieces a row, in one for each half of the wave): the lanes' offsets are
+// constant.
+template <typename T, int D, int FMT, int NW>
+__device__ __forceinline__ void stage_pages(QuantStage<T, D, FMT, NW>& st, const TreeArgs& a,
+                                            const PageIds& pages, int head, int key) {
+  using S = QuantStage<T, D, FMT, NW>;
+  if (S::idle()) return;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = load_elem<T>(p, e);
-  } else {
-    const float s = block_scale(a.Vx[r * (D / 32) + c / 32]);
-    u32x2 w = {0u, 0u};
-    if constexpr (FMT == WF_CACHE_E4M3)
-      w[0] = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(a.V) + r * D + c);
-    else
-      w[0] = *reinterpret_cast<const uint16_t*>(static_cast<const uint8_t*>(a.V) + r * (D / 2) +
-                                                c / 2);
-    float x[8];
-    decode8<FMT>(w, s, x);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = x[e];
+  for (int i = 0; i < S::N; ++i) {
+    auto first = [&](int k) -> long {  // row of the pool of key k, the first of sixteen
+      const long page = __builtin_amdgcn_readfirstlane(pages.of(k));
+      return ((page * a.heads + head) << a.shift) + (k & ((1 << a.shift) - 1));
+    };
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, r16 = S::row(i) & 15;
+    const uint32_t o = (r16 * S::PPR + S::piece()) * 16;
+    const uint32_t e = r16 * (D / 32) + S::piece() * S::CPP / 32;
+    const uint8_t* K = static_cast<const uint8_t*>(a.K);
+    const uint8_t* V = static_cast<const uint8_t*>(a.V);
+    if constexpr (S::PPR > 2) {  // 8 or 16 rows
+      const long r = first(key + (i * NW + wave) * (64 / S::PPR) / 16 * 16);
+      st.w[0][i] = *reinterpret_cast<const u32x4*>(K + r * (S::PPR * 16) + o);
+      st.w[1][i] = *reinterpret_cast<const u32x4*>(V + r * (S::PPR * 16) + o);
+      st.x[0][i] = (a.Kx + r * (D / 32))[e];
+      st.x[1][i] = (a.Vx + r * (D / 32))[e];
+    } else {
+      const int k = key + (i * NW + wave) * 32;
+      const long r0 = first(k), r1 = first(k + 16), r = lane < 32 ? r0 : r1;
+      st.w[0][i] = *reinterpret_cast<const u32x4*>(K + r * (S::PPR * 16) + o);
+      st.w[1][i] = *reinterpret_cast<const u32x4*>(V + r * (S::PPR * 16) + o);
+      st.x[0][i] = a.Kx[r * (D / 32) + e];
+      st.x[1][i] = a.Vx[r * (D / 32) + e];
+    }
   }
-  return v;
 }
 
 // The query rows of a (sequence, head) over a range of its keys.
@@ -173,6 +186,8 @@ __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void tree_attn_kerne
   };
   W w;
   w.init(a.scale);
+  bool odd = false;  // values that are no numbers among the keys from odd_from on
+  int odd_from = 0;
 
   if (nk > 0) {
     // a tile: the keys of one slot, or with eight waves of two
@@ -180,6 +195,7 @@ __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void tree_attn_kerne
     const int nt = (nk + KT - 1) / KT;
     // tiles that every row sees whole
     const int nseen = min(max(s.base - k0, 0), nk) / KT;
+    odd_from = k0 + nseen * KT;
     auto slot_of = [&](int t) { return t % NS * US; };
     PageIds pages;
     pages.ids = ids;
@@ -214,16 +230,9 @@ __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void tree_attn_kerne
       stage_ids(t);
       queued = t + 1;
       if constexpr (QUANT) {
-        if (st[0].idle()) return;
 #pragma unroll
         for (int i = 0; i < US; ++i)
-#pragma unroll
-          for (int j = 0; j < st[0].N; ++j) {
-            const int key = min(k0 + t * KT + i * kTileRows + st[0].row(j), s.L - 1);
-            const long page = pages.of(key);
-            st[i].load(j, a.K, a.V, a.Kx, a.Vx,
-                       ((page * a.heads + head) << a.shift) + (key & ((1 << a.shift) - 1)));
-          }
+          stage_pages(st[i], a, pages, head, k0 + t * KT + i * kTileRows);
       } else {
         dma.template some<0>(0, 2 * dma.N, dma.at(pages, k0 + t * KT, slot_of(t)));
       }
@@ -356,57 +365,34 @@ __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void tree_attn_kerne
             lds_offset(smem) + (slot_of(t) + r / kTileRows) * 2 * MB + r % kTileRows * 64,
             min(32, nr - r));
       };
-      if (k0 + t * KT + min(nr, KT) <= s.base) {
-        blocks([&](int, uint32_t at, int nv) { w.step(at, at + MB, nv); });
-        continue;
-      }
       // Keys that some rows do not see: their scores are taken out, whatever they
       // are.  A weight of 0 times a value that is no number would still be NaN:
-      // where there are such values they are cleared, and put to the rows that see
-      // them behind the products.
-      {
+      // such values are cleared, and put to the rows that see them behind it all.
+      const bool all = k0 + t * KT + min(nr, KT) <= s.base;  // uniform
+      if (!all) {
         bool odd = false;
 #pragma unroll
         for (int i = 0; i < US; ++i)
-          odd |= odd_values<T, D, NW, false>(smem + (slot_of(t) + i) * 2 * MB,
-                                             min(max(nr - i * kTileRows, 0), kTileRows));
+          odd |= odd_values<T, D, NW>(smem + (slot_of(t) + i) * 2 * MB,
+                                      min(max(nr - i * kTileRows, 0), kTileRows));
         if (__builtin_amdgcn_ballot_w64(odd) != 0 && lane == 0) *flag = 1;
-      }
-      lds_barrier();
-      const bool odd = __builtin_amdgcn_readfirstlane(*flag) != 0;
-      if (odd) {
-#pragma unroll
-        for (int i = 0; i < US; ++i)
-          odd_values<T, D, NW, true>(smem + (slot_of(t) + i) * 2 * MB,
-                                     min(max(nr - i * kTileRows, 0), kTileRows));
         lds_barrier();
       }
-      blocks([&](int key, uint32_t at, int nv) {
+      for (int r = 32 * kw; r < min(nr, KT); r += 32 * KW) {
+        const int key = k0 + t * KT + r;
+        const uint32_t at =
+            lds_offset(smem) + (slot_of(t) + r / kTileRows) * 2 * MB + r % kTileRows * 64;
         uint32_t seen[QW];
 #pragma unroll
-        for (int b = 0; b < QW; ++b)
-          seen[b] = seen_keys(a, s, row[b], masks + (row[b] - i0) * a.words, key, nv);
-        w.template step<true>(at, at + MB, nv, seen);
-        if (odd) {  // (rare: from memory again)
-          for (int j = 0; j < nv; ++j) {
-            const long page = min(max(pages.row[(key + j) >> a.shift], 0), a.pages - 1);
-            const long r = ((page * a.heads + head) << a.shift) + ((key + j) & ((1 << a.shift) - 1));
+        for (int b = 0; b < QW; ++b) seen[b] = ~0u;
+        if (!all)
 #pragma unroll
-            for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-              for (int i = 0; i < 16; i += 4) {
-                const f32x4 v = values4<T, D, FMT>(a, r, 32 * d + 2 * i + 4 * h);
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                  if (!(fabsf(v[e]) < INFINITY))
-#pragma unroll
-                    for (int b = 0; b < QW; ++b)
-                      if (seen[b] >> j & 1) w.O[b][d][i + e] += v[e];
-              }
-          }
-        }
-      });
+          for (int b = 0; b < QW; ++b)
+            seen[b] = seen_keys(a, s, row[b], masks + (row[b] - i0) * a.words, key, nr - r);
+        w.template step<true>(at, at + MB, all ? 32 : 0, seen);
+      }
     }
+    odd = __builtin_amdgcn_readfirstlane(*flag) != 0;
     lds_barrier();  // the tiles are idle
   }
 
@@ -433,6 +419,8 @@ __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void tree_attn_kerne
       int x;
       const long tok = token_of(m0 + r, x);
       if (!Sequence::there(a, tok)) continue;
+      if (odd)
+        add_odd<T, D, FMT>(a, s, seq, head, (int)(tok - s.first), odd_from, k0 + nk, 4 * c, g[i].o);
       const int hq = head * a.g + x;
       const long row = tok * a.hq + hq;
       if (a.whole) {

@@ -36,6 +36,49 @@ __device__ __forceinline__ uint32_t seen_keys(const TreeArgs& a, const Sequence&
   return nv < 32 ? seen & ((1u << nv) - 1u) : seen;
 }
 
+// Four channels from c on of row r of V as fp32 numbers.
+template <typename T, int D, int FMT>
+__device__ __forceinline__ f32x4 values4(const TreeArgs& a, long r, int c) {
+  f32x4 v;
+  if constexpr (FMT == WF_CACHE_PLAIN) {
+    const T* p = static_cast<const T*>(a.V) + r * D + c;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = load_elem<T>(p, e);
+  } else {
+    const float s = block_scale(a.Vx[r * (D / 32) + c / 32]);
+    u32x2 w = {0u, 0u};
+    if constexpr (FMT == WF_CACHE_E4M3)
+      w[0] = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(a.V) + r * D + c);
+    else
+      w[0] = *reinterpret_cast<const uint16_t*>(static_cast<const uint8_t*>(a.V) + r * (D / 2) +
+                                                c / 2);
+    float x[8];
+    decode8<FMT>(w, s, x);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = x[e];
+  }
+  return v;
+}
+
+// Values that are no numbers, which the kernels leave out of their products where not
+// all rows see them (a weight of 0 times one would be NaN), put to the four channels
+// c .. c + 3 of query row i: those of the keys from .. to - 1 that it sees.
+template <typename T, int D, int FMT>
+__device__ __forceinline__ void add_odd(const TreeArgs& a, const Sequence& s, int seq, int head,
+                                        int i, int from, int to, int c, f32x4& o) {
+  const uint32_t* words =
+      a.mask ? a.mask + min(max(s.first + i, 0L), a.tokens - 1L) * a.words : nullptr;
+  for (int k = from; k < to; ++k) {
+    if (!(seen_keys(a, s, i, words, k, 32) & 1)) continue;
+    const long page = min(max(a.table[(long)seq * a.tp + (k >> a.shift)], 0), a.pages - 1);
+    const f32x4 v = values4<T, D, FMT>(
+        a, ((page * a.heads + head) << a.shift) + (k & ((1 << a.shift) - 1)), c);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (!(fabsf(v[e]) < INFINITY)) o[e] += v[e];
+  }
+}
+
 hipError_t launch_tree_few(const TreeArgs& a, int head_dim, int format, long items, hipStream_t s);
 
 }  // namespace wf

@@ -63,7 +63,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(TreeArgs a)
   using G = FewGeom<D, FMT>;
   using W = PrefixWave<bf16_t, D, 1>;
   constexpr int NI = G::NI, R = G::R, RB = G::RB, KB = G::KB, XB = G::XB, DT = D / 32;
-  extern __shared__ __align__(16) unsigned char smem[];  // the waves' rings
+  extern __shared__ __align__(16) unsigned char smem[];  // the waves' rings, a flag
+  int* flag = reinterpret_cast<int*>(smem + kFewWaves * G::WAVE);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = lane >> 5, l32 = lane & 31;
@@ -78,6 +79,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(TreeArgs a)
   if (M <= 0 || (nk <= 0 && !a.whole)) return;
   W w;
   w.init(a.scale);
+  if (threadIdx.x == 0) *flag = 0;
+  lds_barrier();
 
   // the wave's blocks: wave, wave + 4, ... of the range
   const int nb = nk > 0 ? (nk + 31) / 32 : 0;
@@ -261,8 +264,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(TreeArgs a)
               u32x4{0u, 0u, 0u, 0u};
       }
       // Values that are no numbers: a block of channels with the exponent byte 255, and
-      // in 8 bits codes of NaN.  They are put to the rows that see them here; codes of
-      // NaN that not all rows see are cleared.
+      // in 8 bits codes of NaN.  Such codes are cleared where not all rows see them; all
+      // are put to the rows that see them behind the last block.
       bool odd;
       {
         uint32_t x = XB == 4 ? lds_read<uint32_t>(vx + 4 * l32) : lds_read<uint16_t>(vx + 2 * l32);
@@ -279,27 +282,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(TreeArgs a)
             }
           }
       }
-      if (__builtin_amdgcn_ballot_w64(odd) != 0) {
-        for (int j = 0; j < nv; ++j) {
-#pragma unroll
-          for (int d = 0; d < DT; ++d) {
-            const float scale = block_scale(lds_read<uint8_t>(vx + j * XB + d));
-#pragma unroll
-            for (int e = 0; e < 16; e += 4) {
-              const int c = 32 * d + 2 * e + 4 * h;  // its channels c .. c + 3
-              u32x2 code = {0u, 0u};
-              if constexpr (FMT == WF_CACHE_E4M3)
-                code[0] = lds_read<uint32_t>(vat + G::at(j, c / 16) + c % 16);
-              else
-                code[0] = lds_read<uint16_t>(vat + G::at(j, c / 32) + c % 32 / 2);
-              float v[8];
-              decode8<FMT>(code, scale, v);
-#pragma unroll
-              for (int k = 0; k < 4; ++k)
-                if (!(fabsf(v[k]) < INFINITY) && (seen >> j & 1)) w.O[0][d][e + k] += v[k];
-            }
-          }
-        }
+      if (__builtin_amdgcn_ballot_w64(odd) != 0) {  // rare
+        if (lane == 0) *flag = 1;
         if constexpr (FMT == WF_CACHE_E4M3)
           for (int c = lane; c < 32 * G::C; c += 64) {
             u32x4 v = lds_read<u32x4>(vat + 16 * c);
@@ -394,6 +378,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(TreeArgs a)
   }
 
   lds_barrier();  // the rings are idle
+  const bool odd = __builtin_amdgcn_readfirstlane(*flag) != 0;
+  lds_barrier();
   OutRows<D, 1, kFewWaves> out(smem);
   out.put(w, wave);
   constexpr int C4 = D / 4, RPP = 64 * kFewWaves / C4;  // rows per round
@@ -405,6 +391,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(TreeArgs a)
     const int i = a.by_g(r);
     const long tok = s.first + i;
     if (!Sequence::there(a, tok)) continue;
+    if (odd) add_odd<bf16_t, D, FMT>(a, s, seq, head, i, k0, k0 + nk, 4 * c, g[0].o);
     const int hq = head * a.g + r - i * a.g;
     const long row = tok * a.hq + hq;
     if (a.whole) {
@@ -422,7 +409,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(TreeArgs a)
 
 template <int D, int FMT>
 static constexpr size_t few_lds() {
-  const size_t rings = (size_t)kFewWaves * FewGeom<D, FMT>::WAVE;
+  const size_t rings = (size_t)kFewWaves * FewGeom<D, FMT>::WAVE + sizeof(int);
   const size_t out = OutRows<D, 1, kFewWaves>::BYTES;
   return rings > out ? rings : out;
 }
