@@ -10,7 +10,10 @@ the library has not been built (``python paper_2606_00724_amd/build.py``).
 from __future__ import annotations
 
 import ctypes
+import functools
+import math
 import os
+import typing
 
 import torch
 
@@ -321,6 +324,8 @@ def _ws(t) -> tuple[int | None, int]:
     return _ptr(t), t.numel() * t.element_size()
 
 
+# the current device without torch's check that the GPU is in use
+_raw_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 # the current stream's handle without the Python object around it, where torch
 # has it (2.5 us of a call's host time)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
@@ -924,46 +929,97 @@ def make_rope_params(*, batch: int, heads: int, rows: int, head_dim: int,
                         i64(*x_strides), i64(*y_strides))
 
 
-def _rows_ptr(name: str, t, dtype: torch.dtype, shape: tuple,
-              strides) -> int:
-    """The pointer of a tensor of this shape whose outer strides are those of
-    the parameters (all 0: contiguous), what is inside of them adjacent."""
-    if not isinstance(t, torch.Tensor):
-        raise TypeError(f"{name}: expected a torch tensor, got {type(t).__name__}")
-    if t.dtype is not dtype:
-        raise TypeError(f"{name}: dtype {t.dtype}, expected {dtype}")
-    if tuple(t.shape) != shape:
-        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {shape} "
-                         f"for these parameters")
+class _Form(typing.NamedTuple):
+    """What a tensor must be for some parameters: contiguous and of so many
+    elements, or of this shape and these strides."""
+    name: str
+    dtype: torch.dtype
+    numel: int
+    nullable: bool = False
+    shape: tuple | None = None
+    strides: tuple | None = None
+
+
+def _rows_form(name, dtype, shape, strides, nullable=False) -> _Form:
+    """Rows of `shape` whose outer strides are those of the parameters (all 0:
+    contiguous), what is inside of them adjacent."""
+    numel = math.prod(shape)
     if not any(strides):
-        good = t.is_contiguous()
+        return _Form(name, dtype, numel, nullable)
+    want, inner = list(strides), 1
+    for n in reversed(shape[len(want):]):
+        want.insert(len(strides), inner)
+        inner *= n
+    return _Form(name, dtype, numel, nullable, shape, tuple(want))
+
+
+def _marshal(forms, tensors) -> list[int | None]:
+    """The pointers of tensors, each of which must have its form, on the
+    current device, which the kernels run on."""
+    # one pass that asks each tensor as little as it can, most of a small call's
+    # host time; what it refuses is looked at again for the message
+    dev = _raw_device() if torch.cuda.is_initialized() else -2
+    out = []
+    for t, (_, dtype, numel, nullable, shape, strides) in zip(tensors, forms):
+        if t is None:
+            if not nullable:
+                break
+            out.append(None)
+        elif (t.__class__ is torch.Tensor and t.dtype is dtype
+              and t.numel() == numel and t.get_device() == dev
+              and (t.is_contiguous() if shape is None
+                   else t.shape == shape and t.stride() == strides)):
+            out.append(t.data_ptr())
+        else:
+            break
     else:
-        want, inner = list(strides), 1
-        for n in reversed(shape[len(want):]):
-            want.insert(len(strides), inner)
-            inner *= n
-        good = all(n <= 1 or h == w for n, h, w in zip(shape, t.stride(), want))
-    if not good:
-        raise ValueError(f"{name}: strides {t.stride()} are not those of the "
-                         f"parameters, {tuple(strides)} (0: contiguous)")
-    return t.data_ptr()
+        return out
+    out = []
+    for t, f in zip(tensors, forms):
+        _expect(t, f.name, f.dtype, f.numel, f.nullable)
+        if t is None:
+            continue
+        if f.shape is None:
+            good = t.is_contiguous()
+        else:
+            good = tuple(t.shape) == f.shape and all(
+                n <= 1 or a == b
+                for n, a, b in zip(f.shape, t.stride(), f.strides))
+        if not good:
+            raise ValueError(
+                f"{f.name}: shape {tuple(t.shape)}, strides {t.stride()} are "
+                f"not those of the parameters, "
+                f"{'contiguous' if f.shape is None else (f.shape, f.strides)}")
+    for t, f in zip(tensors, forms):
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"{f.name} is on {t.device}, not on the current "
+                             f"GPU")
+        out.append(None if t is None else t.data_ptr())
+    return out
 
 
-def _on_current(tensors) -> None:
-    dev = torch.cuda.current_device() if torch.cuda.is_initialized() else -2
-    for name, t in tensors:
-        if t.get_device() != dev:
-            raise ValueError(f"{name} is on {t.device}, not on the current GPU")
+def _queue(stream) -> int | None:
+    """As _stream, once _marshal has seen that the GPU is in use."""
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(_raw_device())
+    return _stream(stream)
+
+
+# The forms of a call's tensors follow from its parameters alone; they are kept
+# for the parameters' bytes.
+@functools.lru_cache(maxsize=256)
+def _rope_forms(raw: bytes) -> tuple[_Form, ...]:
+    p = WfRopeParams.from_buffer_copy(raw)
+    dt, shape = torch_dtype(p), (p.batch, p.heads, p.rows, p.head_dim)
+    return (_rows_form("X", dt, shape, tuple(p.x_strides)),
+            _Form("pos", torch.int32, p.axes * p.batch * p.rows),
+            _Form("inv_freq", torch.float32, p.rot_dim // 2),
+            _rows_form("Y", dt, shape, tuple(p.y_strides)))
 
 
 def wf_rope(p, X, pos, inv_freq, Y, stream=None):
-    dt, shape = torch_dtype(p), (p.batch, p.heads, p.rows, p.head_dim)
-    x = _rows_ptr("X", X, dt, shape, p.x_strides)
-    y = _rows_ptr("Y", Y, dt, shape, p.y_strides)
-    a = _args((("pos", pos, torch.int32, p.axes * p.batch * p.rows, False),
-               ("inv_freq", inv_freq, torch.float32, p.rot_dim // 2, False)))
-    _on_current((("X", X), ("Y", Y)))
-    _check(_lib.wf_rope(p, x, *a, y, _stream(stream)))
+    a = _marshal(_rope_forms(bytes(p)), (X, pos, inv_freq, Y))
+    _check(_lib.wf_rope(p, *a, _queue(stream)))
 
 
 def rope(X, pos, inv_freq, *, out=None, stream=None, **kw):
@@ -1021,37 +1077,36 @@ def alloc_pages(p, device) -> tuple[torch.Tensor | None, ...]:
                  for s in shapes)
 
 
-def _pool_entries(p, Kc, Kx, Vc, Vx) -> tuple:
+def _pool_forms(p) -> tuple[_Form, ...]:
     plain = p.format == CACHE_PLAIN
     dt = torch_dtype(p) if plain else torch.uint8
     rows = p.pages * p.heads * p.page_rows
     codes = rows * (p.head_dim if plain else _code_bytes(p.head_dim, p.format))
     exps = 0 if plain else rows * (p.head_dim // 32)
-    return (("Kc", Kc, dt, codes, False), ("Kx", Kx, torch.uint8, exps, plain),
-            ("Vc", Vc, dt, codes, False), ("Vx", Vx, torch.uint8, exps, plain))
+    return (_Form("Kc", dt, codes), _Form("Kx", torch.uint8, exps, plain),
+            _Form("Vc", dt, codes), _Form("Vx", torch.uint8, exps, plain))
+
+
+@functools.lru_cache(maxsize=256)
+def _append_forms(raw: bytes) -> tuple[_Form, ...]:
+    p = WfAppendParams.from_buffer_copy(raw)
+    dt, i32, n = torch_dtype(p), torch.int32, p.tokens
+    q, kv = (n, p.heads * p.group, p.head_dim), (n, p.heads, p.head_dim)
+    none, still = p.group == 0, p.rot_dim == 0
+    return (_rows_form("Q", dt, q, (p.q_row,), none),
+            _rows_form("K", dt, kv, (p.k_row,)),
+            _rows_form("V", dt, kv, (p.v_row,)),
+            _Form("pos", i32, p.axes * n, still),
+            _Form("inv_freq", torch.float32, p.rot_dim // 2, still),
+            _Form("slot", i32, n), *_pool_forms(p),
+            _rows_form("Qr", dt, q, (p.qr_row,), none))
 
 
 def wf_page_append(p, Q, K, V, pos, inv_freq, slot, Kc, Kx, Vc, Vx, Qr,
                    stream=None):
-    dt, i32 = torch_dtype(p), torch.int32
-    n, h, d = p.tokens, p.heads, p.head_dim
-    k = _rows_ptr("K", K, dt, (n, h, d), (p.k_row,))
-    v = _rows_ptr("V", V, dt, (n, h, d), (p.v_row,))
-    q = qr = None
-    rows = [("K", K), ("V", V)]
-    if p.group:
-        q = _rows_ptr("Q", Q, dt, (n, h * p.group, d), (p.q_row,))
-        qr = _rows_ptr("Qr", Qr, dt, (n, h * p.group, d), (p.qr_row,))
-        rows += [("Q", Q), ("Qr", Qr)]
-    elif Q is not None or Qr is not None:
-        raise ValueError("Q or Qr with a group of 0")
-    turned = p.rot_dim > 0
-    a = _args((("pos", pos, i32, p.axes * n, not turned),
-               ("inv_freq", inv_freq, torch.float32, p.rot_dim // 2,
-                not turned),
-               ("slot", slot, i32, n, False), *_pool_entries(p, Kc, Kx, Vc, Vx)))
-    _on_current(rows)
-    _check(_lib.wf_page_append(p, q, k, v, *a, qr, _stream(stream)))
+    a = _marshal(_append_forms(bytes(p)),
+                 (Q, K, V, pos, inv_freq, slot, Kc, Kx, Vc, Vx, Qr))
+    _check(_lib.wf_page_append(p, *a, _queue(stream)))
 
 
 def make_move_params(*, pages: int, page_rows: int, heads: int, head_dim: int,
@@ -1063,13 +1118,18 @@ def make_move_params(*, pages: int, page_rows: int, heads: int, head_dim: int,
                         batch, table_pages, moves)
 
 
+@functools.lru_cache(maxsize=256)
+def _move_forms(raw: bytes) -> tuple[_Form, ...]:
+    p, i32 = WfMoveParams.from_buffer_copy(raw), torch.int32
+    return (_Form("table", i32, p.batch * p.table_pages),
+            _Form("first", i32, p.batch),
+            _Form("source", i32, p.batch * p.moves), *_pool_forms(p))
+
+
 def wf_page_move(p, table, first, source, Kc, Kx, Vc, Vx, stream=None):
-    i32 = torch.int32
-    a = _args((("table", table, i32, p.batch * p.table_pages, False),
-               ("first", first, i32, p.batch, False),
-               ("source", source, i32, p.batch * p.moves, False),
-               *_pool_entries(p, Kc, Kx, Vc, Vx)))
-    _check(_lib.wf_page_move(p, *a, _stream(stream)))
+    a = _marshal(_move_forms(bytes(p)),
+                 (table, first, source, Kc, Kx, Vc, Vx))
+    _check(_lib.wf_page_move(p, *a, _queue(stream)))
 
 
 # A sequence's new rows (a tree of drafted tokens, a block, a single token) are
@@ -1114,23 +1174,28 @@ def alloc_tree_workspace(p: WfTreeParams, device) -> torch.Tensor | None:
     return torch.empty(nb, dtype=torch.uint8, device=device) if nb else None
 
 
+@functools.lru_cache(maxsize=256)
+def _tree_forms(raw: bytes) -> tuple[_Form, ...]:
+    p, i32 = WfTreeParams.from_buffer_copy(raw), torch.int32
+    dt, hq = torch_dtype(p), p.heads * p.group
+    rows = (p.tokens, hq, p.head_dim)
+    return (_rows_form("Q", dt, rows, (p.q_row,)), *_pool_forms(p),
+            _Form("table", i32, p.batch * p.table_pages),
+            _Form("length", i32, p.batch),
+            _Form("row_start", i32, p.batch + 1, True),
+            _Form("mask", i32, p.tokens * ((p.max_rows + 31) // 32), True),
+            _rows_form("O", dt, rows, (p.o_row,)),
+            _Form("lse", torch.float32, p.tokens * hq, True))
+
+
 def wf_tree_attn(p, Q, Kc, Kx, Vc, Vx, table, length, row_start, mask, O, lse,
                  workspace, stream=None):
-    dt, i32, hq = torch_dtype(p), torch.int32, p.heads * p.group
-    shape = (p.tokens, hq, p.head_dim)
-    q = _rows_ptr("Q", Q, dt, shape, (p.q_row,))
-    o = _rows_ptr("O", O, dt, shape, (p.o_row,))
-    kc, kx, vc, vx, *a, l = _args((
-        *_pool_entries(p, Kc, Kx, Vc, Vx),
-        ("table", table, i32, p.batch * p.table_pages, False),
-        ("length", length, i32, p.batch, False),
-        ("row_start", row_start, i32, p.batch + 1, True),
-        ("mask", mask, i32, p.tokens * ((p.max_rows + 31) // 32), True),
-        ("lse", lse, torch.float32, p.tokens * hq, True)))
+    a = _marshal(_tree_forms(bytes(p)),
+                 (Q, Kc, Kx, Vc, Vx, table, length, row_start, mask, O, lse))
     ws, nb = _ws(workspace)
-    _on_current([("Q", Q), ("O", O)] + [("workspace", workspace)] * bool(nb))
-    _check(_lib.wf_tree_attn(p, q, kc, kx, vc, vx, *a, o, l, ws, nb,
-                             _stream(stream)))
+    if workspace is not None and workspace.get_device() != Q.get_device():
+        raise ValueError(f"workspace is on {workspace.device}, Q on {Q.device}")
+    _check(_lib.wf_tree_attn(p, *a, ws, nb, _queue(stream)))
 
 
 def tree_attend(p: WfTreeParams, Q, pool, table, length, row_start=None,

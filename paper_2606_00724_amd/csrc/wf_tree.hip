@@ -492,72 +492,91 @@ __global__ __launch_bounds__(kBlock) void tree_merge_kernel(TreeArgs a) {
 
 static int merge_threads(int splits) { return splits <= 8 ? 1 : splits <= 32 ? 4 : 8; }
 
+// How a call's work is cut.  The cost of a choice in us, fitted to measured times.
+// A workgroup takes a block of query rows and a range of keys: a fixed part (its
+// first loads, its outputs) and its tiles, each at its products and softmax or at
+// its bytes, which come at 6 TB/s to all CUs and at 32 GB/s to one; and D floats a
+// query row and range are written and read where there are several ranges.
 TreePlan plan_tree(const wf_tree_params& p, size_t have) {
-  TreePlan l{};
   const bool bf = p.dtype == WF_BF16, quant = p.format != WF_CACHE_PLAIN;
   const int D = p.head_dim;
   const long M = (long)p.max_rows * p.group, U = (long)p.batch * p.heads;
   const long rows = (long)p.tokens * p.heads * p.group, cus = device_cu_count();
-  const int mb = kTileRows * D * (bf ? 2 : 4);  // bytes of a K (or V) tile
-  const int slots = 8 * mb > 131072 ? 2 : 4;
-  l.nw = bf && quant ? 8 : 4;
-  const long KT = l.nw == 8 ? 2 * kTileRows : kTileRows;
-  const long tiles = std::max(1L, (p.max_len + KT - 1) / KT);
   const double row_bytes = quant ? D * (p.format == WF_CACHE_E4M3 ? 1.0 : 0.5) + D / 32
                                  : D * (bf ? 2.0 : 4.0);
-  const double partial = (double)rows * D * 8 / 5e6;
-  const bool few = bf && quant && M <= 32;
+  // ranges are as many as the workspace holds partials for, and one at least
   const long most = (long)std::min<size_t>(have / (rows * (D + 2) * sizeof(float)), 1L << 30);
+  auto merge = [&](long s) { return s > 1 ? 4.0 + s * ((double)rows * D * 8 / 5e6) : 0.0; };
+  TreePlan best{};
   double least = 0;
+  auto take = [&](const TreePlan& l, long rps, double cost) {
+    if (least != 0 && cost >= least) return;
+    least = cost;
+    best = l;
+    best.rps = (int)rps;
+  };
+  bool few = bf, many = !bf || M > 32;
+  // Few query rows: 32 a workgroup of four waves, two workgroups a CU; the blocks of
+  // query rows read the same keys, mostly from the L2.
+  if (few) {
+    TreePlan l{};
+    l.few = true;
+    l.qw = 1;
+    l.nw = l.kw = 4;
+    l.mblocks = (int)((M + 31) / 32);
+    const long KT = 128, tiles = std::max(1L, (p.max_len + KT - 1) / KT);
+    const double alone = D / 128.0 * (!quant ? 1.0 : p.format == WF_CACHE_E4M3 ? 1.4 : 1.3);
+    const double both = D / 128.0 * 2.4;
+    for (long n = 1; n <= tiles; n += 1 + n / 16) {
+      const long per = (tiles + n - 1) / n, s = (tiles + per - 1) / per;
+      if (s > 1 && s > most) break;
+      const double groups = (double)(U * l.mblocks * s), per_cu = std::ceil(groups / cus);
+      const double at_once = std::min(per_cu, 2.0);
+      const double bytes = 2 * KT * row_bytes / std::min(l.mblocks, 3) *
+                           std::max(std::min(groups, at_once * cus) / 6e6, at_once / 32e3);
+      const double tile = std::max(per_cu > 1 ? both : alone, bytes);
+      // (lengths that differ leave some CUs idle at the end: a part of a workgroup's time)
+      take(l, per * KT,
+           std::max(1.0, per_cu / 2) * (per * tile + 6.0) + 0.2 * per * tile + merge(s));
+    }
+  }
+  // Many: a block of query rows for the workgroup, as of the attention over a prefix.
+  const int nw = bf && quant ? 8 : 4;
+  const long KT = nw == 8 ? 2 * kTileRows : kTileRows;
+  const long tiles = std::max(1L, (p.max_len + KT - 1) / KT);
   auto consider = [&](int qw, int qwaves, double block, double fixed) {
-    const long mblocks = (M + 32 * qw * qwaves - 1) / (32 * qw * qwaves);
-    const int kw = l.nw / qwaves;
-    const double products = (double)(KT / 32) / kw * D / 128.0 * block + fixed;
-    const long one = std::max(1L, cus / (U * mblocks));  // ranges that fill the chip once
+    TreePlan l{};
+    l.qw = qw;
+    l.nw = nw;
+    l.kw = nw / qwaves;
+    l.mblocks = (int)((M + 32 * qw * qwaves - 1) / (32 * qw * qwaves));
+    const double products = (double)(KT / 32) / l.kw * D / 128.0 * block + fixed;
+    const long one = std::max(1L, cus / (U * l.mblocks));  // ranges that fill the chip once
     auto ranges = [&](long n) {
       const long per = (tiles + n - 1) / n, s = (tiles + per - 1) / per;
       if (s > 1 && s > most) return;
-      const double groups = (double)(U * mblocks * s), at_once = std::min(groups, (double)cus);
-      const double bytes = 2 * KT * row_bytes * std::max(at_once / mblocks / 8e6, 1 / 32e3);
-      const double cost = std::ceil(groups / cus) * (per * std::max(products, bytes) + 5.0) +
-                          (s > 1 ? s * partial : 0.0);
-      if (least != 0 && cost >= least) return;
-      least = cost;
-      l.qw = qw;
-      l.kw = kw;
-      l.mblocks = (int)mblocks;
-      l.rps = (int)(per * KT);
+      const double groups = (double)(U * l.mblocks * s), at_once = std::min(groups, (double)cus);
+      const double bytes = 2 * KT * row_bytes * std::max(at_once / l.mblocks / 6e6, 1 / 32e3);
+      take(l, per * KT,
+           std::ceil(groups / cus) * (per * std::max(products, bytes) + 9.0) + merge(s));
     };
     for (long n = 1; n < std::min(one, tiles); n += 1 + n / 16) ranges(n);
     ranges(std::min(one, tiles));
     ranges(std::min(2 * one, tiles));
   };
-  if (few) {
-    l.few = true;
-    l.qw = l.mblocks = 1;
-    l.nw = l.kw = 4;
-    for (long n = 1; n <= tiles; n += 1 + n / 16) {
-      const long per = (tiles + n - 1) / n, s = (tiles + per - 1) / per;
-      if (s > 1 && s > most) break;
-      const double groups = (double)(U * s), at_once = std::min(groups, 2.0 * cus);
-      const double bytes = 2 * KT * row_bytes * std::max(at_once / 6e6, 1 / 20e3);
-      const double cost = std::ceil(groups / (2 * cus)) * (per * std::max(bytes, 0.7) + 5.0) +
-                          (s > 1 ? s * partial + 3.0 : 0.0);
-      if (least != 0 && cost >= least) continue;
-      least = cost;
-      l.rps = (int)(per * KT);
-    }
-  }
-  for (int qwaves = 2; !few && qwaves <= l.nw && (qwaves == 2 || 16 * qwaves < M); qwaves *= 2)
+  for (int qwaves = 2; many && qwaves <= nw && (qwaves == 2 || 16 * qwaves < M); qwaves *= 2)
     if (!bf)
       consider(1, qwaves, 4.2, quant ? 0.4 : 0.1);
     else if (quant)
       consider(1, qwaves, 0.875, 0.7);
     else
       consider(1, qwaves, 0.45, 0.1);
-  if (bf && !quant && M > 128) consider(2, l.nw, 0.82, 0.1);
+  if (many && bf && !quant && M > 128) consider(2, nw, 0.82, 0.1);
+  TreePlan l = best;
   l.splits = (int)std::max(1L, ((long)p.max_len + l.rps - 1) / l.rps);
   l.items = U * l.mblocks * l.splits;
+  const int mb = kTileRows * D * (bf ? 2 : 4);  // bytes of a K (or V) tile
+  const int slots = 8 * mb > 131072 ? 2 : 4;
   const int words = (p.max_rows + 31) / 32, mrows = l.nw / l.kw * 32 * l.qw;
   const size_t out = (size_t)l.nw * 32 * l.qw * (D + 6) * sizeof(float);
   l.lds_bytes = std::max((size_t)slots * 2 * mb + (kPageIds + 1) * sizeof(int32_t) +

@@ -20,23 +20,31 @@ constexpr int kFewWaves = 4;
 typedef int v2i_few __attribute__((ext_vector_type(2)));
 
 // A wave's ring.  Rows of a block stand after each other, their 16-byte chunks in an
-// order that lets eight rows at one chunk meet all banks.
+// order that lets the lanes that read at once meet all banks: eight rows at one chunk
+// of K, and of V eight rows (8 bits), sixteen (4 bits) or four at two chunks (bf16).
 template <int D, int FMT>
 struct FewGeom {
-  static constexpr int RB = FMT == WF_CACHE_E4M3 ? D : D / 2;  // bytes of a row
+  static constexpr bool QUANT = FMT != WF_CACHE_PLAIN;
+  static constexpr int RB = QUANT ? (FMT == WF_CACHE_E4M3 ? D : D / 2) : 2 * D;  // bytes of a row
   static constexpr int C = RB / 16;                            // chunks of a row
   static constexpr int KB = 32 * RB;                           // bytes of 32 rows
   static constexpr int NI = KB / 1024;                         // loads of 32 rows
+  static constexpr int RPI = 64 / C;                           // rows of a load
   static constexpr int XB = D / 32;                            // exponent bytes of a row
-  static constexpr int R = KB >= 4096 ? 2 : 4;                 // blocks of the ring
+  static constexpr int XL = QUANT ? 1 : 0;                     // loads of a block's exponents
+  static constexpr int R = KB >= 8192 ? 1 : KB >= 4096 ? 2 : 4;  // blocks of the ring
   static constexpr int XR = R + 1;  // a block's exponents outlive its keys
-  static constexpr int WAVE = R * 2 * KB + XR * 256;           // bytes of a wave
-  static constexpr int BI = 2 * NI + 1;                        // loads of a block
+  static constexpr int WAVE = R * 2 * KB + XL * XR * 256;      // bytes of a wave
+  static constexpr int BI = 2 * NI + XL;                       // loads of a block
   // place of row r's chunk c
   __device__ __forceinline__ static constexpr int swz(int r) {
-    return C == 8 ? r & 7 : C == 4 ? (r >> 1) & 3 : (r >> 2) & 1;
+    return C >= 8 ? r & 7 : C == 4 ? (r >> 1) & 3 : (r >> 2) & 1;
+  }
+  __device__ __forceinline__ static constexpr int vswz(int r) {
+    return QUANT ? swz(r) : (r & 3) << 1;
   }
   __device__ __forceinline__ static int at(int r, int c) { return r * RB + 16 * (c ^ swz(r)); }
+  __device__ __forceinline__ static int vat(int r, int c) { return r * RB + 16 * (c ^ vswz(r)); }
 };
 
 template <int N>
@@ -58,11 +66,23 @@ __device__ __forceinline__ V lds_read(uint32_t at) {
   return *(const __attribute__((address_space(3))) V*)(size_t)at;
 }
 
+// The bits of those values of a word that are no numbers.
+template <int FMT>
+__device__ __forceinline__ uint32_t odd_bits(uint32_t w) {
+  uint32_t odd = 0;
+  constexpr int B = FMT == WF_CACHE_PLAIN ? 16 : 8;
+  constexpr uint32_t top = FMT == WF_CACHE_PLAIN ? 0x7f80u : 0x7fu, all = (1u << B) - 1u;
+#pragma unroll
+  for (int k = 0; k < 32; k += B) odd |= (w >> k & top) == top ? all << k : 0u;
+  return odd;
+}
+
 template <int D, int FMT>
 __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(TreeArgs a) {
   using G = FewGeom<D, FMT>;
   using W = PrefixWave<bf16_t, D, 1>;
   constexpr int NI = G::NI, R = G::R, RB = G::RB, KB = G::KB, XB = G::XB, DT = D / 32;
+  constexpr bool QUANT = G::QUANT;
   extern __shared__ __align__(16) unsigned char smem[];  // the waves' rings, a flag
   int* flag = reinterpret_cast<int*>(smem + kFewWaves * G::WAVE);
   const int lane = threadIdx.x & 63;
@@ -71,12 +91,13 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(TreeArgs a)
 
   const int item = xcd_swizzle(blockIdx.x, gridDim.x);
   if (item >= a.items) return;  // (the grid holds whole eights of them)
-  const int sp = item % a.splits, unit = item / a.splits;
+  const int mb = item % a.mblocks, sp = item / a.mblocks % a.splits;
+  const int unit = item / (a.mblocks * a.splits);
   const int head = unit % a.heads, seq = unit / a.heads;
   const Sequence s(a, seq);
-  const int M = s.n * a.g;
+  const int M = s.n * a.g, m0 = 32 * mb;
   const int k0 = sp * a.rps, nk = min(a.rps, s.L - k0);  // the range's keys
-  if (M <= 0 || (nk <= 0 && !a.whole)) return;
+  if (m0 >= M || (nk <= 0 && !a.whole)) return;
   W w;
   w.init(a.scale);
   if (threadIdx.x == 0) *flag = 0;
@@ -99,26 +120,39 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(TreeArgs a)
     const uint32_t ring = lds_offset(smem) + wave * G::WAVE, exps = ring + R * 2 * KB;
     // the lane's 16 bytes of a load: row of those that it holds, chunk
     const int lrow = lane / G::C;
-    const uint32_t off = lrow * RB + 16 * (lane % G::C ^ G::swz(lrow));
+    const uint32_t koff[2] = {(uint32_t)(lrow * RB + 16 * (lane % G::C ^ G::swz(lrow))),
+                              (uint32_t)(lrow * RB + 16 * (lane % G::C ^ G::swz(lrow + G::RPI)))};
+    const uint32_t voff[2] = {(uint32_t)(lrow * RB + 16 * (lane % G::C ^ G::vswz(lrow))),
+                              (uint32_t)(lrow * RB + 16 * (lane % G::C ^ G::vswz(lrow + G::RPI)))};
     // the lane's 4 bytes of the exponents: K's of the 32 rows, then V's (again in the
     // lanes behind them)
     constexpr int XD = 8 * XB;
     const int xl = lane % (2 * XD), xg = xl % XD / (XD / 2);
     const uint8_t* xbase = (xl / XD ? a.Vx : a.Kx) + 4 * (xl % (XD / 2));
     // block i's loads: 32 rows of K or V from r0 and r1 on
-    auto load = [&](const void* P, long r0, long r1, uint32_t lds) __attribute__((always_inline)) {
+    auto load = [&](const void* P, long r0, long r1, uint32_t lds, const uint32_t(&off)[2])
+                    __attribute__((always_inline)) {
       const unsigned char* b0 = static_cast<const unsigned char*>(P) + r0 * RB;
       const unsigned char* b1 = static_cast<const unsigned char*>(P) + r1 * RB;
-      if constexpr (G::C == 8) {
-        tile_load<0, 0>(b0, off, lds);
-        tile_load<1024, 1024>(b0, off, lds);
-        tile_load<0, 2048>(b1, off, lds);
-        tile_load<1024, 3072>(b1, off, lds);
+      if constexpr (G::C == 16) {  // four rows a load
+        tile_load<0, 0>(b0, off[0], lds);
+        tile_load<1024, 1024>(b0, off[1], lds);
+        tile_load<2048, 2048>(b0, off[0], lds);
+        tile_load<3072, 3072>(b0, off[1], lds);
+        tile_load<0, 4096>(b1, off[0], lds);
+        tile_load<1024, 5120>(b1, off[1], lds);
+        tile_load<2048, 6144>(b1, off[0], lds);
+        tile_load<3072, 7168>(b1, off[1], lds);
+      } else if constexpr (G::C == 8) {
+        tile_load<0, 0>(b0, off[0], lds);
+        tile_load<1024, 1024>(b0, off[0], lds);
+        tile_load<0, 2048>(b1, off[0], lds);
+        tile_load<1024, 3072>(b1, off[0], lds);
       } else if constexpr (G::C == 4) {
-        tile_load<0, 0>(b0, off, lds);
-        tile_load<0, 1024>(b1, off, lds);
+        tile_load<0, 0>(b0, off[0], lds);
+        tile_load<0, 1024>(b1, off[0], lds);
       } else {
-        row_load<0>((lane < 32 ? b0 : b1 - 16 * RB) + off, lds);
+        row_load<0>((lane < 32 ? b0 : b1 - 16 * RB) + off[0], lds);
       }
     };
     auto exp_load = [&](long r0, long r1, uint32_t lds) __attribute__((always_inline)) {
@@ -128,12 +162,14 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(TreeArgs a)
     int xin = 0, xout = 0;
     auto next = [&](int x) { return x + 1 == G::XR ? 0 : x + 1; };
     auto queue_keys = [&](int i, long r0, long r1) __attribute__((always_inline)) {
-      load(a.K, r0, r1, ring + i % R * 2 * KB);
-      exp_load(r0, r1, exps + xin * 256);
-      xin = next(xin);
+      load(a.K, r0, r1, ring + i % R * 2 * KB, koff);
+      if constexpr (QUANT) {
+        exp_load(r0, r1, exps + xin * 256);
+        xin = next(xin);
+      }
     };
     auto queue_vals = [&](int i, long r0, long r1) __attribute__((always_inline)) {
-      load(a.V, r0, r1, ring + i % R * 2 * KB + KB);
+      load(a.V, r0, r1, ring + i % R * 2 * KB + KB, voff);
     };
 
     {
@@ -142,7 +178,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(TreeArgs a)
       queue_vals(0, r0, r1);
     }
     // the lane's query row: channels h D / 2 + 8 j of step j
-    const int m = min(l32, M - 1), ti = a.by_g(m);
+    const int m = min(m0 + l32, M - 1), ti = a.by_g(m);
     const long tok = min(max(s.first + ti, 0L), a.tokens - 1L);
     {
       const u32x4* src = reinterpret_cast<const u32x4*>(static_cast<const bf16_t*>(a.Q) + tok * a.qs +
@@ -181,17 +217,20 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(TreeArgs a)
 #pragma unroll
       for (int e = 0; e < 16; ++e) sc[e] = 0.f;
       {
-        constexpr int HC = G::C / 2 > 0 ? G::C / 2 : 1;  // chunks of a lane
+        constexpr int HC = G::C / 2;  // chunks of a lane
         u32x4 kc[HC];
 #pragma unroll
         for (int c = 0; c < HC; ++c) kc[c] = lds_read<u32x4>(kat + G::at(l32, h * HC + c));
-        const uint32_t kx = XB == 4 ? lds_read<uint32_t>(xat + 4 * l32) >> (16 * h)
-                                    : lds_read<uint8_t>(xat + 2 * l32 + h);
+        const uint32_t kx = !QUANT   ? 0u
+                            : XB == 4 ? lds_read<uint32_t>(xat + 4 * l32) >> (16 * h)
+                                      : lds_read<uint8_t>(xat + 2 * l32 + h);
 #pragma unroll
         for (int j = 0; j < W::QS; ++j) {
           const float scale = block_scale(j < 4 ? kx & 0xff : kx >> 8 & 0xff);
           u32x4 kf;
-          if constexpr (FMT == WF_CACHE_E4M3) {
+          if constexpr (!QUANT) {
+            kf = kc[j];
+          } else if constexpr (FMT == WF_CACHE_E4M3) {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
               const uint32_t c = kc[j / 2][2 * (j & 1) + e];
@@ -248,12 +287,12 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(TreeArgs a)
       w.l[0] += z;
 
       if (ahead == R)
-        wait_loads<(R - 1) * G::BI + NI + 1>();
+        wait_loads<(R - 1) * G::BI + NI + G::XL>();
       else if (R == 4 && ahead == 3)
         wait_loads<3 * G::BI>();
       else if (R == 4 && ahead == 2)
         wait_loads<2 * G::BI>();
-      else if (ahead == 1)
+      else if (R > 1 && ahead == 1)
         wait_loads<G::BI>();
       else
         wait_loads<0>();
@@ -264,111 +303,132 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(TreeArgs a)
               u32x4{0u, 0u, 0u, 0u};
       }
       // Values that are no numbers: a block of channels with the exponent byte 255, and
-      // in 8 bits codes of NaN.  Such codes are cleared where not all rows see them; all
-      // are put to the rows that see them behind the last block.
-      bool odd;
-      {
+      // in 8 bits codes of NaN, or NaN and infinities in bf16.  The latter are cleared
+      // where not all rows see them; all are put to the rows that see them behind the
+      // last block.
+      bool odd = false;
+      if constexpr (QUANT) {
         uint32_t x = XB == 4 ? lds_read<uint32_t>(vx + 4 * l32) : lds_read<uint16_t>(vx + 2 * l32);
         x = ~x & (XB == 4 ? ~0u : 0xffffu);
         x |= XB == 4 ? 0u : 0xffff0000u;
         odd = l32 < nv && ((x - 0x01010101u) & ~x & 0x80808080u) != 0;
-        if (FMT == WF_CACHE_E4M3 && masked)
-          for (int c = lane; c < nv * G::C; c += 64) {
-            const u32x4 v = lds_read<u32x4>(vat + 16 * c);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const uint32_t y = ~v[e] & 0x7f7f7f7fu;
-              odd |= ((y - 0x01010101u) & ~y & 0x80808080u) != 0;
-            }
-          }
       }
+      if (FMT != WF_CACHE_E2M1 && masked)
+        for (int c = lane; c < nv * G::C; c += 64) {
+          const u32x4 v = lds_read<u32x4>(vat + 16 * c);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) odd |= odd_bits<FMT>(v[e]) != 0;
+        }
       if (__builtin_amdgcn_ballot_w64(odd) != 0) {  // rare
         if (lane == 0) *flag = 1;
-        if constexpr (FMT == WF_CACHE_E4M3)
+        if constexpr (FMT != WF_CACHE_E2M1)
           for (int c = lane; c < 32 * G::C; c += 64) {
             u32x4 v = lds_read<u32x4>(vat + 16 * c);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-#pragma unroll
-              for (int k = 0; k < 32; k += 8)
-                if ((v[e] >> k & 0x7f) == 0x7f) v[e] &= ~(0xffu << k);
+            for (int e = 0; e < 4; ++e) v[e] &= ~odd_bits<FMT>(v[e]);
             *(__attribute__((address_space(3))) u32x4*)(size_t)(vat + 16 * c) = v;
           }
       }
-      // exponents of the lane's 16 keys, less 128 (the weights are doubled for it)
-      uint32_t xs[16 * XB / 4];
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        if constexpr (XB == 4) {
-          const u32x4 x = lds_read<u32x4>(vx + (8 * q + 4 * h) * 4);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) xs[4 * q + e] = x[e] ^ 0x80808080u;
-        } else {
-          const u32x2 x = lds_read<u32x2>(vx + (8 * q + 4 * h) * 2);
-          xs[2 * q] = x[0] ^ 0x80808080u;
-          xs[2 * q + 1] = x[1] ^ 0x80808080u;
-        }
-      }
-#pragma unroll
-      for (int e = 0; e < 16; ++e) t[e] += t[e];
-      // weight of key e (of the lane's 16) for channels 32 d ..: times 2^(x - 127)
-      auto weight = [&](int e, int d) __attribute__((always_inline)) {
-        const int b = e * XB + d;
-        return __builtin_amdgcn_ldexpf(t[e], (int)(xs[b / 4] << (24 - 8 * (b & 3))) >> 24);
-      };
-      // the lane's place in a transposed load: in 8 bits row e of eight and half of its 16
-      // channels, in 4 bits row e of sixteen
+      // the lane's place in a transposed load: a part of a row of eight in 8 bits, of
+      // sixteen in 4 bits, of four in bf16, each of 16 channels
       const int i16 = lane & 15, half = (lane >> 4) & 1;
-      const int p = FMT == WF_CACHE_E4M3 ? i16 >> 1 : i16;
+      const int p = FMT == WF_CACHE_E4M3 ? i16 >> 1 : FMT == WF_CACHE_E2M1 ? i16 : i16 >> 2;
       const int vrow = 16 * (p >> 3) + 8 * (p >> 2 & 1) + 4 * h + (p & 3);
-      uint32_t vb = vat + (FMT == WF_CACHE_E4M3 ? G::at(vrow, half) + 8 * (i16 & 1)
-                                                : G::at(vrow, 0) + 8 * half);
+      uint32_t vb = vat + (FMT == WF_CACHE_E4M3   ? G::vat(vrow, half) + 8 * (i16 & 1)
+                           : FMT == WF_CACHE_E2M1 ? G::vat(vrow, 0) + 8 * half
+                                                  : G::vat(vrow, 2 * half + (i16 >> 1 & 1)) + 8 * (i16 & 1));
       asm volatile("" : "+v"(vb));
-      if constexpr (FMT == WF_CACHE_E4M3) {
+      if constexpr (!QUANT) {
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
+          u32x4 pf;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) pf[e] = pack_bf16x2(t[8 * kb + 2 * e], t[8 * kb + 2 * e + 1]);
 #pragma unroll
           for (int d = 0; d < DT; ++d) {
-            const v2i_few c = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-                (__attribute__((address_space(3))) v2i_few*)(size_t)((vb ^ (32 * d)) + kb * 16 * RB));
-            u32x4 vf, pf;
+            u32x4 vf;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              vf[2 * e] = __builtin_bit_cast(
-                  uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[e], 1.0f, false));
-              vf[2 * e + 1] = __builtin_bit_cast(
-                  uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[e], 1.0f, true));
+            for (int k = 0; k < 2; ++k) {
+              const u32x2 x = __builtin_bit_cast(
+                  u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                             (__attribute__((address_space(3))) v4i16p*)(size_t)(
+                                 (vb ^ (64 * d)) + (2 * kb + k) * 8 * RB)));
+              vf[2 * k] = x[0];
+              vf[2 * k + 1] = x[1];
             }
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              pf[e] = pack_bf16x2(weight(8 * kb + 2 * e, d), weight(8 * kb + 2 * e + 1, d));
             w.O[0][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf),
                                                                 __builtin_bit_cast(bf16x8, pf),
                                                                 w.O[0][d], 0, 0, 0);
           }
         }
       } else {
+        // exponents of the lane's 16 keys, less 128 (the weights are doubled for it)
+        uint32_t xs[16 * XB / 4];
 #pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          const v2i_few c = __builtin_amdgcn_ds_read_tr4_b64_v2i32(
-              (__attribute__((address_space(3))) v2i_few*)(size_t)(vb ^ (16 * d)));
+        for (int q = 0; q < 4; ++q) {
+          if constexpr (XB == 4) {
+            const u32x4 x = lds_read<u32x4>(vx + (8 * q + 4 * h) * 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) xs[4 * q + e] = x[e] ^ 0x80808080u;
+          } else {
+            const u32x2 x = lds_read<u32x2>(vx + (8 * q + 4 * h) * 2);
+            xs[2 * q] = x[0] ^ 0x80808080u;
+            xs[2 * q + 1] = x[1] ^ 0x80808080u;
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) t[e] += t[e];
+        // weight of key e (of the lane's 16) for channels 32 d ..: times 2^(x - 127)
+        auto weight = [&](int e, int d) __attribute__((always_inline)) {
+          const int b = e * XB + d;
+          return __builtin_amdgcn_ldexpf(t[e], (int)(xs[b / 4] << (24 - 8 * (b & 3))) >> 24);
+        };
+        if constexpr (FMT == WF_CACHE_E4M3) {
 #pragma unroll
           for (int kb = 0; kb < 2; ++kb) {
-            u32x4 vf, pf;
-            vf[0] = __builtin_bit_cast(uint32_t,
-                                       __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[kb], 1.0f, 0));
-            vf[1] = __builtin_bit_cast(uint32_t,
-                                       __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[kb], 1.0f, 1));
-            vf[2] = __builtin_bit_cast(uint32_t,
-                                       __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[kb], 1.0f, 2));
-            vf[3] = __builtin_bit_cast(uint32_t,
-                                       __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[kb], 1.0f, 3));
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              pf[e] = pack_bf16x2(weight(8 * kb + 2 * e, d), weight(8 * kb + 2 * e + 1, d));
-            w.O[0][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf),
-                                                                __builtin_bit_cast(bf16x8, pf),
-                                                                w.O[0][d], 0, 0, 0);
+            for (int d = 0; d < DT; ++d) {
+              const v2i_few c = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                  (__attribute__((address_space(3))) v2i_few*)(size_t)((vb ^ (32 * d)) + kb * 16 * RB));
+              u32x4 vf, pf;
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                vf[2 * e] = __builtin_bit_cast(
+                    uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[e], 1.0f, false));
+                vf[2 * e + 1] = __builtin_bit_cast(
+                    uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[e], 1.0f, true));
+              }
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                pf[e] = pack_bf16x2(weight(8 * kb + 2 * e, d), weight(8 * kb + 2 * e + 1, d));
+              w.O[0][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf),
+                                                                  __builtin_bit_cast(bf16x8, pf),
+                                                                  w.O[0][d], 0, 0, 0);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int d = 0; d < DT; ++d) {
+            const v2i_few c = __builtin_amdgcn_ds_read_tr4_b64_v2i32(
+                (__attribute__((address_space(3))) v2i_few*)(size_t)(vb ^ (16 * d)));
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+              u32x4 vf, pf;
+              vf[0] = __builtin_bit_cast(uint32_t,
+                                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[kb], 1.0f, 0));
+              vf[1] = __builtin_bit_cast(uint32_t,
+                                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[kb], 1.0f, 1));
+              vf[2] = __builtin_bit_cast(uint32_t,
+                                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[kb], 1.0f, 2));
+              vf[3] = __builtin_bit_cast(uint32_t,
+                                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[kb], 1.0f, 3));
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                pf[e] = pack_bf16x2(weight(8 * kb + 2 * e, d), weight(8 * kb + 2 * e + 1, d));
+              w.O[0][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf),
+                                                                  __builtin_bit_cast(bf16x8, pf),
+                                                                  w.O[0][d], 0, 0, 0);
+            }
           }
         }
       }
@@ -384,15 +444,15 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(TreeArgs a)
   out.put(w, wave);
   constexpr int C4 = D / 4, RPP = 64 * kFewWaves / C4;  // rows per round
   const int c = threadIdx.x % C4;
-  for (int r = threadIdx.x / C4; r < M; r += RPP) {
+  for (int r = threadIdx.x / C4; r < min(32, M - m0); r += RPP) {
     const int v[1] = {r};
     Merge4 g[1];
     out.merged(v, kFewWaves, c, g);
-    const int i = a.by_g(r);
+    const int i = a.by_g(m0 + r);
     const long tok = s.first + i;
     if (!Sequence::there(a, tok)) continue;
     if (odd) add_odd<bf16_t, D, FMT>(a, s, seq, head, i, k0, k0 + nk, 4 * c, g[0].o);
-    const int hq = head * a.g + r - i * a.g;
+    const int hq = head * a.g + m0 + r - i * a.g;
     const long row = tok * a.hq + hq;
     if (a.whole) {
       g[0].finish(static_cast<bf16_t*>(a.O) + tok * a.os + (long)hq * D + 4 * c,
@@ -429,11 +489,12 @@ hipError_t launch_tree_few(const TreeArgs& a, int head_dim, int format, long ite
   };
   using D64 = std::integral_constant<int, 64>;
   using D128 = std::integral_constant<int, 128>;
-  using E4 = std::integral_constant<int, WF_CACHE_E4M3>;
-  using E2 = std::integral_constant<int, WF_CACHE_E2M1>;
-  if (head_dim == 128)
-    return format == WF_CACHE_E4M3 ? go(D128{}, E4{}) : go(D128{}, E2{});
-  return format == WF_CACHE_E4M3 ? go(D64{}, E4{}) : go(D64{}, E2{});
+  auto by_format = [&](auto d) {
+    if (format == WF_CACHE_E4M3) return go(d, std::integral_constant<int, WF_CACHE_E4M3>{});
+    if (format == WF_CACHE_E2M1) return go(d, std::integral_constant<int, WF_CACHE_E2M1>{});
+    return go(d, std::integral_constant<int, WF_CACHE_PLAIN>{});
+  };
+  return head_dim == 128 ? by_format(D128{}) : by_format(D64{});
 }
 
 }  // namespace wf

@@ -136,7 +136,7 @@ def test_binding_refuses_what_the_parameters_do_not_describe():
     X, pos, f = torch.zeros((2, 3, 5, 64)).bfloat16(), torch.zeros((1, 2, 5)).int(), torch.ones(32)
     for bad, err in ((dict(X=X.float()), TypeError), (dict(X=X[:, :, :4]), ValueError),
                      (dict(X=X.transpose(0, 1).contiguous().transpose(0, 1)), ValueError),
-                     (dict(Y=X[:, :, :, ::2]), ValueError), (dict(Y=None), TypeError),
+                     (dict(Y=X[:, :, :, ::2]), ValueError), (dict(Y=None), ValueError),
                      (dict(X=torch.zeros(1).bfloat16().expand(2, 3, 5, 64)), ValueError),
                      (dict(pos=pos.long()), TypeError), (dict(f=f[:31]), ValueError),
                      (dict(), ValueError)):  # (the last: tensors of the host)
@@ -154,7 +154,7 @@ def test_binding_refuses_what_the_parameters_do_not_describe():
               V=torch.zeros((5, 2, 64)).bfloat16(), pos=torch.zeros((1, 5)).int(), f=f,
               slot=torch.zeros(5).int(), Kc=Kc, Kx=Kx, Vc=Vc, Vx=Vx,
               Qr=torch.zeros((5, 4, 64)).bfloat16())
-    for bad, err in ((dict(Q=None), TypeError), (dict(K=ok["K"].float()), TypeError),
+    for bad, err in ((dict(Q=None), ValueError), (dict(K=ok["K"].float()), TypeError),
                      (dict(V=ok["Q"][:, :2]), ValueError), (dict(slot=None), ValueError),
                      (dict(Kx=None), ValueError), (dict(Kc=Kc[:3]), ValueError),
                      (dict(Vx=Kc), ValueError), (dict(Qr=ok["K"]), ValueError),
