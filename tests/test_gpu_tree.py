@@ -26,18 +26,21 @@ class Case:
     """A pool, its sequences and their query rows, on the CPU."""
 
     def __init__(self, wf, *, lens, counts=None, rows=1, heads=2, group=1, d=64, P=16, dtype="bf16",
-                 fmt=None, mask="tree", spare=0, seed=1, max_len=None, scale=0.0, bad=False):
+                 fmt=None, mask="tree", spare=0, seed=1, max_len=None, scale=0.0, pool_pages=None):
         g = torch.Generator().manual_seed(seed)
         b = len(lens)
         self.fmt, self.dtype, self.scale = fmt, dtype, scale or 1 / math.sqrt(d)
-        tp = max(1, -(-max(lens) // P)) + (1 if bad else 0)
-        pages = b * tp + 2
+        tp = max(1, -(-max(max(lens), max_len or 0) // P))
+        pages = pool_pages or b * tp + 2
         tokens = (b * rows if counts is None else sum(counts)) + spare
         self.p = wf.make_tree_params(pages=pages, page_rows=P, heads=heads, head_dim=d, batch=b,
                                      tokens=tokens, max_rows=rows, table_pages=tp, group=group,
                                      max_len=max_len, dtype=dtype, format=fmt,
                                      causal=mask == "causal", scale=scale)
-        self.table = torch.randperm(pages, generator=g)[:b * tp].view(b, tp).int()
+        if pool_pages:                      # (sequences share pages)
+            self.table = torch.randint(0, pages, (b, tp), generator=g).int()
+        else:
+            self.table = torch.randperm(pages, generator=g)[:b * tp].view(b, tp).int()
         for i, L in enumerate(lens):        # behind the last page: anything
             self.table[i, max(0, -(-L // P)):] = [-1, 2 ** 31 - 1, -2 ** 31, pages][i % 4]
         shape = (pages, heads, P)
@@ -157,46 +160,84 @@ def test_pages_of_more_keys_than_are_in_lds_at_once(wf):
             c.check(c.run(wf, ws=None))
 
 
+def poison(c, where, fmt, rows):
+    """NaN and infinities in three new rows of each sequence (of `rows` at
+    least), in rows behind the last one, and in the pages of no sequence."""
+    m, P = 0 if where == "K" else 2, c.p.page_rows
+    x = c.pool[m] if fmt is None else c.pool[m + 1]
+    bad, used = 255 if fmt else math.nan, set()
+    for b, L in enumerate(c.len.tolist()):
+        used |= {int(c.table[b, t]) for t in range(-(-L // P))}
+    for b, L in enumerate(c.len.tolist()):
+        if L == 0:
+            continue
+        for t in range(L, -(-L // P) * P):
+            x[int(c.table[b, t // P]), :, t % P] = bad
+        for j, v in ((2, math.inf), (5, math.nan), (7, -math.inf)):
+            t = L - rows + j
+            row = x[int(c.table[b, t // P]), :, t % P]
+            row[:, 1 if fmt else 40] = 255 if fmt else v
+            if where == "V" and fmt is None:
+                row[:, 41] = math.inf
+            if where == "V" and fmt == "e4m3":      # a code of NaN, too
+                c.pool[2][int(c.table[b, t // P]), :, t % P, 3] = 0x7f
+    for page in range(c.p.pages):
+        if page not in used:
+            x[page] = bad
+
+
+def check_poisoned(c, got, where):
+    """As check; for keys: rows that see a NaN key are NaN, the others as ever."""
+    if where == "V":
+        return c.check(got)
+    O, lse = got
+    wO, wl, tol, ltol = c.want()
+    clean = wl.isfinite() & ~wO.isnan().any(-1)
+    assert 5 < int(clean.sum()) < clean.numel() - 5
+    assert ((O.double() - wO).abs() <= tol)[clean].all()
+    assert ((lse.double() - wl).abs() <= ltol)[clean].all()
+    dirty = wl.isnan() & (O != 7).any(-1)
+    assert lse[dirty].isnan().all()
+
+
 @pytest.mark.parametrize("dtype,fmt", FORMATS)
 @pytest.mark.parametrize("where", ["K", "V"])
 def test_hidden_rows_may_hold_anything(wf, dtype, fmt, where):
-    """NaN and infinities in new rows that some rows see and others do not, in
-    rows behind the last one, and in a page of no sequence."""
     for group in (1, 20):
         c = Case(wf, lens=[90, 70, 64], rows=9, dtype=dtype, fmt=fmt, d=128, group=group, P=16,
                  seed=3)
-        m = 0 if where == "K" else 2
-        x = c.pool[m] if fmt is None else c.pool[m + 1]
-        used = set()
-        for b, L in enumerate([90, 70, 64]):
-            for t in range(L, -(-L // 16) * 16):            # behind the last row
-                x[int(c.table[b, t // 16]), :, t % 16] = 255 if fmt else math.nan
-            used |= {int(c.table[b, t]) for t in range(-(-L // 16))}
-            for j, v in ((2, math.inf), (5, math.nan), (7, -math.inf)):
-                t = L - 9 + j
-                row = x[int(c.table[b, t // 16]), :, t % 16]
-                row[:, 1 if fmt else 40] = 255 if fmt else v
-                if where == "V" and fmt is None:
-                    row[:, 41] = math.inf
-        for page in range(c.p.pages):
-            if page not in used:
-                x[page] = 255 if fmt else math.nan
-        # no weight of a visible infinite value is 0: scores lie within 30 of each other
-        O, lse = c.run(wf)
-        if where == "V":
-            c.check((O, lse))
-            continue
-        # rows that see a NaN key are NaN; the others are as ever
-        clean = torch.ones(len(c.Q), dtype=torch.bool)
-        for at in range(len(c.Q)):
-            b, i = divmod(at, 9)
-            L = int(c.len[b])
-            s = pageref.sees(i, 9, L, c.mask[at])
-            clean[at] = not any(s[L - 9 + j] for j in (2, 5, 7))
-        assert 5 < int(clean.sum()) < len(clean) - 5
-        wO, wl, tol, ltol = c.want()
-        assert ((O.double() - wO).abs() <= tol)[clean].all()
-        assert ((lse.double() - wl).abs() <= ltol)[clean].all()
+        poison(c, where, fmt, 9)
+        check_poisoned(c, c.run(wf), where)
+
+
+# sequences, K/V heads, most rows, group, most keys, channels -> query rows of a
+# workgroup, with several ranges of the keys or one (the lengths are far below)
+FORMS = [(16, 1, 17, 3, 16000, 128, 64, True), (16, 8, 33, 2, 1000, 64, 64, False),
+         (16, 1, 33, 2, 16000, 64, 128, True), (64, 1, 100, 3, 300, 128, 128, False),
+         (16, 2, 64, 3, 16000, 128, 256, True), (16, 8, 100, 3, 300, 64, 256, False)]
+
+
+@pytest.mark.parametrize("dtype,fmt", FORMATS)
+@pytest.mark.parametrize("b,h,rows,g,most,d,block,ranges", FORMS)
+@pytest.mark.parametrize("bad", [None, "K", "V"])
+def test_every_form_of_the_kernel_of_many_rows(wf, dtype, fmt, b, h, rows, g, most, d, block,
+                                               ranges, bad):
+    lens, counts = [0] * b, [0] * b
+    for i, (L, n) in enumerate(((290, rows), (130, 9), (300, 12))):
+        lens[5 * i], counts[5 * i] = L, n
+    c = Case(wf, lens=lens, counts=counts, rows=rows, heads=h, group=g, d=d, P=16, dtype=dtype,
+             fmt=fmt, max_len=most, pool_pages=60, seed=4)
+    s = wf.tree_plan(c.p)
+    if dtype == "bf16" and not (fmt and block == 64 and h == 8):
+        assert (s.group_rows, s.ranges > 1) == (block, ranges)
+    if bad:
+        c.table = (torch.randperm(57)[:57].repeat(b * 20)[:b * c.table.shape[1]]
+                   .view(b, -1) % 57).int()
+        for i in (0, 5, 10):                # their own pages, and three of nobody's
+            c.table[i, :19] = torch.arange(19).int() + 19 * (i // 5)
+        poison(c, bad, fmt, 9)
+    got = c.run(wf)
+    check_poisoned(c, got, bad) if bad else c.check(got)
 
 
 def test_strides_of_fused_rows(wf):
