@@ -1532,8 +1532,8 @@ wf_status wf_tree_plan(const wf_tree_params* p, size_t workspace_bytes, wf_prefi
   TreePlan plan;
   WF_TRY(check_tree(p, workspace_bytes, &plan));
   if (!split) return fail(WF_ERR_INVALID_ARG, "split is NULL");
-  *split = wf_prefix_split{plan.splits, plan.rps, plan.nw / plan.kw * 32 * plan.qw, 32 * plan.qw,
-                           plan.kw};
+  const int wave = plan.few ? plan.few : 32 * plan.qw;
+  *split = wf_prefix_split{plan.splits, plan.rps, plan.nw / plan.kw * wave, wave, plan.kw};
   return ok();
 }
 

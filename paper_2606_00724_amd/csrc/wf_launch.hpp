@@ -350,7 +350,7 @@ struct TreeArgs;
 struct TreePlan {
   long items;                      // workgroups
   int splits, rps, mblocks, nw, kw, qw;
-  bool few;                        // the kernel of few query rows over codes
+  int few;                         // query rows of the kernel of few of them, or 0
   long merges;                     // workgroups of the merge (0: none)
   size_t lds_bytes;
   size_t part_bytes, pstat_bytes;  // workspace (0: no partials)

@@ -520,13 +520,13 @@ TreePlan plan_tree(const wf_tree_params& p, size_t have) {
   // query rows read the same keys, mostly from the L2.
   if (few) {
     TreePlan l{};
-    l.few = true;
+    l.few = M <= 16 ? 16 : 32;
     l.qw = 1;
     l.nw = l.kw = 4;
-    l.mblocks = (int)((M + 31) / 32);
+    l.mblocks = (int)((M + l.few - 1) / l.few);
     const long KT = 128, tiles = std::max(1L, (p.max_len + KT - 1) / KT);
-    const double alone = D / 128.0 * (!quant ? 1.0 : p.format == WF_CACHE_E4M3 ? 1.4 : 1.3);
-    const double both = D / 128.0 * 2.4;
+    const double alone = D / 128.0 * (!quant || l.few == 16 ? 1.0 : 1.4);
+    const double both = D / 128.0 * (l.few == 16 ? 1.3 : 2.4);
     for (long n = 1; n <= tiles; n += 1 + n / 16) {
       const long per = (tiles + n - 1) / n, s = (tiles + per - 1) / per;
       if (s > 1 && s > most) break;
@@ -629,7 +629,7 @@ hipError_t launch_tree(const wf_tree_params& p, const TreePlan& l, TreeArgs& a, 
     };
     hipError_t e = hipErrorInvalidValue;
     if (l.few)
-      e = launch_tree_few(a, D, p.format, l.items, s);
+      e = launch_tree_few(a, D, p.format, l.few, l.items, s);
     else if (p.format == WF_CACHE_E4M3)
       e = go(tree_attn_kernel<T, D, WF_CACHE_E4M3, 1>);
     else if (p.format == WF_CACHE_E2M1)

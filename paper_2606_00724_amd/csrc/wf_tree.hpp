@@ -79,6 +79,8 @@ __device__ __forceinline__ void add_odd(const TreeArgs& a, const Sequence& s, in
   }
 }
 
-hipError_t launch_tree_few(const TreeArgs& a, int head_dim, int format, long items, hipStream_t s);
+// (rows: query rows of a workgroup, 16 or 32)
+hipError_t launch_tree_few(const TreeArgs& a, int head_dim, int format, int rows, long items,
+                           hipStream_t s);
 
 }  // namespace wf

@@ -77,17 +77,392 @@ __device__ __forceinline__ uint32_t odd_bits(uint32_t w) {
   return odd;
 }
 
+// Eight codes to the operand of a product, times `scale`: two words in 8 bits, one in 4.
+template <int FMT>
+__device__ __forceinline__ u32x4 operand(uint32_t c0, uint32_t c1, float scale) {
+  u32x4 v;
+  auto bits = [](auto x) { return __builtin_bit_cast(uint32_t, x); };
+  if constexpr (FMT == WF_CACHE_E4M3) {
+    v[0] = bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c0, scale, false));
+    v[1] = bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c0, scale, true));
+    v[2] = bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c1, scale, false));
+    v[3] = bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c1, scale, true));
+  } else {
+    v[0] = bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c0, scale, 0));
+    v[1] = bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c0, scale, 1));
+    v[2] = bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c0, scale, 2));
+    v[3] = bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c0, scale, 3));
+  }
+  return v;
+}
+__device__ __forceinline__ u32x2 read_tr16(uint32_t at) {
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                       (__attribute__((address_space(3))) v4i16p*)(size_t)at));
+}
+template <int FMT>
+__device__ __forceinline__ u32x2 read_codes(uint32_t at) {
+  auto p = (__attribute__((address_space(3))) v2i_few*)(size_t)at;
+  if constexpr (FMT == WF_CACHE_E4M3)
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(p));
+  else
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr4_b64_v2i32(p));
+}
+// V's exponents of four keys, less 128 (weights are doubled for it).
+template <int XB>
+__device__ __forceinline__ void exponents4(uint32_t at, uint32_t* x) {
+  if constexpr (XB == 4) {
+    const u32x4 w = lds_read<u32x4>(at);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = w[e] ^ 0x80808080u;
+  } else {
+    const u32x2 w = lds_read<u32x2>(at);
+#pragma unroll
+    for (int e = 0; e < 2; ++e) x[e] = w[e] ^ 0x80808080u;
+  }
+}
+// w 2^(byte b of x)
+__device__ __forceinline__ float times_exponent(float w, uint32_t x, int b) {
+  return __builtin_amdgcn_ldexpf(w, (int)(x << (24 - 8 * b)) >> 24);
+}
+
+// What a wave makes of a block of 32 keys for 32 query rows: products of 32 x 32.
+// A lane has scores of query row l % 32, keys 8 (e / 4) + 4 h + e % 4.
 template <int D, int FMT>
-__global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(TreeArgs a) {
+struct FewRows32 {
   using G = FewGeom<D, FMT>;
   using W = PrefixWave<bf16_t, D, 1>;
-  constexpr int NI = G::NI, R = G::R, RB = G::RB, KB = G::KB, XB = G::XB, DT = D / 32;
+  static constexpr int QN = 32, RB = G::RB, XB = G::XB, DT = D / 32;
+  W w;
+  f32x16 sc, t;
+
+  __device__ __forceinline__ void init(float scale) { w.init(scale); }
+  __device__ __forceinline__ static int query() { return threadIdx.x & 31; }
+  __device__ __forceinline__ static int half() { return (threadIdx.x & 63) >> 5; }
+  // channels h D / 2 + 8 j of step j
+  __device__ __forceinline__ void load(const bf16_t* row) {
+#pragma unroll
+    for (int j = 0; j < W::QS; ++j)
+      w.q[0][j] = reinterpret_cast<const u32x4*>(row)[half() * (D / 16) + j];
+  }
+  __device__ __forceinline__ void scores(uint32_t kat, uint32_t xat) {
+    const int h = half(), r = query();
+    constexpr int HC = G::C / 2;  // chunks of a lane
+    u32x4 kc[HC];
+#pragma unroll
+    for (int c = 0; c < HC; ++c) kc[c] = lds_read<u32x4>(kat + G::at(r, h * HC + c));
+    const uint32_t kx = !G::QUANT  ? 0u
+                        : XB == 4 ? lds_read<uint32_t>(xat + 4 * r) >> (16 * h)
+                                  : lds_read<uint8_t>(xat + 2 * r + h);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sc[e] = 0.f;
+#pragma unroll
+    for (int j = 0; j < W::QS; ++j) {
+      const float scale = block_scale(j < 4 ? kx & 0xff : kx >> 8 & 0xff);
+      u32x4 kf;
+      if constexpr (!G::QUANT)
+        kf = kc[j];
+      else if constexpr (FMT == WF_CACHE_E4M3)
+        kf = operand<FMT>(kc[j / 2][2 * (j & 1)], kc[j / 2][2 * (j & 1) + 1], scale);
+      else
+        kf = operand<FMT>(kc[j / 4][j & 3], 0, scale);
+      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf),
+                                                   __builtin_bit_cast(bf16x8, w.q[0][j]), sc, 0, 0,
+                                                   0);
+    }
+  }
+  // The block's weights; masked: of the keys whose bits are set in seen.
+  __device__ __forceinline__ void softmax(bool masked, uint32_t seen) {
+    const int h = half();
+    auto hide = [&](float by) __attribute__((always_inline)) {
+      if (!masked) return;
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        t[e] = seen >> (8 * (e >> 2) + 4 * h + (e & 3)) & 1 ? t[e] : by;
+    };
+    w.shift_one(0, sc, t);
+    hide(-INFINITY);
+    float mx[1] = {w.largest(t)};
+    w.raise(
+        mx, [&](int, float by) __attribute__((always_inline)) { w.drop(t, by); },
+        [&](int, float& mn, float& al) __attribute__((always_inline)) {
+          t = sc;
+          hide(-w.c2 * INFINITY);
+          w.anew(0, t, mn, al);
+        });
+    float z = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      t[e] = __builtin_amdgcn_exp2f(t[e]);
+      z += t[e];
+    }
+    w.l[0] += z;
+  }
+  __device__ __forceinline__ void product(int d, const u32x4& vf, const u32x4& pf) {
+    w.O[0][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf),
+                                                        __builtin_bit_cast(bf16x8, pf), w.O[0][d],
+                                                        0, 0, 0);
+  }
+  // The weighted values.  A lane's place in a transposed load is a part of a row of
+  // eight in 8 bits, of sixteen in 4 bits, of four in bf16, each of 16 channels.
+  __device__ __forceinline__ void values(uint32_t vat, uint32_t vx) {
+    const int h = half(), i16 = threadIdx.x & 15, hi = (threadIdx.x >> 4) & 1;
+    const int p = FMT == WF_CACHE_E4M3 ? i16 >> 1 : FMT == WF_CACHE_E2M1 ? i16 : i16 >> 2;
+    const int row = 16 * (p >> 3) + 8 * (p >> 2 & 1) + 4 * h + (p & 3);
+    uint32_t vb = vat + (FMT == WF_CACHE_E4M3   ? G::vat(row, hi) + 8 * (i16 & 1)
+                         : FMT == WF_CACHE_E2M1 ? G::vat(row, 0) + 8 * hi
+                                                : G::vat(row, 2 * hi + (i16 >> 1 & 1)) + 8 * (i16 & 1));
+    asm volatile("" : "+v"(vb));
+    if constexpr (!G::QUANT) {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+        u32x4 pf;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) pf[e] = pack_bf16x2(t[8 * kb + 2 * e], t[8 * kb + 2 * e + 1]);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          const u32x2 lo = read_tr16((vb ^ (64 * d)) + 2 * kb * 8 * RB);
+          const u32x2 up = read_tr16((vb ^ (64 * d)) + (2 * kb + 1) * 8 * RB);
+          product(d, u32x4{lo[0], lo[1], up[0], up[1]}, pf);
+        }
+      }
+    } else {
+      uint32_t xs[4 * XB];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) exponents4<XB>(vx + (8 * q + 4 * h) * XB, xs + XB * q);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) t[e] += t[e];
+      // the weights of half the keys for channels 32 d ..: times 2^(x - 127)
+      auto weights = [&](int kb, int d) __attribute__((always_inline)) {
+        u32x4 pf;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int k = 8 * kb + 2 * e, b0 = k * XB + d, b1 = b0 + XB;
+          pf[e] = pack_bf16x2(times_exponent(t[k], xs[b0 / 4], b0 & 3),
+                              times_exponent(t[k + 1], xs[b1 / 4], b1 & 3));
+        }
+        return pf;
+      };
+      if constexpr (FMT == WF_CACHE_E4M3) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int d = 0; d < DT; ++d) {
+            const u32x2 c = read_codes<FMT>((vb ^ (32 * d)) + kb * 16 * RB);
+            product(d, operand<FMT>(c[0], c[1], 1.f), weights(kb, d));
+          }
+      } else {
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          const u32x2 c = read_codes<FMT>(vb ^ (16 * d));
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb) product(d, operand<FMT>(c[kb], 0, 1.f), weights(kb, d));
+        }
+      }
+    }
+  }
+  // The row's outputs, reference and sum; o, st: of the wave's rows.
+  __device__ __forceinline__ void put(float* o, float* st, int stride) {
+    const int h = half(), r = query();
+    const float l = w.l[0] + partner32(w.l[0]);
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4)
+        *reinterpret_cast<f32x4*>(o + r * stride + 32 * d + 2 * i + 4 * h) =
+            f32x4{w.O[0][d][i], w.O[0][d][i + 1], w.O[0][d][i + 2], w.O[0][d][i + 3]};
+    if (h == 0) {
+      st[2 * r] = w.reference(0);
+      st[2 * r + 1] = l;
+    }
+  }
+};
+
+// For 16 query rows: products of 16 x 16, half the softmax and weights of 32 rows.
+// A lane has scores of query row l % 16, keys 16 (e / 4) + 4 g + e % 4, g = l / 16.
+template <int D, int FMT>
+struct FewRows16 {
+  using G = FewGeom<D, FMT>;
+  static constexpr int QN = 16, RB = G::RB, XB = G::XB, QS = D / 32, CT = D / 16;
+  u32x4 q[QS];
+  f32x4 O[CT];  // channels 16 c + 4 g .. + 3
+  float sc[8], t[8];
+  float mref, l, nref, limit, f, c2, c2p;  // as in PrefixWave
+
+  __device__ __forceinline__ void init(float scale) {
+    c2 = scale * kLog2e;
+    c2p = __uint_as_float(__float_as_uint(c2) & 0xff800000u);
+    mref = limit = -INFINITY;
+    nref = l = 0.f;
+    f = c2;
+#pragma unroll
+    for (int c = 0; c < CT; ++c) O[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  __device__ __forceinline__ static int query() { return threadIdx.x & 15; }
+  __device__ __forceinline__ static int group() { return (threadIdx.x & 63) >> 4; }
+  // channels g D / 4 + 8 j of step j
+  __device__ __forceinline__ void load(const bf16_t* row) {
+#pragma unroll
+    for (int j = 0; j < QS; ++j) q[j] = reinterpret_cast<const u32x4*>(row)[group() * QS + j];
+  }
+  __device__ __forceinline__ void scores(uint32_t kat, uint32_t xat) {
+    const int g = group();
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int r = 16 * k + query();
+      u32x4 kf[QS];
+      if constexpr (!G::QUANT) {
+#pragma unroll
+        for (int j = 0; j < QS; ++j) kf[j] = lds_read<u32x4>(kat + G::at(r, g * QS + j));
+      } else {
+        const float scale = block_scale(lds_read<uint8_t>(xat + XB * r + g * XB / 4));
+        if constexpr (FMT == WF_CACHE_E4M3) {
+#pragma unroll
+          for (int c = 0; c < QS / 2; ++c) {
+            const u32x4 w = lds_read<u32x4>(kat + G::at(r, g * (QS / 2) + c));
+            kf[2 * c] = operand<FMT>(w[0], w[1], scale);
+            kf[2 * c + 1] = operand<FMT>(w[2], w[3], scale);
+          }
+        } else if constexpr (QS == 4) {
+          const u32x4 w = lds_read<u32x4>(kat + G::at(r, g));
+#pragma unroll
+          for (int j = 0; j < 4; ++j) kf[j] = operand<FMT>(w[j], 0, scale);
+        } else {
+          const u32x2 w = lds_read<u32x2>(kat + G::at(r, g >> 1) + 8 * (g & 1));
+#pragma unroll
+          for (int j = 0; j < 2; ++j) kf[j] = operand<FMT>(w[j], 0, scale);
+        }
+      }
+      f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < QS; ++j)
+        s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[j]),
+                                                    __builtin_bit_cast(bf16x8, q[j]), s, 0, 0, 0);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sc[4 * k + e] = s[e];
+    }
+  }
+  __device__ __forceinline__ float ratio() const {  // c2 / c2p
+    return __uint_as_float((__float_as_uint(c2) & 0x7fffffu) | 0x3f800000u);
+  }
+  __device__ __forceinline__ float reference() const { return f == c2 ? mref : mref * ratio(); }
+  // As PrefixWave's: the reference moves when a score passes it by 2^8, and the
+  // scores, which are kept, are then made anew, a far reference with the power of two.
+  __device__ __forceinline__ void softmax(bool masked, uint32_t seen) {
+    const int g = group();
+    auto hide = [&](float by) __attribute__((always_inline)) {
+      if (!masked) return;
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        t[e] = seen >> (16 * (e >> 2) + 4 * g + (e & 3)) & 1 ? t[e] : by;
+    };
+#pragma unroll
+    for (int e = 0; e < 8; ++e) t[e] = fmaf(sc[e], f, nref);
+    hide(-INFINITY);
+    float mx = t[0];
+#pragma unroll
+    for (int e = 1; e < 8; ++e) mx = fmaxf(mx, t[e]);
+    if (__builtin_amdgcn_ballot_w64(mx > limit) != 0) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) t[e] = sc[e];
+      hide(-c2 * INFINITY);
+      float x = t[0] * c2p;  // (exact, and in the order of the products with c2)
+#pragma unroll
+      for (int e = 1; e < 8; ++e) x = fmaxf(x, t[e] * c2p);
+      x = max_xor32(max_xor16(x));
+      const float was = reference(), m = x * ratio();
+      const bool up = m > was;
+      const float by = !up ? f : fabsf(m) >= PrefixWave<bf16_t, D, 1>::kFar ? c2p : c2;
+      const float mn = !up ? mref : by == c2 ? m : x;
+      const float al = !up ? 1.f
+                       : mref == -INFINITY ? 0.f
+                                           : __builtin_amdgcn_exp2f(by == f ? mref - mn : was - m);
+      f = by;
+      mref = mn;
+      nref = mn > -INFINITY ? -mn : 0.f;
+      limit = mn > -INFINITY ? 8.f : -INFINITY;
+      l *= al;
+#pragma unroll
+      for (int c = 0; c < CT; ++c) O[c] *= al;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) t[e] = fmaf(t[e], f, nref);
+    }
+    float z = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      t[e] = __builtin_amdgcn_exp2f(t[e]);
+      z += t[e];
+    }
+    l += z;
+  }
+  // A transposed load's rows: the lane's eight keys (in 4 bits twice).
+  __device__ __forceinline__ void values(uint32_t vat, uint32_t vx) {
+    const int g = group(), i16 = threadIdx.x & 15;
+    const int p = FMT == WF_CACHE_E4M3 ? i16 >> 1 : FMT == WF_CACHE_E2M1 ? i16 & 7 : i16 >> 2;
+    const int row = 16 * (p >> 2) + 4 * g + (p & 3);
+    uint32_t vb = vat + (FMT == WF_CACHE_E4M3   ? G::vat(row, 0) + 8 * (i16 & 1)
+                         : FMT == WF_CACHE_E2M1 ? G::vat(row, 0)
+                                                : G::vat(row, i16 >> 1 & 1) + 8 * (i16 & 1));
+    asm volatile("" : "+v"(vb));
+    uint32_t xs[2 * XB];
+    if constexpr (G::QUANT) {
+      exponents4<XB>(vx + 4 * g * XB, xs);
+      exponents4<XB>(vx + (16 + 4 * g) * XB, xs + XB);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) t[e] += t[e];
+    }
+    u32x4 pf;
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+      if (G::QUANT ? c % 2 == 0 : c == 0) {  // the weights for 32 channels, or for all
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int b0 = 2 * e * XB + c / 2, b1 = b0 + XB;
+          pf[e] = G::QUANT ? pack_bf16x2(times_exponent(t[2 * e], xs[b0 / 4], b0 & 3),
+                                         times_exponent(t[2 * e + 1], xs[b1 / 4], b1 & 3))
+                           : pack_bf16x2(t[2 * e], t[2 * e + 1]);
+        }
+      }
+      u32x4 vf;
+      if constexpr (!G::QUANT) {
+        const u32x2 lo = read_tr16(vb ^ (32 * c)), up = read_tr16((vb ^ (32 * c)) + 16 * RB);
+        vf = u32x4{lo[0], lo[1], up[0], up[1]};
+      } else {
+        const u32x2 w = read_codes<FMT>(vb ^ ((FMT == WF_CACHE_E4M3 ? 16 : 8) * c));
+        vf = operand<FMT>(w[0], w[1], 1.f);
+      }
+      O[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf),
+                                                     __builtin_bit_cast(bf16x8, pf), O[c], 0, 0, 0);
+    }
+  }
+  __device__ __forceinline__ void put(float* o, float* st, int stride) {
+    const float z = add_xor32(add_xor16(l));
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+      *reinterpret_cast<f32x4*>(o + query() * stride + 16 * c + 4 * group()) = O[c];
+    if (group() == 0) {
+      st[2 * query()] = reference();
+      st[2 * query() + 1] = z;
+    }
+  }
+};
+
+// The waves' outputs in LDS: row r of wave k at k QN + r, their references and sums
+// behind them.
+template <int D, int QN>
+struct FewOut {
+  static constexpr int STRIDE = D + 4;
+  static constexpr size_t BYTES = (size_t)kFewWaves * QN * (STRIDE + 2) * sizeof(float);
+};
+
+template <int D, int FMT, int QN>
+__global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(TreeArgs a) {
+  using G = FewGeom<D, FMT>;
+  constexpr int NI = G::NI, R = G::R, RB = G::RB, KB = G::KB, XB = G::XB;
   constexpr bool QUANT = G::QUANT;
   extern __shared__ __align__(16) unsigned char smem[];  // the waves' rings, a flag
   int* flag = reinterpret_cast<int*>(smem + kFewWaves * G::WAVE);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int h = lane >> 5, l32 = lane & 31;
 
   const int item = xcd_swizzle(blockIdx.x, gridDim.x);
   if (item >= a.items) return;  // (the grid holds whole eights of them)
@@ -95,10 +470,10 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(TreeArgs a)
   const int unit = item / (a.mblocks * a.splits);
   const int head = unit % a.heads, seq = unit / a.heads;
   const Sequence s(a, seq);
-  const int M = s.n * a.g, m0 = 32 * mb;
+  const int M = s.n * a.g, m0 = QN * mb;
   const int k0 = sp * a.rps, nk = min(a.rps, s.L - k0);  // the range's keys
   if (m0 >= M || (nk <= 0 && !a.whole)) return;
-  W w;
+  std::conditional_t<QN == 32, FewRows32<D, FMT>, FewRows16<D, FMT>> w;
   w.init(a.scale);
   if (threadIdx.x == 0) *flag = 0;
   lds_barrier();
@@ -177,15 +552,9 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(TreeArgs a)
       queue_keys(0, r0, r1);
       queue_vals(0, r0, r1);
     }
-    // the lane's query row: channels h D / 2 + 8 j of step j
-    const int m = min(m0 + l32, M - 1), ti = a.by_g(m);
+    const int m = min(m0 + w.query(), M - 1), ti = a.by_g(m);  // the lane's query row
     const long tok = min(max(s.first + ti, 0L), a.tokens - 1L);
-    {
-      const u32x4* src = reinterpret_cast<const u32x4*>(static_cast<const bf16_t*>(a.Q) + tok * a.qs +
-                                                        (long)(head * a.g + m - ti * a.g) * D);
-#pragma unroll
-      for (int j = 0; j < W::QS; ++j) w.q[0][j] = src[h * (D / 16) + j];
-    }
+    w.load(static_cast<const bf16_t*>(a.Q) + tok * a.qs + (long)(head * a.g + m - ti * a.g) * D);
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): so that no later wait is for these
     for (int i = 1; i < min(R, mine); ++i) {
       const long r0 = pool_row(key_of(i)), r1 = pool_row(key_of(i) + 16);
@@ -212,49 +581,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(TreeArgs a)
         wait_loads<NI + G::BI>();
       else
         wait_loads<NI>();
-      // scores: lane: keys 8 (i / 4) + 4 h + i % 4 of query l32
-      f32x16 sc, t;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) sc[e] = 0.f;
-      {
-        constexpr int HC = G::C / 2;  // chunks of a lane
-        u32x4 kc[HC];
-#pragma unroll
-        for (int c = 0; c < HC; ++c) kc[c] = lds_read<u32x4>(kat + G::at(l32, h * HC + c));
-        const uint32_t kx = !QUANT   ? 0u
-                            : XB == 4 ? lds_read<uint32_t>(xat + 4 * l32) >> (16 * h)
-                                      : lds_read<uint8_t>(xat + 2 * l32 + h);
-#pragma unroll
-        for (int j = 0; j < W::QS; ++j) {
-          const float scale = block_scale(j < 4 ? kx & 0xff : kx >> 8 & 0xff);
-          u32x4 kf;
-          if constexpr (!QUANT) {
-            kf = kc[j];
-          } else if constexpr (FMT == WF_CACHE_E4M3) {
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const uint32_t c = kc[j / 2][2 * (j & 1) + e];
-              kf[2 * e] = __builtin_bit_cast(
-                  uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, scale, false));
-              kf[2 * e + 1] = __builtin_bit_cast(
-                  uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, scale, true));
-            }
-          } else {
-            const uint32_t c = kc[j / 4][j & 3];
-            kf[0] = __builtin_bit_cast(uint32_t,
-                                       __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 0));
-            kf[1] = __builtin_bit_cast(uint32_t,
-                                       __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 1));
-            kf[2] = __builtin_bit_cast(uint32_t,
-                                       __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 2));
-            kf[3] = __builtin_bit_cast(uint32_t,
-                                       __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 3));
-          }
-          sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf),
-                                                       __builtin_bit_cast(bf16x8, w.q[0][j]), sc,
-                                                       0, 0, 0);
-        }
-      }
+      w.scores(kat, xat);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the codes have been read
       if (ahead == R) queue_keys(i + R, r0, r1);
 
@@ -262,29 +589,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(TreeArgs a)
       const bool masked = key + 32 > min(s.base, kend);
       uint32_t seen = ~0u;
       if (masked) seen = seen_keys(a, s, ti, words, key, nv);
-      auto hide = [&](float by) __attribute__((always_inline)) {
-        if (!masked) return;
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          t[e] = seen >> (8 * (e >> 2) + 4 * h + (e & 3)) & 1 ? t[e] : by;
-      };
-      w.shift_one(0, sc, t);
-      hide(-INFINITY);
-      float mx[1] = {w.largest(t)};
-      w.raise(
-          mx, [&](int, float by) __attribute__((always_inline)) { w.drop(t, by); },
-          [&](int, float& mn, float& al) __attribute__((always_inline)) {
-            t = sc;
-            hide(-w.c2 * INFINITY);
-            w.anew(0, t, mn, al);
-          });
-      float z = 0.f;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        t[e] = __builtin_amdgcn_exp2f(t[e]);
-        z += t[e];
-      }
-      w.l[0] += z;
+      w.softmax(masked, seen);
 
       if (ahead == R)
         wait_loads<(R - 1) * G::BI + NI + G::XL>();
@@ -308,10 +613,11 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(TreeArgs a)
       // last block.
       bool odd = false;
       if constexpr (QUANT) {
-        uint32_t x = XB == 4 ? lds_read<uint32_t>(vx + 4 * l32) : lds_read<uint16_t>(vx + 2 * l32);
+        const int r = lane & 31;
+        uint32_t x = XB == 4 ? lds_read<uint32_t>(vx + 4 * r) : lds_read<uint16_t>(vx + 2 * r);
         x = ~x & (XB == 4 ? ~0u : 0xffffu);
         x |= XB == 4 ? 0u : 0xffff0000u;
-        odd = l32 < nv && ((x - 0x01010101u) & ~x & 0x80808080u) != 0;
+        odd = r < nv && ((x - 0x01010101u) & ~x & 0x80808080u) != 0;
       }
       if (FMT != WF_CACHE_E2M1 && masked)
         for (int c = lane; c < nv * G::C; c += 64) {
@@ -329,109 +635,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(TreeArgs a)
             *(__attribute__((address_space(3))) u32x4*)(size_t)(vat + 16 * c) = v;
           }
       }
-      // the lane's place in a transposed load: a part of a row of eight in 8 bits, of
-      // sixteen in 4 bits, of four in bf16, each of 16 channels
-      const int i16 = lane & 15, half = (lane >> 4) & 1;
-      const int p = FMT == WF_CACHE_E4M3 ? i16 >> 1 : FMT == WF_CACHE_E2M1 ? i16 : i16 >> 2;
-      const int vrow = 16 * (p >> 3) + 8 * (p >> 2 & 1) + 4 * h + (p & 3);
-      uint32_t vb = vat + (FMT == WF_CACHE_E4M3   ? G::vat(vrow, half) + 8 * (i16 & 1)
-                           : FMT == WF_CACHE_E2M1 ? G::vat(vrow, 0) + 8 * half
-                                                  : G::vat(vrow, 2 * half + (i16 >> 1 & 1)) + 8 * (i16 & 1));
-      asm volatile("" : "+v"(vb));
-      if constexpr (!QUANT) {
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-          u32x4 pf;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) pf[e] = pack_bf16x2(t[8 * kb + 2 * e], t[8 * kb + 2 * e + 1]);
-#pragma unroll
-          for (int d = 0; d < DT; ++d) {
-            u32x4 vf;
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              const u32x2 x = __builtin_bit_cast(
-                  u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                             (__attribute__((address_space(3))) v4i16p*)(size_t)(
-                                 (vb ^ (64 * d)) + (2 * kb + k) * 8 * RB)));
-              vf[2 * k] = x[0];
-              vf[2 * k + 1] = x[1];
-            }
-            w.O[0][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf),
-                                                                __builtin_bit_cast(bf16x8, pf),
-                                                                w.O[0][d], 0, 0, 0);
-          }
-        }
-      } else {
-        // exponents of the lane's 16 keys, less 128 (the weights are doubled for it)
-        uint32_t xs[16 * XB / 4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          if constexpr (XB == 4) {
-            const u32x4 x = lds_read<u32x4>(vx + (8 * q + 4 * h) * 4);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) xs[4 * q + e] = x[e] ^ 0x80808080u;
-          } else {
-            const u32x2 x = lds_read<u32x2>(vx + (8 * q + 4 * h) * 2);
-            xs[2 * q] = x[0] ^ 0x80808080u;
-            xs[2 * q + 1] = x[1] ^ 0x80808080u;
-          }
-        }
-#pragma unroll
-        for (int e = 0; e < 16; ++e) t[e] += t[e];
-        // weight of key e (of the lane's 16) for channels 32 d ..: times 2^(x - 127)
-        auto weight = [&](int e, int d) __attribute__((always_inline)) {
-          const int b = e * XB + d;
-          return __builtin_amdgcn_ldexpf(t[e], (int)(xs[b / 4] << (24 - 8 * (b & 3))) >> 24);
-        };
-        if constexpr (FMT == WF_CACHE_E4M3) {
-#pragma unroll
-          for (int kb = 0; kb < 2; ++kb) {
-#pragma unroll
-            for (int d = 0; d < DT; ++d) {
-              const v2i_few c = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-                  (__attribute__((address_space(3))) v2i_few*)(size_t)((vb ^ (32 * d)) + kb * 16 * RB));
-              u32x4 vf, pf;
-#pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                vf[2 * e] = __builtin_bit_cast(
-                    uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[e], 1.0f, false));
-                vf[2 * e + 1] = __builtin_bit_cast(
-                    uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[e], 1.0f, true));
-              }
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                pf[e] = pack_bf16x2(weight(8 * kb + 2 * e, d), weight(8 * kb + 2 * e + 1, d));
-              w.O[0][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf),
-                                                                  __builtin_bit_cast(bf16x8, pf),
-                                                                  w.O[0][d], 0, 0, 0);
-            }
-          }
-        } else {
-#pragma unroll
-          for (int d = 0; d < DT; ++d) {
-            const v2i_few c = __builtin_amdgcn_ds_read_tr4_b64_v2i32(
-                (__attribute__((address_space(3))) v2i_few*)(size_t)(vb ^ (16 * d)));
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb) {
-              u32x4 vf, pf;
-              vf[0] = __builtin_bit_cast(uint32_t,
-                                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[kb], 1.0f, 0));
-              vf[1] = __builtin_bit_cast(uint32_t,
-                                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[kb], 1.0f, 1));
-              vf[2] = __builtin_bit_cast(uint32_t,
-                                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[kb], 1.0f, 2));
-              vf[3] = __builtin_bit_cast(uint32_t,
-                                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[kb], 1.0f, 3));
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                pf[e] = pack_bf16x2(weight(8 * kb + 2 * e, d), weight(8 * kb + 2 * e + 1, d));
-              w.O[0][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf),
-                                                                  __builtin_bit_cast(bf16x8, pf),
-                                                                  w.O[0][d], 0, 0, 0);
-            }
-          }
-        }
-      }
+      w.values(vat, vx);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the codes have been read
       if (ahead == R) queue_vals(i + R, r0, r1);
     }
@@ -440,45 +644,52 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(TreeArgs a)
   lds_barrier();  // the rings are idle
   const bool odd = __builtin_amdgcn_readfirstlane(*flag) != 0;
   lds_barrier();
-  OutRows<D, 1, kFewWaves> out(smem);
-  out.put(w, wave);
+  using Out = FewOut<D, QN>;
+  float* out = reinterpret_cast<float*>(smem);
+  float* stats = out + kFewWaves * QN * Out::STRIDE;
+  w.put(out + wave * QN * Out::STRIDE, stats + wave * QN * 2, Out::STRIDE);
+  lds_barrier();
   constexpr int C4 = D / 4, RPP = 64 * kFewWaves / C4;  // rows per round
   const int c = threadIdx.x % C4;
-  for (int r = threadIdx.x / C4; r < min(32, M - m0); r += RPP) {
-    const int v[1] = {r};
-    Merge4 g[1];
-    out.merged(v, kFewWaves, c, g);
+  for (int r = threadIdx.x / C4; r < min(QN, M - m0); r += RPP) {
+    Merge4 g;
+#pragma unroll
+    for (int k = 0; k < kFewWaves; ++k) {
+      const hw_f32x2 mz = *reinterpret_cast<const hw_f32x2*>(stats + 2 * (k * QN + r));
+      g.add(mz[0], mz[1], *reinterpret_cast<const f32x4*>(out + (k * QN + r) * Out::STRIDE + 4 * c));
+    }
     const int i = a.by_g(m0 + r);
     const long tok = s.first + i;
     if (!Sequence::there(a, tok)) continue;
-    if (odd) add_odd<bf16_t, D, FMT>(a, s, seq, head, i, k0, k0 + nk, 4 * c, g[0].o);
+    if (odd) add_odd<bf16_t, D, FMT>(a, s, seq, head, i, k0, k0 + nk, 4 * c, g.o);
     const int hq = head * a.g + m0 + r - i * a.g;
     const long row = tok * a.hq + hq;
     if (a.whole) {
-      g[0].finish(static_cast<bf16_t*>(a.O) + tok * a.os + (long)hq * D + 4 * c,
+      g.finish(static_cast<bf16_t*>(a.O) + tok * a.os + (long)hq * D + 4 * c,
                   a.lse ? a.lse + row : nullptr, c == 0);
     } else {
       const long at = row * a.splits + sp;
-      *reinterpret_cast<f32x4*>(a.part + at * D + 4 * c) = g[0].o;
-      if (c == 0) *reinterpret_cast<hw_f32x2*>(a.pstat + 2 * at) = hw_f32x2{g[0].M, g[0].z};
+      *reinterpret_cast<f32x4*>(a.part + at * D + 4 * c) = g.o;
+      if (c == 0) *reinterpret_cast<hw_f32x2*>(a.pstat + 2 * at) = hw_f32x2{g.M, g.z};
     }
   }
 }
 
 // ------------------------------------------------------------ host side
 
-template <int D, int FMT>
+template <int D, int FMT, int QN>
 static constexpr size_t few_lds() {
   const size_t rings = (size_t)kFewWaves * FewGeom<D, FMT>::WAVE + sizeof(int);
-  const size_t out = OutRows<D, 1, kFewWaves>::BYTES;
+  const size_t out = FewOut<D, QN>::BYTES;
   return rings > out ? rings : out;
 }
 
-hipError_t launch_tree_few(const TreeArgs& a, int head_dim, int format, long items, hipStream_t s) {
-  auto go = [&](auto d, auto f) {
-    constexpr int D = decltype(d)::value, F = decltype(f)::value;
-    constexpr size_t lds = few_lds<D, F>();
-    auto kern = tree_few_kernel<D, F>;
+hipError_t launch_tree_few(const TreeArgs& a, int head_dim, int format, int rows, long items,
+                           hipStream_t s) {
+  auto go = [&](auto d, auto f, auto n) {
+    constexpr int D = decltype(d)::value, F = decltype(f)::value, QN = decltype(n)::value;
+    constexpr size_t lds = few_lds<D, F, QN>();
+    auto kern = tree_few_kernel<D, F, QN>;
     if (lds > 65536) {
       const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern),
                                                hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -487,14 +698,17 @@ hipError_t launch_tree_few(const TreeArgs& a, int head_dim, int format, long ite
     hipLaunchKernelGGL(kern, dim3((unsigned)((items + 7) & ~7L)), dim3(64 * kFewWaves), lds, s, a);
     return hipGetLastError();
   };
-  using D64 = std::integral_constant<int, 64>;
-  using D128 = std::integral_constant<int, 128>;
-  auto by_format = [&](auto d) {
-    if (format == WF_CACHE_E4M3) return go(d, std::integral_constant<int, WF_CACHE_E4M3>{});
-    if (format == WF_CACHE_E2M1) return go(d, std::integral_constant<int, WF_CACHE_E2M1>{});
-    return go(d, std::integral_constant<int, WF_CACHE_PLAIN>{});
+  auto by_rows = [&](auto d, auto f) {
+    return rows == 16 ? go(d, f, std::integral_constant<int, 16>{})
+                      : go(d, f, std::integral_constant<int, 32>{});
   };
-  return head_dim == 128 ? by_format(D128{}) : by_format(D64{});
+  auto by_format = [&](auto d) {
+    if (format == WF_CACHE_E4M3) return by_rows(d, std::integral_constant<int, WF_CACHE_E4M3>{});
+    if (format == WF_CACHE_E2M1) return by_rows(d, std::integral_constant<int, WF_CACHE_E2M1>{});
+    return by_rows(d, std::integral_constant<int, WF_CACHE_PLAIN>{});
+  };
+  return head_dim == 128 ? by_format(std::integral_constant<int, 128>{})
+                         : by_format(std::integral_constant<int, 64>{});
 }
 
 }  // namespace wf
