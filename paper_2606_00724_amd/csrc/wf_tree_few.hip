@@ -32,7 +32,7 @@ struct FewGeom {
   static constexpr int RPI = 64 / C;                           // rows of a load
   static constexpr int XB = D / 32;                            // exponent bytes of a row
   static constexpr int XL = QUANT ? 1 : 0;                     // loads of a block's exponents
-  static constexpr int R = KB >= 8192 ? 1 : KB >= 4096 ? 2 : 4;  // blocks of the ring
+  static constexpr int R = KB >= 4096 ? 1 : 2;  // blocks of the ring
   static constexpr int XR = R + 1;  // a block's exponents outlive its keys
   static constexpr int WAVE = R * 2 * KB + XL * XR * 256;      // bytes of a wave
   static constexpr int BI = 2 * NI + XL;                       // loads of a block
@@ -107,20 +107,20 @@ __device__ __forceinline__ u32x2 read_codes(uint32_t at) {
   else
     return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr4_b64_v2i32(p));
 }
-// V's exponents of four keys, less 128 (weights are doubled for it).
+// V's exponents of four keys.
 template <int XB>
 __device__ __forceinline__ void exponents4(uint32_t at, uint32_t* x) {
   if constexpr (XB == 4) {
     const u32x4 w = lds_read<u32x4>(at);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = w[e] ^ 0x80808080u;
+    for (int e = 0; e < 4; ++e) x[e] = w[e];
   } else {
     const u32x2 w = lds_read<u32x2>(at);
 #pragma unroll
-    for (int e = 0; e < 2; ++e) x[e] = w[e] ^ 0x80808080u;
+    for (int e = 0; e < 2; ++e) x[e] = w[e];
   }
 }
-// w 2^(byte b of x)
+// w 2^b, b a signed byte of x
 __device__ __forceinline__ float times_exponent(float w, uint32_t x, int b) {
   return __builtin_amdgcn_ldexpf(w, (int)(x << (24 - 8 * b)) >> 24);
 }
@@ -229,6 +229,9 @@ struct FewRows32 {
       uint32_t xs[4 * XB];
 #pragma unroll
       for (int q = 0; q < 4; ++q) exponents4<XB>(vx + (8 * q + 4 * h) * XB, xs + XB * q);
+      // (less 128, for which the weights are doubled)
+#pragma unroll
+      for (int e = 0; e < 4 * XB; ++e) xs[e] ^= 0x80808080u;
 #pragma unroll
       for (int e = 0; e < 16; ++e) t[e] += t[e];
       // the weights of half the keys for channels 32 d ..: times 2^(x - 127)
@@ -306,40 +309,42 @@ struct FewRows16 {
   }
   __device__ __forceinline__ void scores(uint32_t kat, uint32_t xat) {
     const int g = group();
+    // 16-byte chunks of a lane's part of a row; 4 bits of 64 channels: half a chunk
+    constexpr int HC = G::C >= 4 ? G::C / 4 : 1;
+    u32x4 kc[2][HC];
+    uint32_t kx[2] = {0, 0};
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       const int r = 16 * k + query();
-      u32x4 kf[QS];
-      if constexpr (!G::QUANT) {
+      if constexpr (G::QUANT) kx[k] = lds_read<uint8_t>(xat + XB * r + g * XB / 4);
+      if constexpr (G::C >= 4) {
 #pragma unroll
-        for (int j = 0; j < QS; ++j) kf[j] = lds_read<u32x4>(kat + G::at(r, g * QS + j));
+        for (int c = 0; c < HC; ++c) kc[k][c] = lds_read<u32x4>(kat + G::at(r, g * HC + c));
       } else {
-        const float scale = block_scale(lds_read<uint8_t>(xat + XB * r + g * XB / 4));
-        if constexpr (FMT == WF_CACHE_E4M3) {
-#pragma unroll
-          for (int c = 0; c < QS / 2; ++c) {
-            const u32x4 w = lds_read<u32x4>(kat + G::at(r, g * (QS / 2) + c));
-            kf[2 * c] = operand<FMT>(w[0], w[1], scale);
-            kf[2 * c + 1] = operand<FMT>(w[2], w[3], scale);
-          }
-        } else if constexpr (QS == 4) {
-          const u32x4 w = lds_read<u32x4>(kat + G::at(r, g));
-#pragma unroll
-          for (int j = 0; j < 4; ++j) kf[j] = operand<FMT>(w[j], 0, scale);
-        } else {
-          const u32x2 w = lds_read<u32x2>(kat + G::at(r, g >> 1) + 8 * (g & 1));
-#pragma unroll
-          for (int j = 0; j < 2; ++j) kf[j] = operand<FMT>(w[j], 0, scale);
-        }
+        const u32x2 w = lds_read<u32x2>(kat + G::at(r, g >> 1) + 8 * (g & 1));
+        kc[k][0] = u32x4{w[0], w[1], 0u, 0u};
       }
-      f32x4 s = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int j = 0; j < QS; ++j)
-        s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[j]),
-                                                    __builtin_bit_cast(bf16x8, q[j]), s, 0, 0, 0);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sc[4 * k + e] = s[e];
     }
+    __builtin_amdgcn_sched_barrier(0);  // (all reads queued before the first is waited for)
+    f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+    for (int j = 0; j < QS; ++j)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const float scale = block_scale(kx[k]);
+        u32x4 kf;
+        if constexpr (!G::QUANT)
+          kf = kc[k][j];
+        else if constexpr (FMT == WF_CACHE_E4M3)
+          kf = operand<FMT>(kc[k][j / 2][2 * (j & 1)], kc[k][j / 2][2 * (j & 1) + 1], scale);
+        else
+          kf = operand<FMT>(kc[k][0][j], 0, scale);
+        s[k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf),
+                                                       __builtin_bit_cast(bf16x8, q[j]), s[k], 0, 0,
+                                                       0);
+      }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sc[e] = s[e >> 2][e & 3];
   }
   __device__ __forceinline__ float ratio() const {  // c2 / c2p
     return __uint_as_float((__float_as_uint(c2) & 0x7fffffu) | 0x3f800000u);
@@ -403,10 +408,26 @@ struct FewRows16 {
                          : FMT == WF_CACHE_E2M1 ? G::vat(row, 0)
                                                 : G::vat(row, i16 >> 1 & 1) + 8 * (i16 & 1));
     asm volatile("" : "+v"(vb));
+    // (all reads queued before the first is waited for)
+    u32x2 w[CT][G::QUANT ? 1 : 2];
     uint32_t xs[2 * XB];
     if constexpr (G::QUANT) {
       exponents4<XB>(vx + 4 * g * XB, xs);
       exponents4<XB>(vx + (16 + 4 * g) * XB, xs + XB);
+    }
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+      if constexpr (G::QUANT) {
+        w[c][0] = read_codes<FMT>(vb ^ ((FMT == WF_CACHE_E4M3 ? 16 : 8) * c));
+      } else {
+        w[c][0] = read_tr16(vb ^ (32 * c));
+        w[c][1] = read_tr16((vb ^ (32 * c)) + 16 * RB);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (G::QUANT) {  // less 128; the weights are doubled for it
+#pragma unroll
+      for (int e = 0; e < 2 * XB; ++e) xs[e] ^= 0x80808080u;
 #pragma unroll
       for (int e = 0; e < 8; ++e) t[e] += t[e];
     }
@@ -423,13 +444,10 @@ struct FewRows16 {
         }
       }
       u32x4 vf;
-      if constexpr (!G::QUANT) {
-        const u32x2 lo = read_tr16(vb ^ (32 * c)), up = read_tr16((vb ^ (32 * c)) + 16 * RB);
-        vf = u32x4{lo[0], lo[1], up[0], up[1]};
-      } else {
-        const u32x2 w = read_codes<FMT>(vb ^ ((FMT == WF_CACHE_E4M3 ? 16 : 8) * c));
-        vf = operand<FMT>(w[0], w[1], 1.f);
-      }
+      if constexpr (!G::QUANT)
+        vf = u32x4{w[c][0][0], w[c][0][1], w[c][1][0], w[c][1][1]};
+      else
+        vf = operand<FMT>(w[c][0][0], w[c][0][1], 1.f);
       O[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf),
                                                      __builtin_bit_cast(bf16x8, pf), O[c], 0, 0, 0);
     }
@@ -454,8 +472,15 @@ struct FewOut {
   static constexpr size_t BYTES = (size_t)kFewWaves * QN * (STRIDE + 2) * sizeof(float);
 };
 
+// Workgroups per CU, as their registers and LDS fit.
 template <int D, int FMT, int QN>
-__global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(TreeArgs a) {
+constexpr int few_groups() {
+  return QN == 16 && FMT != WF_CACHE_PLAIN ? 3 : 2;
+}
+
+template <int D, int FMT, int QN>
+__global__ __launch_bounds__(64 * kFewWaves, (few_groups<D, FMT, QN>())) void tree_few_kernel(
+    TreeArgs a) {
   using G = FewGeom<D, FMT>;
   constexpr int NI = G::NI, R = G::R, RB = G::RB, KB = G::KB, XB = G::XB;
   constexpr bool QUANT = G::QUANT;
@@ -487,10 +512,21 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(TreeArgs a)
     // (a scalar load: uniform, and no kernel that runs beside this writes tables)
     const __attribute__((address_space(4))) int32_t* table =
         (const __attribute__((address_space(4))) int32_t*)(a.table + (long)seq * a.tp);
-    // row of the pool of key k, the first of sixteen (past the last: any that is there)
-    auto pool_row = [&](int k) -> long {
-      const int page = min(max(table[min(k >> a.shift, last)], 0), a.pages - 1);
-      return (((long)page * a.heads + head) << a.shift) + (k & ((1 << a.shift) - 1));
+    // pages of a block's two sixteens of rows (past the last: any that is there)
+    struct Pages {
+      int a, b;
+    };
+    auto pages_of = [&](int i) __attribute__((always_inline)) {
+      const int k = key_of(i);
+      return Pages{table[min(k >> a.shift, last)], table[min((k + 16) >> a.shift, last)]};
+    };
+    // their first rows in the pool
+    auto rows_of = [&](int i, const Pages& p, long& r0, long& r1) __attribute__((always_inline)) {
+      const int k = key_of(i), in = (1 << a.shift) - 1;
+      r0 = (((long)min(max(p.a, 0), a.pages - 1) * a.heads + head) << a.shift) + (k & in);
+      r1 = a.shift > 4 ? r0 + 16
+                       : (((long)min(max(p.b, 0), a.pages - 1) * a.heads + head) << a.shift) +
+                             ((k + 16) & in);
     };
     const uint32_t ring = lds_offset(smem) + wave * G::WAVE, exps = ring + R * 2 * KB;
     // the lane's 16 bytes of a load: row of those that it holds, chunk
@@ -547,20 +583,20 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(TreeArgs a)
       load(a.V, r0, r1, ring + i % R * 2 * KB + KB, voff);
     };
 
-    {
-      const long r0 = pool_row(key_of(0)), r1 = pool_row(key_of(0) + 16);
-      queue_keys(0, r0, r1);
-      queue_vals(0, r0, r1);
-    }
+    long r0, r1;
+    rows_of(0, pages_of(0), r0, r1);
+    queue_keys(0, r0, r1);
+    queue_vals(0, r0, r1);
     const int m = min(m0 + w.query(), M - 1), ti = a.by_g(m);  // the lane's query row
     const long tok = min(max(s.first + ti, 0L), a.tokens - 1L);
     w.load(static_cast<const bf16_t*>(a.Q) + tok * a.qs + (long)(head * a.g + m - ti * a.g) * D);
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): so that no later wait is for these
     for (int i = 1; i < min(R, mine); ++i) {
-      const long r0 = pool_row(key_of(i)), r1 = pool_row(key_of(i) + 16);
+      rows_of(i, pages_of(i), r0, r1);
       queue_keys(i, r0, r1);
       queue_vals(i, r0, r1);
     }
+    Pages ahead_pages = pages_of(R);  // of the block that is queued next
     const uint32_t* words = a.mask ? a.mask + tok * a.words : nullptr;
 
     for (int i = 0; i < mine; ++i) {
@@ -568,11 +604,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(TreeArgs a)
       const uint32_t kat = ring + i % R * 2 * KB, vat = kat + KB, xat = exps + xout * 256;
       xout = next(xout);
       const int ahead = min(mine - 1 - i, R);  // blocks behind this one, R at most
-      long r0 = 0, r1 = 0;
-      if (ahead == R) {
-        r0 = pool_row(key_of(i + R));
-        r1 = pool_row(key_of(i + R) + 16);
-      }
+      if (ahead == R) rows_of(i + R, ahead_pages, r0, r1);
+      ahead_pages = pages_of(i + R + 1);
       if (ahead >= R - 1)
         wait_loads<NI + (R - 1) * G::BI>();
       else if (R == 4 && ahead == 2)
