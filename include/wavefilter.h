@@ -724,7 +724,7 @@ wf_status wf_tree_plan(const wf_tree_params* p, size_t workspace_bytes,
  *   Q          [tokens][heads group][d] of q_row   dtype
  *   table      [batch][table_pages]  int32: pages (those outside [0, pages)
  *              are taken as the nearest inside); entries behind a sequence's
- *              last row are not read
+ *              last row may hold anything
  *   len        [batch]               int32: L
  *   row_start  nullable [batch + 1]  int32: sequence b's query rows are tokens
  *              row_start[b] .. row_start[b + 1] - 1; NULL: tokens b max_rows

@@ -1084,7 +1084,7 @@ static wf_status check_tree(const wf_tree_params* p, size_t have, TreePlan* plan
   if (p->o_row) WF_TRY(check_stride("o_row", p->o_row, hq * p->head_dim, unit));
   *plan = plan_tree(*p, have);
   // a launch has fewer than 2^32 threads
-  if ((plan->items + 7) * 64 * plan->nw > UINT32_MAX || plan->merges * kBlock > UINT32_MAX)
+  if ((plan->items + 7) * 64 * plan->nw > UINT32_MAX || plan->merges * p->batch * kBlock > UINT32_MAX)
     return fail(WF_ERR_UNSUPPORTED, "too many workgroups in one call");
   return WF_OK;
 }

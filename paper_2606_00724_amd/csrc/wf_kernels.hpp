@@ -319,7 +319,9 @@ struct TreeArgs {
   int mblocks, mrows;    // blocks per unit, query rows of a block
   int kw;                // waves that take the keys of a tile in turn
   int batch, heads, g, hq;
-  FastDiv by_g;
+  FastDiv by_g, by_hq, by_mblocks, by_splits, by_heads;
+  int merges;            // workgroups of the merge per sequence
+  FastDiv by_merge;
   int pages, shift, tp;  // log2 of a page's rows
   int tokens, max_rows, max_len, words;
   int causal;

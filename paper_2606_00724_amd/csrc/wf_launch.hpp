@@ -351,7 +351,7 @@ struct TreePlan {
   long items;                      // workgroups
   int splits, rps, mblocks, nw, kw, qw;
   int few;                         // query rows of the kernel of few of them, or 0
-  long merges;                     // workgroups of the merge (0: none)
+  long merges;                     // workgroups of the merge per sequence (0: none)
   size_t lds_bytes;
   size_t part_bytes, pstat_bytes;  // workspace (0: no partials)
 };

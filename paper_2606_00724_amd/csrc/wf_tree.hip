@@ -167,12 +167,10 @@ __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void tree_attn_kerne
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = lane >> 5, l32 = lane & 31;
 
-  // Blocks of query rows innermost: those that read the same keys run at once on one
-  // XCD.
   const int item = xcd_swizzle(blockIdx.x, gridDim.x);
   if (item >= a.items) return;  // (the grid holds whole eights of them)
-  const int mb = item % a.mblocks, sp = item / a.mblocks % a.splits;
-  const int unit = item / (a.mblocks * a.splits), head = unit % a.heads, seq = unit / a.heads;
+  const TreeItem it(a, item);
+  const int mb = it.mb, sp = it.sp, head = it.head, seq = it.seq;
   const Sequence s(a, seq);
   const int M = s.n * a.g, m0 = mb * a.mrows;
   const int k0 = sp * a.rps, nk = min(a.rps, s.L - k0);  // the range's keys
@@ -441,24 +439,22 @@ __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void tree_attn_kerne
 template <typename T, int D, int SG>
 __global__ __launch_bounds__(kBlock) void tree_merge_kernel(TreeArgs a) {
   constexpr int C4 = D / 4, RPB = kBlock / (C4 * SG), F = 8;
-  const int per = (a.max_rows * a.hq + RPB - 1) / RPB;  // workgroups of a sequence
-  const int seq = blockIdx.x / per;
-  const Sequence s(a, seq);
-  const int rows = s.n * a.hq, r = blockIdx.x % per * RPB + threadIdx.x / (C4 * SG);
-  if (blockIdx.x % per * RPB >= rows) return;  // uniform
-  const int slots = (s.L + a.rps - 1) / a.rps;
+  const int seq = a.by_merge(blockIdx.x), part = blockIdx.x - seq * a.merges;
+  const int r = part * RPB + threadIdx.x / (C4 * SG);  // (query row, head) of the sequence
   const int c = threadIdx.x % C4, sg = threadIdx.x / C4 % SG;
-  const int i = min(r, rows - 1) / a.hq, hq = min(r, rows - 1) % a.hq;
+  const int i = a.by_hq(r), hq = r - i * a.hq;
+  const Sequence s(a, seq);
   const long tok = s.first + i;
-  const bool mine = r < rows && Sequence::there(a, tok);
+  const bool mine = i < s.n && Sequence::there(a, tok);
   const long row = mine ? tok * a.hq + hq : 0;
+  const int slots = (s.L + a.rps - 1) / a.rps;
   Merge4 g;
-  for (int s0 = sg; s0 < slots; s0 += F * SG) {
+  for (int s0 = sg; s0 < (s0 == sg ? a.splits : slots); s0 += F * SG) {
     hw_f32x2 mz[F];
     f32x4 x[F];
 #pragma unroll
     for (int k = 0; k < F; ++k) {  // (all queued; those past the last are dropped)
-      const long at = row * a.splits + min(s0 + k * SG, slots - 1);
+      const long at = row * a.splits + min(s0 + k * SG, a.splits - 1);
       mz[k] = *reinterpret_cast<const hw_f32x2*>(a.pstat + 2 * at);
       x[k] = *reinterpret_cast<const f32x4*>(a.part + at * D + 4 * c);
     }
@@ -586,7 +582,7 @@ TreePlan plan_tree(const wf_tree_params& p, size_t have) {
     l.part_bytes = (size_t)rows * l.splits * D * sizeof(float);
     l.pstat_bytes = (size_t)rows * l.splits * 2 * sizeof(float);
     const long rpb = kBlock / (D / 4 * merge_threads(l.splits));
-    l.merges = p.batch * (((long)p.max_rows * p.heads * p.group + rpb - 1) / rpb);
+    l.merges = ((long)p.max_rows * p.heads * p.group + rpb - 1) / rpb;
   }
   return l;
 }
@@ -603,6 +599,12 @@ hipError_t launch_tree(const wf_tree_params& p, const TreePlan& l, TreeArgs& a, 
   a.g = p.group;
   a.hq = p.heads * p.group;
   a.by_g = FastDiv::by(p.group);
+  a.merges = (int)l.merges;
+  a.by_merge = FastDiv::by(std::max(1, a.merges));
+  a.by_hq = FastDiv::by(a.hq);
+  a.by_mblocks = FastDiv::by(a.mblocks);
+  a.by_splits = FastDiv::by(a.splits);
+  a.by_heads = FastDiv::by(a.heads);
   a.pages = p.pages;
   a.shift = __builtin_ctz(p.page_rows);
   a.tp = p.table_pages;
@@ -639,7 +641,7 @@ hipError_t launch_tree(const wf_tree_params& p, const TreePlan& l, TreeArgs& a, 
     else if constexpr (sizeof(T) == 2)
       e = go(tree_attn_kernel<T, D, WF_CACHE_PLAIN, 2>);
     if (e != hipSuccess || l.merges == 0) return e;
-    const dim3 grid((unsigned)l.merges);
+    const dim3 grid((unsigned)(l.merges * p.batch));
     switch (merge_threads(l.splits)) {
       case 1: hipLaunchKernelGGL((tree_merge_kernel<T, D, 1>), grid, dim3(kBlock), 0, s, a); break;
       case 4: hipLaunchKernelGGL((tree_merge_kernel<T, D, 4>), grid, dim3(kBlock), 0, s, a); break;

@@ -9,14 +9,35 @@ namespace wf {
 struct Sequence {
   int L, n, base;  // keys, query rows, first key that is not seen by all
   long first;      // token of query row 0
+  // (no branch: the loads are queued together, scalar ones, since no kernel that runs
+  // beside this writes lengths)
   __device__ __forceinline__ Sequence(const TreeArgs& a, int b) {
-    L = min(max(a.len[b], 0), a.max_len);
-    first = a.start ? a.start[b] : (long)b * a.max_rows;
-    n = a.start ? (int)min(max((long)a.start[b + 1] - first, 0L), (long)a.max_rows) : a.max_rows;
+    const int len = word(a.len + b);
+    const int r0 = word(a.start ? a.start + b : a.len + b);
+    const int r1 = word(a.start ? a.start + b + 1 : a.len + b);
+    L = min(max(len, 0), a.max_len);
+    first = a.start ? r0 : (long)b * a.max_rows;
+    n = a.start ? (int)min(max((long)r1 - r0, 0L), (long)a.max_rows) : a.max_rows;
     base = L - n;
+  }
+  __device__ __forceinline__ static int word(const int32_t* p) {
+    return *(const __attribute__((address_space(4))) int32_t*)p;
   }
   __device__ __forceinline__ static bool there(const TreeArgs& a, long token) {
     return token >= 0 && token < a.tokens;
+  }
+};
+
+// The workgroup's block of query rows, range of keys and (sequence, K/V head).  Blocks
+// of query rows are innermost: those that read the same keys run at once on one XCD.
+struct TreeItem {
+  int mb, sp, seq, head;
+  __device__ __forceinline__ TreeItem(const TreeArgs& a, int item) {
+    const int range = a.by_mblocks(item), unit = a.by_splits(range);
+    mb = item - range * a.mblocks;
+    sp = range - unit * a.splits;
+    seq = a.by_heads(unit);
+    head = unit - seq * a.heads;
   }
 };
 

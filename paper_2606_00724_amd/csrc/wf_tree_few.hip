@@ -491,35 +491,37 @@ __global__ __launch_bounds__(64 * kFewWaves, (few_groups<D, FMT, QN>())) void tr
 
   const int item = xcd_swizzle(blockIdx.x, gridDim.x);
   if (item >= a.items) return;  // (the grid holds whole eights of them)
-  const int mb = item % a.mblocks, sp = item / a.mblocks % a.splits;
-  const int unit = item / (a.mblocks * a.splits);
-  const int head = unit % a.heads, seq = unit / a.heads;
+  const TreeItem it(a, item);
+  const int sp = it.sp, head = it.head, seq = it.seq;
+  const int k0 = sp * a.rps, m0 = QN * it.mb;
+  // the wave's blocks: wave, wave + 4, ... of the range
+  auto key_of = [&](int i) { return k0 + 32 * (wave + kFewWaves * i); };
+  // (scalar loads: uniform, and no kernel that runs beside this writes tables)
+  const __attribute__((address_space(4))) int32_t* table =
+      (const __attribute__((address_space(4))) int32_t*)(a.table + (long)seq * a.tp);
+  // pages of a block's two sixteens of rows (past the last: whatever the table holds)
+  struct Pages {
+    int a, b;
+  };
+  auto pages_of = [&](int i) __attribute__((always_inline)) {
+    const int k = key_of(i);
+    return Pages{table[min(k >> a.shift, a.tp - 1)], table[min((k + 16) >> a.shift, a.tp - 1)]};
+  };
+  Pages pages = pages_of(0);
   const Sequence s(a, seq);
-  const int M = s.n * a.g, m0 = QN * mb;
-  const int k0 = sp * a.rps, nk = min(a.rps, s.L - k0);  // the range's keys
+  asm volatile("" : "+s"(pages.a), "+s"(pages.b));  // (beside the sequence's length)
+  const int M = s.n * a.g;
+  const int nk = min(a.rps, s.L - k0);  // the range's keys
   if (m0 >= M || (nk <= 0 && !a.whole)) return;
   std::conditional_t<QN == 32, FewRows32<D, FMT>, FewRows16<D, FMT>> w;
   w.init(a.scale);
   if (threadIdx.x == 0) *flag = 0;
   lds_barrier();
 
-  // the wave's blocks: wave, wave + 4, ... of the range
   const int nb = nk > 0 ? (nk + 31) / 32 : 0;
   const int mine = nb > wave ? (nb - wave + kFewWaves - 1) / kFewWaves : 0;
   if (mine > 0) {
-    const int kend = k0 + nk, last = (s.L - 1) >> a.shift;
-    auto key_of = [&](int i) { return k0 + 32 * (wave + kFewWaves * i); };
-    // (a scalar load: uniform, and no kernel that runs beside this writes tables)
-    const __attribute__((address_space(4))) int32_t* table =
-        (const __attribute__((address_space(4))) int32_t*)(a.table + (long)seq * a.tp);
-    // pages of a block's two sixteens of rows (past the last: any that is there)
-    struct Pages {
-      int a, b;
-    };
-    auto pages_of = [&](int i) __attribute__((always_inline)) {
-      const int k = key_of(i);
-      return Pages{table[min(k >> a.shift, last)], table[min((k + 16) >> a.shift, last)]};
-    };
+    const int kend = k0 + nk;
     // their first rows in the pool
     auto rows_of = [&](int i, const Pages& p, long& r0, long& r1) __attribute__((always_inline)) {
       const int k = key_of(i), in = (1 << a.shift) - 1;
@@ -584,7 +586,7 @@ __global__ __launch_bounds__(64 * kFewWaves, (few_groups<D, FMT, QN>())) void tr
     };
 
     long r0, r1;
-    rows_of(0, pages_of(0), r0, r1);
+    rows_of(0, pages, r0, r1);
     queue_keys(0, r0, r1);
     queue_vals(0, r0, r1);
     const int m = min(m0 + w.query(), M - 1), ti = a.by_g(m);  // the lane's query row
@@ -596,7 +598,7 @@ __global__ __launch_bounds__(64 * kFewWaves, (few_groups<D, FMT, QN>())) void tr
       queue_keys(i, r0, r1);
       queue_vals(i, r0, r1);
     }
-    Pages ahead_pages = pages_of(R);  // of the block that is queued next
+    pages = pages_of(R);  // of the block that is queued next
     const uint32_t* words = a.mask ? a.mask + tok * a.words : nullptr;
 
     for (int i = 0; i < mine; ++i) {
@@ -604,8 +606,8 @@ __global__ __launch_bounds__(64 * kFewWaves, (few_groups<D, FMT, QN>())) void tr
       const uint32_t kat = ring + i % R * 2 * KB, vat = kat + KB, xat = exps + xout * 256;
       xout = next(xout);
       const int ahead = min(mine - 1 - i, R);  // blocks behind this one, R at most
-      if (ahead == R) rows_of(i + R, ahead_pages, r0, r1);
-      ahead_pages = pages_of(i + R + 1);
+      if (ahead == R) rows_of(i + R, pages, r0, r1);
+      pages = pages_of(i + R + 1);
       if (ahead >= R - 1)
         wait_loads<NI + (R - 1) * G::BI>();
       else if (R == 4 && ahead == 2)
