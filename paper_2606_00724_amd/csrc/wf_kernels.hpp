@@ -191,6 +191,22 @@ struct CacheArgs {
   int blocks;           // workgroups per unit
 };
 
+// Division of 0 <= n < 2^31 by a constant d >= 1: with 2^(l-1) < d <= 2^l, n times
+// ceil(2^(31 + l) / d), shifted right by 31 + l, is the quotient (Granlund and
+// Montgomery 1994).
+struct FastDiv {
+  uint32_t mul;
+  int shift;            // l - 1; -1 for d = 1
+  static FastDiv by(uint32_t d) {
+    int l = 0;
+    while ((1ull << l) < d) ++l;
+    return FastDiv{(uint32_t)(((1ull << (31 + l)) + d - 1) / d), l - 1};
+  }
+  __device__ __forceinline__ int operator()(int n) const {
+    return shift < 0 ? n : (int)(__umulhi((uint32_t)n, mul) >> shift);
+  }
+};
+
 // Angles of rotated rows: positions of several axes times the pairs' frequencies.
 struct TurnArgs {
   const int32_t* pos;   // [axes][rows in all]
@@ -238,7 +254,8 @@ struct MoveArgs {
   uint8_t* x[2];         // exponent bytes, xb a row (quantised)
   int pages, heads, tp, moves, shift;
   int rb, xb;
-  int pc, cols;          // 16-byte pieces of a row in a workgroup, workgroups a row takes
+  int pshift, cols;      // log2 of a row's 16-byte pieces in a workgroup, workgroups a row takes
+  FastDiv by_cols, by_heads;
 };
 
 // Work of the prefix kernel: units x ranges of their keys x blocks of their query
@@ -256,22 +273,6 @@ struct PrefixPart {
 struct OwnPart {
   int mblocks, mrows;   // blocks per unit, query rows per workgroup
   int kw, qw;           // waves over the keys of a tile, waves over the query rows
-};
-
-// Division of 0 <= n < 2^31 by a constant d >= 1: with 2^(l-1) < d <= 2^l, n times
-// ceil(2^(31 + l) / d), shifted right by 31 + l, is the quotient (Granlund and
-// Montgomery 1994).
-struct FastDiv {
-  uint32_t mul;
-  int shift;            // l - 1; -1 for d = 1
-  static FastDiv by(uint32_t d) {
-    int l = 0;
-    while ((1ull << l) < d) ++l;
-    return FastDiv{(uint32_t)(((1ull << (31 + l)) + d - 1) / d), l - 1};
-  }
-  __device__ __forceinline__ int operator()(int n) const {
-    return shift < 0 ? n : (int)(__umulhi((uint32_t)n, mul) >> shift);
-  }
 };
 
 struct PrefixArgs {

@@ -303,56 +303,71 @@ __global__ __launch_bounds__(kBlock) void append_kernel(AppendArgs a) {
 }
 
 // A workgroup has a column of all rows that one head of a sequence moves, in K or
-// in V: it reads every row before it writes the first.  One round trip each for
-// the sources, their pages and the rows bounds a small call.
+// in V: it reads every row before it writes the first.  Round trips bound a small
+// call, one each for the sources, their pages and the rows: a thread's loads of one
+// kind are queued together, those of the exponents' row beside the others, from
+// places that are always there, and what moves nothing is left out at the end.
 constexpr int kMovePieces = 4;  // 16-byte pieces of a thread
 __global__ __launch_bounds__(kBlock) void move_kernel(MoveArgs a) {
-  const int col = blockIdx.x % a.cols, m = blockIdx.x / a.cols & 1;
-  const int unit = blockIdx.x / (2 * a.cols), head = unit % a.heads, b = unit / a.heads;
+  const int part = a.by_cols(blockIdx.x), col = blockIdx.x - part * a.cols;
+  const int m = part & 1, unit = part >> 1, b = a.by_heads(unit), head = unit - b * a.heads;
+  constexpr int N = kMovePieces + 1;  // (the last one: a row's exponent bytes)
+  const bool exps = a.xb != 0 && col == 0;  // uniform
   const long first = a.first[b];
-  // row t of the sequence in its head's rows of the pool, or -1
-  auto place = [&](long t) -> long {
-    if (t < 0 || t >= (long)a.tp << a.shift) return -1;
-    const long page = a.table[(long)b * a.tp + (t >> a.shift)];
-    if (page < 0 || page >= a.pages) return -1;
-    return ((page * a.heads + head) << a.shift) + (t & ((1 << a.shift) - 1));
+  const int32_t* src = a.src + (long)b * a.moves;
+  const int32_t* table = a.table + (long)b * a.tp;
+  const int in = (1 << a.shift) - 1;
+  auto used = [&](int k) {  // uniform
+    return k < kMovePieces ? k * kBlock < a.moves << a.pshift : exps;
   };
-  auto move = [&](int r, long& from, long& to) {
-    const long s = r < a.moves ? a.src[(long)b * a.moves + r] : -1;
-    from = s < 0 ? -1 : place(first + s);
-    to = s < 0 ? -1 : place(first + r);
-    if (to < 0) from = -1;
-  };
-  char* c = static_cast<char*>(a.c[m]) + (long)col * a.pc * 16;
-  u32x4 v[kMovePieces];
-  long from[kMovePieces], to[kMovePieces];
+  int row[N], s[N], pf[N], pt[N];
 #pragma unroll
-  for (int k = 0; k < kMovePieces; ++k) {
-    const int p = threadIdx.x + k * kBlock;
-    move(p / a.pc, from[k], to[k]);
+  for (int k = 0; k < N; ++k) {
+    row[k] = k < kMovePieces ? (int)(threadIdx.x + k * kBlock) >> a.pshift : (int)threadIdx.x;
+    if (used(k)) s[k] = src[min(row[k], a.moves - 1)];
   }
+  auto index = [&](long t) { return (int)min(max(t >> a.shift, 0L), a.tp - 1L); };
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+    if (used(k)) {
+      pf[k] = table[index(first + s[k])];
+      pt[k] = table[index(first + row[k])];
+    }
+  // row t of the sequence, in page `page`, in its head's rows of the pool
+  auto place = [&](long t, int page) {
+    return (((long)min(max(page, 0), a.pages - 1) * a.heads + head) << a.shift) + (t & in);
+  };
+  auto there = [&](long t, int page) {
+    return t >= 0 && t < (long)a.tp << a.shift && page >= 0 && page < a.pages;
+  };
+  auto moves = [&](int k) {
+    return row[k] < a.moves && s[k] >= 0 && there(first + s[k], pf[k]) &&
+           there(first + row[k], pt[k]);
+  };
+  const int piece = threadIdx.x & ((1 << a.pshift) - 1);
+  char* c = static_cast<char*>(a.c[m]) + (((long)col << a.pshift) + piece) * 16;
+  u32x4 v[kMovePieces];
+  uint32_t x = 0;
 #pragma unroll
   for (int k = 0; k < kMovePieces; ++k)
-    if (from[k] >= 0)
-      v[k] = *reinterpret_cast<const u32x4*>(c + from[k] * a.rb + (threadIdx.x + k * kBlock) % a.pc * 16);
-  long xfrom = -1, xto = -1;
-  uint32_t x = 0;
-  if (a.xb && col == 0) {  // the exponent bytes: a row of a thread
-    move(threadIdx.x, xfrom, xto);
-    if (xfrom >= 0)
-      x = a.xb == 4 ? *reinterpret_cast<const uint32_t*>(a.x[m] + xfrom * 4)
-                    : *reinterpret_cast<const uint16_t*>(a.x[m] + xfrom * 2);
+    if (used(k)) v[k] = *reinterpret_cast<const u32x4*>(c + place(first + s[k], pf[k]) * a.rb);
+  constexpr int X = kMovePieces;
+  if (exps) {
+    const uint8_t* from = a.x[m] + place(first + s[X], pf[X]) * a.xb;
+    x = a.xb == 4 ? *reinterpret_cast<const uint32_t*>(from)
+                  : *reinterpret_cast<const uint16_t*>(from);
   }
   __syncthreads();  // (waits for the loads)
 #pragma unroll
   for (int k = 0; k < kMovePieces; ++k)
-    if (from[k] >= 0)
-      *reinterpret_cast<u32x4*>(c + to[k] * a.rb + (threadIdx.x + k * kBlock) % a.pc * 16) = v[k];
-  if (xfrom >= 0) {
+    if (used(k) && moves(k))
+      *reinterpret_cast<u32x4*>(c + place(first + row[k], pt[k]) * a.rb) = v[k];
+  if (exps && moves(X)) {
+    uint8_t* to = a.x[m] + place(first + row[X], pt[X]) * a.xb;
     if (a.xb == 4)
-      *reinterpret_cast<uint32_t*>(a.x[m] + xto * 4) = x;
+      *reinterpret_cast<uint32_t*>(to) = x;
     else
-      *reinterpret_cast<uint16_t*>(a.x[m] + xto * 2) = (uint16_t)x;
+      *reinterpret_cast<uint16_t*>(to) = (uint16_t)x;
   }
 }
 
@@ -492,7 +507,11 @@ hipError_t launch_move(const wf_move_params& p, const int32_t* table, const int3
   a.shift = __builtin_ctz(p.page_rows);
   a.rb = row_bytes(p.head_dim, p.dtype, p.format);
   a.xb = p.format == WF_CACHE_PLAIN ? 0 : p.head_dim / 32;
-  move_split(p, a.pc, a.cols);
+  int pc;
+  move_split(p, pc, a.cols);
+  a.pshift = __builtin_ctz(pc);
+  a.by_cols = FastDiv::by(a.cols);
+  a.by_heads = FastDiv::by(a.heads);
   hipLaunchKernelGGL(move_kernel, dim3((unsigned)move_groups(p)), dim3(kBlock), 0, s, a);
   return hipGetLastError();
 }
