@@ -18,7 +18,7 @@ namespace wf {
 template <int D>
 constexpr int kTurnRows = 2 * kBlock / D;
 constexpr int kTurnHeads = 8;
-constexpr int kTurnBatch = 4;  // heads whose rows a thread has in flight
+constexpr int kTurnBatch = 2;  // rows of a thread, both on their way at once
 
 // Sine and cosine in 64 bits.  The angle is taken to [-pi/4, pi/4] by a multiple
 // of pi/2 in two parts (Cody and Waite 1980; the product is not rounded before it
@@ -169,37 +169,31 @@ __global__ __launch_bounds__(kBlock) void rope_kernel(RopeArgs a) {
   const T* X = static_cast<const T*>(a.X) + b * a.xs[0] + min(r, a.rows - 1) * a.xs[2];
   T* Y = static_cast<T*>(a.Y) + b * a.ys[0] + min(r, a.rows - 1) * a.ys[2];
   Raw8<T> va[kTurnBatch], vb[kTurnBatch];
-  auto load = [&](int i0) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < kTurnBatch; ++i) {
-      const long h = h0 + (i0 + i) * kTurnHeads;
-      if (i0 + i >= a.iters || h >= a.heads || r >= a.rows) continue;
-      va[i].load(X + h * a.xs[1] + at.oa);
-      vb[i].load(X + h * a.xs[1] + at.ob);
-    }
-  };
-  load(0);
+  for (int i = 0; i < kTurnBatch; ++i) {
+    const long h = h0 + i * kTurnHeads;
+    if (i >= a.iters || h >= a.heads || r >= a.rows) continue;
+    va[i].load(X + h * a.xs[1] + at.oa);
+    vb[i].load(X + h * a.xs[1] + at.ob);
+  }
   turns.stage(a.turn, [&](int i) { return (long)b * a.rows + min(r0 + i, a.rows - 1); });
   Turn8 t;
   t.read(turns, at.token, at.turns ? 8 * at.c : 0);
-  for (int i0 = 0; i0 < a.iters; i0 += kTurnBatch) {
-    if (i0 > 0) load(i0);
 #pragma unroll
-    for (int i = 0; i < kTurnBatch; ++i) {
-      const long h = h0 + (i0 + i) * kTurnHeads;
-      if (i0 + i >= a.iters || h >= a.heads || r >= a.rows) continue;
-      T* y = Y + h * a.ys[1];
-      if (at.turns) {
-        float x1[8], x2[8];
-        va[i].values(x1);
-        vb[i].values(x2);
-        t.turn(x1, x2, a.turn.pairs);
-        put8(y + at.oa, x1);
-        put8(y + at.ob, x2);
-      } else {
-        va[i].store(y + at.oa);
-        vb[i].store(y + at.ob);
-      }
+  for (int i = 0; i < kTurnBatch; ++i) {
+    const long h = h0 + i * kTurnHeads;
+    if (i >= a.iters || h >= a.heads || r >= a.rows) continue;
+    T* y = Y + h * a.ys[1];
+    if (at.turns) {
+      float x1[8], x2[8];
+      va[i].values(x1);
+      vb[i].values(x2);
+      t.turn(x1, x2, a.turn.pairs);
+      put8(y + at.oa, x1);
+      put8(y + at.ob, x2);
+    } else {
+      va[i].store(y + at.oa);
+      vb[i].store(y + at.ob);
     }
   }
 }
@@ -220,84 +214,78 @@ __global__ __launch_bounds__(kBlock) void append_kernel(AppendArgs a) {
   const long token = min(n, a.tokens - 1);
   const long slot = a.slot[token];
   Raw8<T> va[kTurnBatch], vb[kTurnBatch];
-  auto load = [&](int i0) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < kTurnBatch; ++i) {
-      const int h = h0 + (i0 + i) * kTurnHeads;
-      if (i0 + i >= a.iters || h >= all || n >= a.tokens) continue;
-      const T* x = h < a.hq ? static_cast<const T*>(a.Q) + token * a.qs + (long)h * D
-                   : h < a.hq + a.heads
-                       ? static_cast<const T*>(a.K) + token * a.ks + (long)(h - a.hq) * D
-                       : static_cast<const T*>(a.V) + token * a.vs + (long)(h - a.hq - a.heads) * D;
-      va[i].load(x + at.oa);
-      vb[i].load(x + at.ob);
-    }
-  };
-  load(0);
+  for (int i = 0; i < kTurnBatch; ++i) {
+    const int h = h0 + i * kTurnHeads;
+    if (i >= a.iters || h >= all || n >= a.tokens) continue;
+    const T* x = h < a.hq ? static_cast<const T*>(a.Q) + token * a.qs + (long)h * D
+                 : h < a.hq + a.heads
+                     ? static_cast<const T*>(a.K) + token * a.ks + (long)(h - a.hq) * D
+                     : static_cast<const T*>(a.V) + token * a.vs + (long)(h - a.hq - a.heads) * D;
+    va[i].load(x + at.oa);
+    vb[i].load(x + at.ob);
+  }
   turns.stage(a.turn, [&](int i) { return (long)min(t0 + i, a.tokens - 1); });
   Turn8 t;
   t.read(turns, at.token, at.turns ? 8 * at.c : 0);
   const bool kept = slot >= 0 && slot < a.slots;
   const long page = slot >> a.shift, row = slot & ((1 << a.shift) - 1);
-  for (int i0 = 0; i0 < a.iters; i0 += kTurnBatch) {
-    if (i0 > 0) load(i0);
 #pragma unroll
-    for (int i = 0; i < kTurnBatch; ++i) {
-      const int h = h0 + (i0 + i) * kTurnHeads;
-      if (i0 + i >= a.iters || h >= all || n >= a.tokens) continue;
-      const bool query = h < a.hq, value = h >= a.hq + a.heads;
-      if (!query && !kept) continue;
-      const int head = h - a.hq - (value ? a.heads : 0);  // of the pool
-      const long to = ((page * a.heads + head) << a.shift) + row;
-      float x1[8], x2[8];
-      va[i].values(x1);
-      vb[i].values(x2);
-      const bool turned = at.turns && !value;
-      if (turned) t.turn(x1, x2, a.turn.pairs);
-      if (query || !QUANT) {
-        T* y = query ? static_cast<T*>(a.Qr) + token * a.os + (long)h * D
-                     : static_cast<T*>(value ? a.Vc : a.Kc) + to * D;
-        if (turned) {
-          put8(y + at.oa, x1);
-          put8(y + at.ob, x2);
-        } else {  // (their bits, NaN's too)
-          va[i].store(y + at.oa);
-          vb[i].store(y + at.ob);
-        }
-      } else {
-        // a block's largest magnitude over its four eights, which may be other
-        // threads' of the row: they are in one wave, whose LDS operations go in order
-        uint32_t ma = 0, mb = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          ma = max(ma, __float_as_uint(x1[e]) & 0x7fffffffu);
-          mb = max(mb, __float_as_uint(x2[e]) & 0x7fffffffu);
-        }
-        uint32_t* m = top[threadIdx.x / C];
-        m[at.oa / 8] = ma;
-        m[at.ob / 8] = mb;
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const int o = k ? at.ob : at.oa;
-          const u32x4 w = *reinterpret_cast<const u32x4*>(m + o / 32 * 4);
-          const uint32_t x = block_exponent<FMT>(max(max(w[0], w[1]), max(w[2], w[3])));
-          const float s = block_unscale(x);
-          float y[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) y[e] = x == 255u ? 0.f : (k ? x2 : x1)[e] * s;
-          const u32x2 code = encode8<FMT>(y);
-          uint8_t* c = static_cast<uint8_t*>(value ? a.Vc : a.Kc) + (to * (D / 8) + o / 8) * CB;
-          if constexpr (CB == 8)
-            *reinterpret_cast<u32x2*>(c) = code;
-          else
-            *reinterpret_cast<uint32_t*>(c) = code[0];
-          if (o % 32 == 0) (value ? a.Vx : a.Kx)[to * (D / 32) + o / 32] = (uint8_t)x;
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
+  for (int i = 0; i < kTurnBatch; ++i) {
+    const int h = h0 + i * kTurnHeads;
+    if (i >= a.iters || h >= all || n >= a.tokens) continue;
+    const bool query = h < a.hq, value = h >= a.hq + a.heads;
+    if (!query && !kept) continue;
+    const int head = h - a.hq - (value ? a.heads : 0);  // of the pool
+    const long to = ((page * a.heads + head) << a.shift) + row;
+    float x1[8], x2[8];
+    va[i].values(x1);
+    vb[i].values(x2);
+    const bool turned = at.turns && !value;
+    if (turned) t.turn(x1, x2, a.turn.pairs);
+    if (query || !QUANT) {
+      T* y = query ? static_cast<T*>(a.Qr) + token * a.os + (long)h * D
+                   : static_cast<T*>(value ? a.Vc : a.Kc) + to * D;
+      if (turned) {
+        put8(y + at.oa, x1);
+        put8(y + at.ob, x2);
+      } else {  // (their bits, NaN's too)
+        va[i].store(y + at.oa);
+        vb[i].store(y + at.ob);
       }
+    } else {
+      // a block's largest magnitude over its four eights, which may be other
+      // threads' of the row: they are in one wave, whose LDS operations go in order
+      uint32_t ma = 0, mb = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        ma = max(ma, __float_as_uint(x1[e]) & 0x7fffffffu);
+        mb = max(mb, __float_as_uint(x2[e]) & 0x7fffffffu);
+      }
+      uint32_t* m = top[threadIdx.x / C];
+      m[at.oa / 8] = ma;
+      m[at.ob / 8] = mb;
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int o = k ? at.ob : at.oa;
+        const u32x4 w = *reinterpret_cast<const u32x4*>(m + o / 32 * 4);
+        const uint32_t x = block_exponent<FMT>(max(max(w[0], w[1]), max(w[2], w[3])));
+        const float s = block_unscale(x);
+        float y[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = x == 255u ? 0.f : (k ? x2 : x1)[e] * s;
+        const u32x2 code = encode8<FMT>(y);
+        uint8_t* c = static_cast<uint8_t*>(value ? a.Vc : a.Kc) + (to * (D / 8) + o / 8) * CB;
+        if constexpr (CB == 8)
+          *reinterpret_cast<u32x2*>(c) = code;
+        else
+          *reinterpret_cast<uint32_t*>(c) = code[0];
+        if (o % 32 == 0) (value ? a.Vx : a.Kx)[to * (D / 32) + o / 32] = (uint8_t)x;
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
     }
   }
 }
@@ -373,14 +361,13 @@ __global__ __launch_bounds__(kBlock) void move_kernel(MoveArgs a) {
 
 // ------------------------------------------------------------ host side
 
-// Workgroups over `all` heads for `blocks` blocks of tokens: each takes as many
-// eights of heads as leave the chip several workgroups a CU, up to eight.
+// Workgroups over `all` heads for `blocks` blocks of tokens: each takes two eights of
+// heads where that leaves the chip several workgroups a CU.  (32K tokens of 48 heads
+// in 8 bits 132 us, and 150 with four eights in flight, which leave a SIMD fewer
+// waves, 141 with one, whose angles are as much work as the rows.)
 static void split_heads(long blocks, int all, int& hgroups, int& iters) {
   const int eights = (all + kTurnHeads - 1) / kTurnHeads;
-  iters = 1;
-  while (2 * iters <= 8 && 2 * iters <= eights &&
-         blocks * ((eights + 2 * iters - 1) / (2 * iters)) >= 8L * device_cu_count())
-    iters *= 2;
+  iters = eights > 1 && blocks * ((eights + 1) / 2) >= 8L * device_cu_count() ? kTurnBatch : 1;
   hgroups = (eights + iters - 1) / iters;
 }
 
