@@ -511,29 +511,31 @@ TreePlan plan_tree(const wf_tree_params& p, size_t have) {
     best = l;
     best.rps = (int)rps;
   };
-  bool few = bf, many = !bf || M > 32;
+  bool few = true, many = M > (bf ? 32 : 16);
   // Few query rows: 32 a workgroup of four waves, two workgroups a CU; the blocks of
   // query rows read the same keys, mostly from the L2.
   if (few) {
     TreePlan l{};
-    l.few = M <= 16 ? 16 : 32;
+    l.few = !bf || M <= 16 ? 16 : 32;
     l.qw = 1;
     l.nw = l.kw = 4;
     l.mblocks = (int)((M + l.few - 1) / l.few);
     const long KT = 128, tiles = std::max(1L, (p.max_len + KT - 1) / KT);
-    const double alone = D / 128.0 * (!quant || l.few == 16 ? 1.0 : 1.4);
-    const double both = D / 128.0 * (l.few == 16 ? 1.3 : 2.4);
+    // a tile of a workgroup that has its CU alone, and of one that shares it
+    const double alone = !bf ? 1.6 + D / 160.0 : D / 128.0 * (!quant || l.few == 16 ? 1.0 : 1.4);
+    const double both = D / 128.0 * (!bf ? 5.4 : l.few == 16 ? 1.3 : 2.4);
+    const double most_at_once = !bf && !quant && D == 128 ? 1.0 : 2.0;
     for (long n = 1; n <= tiles; n += 1 + n / 16) {
       const long per = (tiles + n - 1) / n, s = (tiles + per - 1) / per;
       if (s > 1 && s > most) break;
       const double groups = (double)(U * l.mblocks * s), per_cu = std::ceil(groups / cus);
-      const double at_once = std::min(per_cu, 2.0);
+      const double at_once = std::min(per_cu, most_at_once);
       const double bytes = 2 * KT * row_bytes / std::min(l.mblocks, 3) *
                            std::max(std::min(groups, at_once * cus) / 6e6, at_once / 32e3);
-      const double tile = std::max(per_cu > 1 ? both : alone, bytes);
+      const double tile = std::max(at_once > 1 ? both : alone, bytes);
       // (lengths that differ leave some CUs idle at the end: a part of a workgroup's time)
       take(l, per * KT,
-           std::max(1.0, per_cu / 2) * (per * tile + 6.0) + 0.2 * per * tile + merge(s));
+           std::max(1.0, per_cu / most_at_once) * (per * tile + 6.0) + 0.2 * per * tile + merge(s));
     }
   }
   // Many: a block of query rows for the workgroup, as of the attention over a prefix.
@@ -631,7 +633,7 @@ hipError_t launch_tree(const wf_tree_params& p, const TreePlan& l, TreeArgs& a, 
     };
     hipError_t e = hipErrorInvalidValue;
     if (l.few)
-      e = launch_tree_few(a, D, p.format, l.few, l.items, s);
+      e = launch_tree_few(a, p.dtype, D, p.format, l.few, l.items, s);
     else if (p.format == WF_CACHE_E4M3)
       e = go(tree_attn_kernel<T, D, WF_CACHE_E4M3, 1>);
     else if (p.format == WF_CACHE_E2M1)

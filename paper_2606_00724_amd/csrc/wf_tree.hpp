@@ -100,8 +100,8 @@ __device__ __forceinline__ void add_odd(const TreeArgs& a, const Sequence& s, in
   }
 }
 
-// (rows: query rows of a workgroup, 16 or 32)
-hipError_t launch_tree_few(const TreeArgs& a, int head_dim, int format, int rows, long items,
-                           hipStream_t s);
+// (rows: query rows of a workgroup, 16 or, in bf16, 32)
+hipError_t launch_tree_few(const TreeArgs& a, int dtype, int head_dim, int format, int rows,
+                           long items, hipStream_t s);
 
 }  // namespace wf

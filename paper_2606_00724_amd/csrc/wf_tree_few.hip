@@ -21,18 +21,20 @@ typedef int v2i_few __attribute__((ext_vector_type(2)));
 
 // A wave's ring.  Rows of a block stand after each other, their 16-byte chunks in an
 // order that lets the lanes that read at once meet all banks: eight rows at one chunk
-// of K, and of V eight rows (8 bits), sixteen (4 bits) or four at two chunks (bf16).
-template <int D, int FMT>
+// of K, and of V eight rows (8 bits), sixteen (4 bits), four at two chunks (bf16) or
+// every fourth one at 64 bytes (fp32).
+template <typename T, int D, int FMT>
 struct FewGeom {
   static constexpr bool QUANT = FMT != WF_CACHE_PLAIN;
-  static constexpr int RB = QUANT ? (FMT == WF_CACHE_E4M3 ? D : D / 2) : 2 * D;  // bytes of a row
+  static constexpr int RB = QUANT ? (FMT == WF_CACHE_E4M3 ? D : D / 2)
+                                  : D * (int)sizeof(T);        // bytes of a row
   static constexpr int C = RB / 16;                            // chunks of a row
   static constexpr int KB = 32 * RB;                           // bytes of 32 rows
   static constexpr int NI = KB / 1024;                         // loads of 32 rows
   static constexpr int RPI = 64 / C;                           // rows of a load
   static constexpr int XB = D / 32;                            // exponent bytes of a row
   static constexpr int XL = QUANT ? 1 : 0;                     // loads of a block's exponents
-  static constexpr int R = KB >= 4096 ? 1 : 2;  // blocks of the ring
+  static constexpr int R = KB >= 4096 ? 1 : 2;                 // blocks of the ring
   static constexpr int XR = R + 1;  // a block's exponents outlive its keys
   static constexpr int WAVE = R * 2 * KB + XL * XR * 256;      // bytes of a wave
   static constexpr int BI = 2 * NI + XL;                       // loads of a block
@@ -41,10 +43,24 @@ struct FewGeom {
     return C >= 8 ? r & 7 : C == 4 ? (r >> 1) & 3 : (r >> 2) & 1;
   }
   __device__ __forceinline__ static constexpr int vswz(int r) {
-    return QUANT ? swz(r) : (r & 3) << 1;
+    return QUANT ? swz(r) : sizeof(T) == 2 ? (r & 3) << 1 : (r >> 2 & 3) << 2;
   }
   __device__ __forceinline__ static int at(int r, int c) { return r * RB + 16 * (c ^ swz(r)); }
   __device__ __forceinline__ static int vat(int r, int c) { return r * RB + 16 * (c ^ vswz(r)); }
+  // Loads Q, Q + 1, ... of 32 rows of K, or V, from b0 and b1 on (sixteen each); off:
+  // the lane's place in the first one (row and chunk orders are xors of their bits).
+  template <bool V, int Q = 0>
+  __device__ __forceinline__ static void load(const unsigned char* b0, const unsigned char* b1,
+                                              uint32_t off, uint32_t lds) {
+    if constexpr (C == 2) {  // sixteen rows in each half of the wave
+      row_load<0>(((threadIdx.x & 32) == 0 ? b0 : b1 - 16 * RB) + off, lds);
+    } else if constexpr (Q < NI) {
+      constexpr int in = Q * 1024 % (16 * RB), imm = in & 4095;
+      constexpr uint32_t x = 16 * (V ? vswz(Q * RPI) : swz(Q * RPI));
+      tile_load<imm, Q * 1024>((Q * 1024 >= 16 * RB ? b1 : b0) + (in - imm), off ^ x, lds);
+      load<V, Q + 1>(b0, b1, off, lds);
+    }
+  }
 };
 
 template <int N>
@@ -67,11 +83,12 @@ __device__ __forceinline__ V lds_read(uint32_t at) {
 }
 
 // The bits of those values of a word that are no numbers.
-template <int FMT>
+template <typename T, int FMT>
 __device__ __forceinline__ uint32_t odd_bits(uint32_t w) {
   uint32_t odd = 0;
-  constexpr int B = FMT == WF_CACHE_PLAIN ? 16 : 8;
-  constexpr uint32_t top = FMT == WF_CACHE_PLAIN ? 0x7f80u : 0x7fu, all = (1u << B) - 1u;
+  constexpr int B = FMT != WF_CACHE_PLAIN ? 8 : 8 * (int)sizeof(T);
+  constexpr uint32_t top = FMT != WF_CACHE_PLAIN ? 0x7fu : sizeof(T) == 2 ? 0x7f80u : 0x7f800000u;
+  constexpr uint32_t all = B == 32 ? ~0u : (1u << (B & 31)) - 1u;
 #pragma unroll
   for (int k = 0; k < 32; k += B) odd |= (w >> k & top) == top ? all << k : 0u;
   return odd;
@@ -129,7 +146,7 @@ __device__ __forceinline__ float times_exponent(float w, uint32_t x, int b) {
 // A lane has scores of query row l % 32, keys 8 (e / 4) + 4 h + e % 4.
 template <int D, int FMT>
 struct FewRows32 {
-  using G = FewGeom<D, FMT>;
+  using G = FewGeom<bf16_t, D, FMT>;
   using W = PrefixWave<bf16_t, D, 1>;
   static constexpr int QN = 32, RB = G::RB, XB = G::XB, DT = D / 32;
   W w;
@@ -282,10 +299,14 @@ struct FewRows32 {
 
 // For 16 query rows: products of 16 x 16, half the softmax and weights of 32 rows.
 // A lane has scores of query row l % 16, keys 16 (e / 4) + 4 g + e % 4, g = l / 16.
-template <int D, int FMT>
+// bf16 products take 32 channels, or the block's keys, at once (a lane's eight of
+// them), fp32 ones four (a lane's one).
+template <typename T, int D, int FMT>
 struct FewRows16 {
-  using G = FewGeom<D, FMT>;
-  static constexpr int QN = 16, RB = G::RB, XB = G::XB, QS = D / 32, CT = D / 16;
+  using G = FewGeom<T, D, FMT>;
+  static constexpr bool BF = sizeof(T) == 2;
+  static constexpr int QN = 16, RB = G::RB, XB = G::XB, CT = D / 16;
+  static constexpr int QS = BF ? D / 32 : D / 16;  // 16-byte query operands of a lane
   u32x4 q[QS];
   f32x4 O[CT];  // channels 16 c + 4 g .. + 3
   float sc[8], t[8];
@@ -302,8 +323,8 @@ struct FewRows16 {
   }
   __device__ __forceinline__ static int query() { return threadIdx.x & 15; }
   __device__ __forceinline__ static int group() { return (threadIdx.x & 63) >> 4; }
-  // channels g D / 4 + 8 j of step j
-  __device__ __forceinline__ void load(const bf16_t* row) {
+  // channels g D / 4 on
+  __device__ __forceinline__ void load(const T* row) {
 #pragma unroll
     for (int j = 0; j < QS; ++j) q[j] = reinterpret_cast<const u32x4*>(row)[group() * QS + j];
   }
@@ -327,22 +348,47 @@ struct FewRows16 {
     }
     __builtin_amdgcn_sched_barrier(0);  // (all reads queued before the first is waited for)
     f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    if constexpr (BF) {
 #pragma unroll
-    for (int j = 0; j < QS; ++j)
+      for (int j = 0; j < QS; ++j)
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const float scale = block_scale(kx[k]);
-        u32x4 kf;
-        if constexpr (!G::QUANT)
-          kf = kc[k][j];
-        else if constexpr (FMT == WF_CACHE_E4M3)
-          kf = operand<FMT>(kc[k][j / 2][2 * (j & 1)], kc[k][j / 2][2 * (j & 1) + 1], scale);
-        else
-          kf = operand<FMT>(kc[k][0][j], 0, scale);
-        s[k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf),
-                                                       __builtin_bit_cast(bf16x8, q[j]), s[k], 0, 0,
-                                                       0);
+        for (int k = 0; k < 2; ++k) {
+          const float scale = block_scale(kx[k]);
+          u32x4 kf;
+          if constexpr (!G::QUANT)
+            kf = kc[k][j];
+          else if constexpr (FMT == WF_CACHE_E4M3)
+            kf = operand<FMT>(kc[k][j / 2][2 * (j & 1)], kc[k][j / 2][2 * (j & 1) + 1], scale);
+          else
+            kf = operand<FMT>(kc[k][0][j], 0, scale);
+          s[k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf),
+                                                         __builtin_bit_cast(bf16x8, q[j]), s[k], 0,
+                                                         0, 0);
+        }
+    } else {
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j) {  // eight channels
+        float v[2][8];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          if constexpr (FMT == WF_CACHE_E4M3) {
+            decode8<FMT>(u32x2{kc[k][j / 2][2 * (j & 1)], kc[k][j / 2][2 * (j & 1) + 1]},
+                         block_scale(kx[k]), v[k]);
+          } else if constexpr (FMT == WF_CACHE_E2M1) {
+            decode8<FMT>(u32x2{kc[k][0][j], 0u}, block_scale(kx[k]), v[k]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[k][e] = __uint_as_float(kc[k][2 * j + e / 4][e & 3]);
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+          for (int k = 0; k < 2; ++k)
+            s[k] = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                v[k][e], __uint_as_float(q[2 * j + e / 4][e & 3]), s[k], 0, 0, 0);
       }
+    }
 #pragma unroll
     for (int e = 0; e < 8; ++e) sc[e] = s[e >> 2][e & 3];
   }
@@ -402,6 +448,22 @@ struct FewRows16 {
   // A transposed load's rows: the lane's eight keys (in 4 bits twice).
   __device__ __forceinline__ void values(uint32_t vat, uint32_t vx) {
     const int g = group(), i16 = threadIdx.x & 15;
+    if constexpr (!BF && !G::QUANT) {
+      // (fp32: a channel of a lane, row by row)
+      uint32_t vb = vat + G::vat(4 * g, i16 >> 2) + 4 * (i16 & 3);
+      asm volatile("" : "+v"(vb));
+#pragma unroll
+      for (int c = 0; c < CT; ++c) {
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          v[e] = lds_read<float>((vb ^ (64 * c)) + (16 * (e >> 2) + (e & 3)) * RB);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          O[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e], t[e], O[c], 0, 0, 0);
+      }
+      return;
+    }
     const int p = FMT == WF_CACHE_E4M3 ? i16 >> 1 : FMT == WF_CACHE_E2M1 ? i16 & 7 : i16 >> 2;
     const int row = 16 * (p >> 2) + 4 * g + (p & 3);
     uint32_t vb = vat + (FMT == WF_CACHE_E4M3   ? G::vat(row, 0) + 8 * (i16 & 1)
@@ -431,25 +493,38 @@ struct FewRows16 {
 #pragma unroll
       for (int e = 0; e < 8; ++e) t[e] += t[e];
     }
+    // the weight of the lane's key e for channels 32 d ..: times 2^(x - 127)
+    auto weight = [&](int e, int d) __attribute__((always_inline)) {
+      const int b = e * XB + d;
+      return times_exponent(t[e], xs[b / 4], b & 3);
+    };
     u32x4 pf;
+    float pw[8];
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
       if (G::QUANT ? c % 2 == 0 : c == 0) {  // the weights for 32 channels, or for all
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int b0 = 2 * e * XB + c / 2, b1 = b0 + XB;
-          pf[e] = G::QUANT ? pack_bf16x2(times_exponent(t[2 * e], xs[b0 / 4], b0 & 3),
-                                         times_exponent(t[2 * e + 1], xs[b1 / 4], b1 & 3))
-                           : pack_bf16x2(t[2 * e], t[2 * e + 1]);
-        }
+        for (int e = 0; e < 8; ++e) pw[e] = G::QUANT ? weight(e, c / 2) : t[e];
+        if constexpr (BF)
+          pf = u32x4{pack_bf16x2(pw[0], pw[1]), pack_bf16x2(pw[2], pw[3]),
+                     pack_bf16x2(pw[4], pw[5]), pack_bf16x2(pw[6], pw[7])};
       }
-      u32x4 vf;
-      if constexpr (!G::QUANT)
-        vf = u32x4{w[c][0][0], w[c][0][1], w[c][1][0], w[c][1][1]};
-      else
-        vf = operand<FMT>(w[c][0][0], w[c][0][1], 1.f);
-      O[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf),
-                                                     __builtin_bit_cast(bf16x8, pf), O[c], 0, 0, 0);
+      if constexpr (BF) {
+        u32x4 vf;
+        if constexpr (!G::QUANT)
+          vf = u32x4{w[c][0][0], w[c][0][1], w[c][1][0], w[c][1][1]};
+        else
+          vf = operand<FMT>(w[c][0][0], w[c][0][1], 1.f);
+        O[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf),
+                                                       __builtin_bit_cast(bf16x8, pf), O[c], 0, 0,
+                                                       0);
+      } else if constexpr (G::QUANT) {
+        float v[8];
+        decode8<FMT>(w[c][0], 1.f, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          O[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e], pw[e], O[c], 0, 0, 0);
+      }
     }
   }
   __device__ __forceinline__ void put(float* o, float* st, int stride) {
@@ -473,15 +548,16 @@ struct FewOut {
 };
 
 // Workgroups per CU, as their registers and LDS fit.
-template <int D, int FMT, int QN>
+template <typename T, int D, int FMT, int QN>
 constexpr int few_groups() {
-  return QN == 16 && FMT != WF_CACHE_PLAIN ? 3 : 2;
+  const bool quant = FMT != WF_CACHE_PLAIN;
+  return sizeof(T) == 4 ? (quant || D == 64 ? 2 : 1) : QN == 16 && quant ? 3 : 2;
 }
 
-template <int D, int FMT, int QN>
-__global__ __launch_bounds__(64 * kFewWaves, (few_groups<D, FMT, QN>())) void tree_few_kernel(
+template <typename T, int D, int FMT, int QN>
+__global__ __launch_bounds__(64 * kFewWaves, (few_groups<T, D, FMT, QN>())) void tree_few_kernel(
     TreeArgs a) {
-  using G = FewGeom<D, FMT>;
+  using G = FewGeom<T, D, FMT>;
   constexpr int NI = G::NI, R = G::R, RB = G::RB, KB = G::KB, XB = G::XB;
   constexpr bool QUANT = G::QUANT;
   extern __shared__ __align__(16) unsigned char smem[];  // the waves' rings, a flag
@@ -513,7 +589,7 @@ __global__ __launch_bounds__(64 * kFewWaves, (few_groups<D, FMT, QN>())) void tr
   const int M = s.n * a.g;
   const int nk = min(a.rps, s.L - k0);  // the range's keys
   if (m0 >= M || (nk <= 0 && !a.whole)) return;
-  std::conditional_t<QN == 32, FewRows32<D, FMT>, FewRows16<D, FMT>> w;
+  std::conditional_t<QN == 32, FewRows32<D, FMT>, FewRows16<T, D, FMT>> w;
   w.init(a.scale);
   if (threadIdx.x == 0) *flag = 0;
   lds_barrier();
@@ -533,41 +609,16 @@ __global__ __launch_bounds__(64 * kFewWaves, (few_groups<D, FMT, QN>())) void tr
     const uint32_t ring = lds_offset(smem) + wave * G::WAVE, exps = ring + R * 2 * KB;
     // the lane's 16 bytes of a load: row of those that it holds, chunk
     const int lrow = lane / G::C;
-    const uint32_t koff[2] = {(uint32_t)(lrow * RB + 16 * (lane % G::C ^ G::swz(lrow))),
-                              (uint32_t)(lrow * RB + 16 * (lane % G::C ^ G::swz(lrow + G::RPI)))};
-    const uint32_t voff[2] = {(uint32_t)(lrow * RB + 16 * (lane % G::C ^ G::vswz(lrow))),
-                              (uint32_t)(lrow * RB + 16 * (lane % G::C ^ G::vswz(lrow + G::RPI)))};
+    const uint32_t koff = lrow * RB + 16 * (lane % G::C ^ G::swz(lrow));
+    const uint32_t voff = lrow * RB + 16 * (lane % G::C ^ G::vswz(lrow));
     // the lane's 4 bytes of the exponents: K's of the 32 rows, then V's (again in the
     // lanes behind them)
     constexpr int XD = 8 * XB;
     const int xl = lane % (2 * XD), xg = xl % XD / (XD / 2);
     const uint8_t* xbase = (xl / XD ? a.Vx : a.Kx) + 4 * (xl % (XD / 2));
-    // block i's loads: 32 rows of K or V from r0 and r1 on
-    auto load = [&](const void* P, long r0, long r1, uint32_t lds, const uint32_t(&off)[2])
-                    __attribute__((always_inline)) {
-      const unsigned char* b0 = static_cast<const unsigned char*>(P) + r0 * RB;
-      const unsigned char* b1 = static_cast<const unsigned char*>(P) + r1 * RB;
-      if constexpr (G::C == 16) {  // four rows a load
-        tile_load<0, 0>(b0, off[0], lds);
-        tile_load<1024, 1024>(b0, off[1], lds);
-        tile_load<2048, 2048>(b0, off[0], lds);
-        tile_load<3072, 3072>(b0, off[1], lds);
-        tile_load<0, 4096>(b1, off[0], lds);
-        tile_load<1024, 5120>(b1, off[1], lds);
-        tile_load<2048, 6144>(b1, off[0], lds);
-        tile_load<3072, 7168>(b1, off[1], lds);
-      } else if constexpr (G::C == 8) {
-        tile_load<0, 0>(b0, off[0], lds);
-        tile_load<1024, 1024>(b0, off[0], lds);
-        tile_load<0, 2048>(b1, off[0], lds);
-        tile_load<1024, 3072>(b1, off[0], lds);
-      } else if constexpr (G::C == 4) {
-        tile_load<0, 0>(b0, off[0], lds);
-        tile_load<0, 1024>(b1, off[0], lds);
-      } else {
-        row_load<0>((lane < 32 ? b0 : b1 - 16 * RB) + off[0], lds);
-      }
-    };
+    // block i's loads: rows from r0 and r1 on
+    const unsigned char* K = static_cast<const unsigned char*>(a.K);
+    const unsigned char* V = static_cast<const unsigned char*>(a.V);
     auto exp_load = [&](long r0, long r1, uint32_t lds) __attribute__((always_inline)) {
       word_load(xbase + (xg ? r1 : r0) * XB, lds);
     };
@@ -575,14 +626,14 @@ __global__ __launch_bounds__(64 * kFewWaves, (few_groups<D, FMT, QN>())) void tr
     int xin = 0, xout = 0;
     auto next = [&](int x) { return x + 1 == G::XR ? 0 : x + 1; };
     auto queue_keys = [&](int i, long r0, long r1) __attribute__((always_inline)) {
-      load(a.K, r0, r1, ring + i % R * 2 * KB, koff);
+      G::template load<false>(K + r0 * RB, K + r1 * RB, koff, ring + i % R * 2 * KB);
       if constexpr (QUANT) {
         exp_load(r0, r1, exps + xin * 256);
         xin = next(xin);
       }
     };
     auto queue_vals = [&](int i, long r0, long r1) __attribute__((always_inline)) {
-      load(a.V, r0, r1, ring + i % R * 2 * KB + KB, voff);
+      G::template load<true>(V + r0 * RB, V + r1 * RB, voff, ring + i % R * 2 * KB + KB);
     };
 
     long r0, r1;
@@ -591,7 +642,7 @@ __global__ __launch_bounds__(64 * kFewWaves, (few_groups<D, FMT, QN>())) void tr
     queue_vals(0, r0, r1);
     const int m = min(m0 + w.query(), M - 1), ti = a.by_g(m);  // the lane's query row
     const long tok = min(max(s.first + ti, 0L), a.tokens - 1L);
-    w.load(static_cast<const bf16_t*>(a.Q) + tok * a.qs + (long)(head * a.g + m - ti * a.g) * D);
+    w.load(static_cast<const T*>(a.Q) + tok * a.qs + (long)(head * a.g + m - ti * a.g) * D);
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): so that no later wait is for these
     for (int i = 1; i < min(R, mine); ++i) {
       rows_of(i, pages_of(i), r0, r1);
@@ -658,7 +709,7 @@ __global__ __launch_bounds__(64 * kFewWaves, (few_groups<D, FMT, QN>())) void tr
         for (int c = lane; c < nv * G::C; c += 64) {
           const u32x4 v = lds_read<u32x4>(vat + 16 * c);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) odd |= odd_bits<FMT>(v[e]) != 0;
+          for (int e = 0; e < 4; ++e) odd |= odd_bits<T, FMT>(v[e]) != 0;
         }
       if (__builtin_amdgcn_ballot_w64(odd) != 0) {  // rare
         if (lane == 0) *flag = 1;
@@ -666,7 +717,7 @@ __global__ __launch_bounds__(64 * kFewWaves, (few_groups<D, FMT, QN>())) void tr
           for (int c = lane; c < 32 * G::C; c += 64) {
             u32x4 v = lds_read<u32x4>(vat + 16 * c);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] &= ~odd_bits<FMT>(v[e]);
+            for (int e = 0; e < 4; ++e) v[e] &= ~odd_bits<T, FMT>(v[e]);
             *(__attribute__((address_space(3))) u32x4*)(size_t)(vat + 16 * c) = v;
           }
       }
@@ -696,11 +747,11 @@ __global__ __launch_bounds__(64 * kFewWaves, (few_groups<D, FMT, QN>())) void tr
     const int i = a.by_g(m0 + r);
     const long tok = s.first + i;
     if (!Sequence::there(a, tok)) continue;
-    if (odd) add_odd<bf16_t, D, FMT>(a, s, seq, head, i, k0, k0 + nk, 4 * c, g.o);
+    if (odd) add_odd<T, D, FMT>(a, s, seq, head, i, k0, k0 + nk, 4 * c, g.o);
     const int hq = head * a.g + m0 + r - i * a.g;
     const long row = tok * a.hq + hq;
     if (a.whole) {
-      g.finish(static_cast<bf16_t*>(a.O) + tok * a.os + (long)hq * D + 4 * c,
+      g.finish(static_cast<T*>(a.O) + tok * a.os + (long)hq * D + 4 * c,
                   a.lse ? a.lse + row : nullptr, c == 0);
     } else {
       const long at = row * a.splits + sp;
@@ -712,19 +763,20 @@ __global__ __launch_bounds__(64 * kFewWaves, (few_groups<D, FMT, QN>())) void tr
 
 // ------------------------------------------------------------ host side
 
-template <int D, int FMT, int QN>
+template <typename T, int D, int FMT, int QN>
 static constexpr size_t few_lds() {
-  const size_t rings = (size_t)kFewWaves * FewGeom<D, FMT>::WAVE + sizeof(int);
+  const size_t rings = (size_t)kFewWaves * FewGeom<T, D, FMT>::WAVE + sizeof(int);
   const size_t out = FewOut<D, QN>::BYTES;
   return rings > out ? rings : out;
 }
 
-hipError_t launch_tree_few(const TreeArgs& a, int head_dim, int format, int rows, long items,
-                           hipStream_t s) {
-  auto go = [&](auto d, auto f, auto n) {
+hipError_t launch_tree_few(const TreeArgs& a, int dtype, int head_dim, int format, int rows,
+                           long items, hipStream_t s) {
+  auto go = [&](auto t, auto d, auto f, auto n) {
+    using T = decltype(t);
     constexpr int D = decltype(d)::value, F = decltype(f)::value, QN = decltype(n)::value;
-    constexpr size_t lds = few_lds<D, F, QN>();
-    auto kern = tree_few_kernel<D, F, QN>;
+    constexpr size_t lds = few_lds<T, D, F, QN>();
+    auto kern = tree_few_kernel<T, D, F, QN>;
     if (lds > 65536) {
       const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern),
                                                hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -734,8 +786,10 @@ hipError_t launch_tree_few(const TreeArgs& a, int head_dim, int format, int rows
     return hipGetLastError();
   };
   auto by_rows = [&](auto d, auto f) {
-    return rows == 16 ? go(d, f, std::integral_constant<int, 16>{})
-                      : go(d, f, std::integral_constant<int, 32>{});
+    using N16 = std::integral_constant<int, 16>;
+    if (dtype == WF_F32) return go(float{}, d, f, N16{});
+    return rows == 16 ? go(bf16_t{}, d, f, N16{})
+                      : go(bf16_t{}, d, f, std::integral_constant<int, 32>{});
   };
   auto by_format = [&](auto d) {
     if (format == WF_CACHE_E4M3) return by_rows(d, std::integral_constant<int, WF_CACHE_E4M3>{});
