@@ -324,6 +324,7 @@ def _ws(t) -> tuple[int | None, int]:
     return _ptr(t), t.numel() * t.element_size()
 
 
+_Tensor = torch.Tensor
 # the current device without torch's check that the GPU is in use
 _raw_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 # the current stream's handle without the Python object around it, where torch
@@ -950,6 +951,9 @@ def _rows_form(name, dtype, shape, strides, nullable=False) -> _Form:
     for n in reversed(shape[len(want):]):
         want.insert(len(strides), inner)
         inner *= n
+    dense = [math.prod(shape[i + 1:]) for i in range(len(shape))]
+    if want == dense:
+        return _Form(name, dtype, numel, nullable)
     return _Form(name, dtype, numel, nullable, shape, tuple(want))
 
 
@@ -965,10 +969,10 @@ def _marshal(forms, tensors) -> list[int | None]:
             if not nullable:
                 break
             out.append(None)
-        elif (t.__class__ is torch.Tensor and t.dtype is dtype
+        elif (t.__class__ is _Tensor and t.dtype is dtype
               and t.numel() == numel and t.get_device() == dev
               and (t.is_contiguous() if shape is None
-                   else t.shape == shape and t.stride() == strides)):
+                   else t.stride() == strides and t.shape == shape)):
             out.append(t.data_ptr())
         else:
             break
