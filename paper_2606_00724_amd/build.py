@@ -35,7 +35,8 @@ HIPCC_FLAGS = [
 # in the accumulation half, and the softmax between two products moves them
 # (prefix attention, 64 query rows a wave: 240 moves for 32 products).  The
 # warning left out says at each of its tile loads that m0 is a reserved register
-# (tests/test_build_m0.py holds that the compiler does not use it there).
+# (tests/test_build_m0.py and test_build_m0_tree.py hold that the compiler does not
+# use it there).
 _PRODUCTS = ["-mllvm", "-amdgpu-mfma-vgpr-form=1", "-Wno-inline-asm"]
 EXTRA_FLAGS = {"wf_prefix.hip": _PRODUCTS, "wf_tree.hip": _PRODUCTS,
                "wf_tree_few.hip": _PRODUCTS}
