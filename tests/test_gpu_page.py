@@ -258,6 +258,22 @@ def test_move(wf, fmt, dtype, b, h, d, P, tp, moves):
             same(name, x, y)
 
 
+def test_moves_from_a_page_that_sequences_share(wf):
+    """Rows read from a page of several tables, written into each one's own."""
+    p = wf.make_move_params(pages=6, page_rows=16, heads=2, head_dim=64, batch=3, table_pages=3,
+                            moves=9, format="e4m3")
+    pool = pageref.pool_like(wf, p, 3)
+    table = torch.tensor([[0, 1, 5], [2, 5, 5], [3, 4, 5]]).int()
+    first = torch.tensor([20, 3, 30]).int()
+    source = torch.tensor([[12, 13, 14, 20, 12, -1, 1, 0, 27], [13, 13, 20, 30, 40, 44, -1, -1, 16],
+                           [2, 5, -1, -1, -1, -1, -1, -1, -1]]).int()
+    want = pageref.move(pool, table, first, source, 16)
+    dev = [t.cuda() for t in pool]
+    wf.wf_page_move(p, table.cuda(), first.cuda(), source.cuda(), *dev)
+    for name, x, y in zip(("Kc", "Kx", "Vc", "Vx"), dev, want):
+        same(name, x, y)
+
+
 # ------------------------------------------------------------ as a program uses them
 
 def test_graph_replays_on_another_stream(wf):

@@ -391,3 +391,64 @@ def test_two_streams_at_once(wf):
     for c, (O, lse) in outs:
         want = alone[cases.index(c)]
         assert torch.equal(O.cpu(), want[0]) and torch.equal(lse.cpu(), want[1])
+
+
+@pytest.mark.parametrize("dtype,fmt", FORMATS)
+def test_a_batch_of_many_sequences(wf, dtype, fmt):
+    """Single tokens of 700 sequences that share pages, empty ones among them, with
+    an odd group of heads."""
+    g = torch.Generator().manual_seed(7)
+    lens = torch.randint(-20, 90, (700,), generator=g).clamp(min=0).tolist()
+    c = Case(wf, lens=lens, group=7, mask="none", d=128, dtype=dtype, fmt=fmt, pool_pages=31)
+    c.check(c.run(wf))
+
+
+@pytest.mark.parametrize("dtype,fmt", FORMATS)
+def test_lengths_far_below_the_most(wf, dtype, fmt):
+    """Ranges that no sequence reaches are empty."""
+    for rows, mask in ((1, "none"), (60, "tree")):
+        c = Case(wf, lens=[70, 0, 2500], rows=rows, mask=mask, P=64, max_len=400000, dtype=dtype,
+                 fmt=fmt, pool_pages=50)
+        assert wf.tree_plan(c.p).ranges > 8
+        c.check(c.run(wf))
+
+
+@pytest.mark.parametrize("dtype,fmt", FORMATS)
+def test_many_heads_of_a_group(wf, dtype, fmt):
+    c = Case(wf, lens=[300, 77], rows=256, counts=[256, 3], heads=1, group=32, dtype=dtype,
+             fmt=fmt)
+    c.check(c.run(wf))
+    c = Case(wf, lens=[90, 5], rows=3, heads=2, group=71, dtype=dtype, fmt=fmt, d=128)
+    c.check(c.run(wf))
+
+
+def test_two_graphs_share_a_workspace(wf):
+    """Calls of other shapes, captured each in a graph, leave their partials in one
+    workspace and take no notice of what stands in it."""
+    cases = [Case(wf, lens=[900, 1500], rows=rows, group=2, fmt=fmt, heads=1, seed=rows)
+             for rows, fmt in ((1, None), (40, None), (20, "e2m1"))]
+    want = [c.run(wf) for c in cases]
+    assert all(wf.tree_plan(c.p).ranges > 1 for c in cases)
+    ws = torch.empty(max(wf.tree_workspace_bytes(c.p) for c in cases), dtype=torch.uint8,
+                     device="cuda")
+    s = torch.cuda.Stream()
+    graphs, outs, keep = [], [], []
+    for c, (O, lse) in zip(cases, want):
+        up = [t if t is None else t.cuda() for t in c.pool + [c.table, c.len, None, c.mask]]
+        out = (torch.zeros_like(O, device="cuda"), torch.zeros_like(lse, device="cuda"))
+        Q = c.Q.cuda()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            # (the whole workspace: the split is of the parameters, not of its size)
+            wf.wf_tree_attn(c.p, Q, *up, *out, ws)
+        graphs.append(graph)
+        outs.append(out)
+        keep.append((up, Q))
+    for i in (0, 1, 2, 1, 0, 2, 2, 0):
+        for x in outs[i]:
+            x.fill_(7)
+        graphs[i].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x.cpu(), y) for x, y in zip(outs[i], want[i]))
+        ws.random_(0, 256)  # eager work between the replays
