@@ -9,6 +9,11 @@
 // sixteen rows of a tile lie in one page, whose number it takes from a part of the
 // table in LDS, and the last tiles, which hold keys that some of the new rows do
 // not see, are masked by a word of bits for each query row and 32 keys.
+//
+// What bounds it depends on M: 4 d operations for each query row and key against
+// 4 d bytes of a bf16 key and value.  Up to M = 32 the cache's bytes do, in a kernel
+// made for that (wf_tree_few.hip); from some 200 rows on the products (64 drafted rows
+// of 4 heads, M = 256); between them whichever kernel plan_tree's cost prefers.
 #include "wf_tree.hpp"
 #include "wf_launch.hpp"
 
@@ -151,7 +156,18 @@ __device__ __forceinline__ void stage_pages(QuantStage<T, D, FMT, NW>& st, const
   }
 }
 
-// The query rows of a (sequence, head) over a range of its keys.
+// The query rows of a (sequence, head) over a range of its keys: the kernel of many
+// rows.  In bf16 the tiles that every row sees run in the pipelined loop of PrefixWave
+// (four tile slots in LDS filled three tiles ahead by direct loads, the softmax of a
+// block beside the products of the next); the few behind them, and rows of other
+// kinds, one tile at a time.  64 query rows a wave (QW = 2) read each tile from LDS
+// for twice the products: where M > 128 that is what lets them run at the rate that
+// the power limit leaves.  16 sequences of 64 rows, 32 heads over 8, 16K keys:
+// 258 us in the first calls and 310 after, 0.93 PFLOP/s sustained, the matrix units
+// busy in 53% of its cycles; with one range for each sequence and head, and so no
+// merge, 340.  Codes (eight waves, two tile slots at once, decoded on their way to
+// LDS): two blocks of 32 rows over 128K keys in 4 bits 164 us, 0.84 PFLOP/s; 39% of
+// its cycles have products, the decoding and softmax the rest.
 template <typename T, int D, int FMT, int QW>
 __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void tree_attn_kernel(TreeArgs a) {
   constexpr int NW = prefix_waves<T, FMT>();
@@ -435,7 +451,8 @@ __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void tree_attn_kerne
 
 // Merges the partials of each query row, as many as its sequence has ranges.  A
 // thread takes four channels of every SG-th partial of a row, eight in flight; the
-// SG threads of a row's channels meet in LDS.
+// SG threads of a row's channels meet in LDS.  Bound by its partials' bytes where they
+// are many (16K rows of two ranges: 12.6 us) and else by its round trips: 4 us.
 template <typename T, int D, int SG>
 __global__ __launch_bounds__(kBlock) void tree_merge_kernel(TreeArgs a) {
   constexpr int C4 = D / 4, RPB = kBlock / (C4 * SG), F = 8;
@@ -513,7 +530,8 @@ TreePlan plan_tree(const wf_tree_params& p, size_t have) {
   };
   bool few = true, many = M > (bf ? 32 : 16);
   // Few query rows: 32 a workgroup of four waves, two workgroups a CU; the blocks of
-  // query rows read the same keys, mostly from the L2.
+  // query rows read the same keys, mostly from the L2.  (Eight waves and one workgroup
+  // a CU, with half as many ranges: within 3% either way over 27 shapes.)
   if (few) {
     TreePlan l{};
     l.few = !bf || M <= 16 ? 16 : 32;

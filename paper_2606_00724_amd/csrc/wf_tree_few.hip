@@ -1,15 +1,33 @@
-// Attention of few query rows (32 of a sequence's K/V head at most) over the codes
-// of a cache in pages: bound by the cache's bytes.
+// Attention of few query rows over a cache in pages: a sequence's single token, or the
+// few drafted ones whose rows and heads of a group are 16 or 32 query rows of a K/V
+// head.  Bound by the cache's bytes: each key is read once, for 8 d operations or so a
+// byte.
 //
-// Each wave has keys, and a ring of blocks of 32 of them, of its own: it loads
-// their codes straight to LDS, waits for them by the count of its loads and meets
-// the workgroup's other waves only when its last block is done.  K's codes are
-// read row by row and decoded with the row's scale into the operand of S^T = K Q^T
-// (which channels make up one step of that product is free: here a lane has
-// consecutive ones of its row).  V's codes are read transposed, by the LDS loads
-// made for operands of 8 and 4 bits, and decoded without their scales; these, one
-// for each key and 32 channels, are put to the weights instead, which are the
-// other operand of O^T = V^T P^T for those 32 channels.
+// Each wave has keys, in blocks of 32, and a part of LDS of its own: it loads their
+// rows, or codes, straight to LDS as they are in memory, waits for them by the count
+// of its loads and meets the workgroup's other waves only when its last block is
+// done. Two workgroups a CU have 128 KB (64 KB of 8-bit codes) queued or being read.
+// The scores are S^T = K Q^T and the outputs O^T = V^T P^T, so that a lane has all
+// of its keys' scores of one query row, as the second product wants its weights.
+// Which channels make up one step of the first product is free: a lane has
+// consecutive ones of its row of K, 16-byte chunks.  V's rows are read transposed,
+// by the LDS loads made for operands of 16, 8 and 4 bits (fp32: a channel of a lane,
+// word by word).  Codes are decoded behind these reads, K's with their row's scale;
+// V's scales, one for each key and 32 channels, are put to the weights instead,
+// which are the other operand for those 32 channels, as powers of two: exact. The
+// weights are rounded to bf16 for the second product, as in the attention over a
+// prefix; their sum is taken of the unrounded ones.
+//
+// Products of 16 x 16 where M <= 16 (half the softmax and decoding of 32 x 32: 16
+// sequences of 32K rows in 8 bits 198 us, 204 with 32; single tokens over 16K 16.4,
+// 18.1), and for all of fp32; else of 32 x 32.
+//
+// Single tokens, 32 query heads over 8 of 128 channels: 64 sequences of 8K bf16 rows
+// (ragged) 275 to 283 us, 5.7 to 5.9 TB/s, where the loads alone reach 6.1; 32 of 32K
+// rows in 8 bits 293 to 302, 5.5 to 5.7 TB/s, the rate of its loads alone; 32 of 8K
+// fp32 rows 359 us, 6.0 TB/s.  24 drafted rows over 4K bf16 rows: 13.6 us, a chain of
+// round trips (lengths, pages, four blocks a wave, each queued when the one before it
+// has been read).
 #include "wf_tree.hpp"
 #include "wf_launch.hpp"
 
@@ -19,10 +37,15 @@ constexpr int kFewWaves = 4;
 
 typedef int v2i_few __attribute__((ext_vector_type(2)));
 
-// A wave's ring.  Rows of a block stand after each other, their 16-byte chunks in an
-// order that lets the lanes that read at once meet all banks: eight rows at one chunk
-// of K, and of V eight rows (8 bits), sixteen (4 bits), four at two chunks (bf16) or
-// every fourth one at 64 bytes (fp32).
+// A wave's part of LDS: a block's rows of K, of V, and the exponents of this block
+// and of the next, which come before this one's values are through.  Each part is
+// queued anew as soon as it has been read, K's while the softmax and V's product
+// run, V's over the next block's scores.  (Two blocks of 4 KB or less instead of
+// one: the same times, up to 4% longer at 64 channels.)  Rows of a block stand after
+// each other, their 16-byte chunks in an order that lets the lanes that read at once
+// meet all banks: eight rows at one chunk of K, and of V eight rows (8 bits),
+// sixteen (4 bits), four at two chunks (bf16) or every fourth one at 64 bytes
+// (fp32).
 template <typename T, int D, int FMT>
 struct FewGeom {
   static constexpr bool QUANT = FMT != WF_CACHE_PLAIN;
@@ -34,10 +57,7 @@ struct FewGeom {
   static constexpr int RPI = 64 / C;                           // rows of a load
   static constexpr int XB = D / 32;                            // exponent bytes of a row
   static constexpr int XL = QUANT ? 1 : 0;                     // loads of a block's exponents
-  static constexpr int R = KB >= 4096 ? 1 : 2;                 // blocks of the ring
-  static constexpr int XR = R + 1;  // a block's exponents outlive its keys
-  static constexpr int WAVE = R * 2 * KB + XL * XR * 256;      // bytes of a wave
-  static constexpr int BI = 2 * NI + XL;                       // loads of a block
+  static constexpr int WAVE = 2 * KB + XL * 2 * 256;           // bytes of a wave
   // place of row r's chunk c
   __device__ __forceinline__ static constexpr int swz(int r) {
     return C >= 8 ? r & 7 : C == 4 ? (r >> 1) & 3 : (r >> 2) & 1;
@@ -547,20 +567,20 @@ struct FewOut {
   static constexpr size_t BYTES = (size_t)kFewWaves * QN * (STRIDE + 2) * sizeof(float);
 };
 
-// Workgroups per CU, as their registers and LDS fit.
-template <typename T, int D, int FMT, int QN>
+// Two workgroups per CU, of which fp32 rows of 128 channels have the LDS for one.
+// (Registers for three of 16 rows over codes: the same times.)
+template <typename T, int D, int FMT>
 constexpr int few_groups() {
-  const bool quant = FMT != WF_CACHE_PLAIN;
-  return sizeof(T) == 4 ? (quant || D == 64 ? 2 : 1) : QN == 16 && quant ? 3 : 2;
+  return FewGeom<T, D, FMT>::WAVE * kFewWaves > 80 * 1024 ? 1 : 2;
 }
 
 template <typename T, int D, int FMT, int QN>
-__global__ __launch_bounds__(64 * kFewWaves, (few_groups<T, D, FMT, QN>())) void tree_few_kernel(
+__global__ __launch_bounds__(64 * kFewWaves, (few_groups<T, D, FMT>())) void tree_few_kernel(
     TreeArgs a) {
   using G = FewGeom<T, D, FMT>;
-  constexpr int NI = G::NI, R = G::R, RB = G::RB, KB = G::KB, XB = G::XB;
+  constexpr int NI = G::NI, RB = G::RB, KB = G::KB, XB = G::XB;
   constexpr bool QUANT = G::QUANT;
-  extern __shared__ __align__(16) unsigned char smem[];  // the waves' rings, a flag
+  extern __shared__ __align__(16) unsigned char smem[];  // the waves' blocks, a flag
   int* flag = reinterpret_cast<int*>(smem + kFewWaves * G::WAVE);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -606,7 +626,7 @@ __global__ __launch_bounds__(64 * kFewWaves, (few_groups<T, D, FMT, QN>())) void
                        : (((long)min(max(p.b, 0), a.pages - 1) * a.heads + head) << a.shift) +
                              ((k + 16) & in);
     };
-    const uint32_t ring = lds_offset(smem) + wave * G::WAVE, exps = ring + R * 2 * KB;
+    const uint32_t kat = lds_offset(smem) + wave * G::WAVE, vat = kat + KB, exps = vat + KB;
     // the lane's 16 bytes of a load: row of those that it holds, chunk
     const int lrow = lane / G::C;
     const uint32_t koff = lrow * RB + 16 * (lane % G::C ^ G::swz(lrow));
@@ -622,54 +642,35 @@ __global__ __launch_bounds__(64 * kFewWaves, (few_groups<T, D, FMT, QN>())) void
     auto exp_load = [&](long r0, long r1, uint32_t lds) __attribute__((always_inline)) {
       word_load(xbase + (xg ? r1 : r0) * XB, lds);
     };
-    // the exponents' slot of the block that is next to be loaded, and of this one
-    int xin = 0, xout = 0;
-    auto next = [&](int x) { return x + 1 == G::XR ? 0 : x + 1; };
     auto queue_keys = [&](int i, long r0, long r1) __attribute__((always_inline)) {
-      G::template load<false>(K + r0 * RB, K + r1 * RB, koff, ring + i % R * 2 * KB);
-      if constexpr (QUANT) {
-        exp_load(r0, r1, exps + xin * 256);
-        xin = next(xin);
-      }
+      G::template load<false>(K + r0 * RB, K + r1 * RB, koff, kat);
+      if constexpr (QUANT) exp_load(r0, r1, exps + (i & 1) * 256);
     };
-    auto queue_vals = [&](int i, long r0, long r1) __attribute__((always_inline)) {
-      G::template load<true>(V + r0 * RB, V + r1 * RB, voff, ring + i % R * 2 * KB + KB);
+    auto queue_vals = [&](long r0, long r1) __attribute__((always_inline)) {
+      G::template load<true>(V + r0 * RB, V + r1 * RB, voff, vat);
     };
 
     long r0, r1;
     rows_of(0, pages, r0, r1);
     queue_keys(0, r0, r1);
-    queue_vals(0, r0, r1);
+    queue_vals(r0, r1);
     const int m = min(m0 + w.query(), M - 1), ti = a.by_g(m);  // the lane's query row
     const long tok = min(max(s.first + ti, 0L), a.tokens - 1L);
     w.load(static_cast<const T*>(a.Q) + tok * a.qs + (long)(head * a.g + m - ti * a.g) * D);
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): so that no later wait is for these
-    for (int i = 1; i < min(R, mine); ++i) {
-      rows_of(i, pages_of(i), r0, r1);
-      queue_keys(i, r0, r1);
-      queue_vals(i, r0, r1);
-    }
-    pages = pages_of(R);  // of the block that is queued next
+    pages = pages_of(1);  // of the block that is queued next
     const uint32_t* words = a.mask ? a.mask + tok * a.words : nullptr;
 
     for (int i = 0; i < mine; ++i) {
       const int key = key_of(i), nv = min(32, kend - key);
-      const uint32_t kat = ring + i % R * 2 * KB, vat = kat + KB, xat = exps + xout * 256;
-      xout = next(xout);
-      const int ahead = min(mine - 1 - i, R);  // blocks behind this one, R at most
-      if (ahead == R) rows_of(i + R, pages, r0, r1);
-      pages = pages_of(i + R + 1);
-      if (ahead >= R - 1)
-        wait_loads<NI + (R - 1) * G::BI>();
-      else if (R == 4 && ahead == 2)
-        wait_loads<NI + 2 * G::BI>();
-      else if (R == 4 && ahead == 1)
-        wait_loads<NI + G::BI>();
-      else
-        wait_loads<NI>();
+      const uint32_t xat = exps + (i & 1) * 256;
+      const bool more = i + 1 < mine;
+      if (more) rows_of(i + 1, pages, r0, r1);
+      pages = pages_of(i + 2);
+      wait_loads<NI>();  // (V's may still be on their way)
       w.scores(kat, xat);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the codes have been read
-      if (ahead == R) queue_keys(i + R, r0, r1);
+      if (more) queue_keys(i + 1, r0, r1);
 
       // softmax, with the keys that the row does not see taken out
       const bool masked = key + 32 > min(s.base, kend);
@@ -677,14 +678,8 @@ __global__ __launch_bounds__(64 * kFewWaves, (few_groups<T, D, FMT, QN>())) void
       if (masked) seen = seen_keys(a, s, ti, words, key, nv);
       w.softmax(masked, seen);
 
-      if (ahead == R)
-        wait_loads<(R - 1) * G::BI + NI + G::XL>();
-      else if (R == 4 && ahead == 3)
-        wait_loads<3 * G::BI>();
-      else if (R == 4 && ahead == 2)
-        wait_loads<2 * G::BI>();
-      else if (R > 1 && ahead == 1)
-        wait_loads<G::BI>();
+      if (more)
+        wait_loads<NI + G::XL>();
       else
         wait_loads<0>();
       const uint32_t vx = xat + 32 * XB;  // V's exponents
@@ -723,11 +718,11 @@ __global__ __launch_bounds__(64 * kFewWaves, (few_groups<T, D, FMT, QN>())) void
       }
       w.values(vat, vx);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the codes have been read
-      if (ahead == R) queue_vals(i + R, r0, r1);
+      if (more) queue_vals(r0, r1);
     }
   }
 
-  lds_barrier();  // the rings are idle
+  lds_barrier();  // the blocks are idle
   const bool odd = __builtin_amdgcn_readfirstlane(*flag) != 0;
   lds_barrier();
   using Out = FewOut<D, QN>;
@@ -765,9 +760,9 @@ __global__ __launch_bounds__(64 * kFewWaves, (few_groups<T, D, FMT, QN>())) void
 
 template <typename T, int D, int FMT, int QN>
 static constexpr size_t few_lds() {
-  const size_t rings = (size_t)kFewWaves * FewGeom<T, D, FMT>::WAVE + sizeof(int);
+  const size_t blocks = (size_t)kFewWaves * FewGeom<T, D, FMT>::WAVE + sizeof(int);
   const size_t out = FewOut<D, QN>::BYTES;
-  return rings > out ? rings : out;
+  return blocks > out ? blocks : out;
 }
 
 hipError_t launch_tree_few(const TreeArgs& a, int dtype, int head_dim, int format, int rows,
