@@ -190,6 +190,7 @@ struct FewRows32 {
     const uint32_t kx = !G::QUANT  ? 0u
                         : XB == 4 ? lds_read<uint32_t>(xat + 4 * r) >> (16 * h)
                                   : lds_read<uint8_t>(xat + 2 * r + h);
+    __builtin_amdgcn_sched_barrier(0);  // (all reads queued before the first is waited for)
 #pragma unroll
     for (int e = 0; e < 16; ++e) sc[e] = 0.f;
 #pragma unroll
@@ -250,22 +251,38 @@ struct FewRows32 {
                                                 : G::vat(row, 2 * hi + (i16 >> 1 & 1)) + 8 * (i16 & 1));
     asm volatile("" : "+v"(vb));
     if constexpr (!G::QUANT) {
+      u32x2 v[2][DT][2];  // (all reads queued before the first is waited for, here too)
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int k = 0; k < 2; ++k)
+            v[kb][d][k] = read_tr16((vb ^ (64 * d)) + (2 * kb + k) * 8 * RB);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
         u32x4 pf;
 #pragma unroll
         for (int e = 0; e < 4; ++e) pf[e] = pack_bf16x2(t[8 * kb + 2 * e], t[8 * kb + 2 * e + 1]);
 #pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          const u32x2 lo = read_tr16((vb ^ (64 * d)) + 2 * kb * 8 * RB);
-          const u32x2 up = read_tr16((vb ^ (64 * d)) + (2 * kb + 1) * 8 * RB);
-          product(d, u32x4{lo[0], lo[1], up[0], up[1]}, pf);
-        }
+        for (int d = 0; d < DT; ++d)
+          product(d, u32x4{v[kb][d][0][0], v[kb][d][0][1], v[kb][d][1][0], v[kb][d][1][1]}, pf);
       }
     } else {
+      u32x2 c[DT][FMT == WF_CACHE_E4M3 ? 2 : 1];
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+        if constexpr (FMT == WF_CACHE_E4M3) {
+          c[d][0] = read_codes<FMT>(vb ^ (32 * d));
+          c[d][1] = read_codes<FMT>((vb ^ (32 * d)) + 16 * RB);
+        } else {
+          c[d][0] = read_codes<FMT>(vb ^ (16 * d));
+        }
       uint32_t xs[4 * XB];
 #pragma unroll
       for (int q = 0; q < 4; ++q) exponents4<XB>(vx + (8 * q + 4 * h) * XB, xs + XB * q);
+      __builtin_amdgcn_sched_barrier(0);
       // (less 128, for which the weights are doubled)
 #pragma unroll
       for (int e = 0; e < 4 * XB; ++e) xs[e] ^= 0x80808080u;
@@ -282,22 +299,14 @@ struct FewRows32 {
         }
         return pf;
       };
-      if constexpr (FMT == WF_CACHE_E4M3) {
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int d = 0; d < DT; ++d) {
-            const u32x2 c = read_codes<FMT>((vb ^ (32 * d)) + kb * 16 * RB);
-            product(d, operand<FMT>(c[0], c[1], 1.f), weights(kb, d));
-          }
-      } else {
-#pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          const u32x2 c = read_codes<FMT>(vb ^ (16 * d));
-#pragma unroll
-          for (int kb = 0; kb < 2; ++kb) product(d, operand<FMT>(c[kb], 0, 1.f), weights(kb, d));
-        }
-      }
+          product(d,
+                  FMT == WF_CACHE_E4M3 ? operand<FMT>(c[d][kb][0], c[d][kb][1], 1.f)
+                                       : operand<FMT>(c[d][0][kb], 0, 1.f),
+                  weights(kb, d));
     }
   }
   // The row's outputs, reference and sum; o, st: of the wave's rows.
