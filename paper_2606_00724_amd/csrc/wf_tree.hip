@@ -678,8 +678,9 @@ hipError_t launch_tree(const wf_tree_params& p, const TreePlan& l, TreeArgs& a, 
 
 hipError_t load_tree_kernels() {
   hipFuncAttributes fa;
-  return hipFuncGetAttributes(
+  const hipError_t e = hipFuncGetAttributes(
       &fa, reinterpret_cast<const void*>(tree_attn_kernel<bf16_t, 128, WF_CACHE_PLAIN, 1>));
+  return e != hipSuccess ? e : load_tree_few_kernels();
 }
 
 }  // namespace wf

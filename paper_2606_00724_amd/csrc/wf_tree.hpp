@@ -103,5 +103,6 @@ __device__ __forceinline__ void add_odd(const TreeArgs& a, const Sequence& s, in
 // (rows: query rows of a workgroup, 16 or, in bf16, 32)
 hipError_t launch_tree_few(const TreeArgs& a, int dtype, int head_dim, int format, int rows,
                            long items, hipStream_t s);
+hipError_t load_tree_few_kernels();
 
 }  // namespace wf

@@ -804,4 +804,10 @@ hipError_t launch_tree_few(const TreeArgs& a, int dtype, int head_dim, int forma
                          : by_format(std::integral_constant<int, 64>{});
 }
 
+hipError_t load_tree_few_kernels() {
+  hipFuncAttributes fa;
+  return hipFuncGetAttributes(
+      &fa, reinterpret_cast<const void*>(tree_few_kernel<bf16_t, 128, WF_CACHE_PLAIN, 16>));
+}
+
 }  // namespace wf

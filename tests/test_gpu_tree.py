@@ -2,6 +2,9 @@
 from __future__ import annotations
 
 import math
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -452,3 +455,37 @@ def test_two_graphs_share_a_workspace(wf):
         torch.cuda.synchronize()
         assert all(torch.equal(x.cpu(), y) for x, y in zip(outs[i], want[i]))
         ws.random_(0, 256)  # eager work between the replays
+
+
+FRESH = """
+import torch
+import paper_2606_00724_amd as wf
+wf.wf_init()
+g = torch.Generator().manual_seed(1)
+for rows in (1, 250):
+    p = wf.make_tree_params(pages=40, page_rows=64, heads=2, head_dim=128, batch=1,
+                            max_rows=rows, table_pages=40, group=16, causal=True)
+    Q, K, V = (torch.randn(s, generator=g).bfloat16().cuda()
+               for s in ((rows, 32, 128), (40, 2, 64, 128), (40, 2, 64, 128)))
+    table = torch.arange(40, dtype=torch.int32, device="cuda").flip(0)[None].contiguous()
+    length = torch.tensor([2500], dtype=torch.int32, device="cuda")
+    assert wf.tree_plan(p).group_rows == (16 if rows == 1 else 128)
+    ws, O = wf.alloc_tree_workspace(p, "cuda"), torch.zeros_like(Q)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        wf.wf_tree_attn(p, Q, K, None, V, None, table, length, None, None, O, None, ws)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(O, wf.tree_attend(p, Q, (K, None, V, None), table, length))
+    assert O.abs().sum() > 0
+print("done")
+"""
+
+
+def test_first_calls_of_a_process_may_be_captured(wf):
+    """After wf_init nothing is left to load: each kernel's first launch is captured."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    run = subprocess.run([sys.executable, "-c", FRESH], cwd=root, capture_output=True, text=True,
+                         timeout=100)
+    assert run.returncode == 0 and "done" in run.stdout, run.stderr
