@@ -281,6 +281,15 @@ def test_scales_of_either_sign_and_far_scores(wf):
         c.check(c.run(wf))
 
 
+@pytest.mark.parametrize("dtype,fmt", FORMATS)
+@pytest.mark.parametrize("scale", [-0.125, 40.0, 1e-39])
+def test_scales_in_every_kernel(wf, dtype, fmt, scale):
+    for rows, lens in ((1, [200, 90, 5]), (12, [200, 90, 5]), (150, [260, 170])):
+        c = Case(wf, lens=lens, rows=rows, scale=scale, dtype=dtype, fmt=fmt, d=128, group=2,
+                 heads=1)
+        c.check(c.run(wf))
+
+
 def test_a_pool_past_two_to_the_32_bytes(wf):
     """Pages whose rows lie behind 2^32 bytes of K (2^21 rows of 8 heads)."""
     heads, d, P = 8, 128, 64
