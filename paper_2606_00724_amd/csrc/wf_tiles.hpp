@@ -512,7 +512,7 @@ __device__ __forceinline__ void put4<float>(float* p, const f32x4& v) {
 // (E2M1), 16 bytes, and their block's exponent byte.  Four lanes load 64 bytes in
 // a row; they write their granules in an order of their own each (by x below), so
 // that eight lanes meet all banks.
-template <typename T, int D, int FMT, int NW>
+template <typename T, int D, int FMT, int NW, int OF = NW>
 struct QuantStage {
   using Geom = TileGeom<T, D>;
   static constexpr int CPP = FMT == WF_CACHE_E2M1 ? 32 : 16;  // channels per piece
@@ -522,10 +522,14 @@ struct QuantStage {
   u32x4 w[2][N];
   uint32_t x[2][N];
 
+  // the wave of those that load a tile: NW of the workgroup's OF
+  __device__ __forceinline__ static int wave() {
+    return OF == NW ? threadIdx.x >> 6 : (threadIdx.x >> 6) % NW;
+  }
   // a wave's 64 pieces: 8 rows of 8 (two halves of a row's pieces after each
   // other), 16 rows of 4 or 32 rows of 2
   __device__ __forceinline__ static int row(int i) {
-    const int lane = threadIdx.x & 63, w64 = i * NW + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, w64 = i * NW + wave();
     return PPR == 8 ? w64 * 8 + ((lane >> 2) & 7) : w64 * (64 / PPR) + lane / PPR;
   }
   __device__ __forceinline__ static int piece() {

@@ -122,10 +122,10 @@ __device__ __forceinline__ bool odd_values(unsigned char* tile, int nr) {
 // A tile's codes as a thread stages them.  The rows of a wave's load lie in one page
 // (or, two pieces a row, in one for each half of the wave): the lanes' offsets are
 // constant.
-template <typename T, int D, int FMT, int NW>
-__device__ __forceinline__ void stage_pages(QuantStage<T, D, FMT, NW>& st, const TreeArgs& a,
+template <typename T, int D, int FMT, int NW, int OF>
+__device__ __forceinline__ void stage_pages(QuantStage<T, D, FMT, NW, OF>& st, const TreeArgs& a,
                                             const PageIds& pages, int head, int key) {
-  using S = QuantStage<T, D, FMT, NW>;
+  using S = QuantStage<T, D, FMT, NW, OF>;
   if (S::idle()) return;
 #pragma unroll
   for (int i = 0; i < S::N; ++i) {
@@ -133,7 +133,7 @@ __device__ __forceinline__ void stage_pages(QuantStage<T, D, FMT, NW>& st, const
       const long page = __builtin_amdgcn_readfirstlane(pages.of(k));
       return ((page * a.heads + head) << a.shift) + (k & ((1 << a.shift) - 1));
     };
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave = __builtin_amdgcn_readfirstlane(S::wave());
     const int lane = threadIdx.x & 63, r16 = S::row(i) & 15;
     const uint32_t o = (r16 * S::PPR + S::piece()) * 16;
     const uint32_t e = r16 * (D / 32) + S::piece() * S::CPP / 32;
@@ -236,7 +236,16 @@ __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void tree_attn_kerne
       __syncthreads();
     };
     PageLoads<T, D> dma;
-    QuantStage<T, D, QUANT ? FMT : WF_CACHE_E4M3, NW> st[US];
+    // Codes of a slot that fewer waves than there are have pieces of: at 64 channels each
+    // slot is loaded and decoded by waves of its own (64 query rows a head over 8K rows
+    // of 32 sequences: 8 bits 94 -> 92 us, 4 bits 92 -> 84; at 128 channels, where two
+    // waves of a SIMD share the same work either way, 4 bits over 128K 182 -> 188).
+    constexpr int F = QUANT ? FMT : WF_CACHE_E4M3;
+    constexpr int PW = QuantStage<T, D, F, NW>::PT / 64;
+    constexpr bool APART = US > 1 && D == 64 && PW < NW;
+    const int slot = APART ? wave / PW : 0;  // the first of the wave's
+    QuantStage<T, D, F, APART ? PW : NW, NW> st[APART ? 1 : US];
+    static_assert(!APART || US * PW <= NW, "a wave loads codes of one slot");
     if constexpr (!QUANT) dma.init(a, head, lds_offset(smem));
     // tile t queued: on its way to its slot, or to registers
     int queued = 0;
@@ -245,15 +254,16 @@ __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void tree_attn_kerne
       queued = t + 1;
       if constexpr (QUANT) {
 #pragma unroll
-        for (int i = 0; i < US; ++i)
-          stage_pages(st[i], a, pages, head, k0 + t * KT + i * kTileRows);
+        for (int i = 0; i < (APART ? 1 : US); ++i)
+          if (slot + i < US) stage_pages(st[i], a, pages, head, k0 + t * KT + (slot + i) * kTileRows);
       } else {
         dma.template some<0>(0, 2 * dma.N, dma.at(pages, k0 + t * KT, slot_of(t)));
       }
     };
     auto commit = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < US; ++i) st[i].commit(smem + (slot_of(t) + i) * 2 * MB);
+      for (int i = 0; i < (APART ? 1 : US); ++i)
+        if (slot + i < US) st[i].commit(smem + (slot_of(t) + slot + i) * 2 * MB);
     };
     // tile t is in its slot once every wave has passed the barrier behind this
     auto landed = [&](int t) __attribute__((always_inline)) {
