@@ -515,11 +515,13 @@ __global__ __launch_bounds__(kBlock) void tree_merge_kernel(TreeArgs a) {
 
 static int merge_threads(int splits) { return splits <= 8 ? 1 : splits <= 32 ? 4 : 8; }
 
-// How a call's work is cut.  The cost of a choice in us, fitted to measured times.
-// A workgroup takes a block of query rows and a range of keys: a fixed part (its
-// first loads, its outputs) and its tiles, each at its products and softmax or at
-// its bytes, which come at 6 TB/s to all CUs and at 32 GB/s to one; and D floats a
-// query row and range are written and read where there are several ranges.
+// How a call's work is cut.  The cost of a choice in us, fitted to measured times (a
+// kernel's ranges to 388 shapes of 1 to 48 sequences, 1K to 64K rows and every type and
+// format: 1.5% slower than the best of some ten ranges, in the mean).  A workgroup takes
+// a block of query rows and a range of keys: a fixed part (its first loads, its outputs)
+// and its tiles, each at its products and softmax or at its bytes, which come at the
+// chip's rate to all CUs and at 32 GB/s (many query rows) or 50 (few) to one; and D
+// floats a query row and range are written and read where there are several ranges.
 TreePlan plan_tree(const wf_tree_params& p, size_t have) {
   const bool bf = p.dtype == WF_BF16, quant = p.format != WF_CACHE_PLAIN;
   const int D = p.head_dim;
@@ -550,20 +552,28 @@ TreePlan plan_tree(const wf_tree_params& p, size_t have) {
     l.mblocks = (int)((M + l.few - 1) / l.few);
     const long KT = 128, tiles = std::max(1L, (p.max_len + KT - 1) / KT);
     // a tile of a workgroup that has its CU alone, and of one that shares it
-    const double alone = !bf ? 1.6 + D / 160.0 : D / 128.0 * (!quant || l.few == 16 ? 1.0 : 1.4);
-    const double both = D / 128.0 * (!bf ? 5.4 : l.few == 16 ? 1.3 : 2.4);
+    const double slope = !bf ? 2.6 : l.few == 16 ? (quant ? 0.45 : 0.2) : quant ? 0.9 : 0.65;
+    const double alone = (!bf ? 0.2 : l.few == 16 && !quant ? 0.6 : 0.4) + slope * D / 128.0;
+    const double both = 1.6 * alone;
     const double most_at_once = !bf && !quant && D == 128 ? 1.0 : 2.0;
+    // bytes a us: to the chip (more of a cache that stays on it), to one CU (more of what
+    // another block of query rows has brought to the L2)
+    const double rate = 2.0 * U * p.max_len * row_bytes < 2e8 ? 7.4e6 : 6e6;
+    const double cu_rate = l.mblocks > 1 ? 75e3 : 50e3;
     for (long n = 1; n <= tiles; n += 1 + n / 16) {
       const long per = (tiles + n - 1) / n, s = (tiles + per - 1) / per;
       if (s > 1 && s > most) break;
       const double groups = (double)(U * l.mblocks * s), per_cu = std::ceil(groups / cus);
       const double at_once = std::min(per_cu, most_at_once);
-      const double bytes = 2 * KT * row_bytes / std::min(l.mblocks, 3) *
-                           std::max(std::min(groups, at_once * cus) / 6e6, at_once / 32e3);
+      const double running = std::min(groups, at_once * cus);
+      const double bytes = 2 * KT * row_bytes *
+                           std::max({running / std::min(l.mblocks, 3) / rate, running / 14e6,
+                                     at_once / cu_rate});
       const double tile = std::max(at_once > 1 ? both : alone, bytes);
+      const double rounds = std::max(1.0, per_cu / most_at_once);
       // (lengths that differ leave some CUs idle at the end: a part of a workgroup's time)
-      take(l, per * KT,
-           std::max(1.0, per_cu / most_at_once) * (per * tile + 6.0) + 0.2 * per * tile + merge(s));
+      take(l, per * KT, rounds * per * tile + 4.0 + 6.0 * (rounds - 1) + 0.2 * per * tile +
+                            (s > 1 ? merge(s) + 0.035 * s : 0.0));
     }
   }
   // Many: a block of query rows for the workgroup, as of the attention over a prefix.

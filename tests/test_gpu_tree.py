@@ -215,7 +215,7 @@ def test_hidden_rows_may_hold_anything(wf, dtype, fmt, where):
 
 # sequences, K/V heads, most rows, group, most keys, channels -> query rows of a
 # workgroup, with several ranges of the keys or one (the lengths are far below)
-FORMS = [(16, 1, 17, 3, 16000, 128, 64, True), (16, 8, 33, 2, 1000, 64, 64, False),
+FORMS = [(16, 2, 17, 3, 16000, 128, 64, True), (32, 8, 21, 3, 8000, 64, 64, False),
          (16, 1, 33, 2, 16000, 64, 128, True), (64, 1, 100, 3, 300, 128, 128, False),
          (16, 2, 64, 3, 16000, 128, 256, True), (16, 8, 100, 3, 300, 64, 256, False)]
 
@@ -231,7 +231,7 @@ def test_every_form_of_the_kernel_of_many_rows(wf, dtype, fmt, b, h, rows, g, mo
     c = Case(wf, lens=lens, counts=counts, rows=rows, heads=h, group=g, d=d, P=16, dtype=dtype,
              fmt=fmt, max_len=most, pool_pages=60, seed=4)
     s = wf.tree_plan(c.p)
-    if dtype == "bf16" and not (fmt and block == 64 and h == 8):
+    if dtype == "bf16":
         assert (s.group_rows, s.ranges > 1) == (block, ranges)
     if bad:
         c.table = (torch.randperm(57)[:57].repeat(b * 20)[:b * c.table.shape[1]]
