@@ -23,8 +23,8 @@
 // 18.1), and for all of fp32; else of 32 x 32.
 //
 // Single tokens, 32 query heads over 8 of 128 channels: 64 sequences of 8K bf16 rows
-// (ragged) 275 to 283 us, 5.7 to 5.9 TB/s, where the loads alone reach 6.1; 32 of 32K
-// rows in 8 bits 293 to 302, 5.5 to 5.7 TB/s, the rate of its loads alone; 32 of 8K
+// (ragged) 271 to 283 us, 5.7 to 5.9 TB/s, where the loads alone reach 6.1; 32 of 32K
+// rows in 8 bits 293 to 307, 5.4 to 5.7 TB/s, the rate of its loads alone; 32 of 8K
 // fp32 rows 359 us, 6.0 TB/s.  24 drafted rows over 4K bf16 rows: 13.6 us, a chain of
 // round trips (lengths, pages, four blocks a wave, each queued when the one before it
 // has been read).
