@@ -589,8 +589,10 @@ __global__ __launch_bounds__(64 * kFewWaves, (few_groups<T, D, FMT>())) void tre
   using G = FewGeom<T, D, FMT>;
   constexpr int NI = G::NI, RB = G::RB, KB = G::KB, XB = G::XB;
   constexpr bool QUANT = G::QUANT;
-  extern __shared__ __align__(16) unsigned char smem[];  // the waves' blocks, a flag
-  int* flag = reinterpret_cast<int*>(smem + kFewWaves * G::WAVE);
+  extern __shared__ __align__(16) unsigned char smem[];  // the waves' blocks, two flags
+  // values that are no numbers: whether there are any in blocks of keys that not all
+  // rows see; in the others, the top bit of the byte of each 32 channels that have one
+  uint32_t* flag = reinterpret_cast<uint32_t*>(smem + kFewWaves * G::WAVE);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
@@ -620,7 +622,7 @@ __global__ __launch_bounds__(64 * kFewWaves, (few_groups<T, D, FMT>())) void tre
   if (m0 >= M || (nk <= 0 && !a.whole)) return;
   std::conditional_t<QN == 32, FewRows32<D, FMT>, FewRows16<T, D, FMT>> w;
   w.init(a.scale);
-  if (threadIdx.x == 0) *flag = 0;
+  if (threadIdx.x <= QUANT) flag[threadIdx.x] = 0;
   lds_barrier();
 
   const int nb = nk > 0 ? (nk + 31) / 32 : 0;
@@ -698,16 +700,20 @@ __global__ __launch_bounds__(64 * kFewWaves, (few_groups<T, D, FMT>())) void tre
               u32x4{0u, 0u, 0u, 0u};
       }
       // Values that are no numbers: a block of channels with the exponent byte 255, and
-      // in 8 bits codes of NaN, or NaN and infinities in bf16.  The latter are cleared
-      // where not all rows see them; all are put to the rows that see them behind the
-      // last block.
+      // in 8 bits codes of NaN, or NaN and infinities in bf16.  Where not all rows see
+      // them they are cleared, and put to the rows that do behind the last block.  Where
+      // all do, the product makes NaN of those codes and values; of a byte 255, which is
+      // no power of two for the weights, the channels are noted, NaN in every row.
       bool odd = false;
       if constexpr (QUANT) {
         const int r = lane & 31;
-        uint32_t x = XB == 4 ? lds_read<uint32_t>(vx + 4 * r) : lds_read<uint16_t>(vx + 2 * r);
-        x = ~x & (XB == 4 ? ~0u : 0xffffu);
-        x |= XB == 4 ? 0u : 0xffff0000u;
-        odd = r < nv && ((x - 0x01010101u) & ~x & 0x80808080u) != 0;
+        const uint32_t x =
+            XB == 4 ? lds_read<uint32_t>(vx + 4 * r) : lds_read<uint16_t>(vx + 2 * r);
+        const uint32_t bad = r < nv ? ((x & 0x7f7f7f7fu) + 0x01010101u) & x & 0x80808080u : 0u;
+        if (masked)
+          odd = bad != 0;
+        else if (bad != 0)  // rare
+          atomicOr(flag + 1, bad);
       }
       if (FMT != WF_CACHE_E2M1 && masked)
         for (int c = lane; c < nv * G::C; c += 64) {
@@ -733,6 +739,9 @@ __global__ __launch_bounds__(64 * kFewWaves, (few_groups<T, D, FMT>())) void tre
 
   lds_barrier();  // the blocks are idle
   const bool odd = __builtin_amdgcn_readfirstlane(*flag) != 0;
+  const uint32_t none = QUANT ? __builtin_amdgcn_readfirstlane(flag[1]) : 0u;  // (channels)
+  // the first block that not all rows see
+  const int odd_from = k0 + max(min(s.base - k0, nk), 0) / 32 * 32;
   lds_barrier();
   using Out = FewOut<D, QN>;
   float* out = reinterpret_cast<float*>(smem);
@@ -751,7 +760,8 @@ __global__ __launch_bounds__(64 * kFewWaves, (few_groups<T, D, FMT>())) void tre
     const int i = a.by_g(m0 + r);
     const long tok = s.first + i;
     if (!Sequence::there(a, tok)) continue;
-    if (odd) add_odd<T, D, FMT>(a, s, seq, head, i, k0, k0 + nk, 4 * c, g.o);
+    if (odd) add_odd<T, D, FMT>(a, s, seq, head, i, odd_from, k0 + nk, 4 * c, g.o);
+    if (QUANT && (none >> c / 8 * 8 & 0x80u)) g.o = f32x4{NAN, NAN, NAN, NAN};
     const int hq = head * a.g + m0 + r - i * a.g;
     const long row = tok * a.hq + hq;
     if (a.whole) {
@@ -769,7 +779,7 @@ __global__ __launch_bounds__(64 * kFewWaves, (few_groups<T, D, FMT>())) void tre
 
 template <typename T, int D, int FMT, int QN>
 static constexpr size_t few_lds() {
-  const size_t blocks = (size_t)kFewWaves * FewGeom<T, D, FMT>::WAVE + sizeof(int);
+  const size_t blocks = (size_t)kFewWaves * FewGeom<T, D, FMT>::WAVE + 2 * sizeof(uint32_t);
   const size_t out = FewOut<D, QN>::BYTES;
   return blocks > out ? blocks : out;
 }
