@@ -304,11 +304,11 @@ __global__ __launch_bounds__(kBlock) void append_kernel(AppendArgs a) {
 
 // A workgroup has a column of all rows that one head of a sequence moves, in K or
 // in V: it reads every row before it writes the first.  Round trips bound a small
-// call, one each for the sources, their pages and the rows: a thread's loads of one
-// kind are queued together, those of the exponents' row beside the others, from
-// places that are always there, and what moves nothing is left out at the end.  Six
-// rows of 32 sequences of 8 heads: 3.5 us; 64 of 128 in 8 bits, 34 MB read and written:
-// 8.9 us.
+// call: one for the sources, then, since each of a thread's pieces stands behind a branch
+// that waits for the loads before it, one for each piece's pages and one for its row, the
+// exponents' row among them; loads are from places that are always there, and what moves
+// nothing is left out at the end.  Six rows of 32 sequences of 8 heads, one piece: 3.5 us;
+// 64 of 128 in 8 bits, two pieces and the exponents, 34 MB read and written: 8.9 us.
 constexpr int kMovePieces = 4;  // 16-byte pieces of a thread
 __global__ __launch_bounds__(kBlock) void move_kernel(MoveArgs a) {
   const int part = a.by_cols(blockIdx.x), col = blockIdx.x - part * a.cols;
@@ -359,7 +359,9 @@ __global__ __launch_bounds__(kBlock) void move_kernel(MoveArgs a) {
     x = a.xb == 4 ? *reinterpret_cast<const uint32_t*>(from)
                   : *reinterpret_cast<const uint16_t*>(from);
   }
-  __syncthreads();  // (waits for the loads)
+  // (a barrier alone waits for no load: every row has come before another wave writes)
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
 #pragma unroll
   for (int k = 0; k < kMovePieces; ++k)
     if (used(k) && moves(k))
