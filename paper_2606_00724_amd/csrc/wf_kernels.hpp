@@ -319,7 +319,7 @@ struct TreeArgs {
   int splits, rps;       // key ranges per unit at most, keys of a range (whole tiles)
   int mblocks, mrows;    // blocks per unit, query rows of a block
   int kw;                // waves that take the keys of a tile in turn
-  int batch, heads, g, hq;
+  int heads, g, hq;
   FastDiv by_g, by_hq, by_mblocks, by_splits, by_heads;
   int merges;            // workgroups of the merge per sequence
   FastDiv by_merge;

@@ -65,7 +65,6 @@ __device__ __forceinline__ void sine_cosine(double th, double& sn, double& cs) {
 template <int D>
 struct Place {
   static constexpr int C = D / 16;                  // threads a row
-  static constexpr int TR = kTurnRows<D>;
   int c, head, token;                               // part of the row, head of eight, token
   int oa, ob;                                       // the two vectors' channels
   bool turns;

@@ -383,23 +383,17 @@ __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void tree_attn_kerne
         if (nr % kTileRows)
           clear_rows<T, D, NW>(smem + (slot_of(t) + last) * 2 * MB, nr - last * kTileRows);
       }
-      auto blocks = [&](auto f) __attribute__((always_inline)) {
-        for (int r = 32 * kw; r < min(nr, KT); r += 32 * KW)
-          f(k0 + t * KT + r,
-            lds_offset(smem) + (slot_of(t) + r / kTileRows) * 2 * MB + r % kTileRows * 64,
-            min(32, nr - r));
-      };
       // Keys that some rows do not see: their scores are taken out, whatever they
       // are.  A weight of 0 times a value that is no number would still be NaN:
       // such values are cleared, and put to the rows that see them behind it all.
       const bool all = k0 + t * KT + min(nr, KT) <= s.base;  // uniform
       if (!all) {
-        bool odd = false;
+        bool here = false;
 #pragma unroll
         for (int i = 0; i < US; ++i)
-          odd |= odd_values<T, D, NW>(smem + (slot_of(t) + i) * 2 * MB,
-                                      min(max(nr - i * kTileRows, 0), kTileRows));
-        if (__builtin_amdgcn_ballot_w64(odd) != 0 && lane == 0) *flag = 1;
+          here |= odd_values<T, D, NW>(smem + (slot_of(t) + i) * 2 * MB,
+                                       min(max(nr - i * kTileRows, 0), kTileRows));
+        if (__builtin_amdgcn_ballot_w64(here) != 0 && lane == 0) *flag = 1;
         lds_barrier();
       }
       for (int r = 32 * kw; r < min(nr, KT); r += 32 * KW) {
@@ -540,11 +534,10 @@ TreePlan plan_tree(const wf_tree_params& p, size_t have) {
     best = l;
     best.rps = (int)rps;
   };
-  bool few = true, many = M > (bf ? 32 : 16);
   // Few query rows: 32 a workgroup of four waves, two workgroups a CU; the blocks of
   // query rows read the same keys, mostly from the L2.  (Eight waves and one workgroup
   // a CU, with half as many ranges: within 3% either way over 27 shapes.)
-  if (few) {
+  {
     TreePlan l{};
     l.few = !bf || M <= 16 ? 16 : 32;
     l.qw = 1;
@@ -577,6 +570,7 @@ TreePlan plan_tree(const wf_tree_params& p, size_t have) {
     }
   }
   // Many: a block of query rows for the workgroup, as of the attention over a prefix.
+  const bool many = M > (bf ? 32 : 16);
   const int nw = bf && quant ? 8 : 4;
   const long KT = nw == 8 ? 2 * kTileRows : kTileRows;
   const long tiles = std::max(1L, (p.max_len + KT - 1) / KT);
@@ -634,7 +628,6 @@ hipError_t launch_tree(const wf_tree_params& p, const TreePlan& l, TreeArgs& a, 
   a.mblocks = l.mblocks;
   a.mrows = l.nw / l.kw * 32 * l.qw;
   a.kw = l.kw;
-  a.batch = p.batch;
   a.heads = p.heads;
   a.g = p.group;
   a.hq = p.heads * p.group;
