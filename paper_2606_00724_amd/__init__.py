@@ -1204,13 +1204,15 @@ def wf_tree_attn(p, Q, Kc, Kx, Vc, Vx, table, length, row_start, mask, O, lse,
 
 def tree_attend(p: WfTreeParams, Q, pool, table, length, row_start=None,
                 mask=None, workspace=None, want_lse: bool = False, stream=None):
-    """Allocates O (and lse), zeros and -inf for tokens of no sequence, and
-    runs wf_tree_attn over a pool (Kc, Kx, Vc, Vx).  Returns O, or (O, lse)
-    when want_lse.  What it allocates belongs to the stream the kernels run
+    """Allocates O (its rows o_row apart, and lse), zeros and -inf for tokens of
+    no sequence, and runs wf_tree_attn over a pool (Kc, Kx, Vc, Vx).  Returns O,
+    or (O, lse) when want_lse.  What it allocates belongs to the stream the kernels run
     on."""
     with torch.cuda.stream(_torch_stream(stream)):
         rows = (p.tokens, p.heads * p.group)
-        O = torch.zeros(rows + (p.head_dim,), dtype=Q.dtype, device=Q.device)
+        n = p.heads * p.group * p.head_dim
+        O = torch.zeros((p.tokens, max(n, p.o_row)), dtype=Q.dtype,
+                        device=Q.device)[:, :n].unflatten(1, (-1, p.head_dim))
         lse = (torch.full(rows, float("-inf"), device=Q.device)
                if want_lse else None)
         if workspace is None:
