@@ -1150,12 +1150,14 @@ def make_tree_params(*, pages: int, page_rows: int, heads: int, head_dim: int,
     """tokens: rows of Q (batch * max_rows by default); max_len: most rows of a
     sequence's cache (all of its table's by default; the nearer to the lengths,
     the better the split)."""
+    most = 2 ** 31 - 1  # (a field's; the library refuses it)
     return WfTreeParams(pages, page_rows, heads, head_dim,
                         _DTYPES.get(dtype, dtype), _FORMATS.get(format, format),
                         group, batch,
-                        batch * max_rows if tokens is None else tokens,
+                        min(batch * max_rows, most) if tokens is None else tokens,
                         max_rows, table_pages,
-                        table_pages * page_rows if max_len is None else max_len,
+                        min(table_pages * page_rows, most) if max_len is None
+                        else max_len,
                         int(causal), scale, q_row, o_row)
 
 
