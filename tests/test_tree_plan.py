@@ -2,6 +2,7 @@
 import pytest
 
 import paper_2606_00724_amd as wf
+import treeforms
 
 
 def params(**kw):
@@ -29,3 +30,10 @@ def test_defaults():
     assert (p.tokens, p.max_len) == (6, 32)
     p = params(table_pages=1 << 20, page_rows=1024)
     assert p.max_len == 1 << 30 and wf.tree_plan(p, 0).ranges == 1
+
+
+@pytest.mark.parametrize("dtype,fmt,d,kernel,block,ranges", treeforms.ALL)
+def test_every_form_has_a_shape(dtype, fmt, d, kernel, block, ranges):
+    """What the tests of each form rely on."""
+    kw = treeforms.find(wf, dtype, fmt, d, kernel, block, ranges)
+    assert kw["max_rows"] <= kw["length"] <= kw["max_len"]
