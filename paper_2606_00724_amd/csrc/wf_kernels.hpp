@@ -251,9 +251,9 @@ struct MoveArgs {
   const int32_t* first;  // [batch]
   const int32_t* src;    // [batch][moves]
   void* c[2];            // K, V: rows of rb bytes
-  uint8_t* x[2];         // exponent bytes, xb a row (quantised)
+  uint8_t* x[2];         // exponent bytes (quantised)
   int pages, heads, tp, moves, shift;
-  int rb, xb;
+  int rb;
   int pshift, cols;      // log2 of a row's 16-byte pieces in a workgroup, workgroups a row takes
   FastDiv by_cols, by_heads;
 };

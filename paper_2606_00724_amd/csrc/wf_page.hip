@@ -303,37 +303,44 @@ __global__ __launch_bounds__(kBlock) void append_kernel(AppendArgs a) {
 
 // A workgroup has a column of all rows that one head of a sequence moves, in K or
 // in V: it reads every row before it writes the first.  Round trips bound a small
-// call: one for the sources, then, since each of a thread's pieces stands behind a branch
-// that waits for the loads before it, one for each piece's pages and one for its row, the
-// exponents' row among them; loads are from places that are always there, and what moves
-// nothing is left out at the end.  Six rows of 32 sequences of 8 heads, one piece: 3.5 us;
-// 64 of 128 in 8 bits, two pieces and the exponents, 34 MB read and written: 8.9 us.
+// call, one each for the sources, their pages and the rows: a thread's loads of one
+// kind are queued together, those of the exponents' row beside the others, from
+// places that are always there, and what moves nothing is left out at the end.  (How
+// many there are is a constant, N: behind a branch the compiler waits for every load
+// before it, and a thread's second piece and its exponents took four more trips.)  Six
+// rows of 32 sequences of 8 heads: 2.7 us (3.4 behind branches); 64 of 128 in 8 bits, 34 MB
+// read and written: 7.3 us (9.8).
 constexpr int kMovePieces = 4;  // 16-byte pieces of a thread
+// N pieces and, for codes, one load more: XB exponent bytes of a row
+template <int N, int XB>
 __global__ __launch_bounds__(kBlock) void move_kernel(MoveArgs a) {
   const int part = a.by_cols(blockIdx.x), col = blockIdx.x - part * a.cols;
   const int m = part & 1, unit = part >> 1, b = a.by_heads(unit), head = unit - b * a.heads;
-  constexpr int N = kMovePieces + 1;  // (the last one: a row's exponent bytes)
-  const bool exps = a.xb != 0 && col == 0;  // uniform
+  constexpr int ALL = N + (XB != 0), X = N;  // (the last one: a row's exponent bytes)
   const long first = a.first[b];
   const int32_t* src = a.src + (long)b * a.moves;
   const int32_t* table = a.table + (long)b * a.tp;
   const int in = (1 << a.shift) - 1;
-  auto used = [&](int k) {  // uniform
-    return k < kMovePieces ? k * kBlock < a.moves << a.pshift : exps;
-  };
-  int row[N], s[N], pf[N], pt[N];
+  int row[ALL], s[ALL], pf[ALL], pt[ALL];
 #pragma unroll
-  for (int k = 0; k < N; ++k) {
-    row[k] = k < kMovePieces ? (int)(threadIdx.x + k * kBlock) >> a.pshift : (int)threadIdx.x;
-    if (used(k)) s[k] = src[min(row[k], a.moves - 1)];
+  for (int k = 0; k < ALL; ++k) {
+    row[k] = k < N ? (int)(threadIdx.x + k * kBlock) >> a.pshift : (int)threadIdx.x;
+    s[k] = src[min(row[k], a.moves - 1)];
   }
+  // all queued before the first is waited for
+  auto queued = [](int(&x)[ALL]) {
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int k = 0; k < ALL; ++k) asm volatile("" : "+v"(x[k]));
+  };
+  queued(s);
   auto index = [&](long t) { return (int)min(max(t >> a.shift, 0L), a.tp - 1L); };
 #pragma unroll
-  for (int k = 0; k < N; ++k)
-    if (used(k)) {
-      pf[k] = table[index(first + s[k])];
-      pt[k] = table[index(first + row[k])];
-    }
+  for (int k = 0; k < ALL; ++k) {
+    pf[k] = table[index(first + s[k])];
+    pt[k] = table[index(first + row[k])];
+  }
+  queued(pf);
   // row t of the sequence, in page `page`, in its head's rows of the pool
   auto place = [&](long t, int page) {
     return (((long)min(max(page, 0), a.pages - 1) * a.heads + head) << a.shift) + (t & in);
@@ -347,31 +354,23 @@ __global__ __launch_bounds__(kBlock) void move_kernel(MoveArgs a) {
   };
   const int piece = threadIdx.x & ((1 << a.pshift) - 1);
   char* c = static_cast<char*>(a.c[m]) + (((long)col << a.pshift) + piece) * 16;
-  u32x4 v[kMovePieces];
-  uint32_t x = 0;
+  u32x4 v[N];
 #pragma unroll
-  for (int k = 0; k < kMovePieces; ++k)
-    if (used(k)) v[k] = *reinterpret_cast<const u32x4*>(c + place(first + s[k], pf[k]) * a.rb);
-  constexpr int X = kMovePieces;
-  if (exps) {
-    const uint8_t* from = a.x[m] + place(first + s[X], pf[X]) * a.xb;
-    x = a.xb == 4 ? *reinterpret_cast<const uint32_t*>(from)
-                  : *reinterpret_cast<const uint16_t*>(from);
-  }
+  for (int k = 0; k < N; ++k)
+    v[k] = *reinterpret_cast<const u32x4*>(c + place(first + s[k], pf[k]) * a.rb);
+  using Exps = std::conditional_t<XB == 4, uint32_t, uint16_t>;
+  Exps x = 0;
+  if constexpr (XB != 0)
+    x = *reinterpret_cast<const Exps*>(a.x[m] + place(first + s[X], pf[X]) * XB);
   // (a barrier alone waits for no load: every row has come before another wave writes)
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
 #pragma unroll
-  for (int k = 0; k < kMovePieces; ++k)
-    if (used(k) && moves(k))
-      *reinterpret_cast<u32x4*>(c + place(first + row[k], pt[k]) * a.rb) = v[k];
-  if (exps && moves(X)) {
-    uint8_t* to = a.x[m] + place(first + row[X], pt[X]) * a.xb;
-    if (a.xb == 4)
-      *reinterpret_cast<uint32_t*>(to) = x;
-    else
-      *reinterpret_cast<uint16_t*>(to) = (uint16_t)x;
-  }
+  for (int k = 0; k < N; ++k)
+    if (moves(k)) *reinterpret_cast<u32x4*>(c + place(first + row[k], pt[k]) * a.rb) = v[k];
+  if constexpr (XB != 0)
+    if (col == 0 && moves(X))  // (the row's first column of workgroups writes them)
+      *reinterpret_cast<Exps*>(a.x[m] + place(first + row[X], pt[X]) * XB) = x;
 }
 
 // ------------------------------------------------------------ host side
@@ -508,19 +507,30 @@ hipError_t launch_move(const wf_move_params& p, const int32_t* table, const int3
   a.moves = p.moves;
   a.shift = __builtin_ctz(p.page_rows);
   a.rb = row_bytes(p.head_dim, p.dtype, p.format);
-  a.xb = p.format == WF_CACHE_PLAIN ? 0 : p.head_dim / 32;
   int pc;
   move_split(p, pc, a.cols);
   a.pshift = __builtin_ctz(pc);
   a.by_cols = FastDiv::by(a.cols);
   a.by_heads = FastDiv::by(a.heads);
-  hipLaunchKernelGGL(move_kernel, dim3((unsigned)move_groups(p)), dim3(kBlock), 0, s, a);
-  return hipGetLastError();
+  const dim3 grid((unsigned)move_groups(p));
+  auto by_pieces = [&](auto xb) {
+    constexpr int XB = decltype(xb)::value;
+    switch ((pc * p.moves + kBlock - 1) / kBlock) {  // of a thread
+      case 1: hipLaunchKernelGGL((move_kernel<1, XB>), grid, dim3(kBlock), 0, s, a); break;
+      case 2: hipLaunchKernelGGL((move_kernel<2, XB>), grid, dim3(kBlock), 0, s, a); break;
+      case 3: hipLaunchKernelGGL((move_kernel<3, XB>), grid, dim3(kBlock), 0, s, a); break;
+      default: hipLaunchKernelGGL((move_kernel<kMovePieces, XB>), grid, dim3(kBlock), 0, s, a);
+    }
+    return hipGetLastError();
+  };
+  if (p.format == WF_CACHE_PLAIN) return by_pieces(std::integral_constant<int, 0>{});
+  if (p.head_dim == 128) return by_pieces(std::integral_constant<int, 4>{});
+  return by_pieces(std::integral_constant<int, 2>{});
 }
 
 hipError_t load_page_kernels() {
   hipFuncAttributes fa;
-  return hipFuncGetAttributes(&fa, reinterpret_cast<const void*>(move_kernel));
+  return hipFuncGetAttributes(&fa, reinterpret_cast<const void*>(move_kernel<1, 0>));
 }
 
 }  // namespace wf
