@@ -163,11 +163,14 @@ __device__ __forceinline__ void stage_pages(QuantStage<T, D, FMT, NW, OF>& st, c
 // kinds, one tile at a time.  64 query rows a wave (QW = 2) read each tile from LDS
 // for twice the products: where M > 128 that is what lets them run at the rate that
 // the power limit leaves.  16 sequences of 64 rows, 32 heads over 8, 16K keys:
-// 258 us in the first calls and 310 after, 0.93 PFLOP/s sustained, the matrix units
+// 258 us in the first calls and 310 after, 0.89 PFLOP/s sustained, the matrix units
 // busy in 53% of its cycles; with one range for each sequence and head, and so no
 // merge, 340.  Codes (eight waves, two tile slots at once, decoded on their way to
-// LDS): two blocks of 32 rows over 128K keys in 4 bits 164 us, 0.84 PFLOP/s; 39% of
-// its cycles have products, the decoding and softmax the rest.
+// LDS): two blocks of 32 rows over 128K keys in 4 bits 168 us, 0.82 PFLOP/s.  The matrix
+// units are busy in 39% of its cycles and the vector units in about half: all waves
+// decode a tile, meet at its barrier and then multiply, so that the two of a SIMD do the
+// same at once.  fp32: 8 sequences of 64 rows over 4K keys 332 us, 0.10 PFLOP/s, two
+// thirds of the rate of large fp32 products; over codes 309 and 306.
 template <typename T, int D, int FMT, int QW>
 __global__ __launch_bounds__((64 * prefix_waves<T, FMT>())) void tree_attn_kernel(TreeArgs a) {
   constexpr int NW = prefix_waves<T, FMT>();

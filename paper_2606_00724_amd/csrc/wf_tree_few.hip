@@ -14,9 +14,13 @@
 // by the LDS loads made for operands of 16, 8 and 4 bits (fp32: a channel of a lane,
 // word by word).  Codes are decoded behind these reads, K's with their row's scale;
 // V's scales, one for each key and 32 channels, are put to the weights instead,
-// which are the other operand for those 32 channels, as powers of two: exact. The
-// weights are rounded to bf16 for the second product, as in the attention over a
-// prefix; their sum is taken of the unrounded ones.
+// which are the other operand for those 32 channels, as powers of two: exact.
+//
+// For bf16 queries the weights are rounded to bf16 for the second product, as in the
+// attention over a prefix: the type of its operands, and weights in two parts would
+// double it.  Their sum is taken of the unrounded ones.  Outputs are off by 0.0023 of
+// their norm, of which the outputs' own rounding is 0.0017.  fp32 queries keep fp32
+// weights.
 //
 // Products of 16 x 16 where M <= 16 (half the softmax and decoding of 32 x 32: 16
 // sequences of 32K rows in 8 bits 198 us, 204 with 32; single tokens over 16K 16.4,
@@ -24,10 +28,12 @@
 //
 // Single tokens, 32 query heads over 8 of 128 channels: 64 sequences of 8K bf16 rows
 // (ragged) 271 to 283 us, 5.7 to 5.9 TB/s, where the loads alone reach 6.1; 32 of 32K
-// rows in 8 bits 293 to 307, 5.4 to 5.7 TB/s, the rate of its loads alone; 32 of 8K
-// fp32 rows 359 us, 6.0 TB/s.  24 drafted rows over 4K bf16 rows: 13.6 us, a chain of
-// round trips (lengths, pages, four blocks a wave, each queued when the one before it
-// has been read).
+// rows in 8 bits 289 to 307, 5.4 to 5.7 TB/s, the rate of its loads alone; 32 of 8K
+// fp32 rows 359 to 369 us, 5.8 to 6.0 TB/s.  fp32 queries over codes are bound by the fp32
+// products, a group's four rows padded to sixteen (32 sequences of 8K rows: 17 GFLOP,
+// 112 us), and the decoding before them: 182 us in 8 bits, 176 in 4.  24 drafted rows over
+// 4K bf16 rows: 13.0 us, a chain of round trips (lengths, pages, four blocks a wave, each
+// queued when the one before it has been read).
 #include "wf_tree.hpp"
 #include "wf_launch.hpp"
 
